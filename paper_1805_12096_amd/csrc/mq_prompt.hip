@@ -45,37 +45,63 @@ struct PromptParams {
   const void *q, *k, *v;
   void* out;
   const int32_t *q_first, *k_first;
-  uint8_t* units;                          // [slots][kv_heads][unit]
-  unsigned* bad;                           // [slots][kv_heads]: keys that are not finite
+  uint8_t* units;                          // [kv_heads][k_slots][unit]
+  unsigned* bad;                           // [kv_heads][k_slots]: keys that are not finite
   size_t ldq, ldk, ldv, ldo;
-  unsigned B, Tq, Tk, heads, kv_heads, d, q_slots;
+  unsigned B, Tq, Tk, heads, kv_heads, d, q_slots, k_slots;
   int causal;
+  int negative;                            // scale2 is the scale's magnitude
+  int vec;                                 // every row and head starts on 16 bytes
   float scale2;
 };
 
-// (the largest binary32 values would round to a bfloat16 infinity: they leave their last bits to the next part)
-template <int DT, bool ANY = true>
+// Binary32: the first part is the upper half of the word (no rounding, which could carry the largest values to infinity), the
+// second the rest rounded, the third what is left, 8 bits at most.  NaN and infinities end up as NaN in the second.
+template <int DT>
 __device__ __forceinline__ void split_parts(const float (&x)[8], Part8<DT> (&part)[kParts<DT>]) {
+  if constexpr (DT == MQ_F32) {
+    u4 w;
+    float r[8], r2[8];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    float rest = x[j];
-    if constexpr (ANY && DT == MQ_F32) {
-      const float most = fabsf(rest) <= 3.402823466e38f ? __uint_as_float(0x7F7F0000u) : INFINITY;
-      part[0][j] = (Part<DT>)fminf(fmaxf(rest, -most), most);
-      rest -= (float)part[0][j];
+    for (int j = 0; j < 4; ++j)
+      w[j] = __builtin_amdgcn_perm(__float_as_uint(x[2 * j + 1]), __float_as_uint(x[2 * j]), 0x07060302u);
+    part[0] = __builtin_bit_cast(b8, w);
 #pragma unroll
-      for (int i = 1; i < kParts<DT>; ++i) {
-        part[i][j] = (Part<DT>)rest;
-        rest -= (float)part[i][j];
-      }
-      continue;
-    }
+    for (int j = 0; j < 8; ++j) r[j] = x[j] - __uint_as_float(__float_as_uint(x[j]) & 0xFFFF0000u);
 #pragma unroll
-    for (int i = 0; i < kParts<DT>; ++i) {
-      part[i][j] = (Part<DT>)rest;
-      rest -= (float)part[i][j];
-    }
+    for (int j = 0; j < 8; ++j) part[1][j] = (__bf16)r[j];
+    w = __builtin_bit_cast(u4, part[1]);
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      r2[j] = r[j] - __uint_as_float(j % 2 == 0 ? w[j / 2] << 16 : w[j / 2] & 0xFFFF0000u);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) part[2][j] = (__bf16)r2[j];
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) part[0][j] = (Part<DT>)x[j];
   }
+}
+
+// 8 neighbouring columns from c on of a row, zeros past d.  Loads in front of every choice: a load behind a condition is waited
+// for on its own.  vec: rows are whole 16-byte pieces.
+template <int DT>
+__device__ __forceinline__ void row8(const typename Elem<DT>::T* row, unsigned c, unsigned d, bool vec, float (&x)[8]) {
+  using T = typename Elem<DT>::T;
+  if (vec) {
+    constexpr int W = 16 / sizeof(T);
+    typedef T tw __attribute__((ext_vector_type(W)));
+#pragma unroll
+    for (int i = 0; i < 8; i += W) {
+      const tw v = *reinterpret_cast<const tw*>(row + (c < d ? c + i : 0));
+#pragma unroll
+      for (int j = 0; j < W; ++j) x[i + j] = (float)v[j];
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = (float)row[c + j < d ? c + j : 0];
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) x[j] = c + j < d ? x[j] : 0.f;
 }
 
 // keys of sequence b start at unit first[b] / 32 + b: room for every sequence's last, partly filled one
@@ -96,36 +122,40 @@ __global__ __launch_bounds__(256) void k_prompt_pack(const PromptParams p) {
   const T* k = static_cast<const T*>(p.k) + (size_t)(f0 + j0) * p.ldk + (size_t)h * d;
   const T* v = static_cast<const T*>(p.v) + (size_t)(f0 + j0) * p.ldv + (size_t)h * d;
   const unsigned dp = (d + 31) / 32 * 32;
-  uint8_t* unit = p.units + ((size_t)slot * p.kv_heads + h) * unit_bytes(d, NP);
-  auto value = [&](const T* row, unsigned key, unsigned i, size_t ld) -> float {
-    if (key >= keys || i >= d) return 0.f;
-    const float x = (float)row[key * ld + i];
-    if (fabsf(x) <= 3.402823466e38f) return x;
-    atomicOr(&bad, 1u << key);
-    return 0.f;
-  };
-  auto put = [&](const float (&x)[8], uint8_t* to) {
+  uint8_t* unit = p.units + ((size_t)h * p.k_slots + slot) * unit_bytes(d, NP);
+  auto put = [&](float (&x)[8], auto key_of, uint8_t* to) {
+    float check = 0.f;                       // NaN as soon as one of them is not finite
+#pragma unroll
+    for (int j = 0; j < 8; ++j) check = fmaf(x[j], 0.f, check);
+    if (__builtin_expect(check != check, 0))
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (!(fabsf(x[j]) <= 3.402823466e38f)) {
+          atomicOr(&bad, 1u << key_of(j));
+          x[j] = 0.f;
+        }
     Part8<DT> part[NP];
     split_parts<DT>(x, part);
 #pragma unroll
     for (int i = 0; i < NP; ++i) *reinterpret_cast<Part8<DT>*>(to + i * 1024) = part[i];
   };
+  // (keys past the end repeat the last one: masked where they are used)
   for (unsigned i = tid; i < dp / 16 * 64; i += 256) {
-    const unsigned f = i / 64, lane = i % 64;
+    const unsigned f = i / 64, lane = i % 64, key = min(lane % 32, keys - 1);
     float x[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = value(k, lane % 32, f * 16 + lane / 32 * 8 + j, p.ldk);
-    put(x, unit + (size_t)f * NP * 1024 + lane * 16);
+    row8<DT>(k + (size_t)key * p.ldk, f * 16 + lane / 32 * 8, d, p.vec, x);
+    put(x, [&](int) { return key; }, unit + (size_t)f * NP * 1024 + lane * 16);
   }
   for (unsigned i = tid; i < dp / 16 * 64; i += 256) {
-    const unsigned f = i / 64, lane = i % 64;                // f = 2 t + s
+    const unsigned f = i / 64, lane = i % 64, c = f / 2 * 32 + lane % 32;                // f = 2 t + s
+    auto key_of = [&](int j) { return min(f % 2 * 16 + j / 4 * 8 + lane / 32 * 4 + j % 4, keys - 1); };
     float x[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = value(v, f % 2 * 16 + j / 4 * 8 + lane / 32 * 4 + j % 4, f / 2 * 32 + lane % 32, p.ldv);
-    put(x, unit + (size_t)(dp / 16 + f) * NP * 1024 + lane * 16);
+    for (int j = 0; j < 8; ++j) x[j] = (float)v[key_of(j) * p.ldv + (c < d ? c : 0)];
+    put(x, key_of, unit + (size_t)(dp / 16 + f) * NP * 1024 + lane * 16);
   }
   __syncthreads();
-  if (tid == 0) p.bad[(size_t)slot * p.kv_heads + h] = bad;
+  if (tid == 0) p.bad[(size_t)h * p.k_slots + slot] = bad;
 }
 
 __device__ __forceinline__ v16f mfma(b8 a, b8 b, v16f c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
@@ -138,6 +168,22 @@ __device__ __forceinline__ v16f mfma_parts(const P8 (&a)[NP], const P8 (&b)[NP],
 #pragma unroll
     for (int i = 0; i <= sum; ++i) c = mfma(a[i], b[sum - i], c);
   return c;
+}
+
+// Four neighbouring columns of an output row, times inv.  vec: rows are whole 16-byte pieces.
+template <int DT>
+__device__ __forceinline__ void store4(typename Elem<DT>::T* row, float a, float b, float c, float e, float inv, unsigned at,
+                                       unsigned d, bool vec) {
+  using T = typename Elem<DT>::T;
+  typedef T t4 __attribute__((ext_vector_type(4)));
+  const t4 v = {(T)(a * inv), (T)(b * inv), (T)(c * inv), (T)(e * inv)};
+  if (vec) {
+    if (at < d) *reinterpret_cast<t4*>(row + at) = v;
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (at + j < d) row[at + j] = v[j];
+  }
 }
 
 // ND: 32-column pieces of a head.  NU: units of a tile.  BUF: tiles in LDS.
@@ -183,22 +229,17 @@ __global__ __launch_bounds__(kW * kWave) void k_prompt_attention(const PromptPar
 #pragma unroll
     for (int f = 0; f < 2 * ND; ++f) {
       float x[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const unsigned c = f * 16 + half * 8 + j;
-        x[j] = mine && c < d ? (float)src[c] : 0.f;
-      }
+      row8<DT>(src, f * 16 + half * 8, d, p.vec, x);
       split_parts<DT>(x, qf[f]);
     }
   }
   const unsigned units = (nk + kUnit - 1) / kUnit;          // that the sequence has
-  const uint8_t* base = p.units + ((size_t)unit0 * p.kv_heads + kvh) * UNIT;
-  const size_t pitch = (size_t)p.kv_heads * UNIT;
+  const uint8_t* base = p.units + ((size_t)kvh * p.k_slots + unit0) * UNIT;
   auto fetch = [&](unsigned tile, unsigned buf) {
 #pragma unroll
     for (unsigned u = 0; u < NU; ++u) {
       const unsigned n = tile * NU + u < units ? tile * NU + u : units - 1;      // past the end: the last one, masked
-      const uint8_t* src = base + n * pitch + lane * 16;
+      const uint8_t* src = base + (size_t)n * UNIT + lane * 16;
       uint8_t* dst = smem + buf * TILE + u * UNIT;
 #pragma unroll
       for (unsigned c = 0; c < UNIT / 1024 / kW; ++c) {
@@ -254,7 +295,7 @@ __global__ __launch_bounds__(kW * kWave) void k_prompt_attention(const PromptPar
     for (int u = 0; u < NU; ++u) {
       const unsigned n = tile * NU + u;
       if (n < units) {
-        const unsigned w = p.bad[(size_t)(unit0 + n) * p.kv_heads + kvh];
+        const unsigned w = p.bad[(size_t)kvh * p.k_slots + unit0 + n];
         const unsigned first = n * kUnit;
         if (w != 0 && seen > first) poison |= (seen - first >= 32 ? w : w & ((1u << (seen - first)) - 1)) != 0;
       }
@@ -276,7 +317,7 @@ __global__ __launch_bounds__(kW * kWave) void k_prompt_attention(const PromptPar
           total += e[j];
         }
         P8 pf[NP];
-        split_parts<DT, false>(e, pf);
+        split_parts<DT>(e, pf);
 #pragma unroll
         for (int t = 0; t < ND; ++t) {
           P8 vf[NP];
@@ -294,10 +335,457 @@ __global__ __launch_bounds__(kW * kWave) void k_prompt_attention(const PromptPar
 #pragma unroll
   for (int t = 0; t < ND; ++t)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const unsigned c = 32 * t + 8 * (r / 4) + 4 * half + r % 4;
-      if (c < d) dst[c] = (T)(o[t][r] * inv);
+    for (int r = 0; r < 16; r += 4)
+      store4<DT>(dst, o[t][r], o[t][r + 1], o[t][r + 2], o[t][r + 3], inv, 32 * t + 2 * r + 4 * half, d, p.vec);
+}
+
+// ---- long sequences, 16-bit types ------------------------------------------------------------------------------------------
+// With 32 queries per wave every piece of K or V that a wave takes from LDS feeds one matrix instruction, and the four SIMDs'
+// 4 KB in 32 clocks are all that LDS gives; the softmax's vector instructions take as long as the matrix ones besides.  So
+// here a wave has two tiles of 32 queries, which halves what it reads, alone on its SIMD with twice the registers, and works
+// on three units at a time, so that nothing in a step waits for anything else in it:
+//   S = K Q^T of unit n + 2 and O += V P of unit n (matrix)   beside   P = exp2(S - m) of unit n + 1 (vector),
+// K and V pieces on their way from LDS a few instructions ahead.
+// The reference m of a query's softmax moves only when a score exceeds it by more than 2^kSlack (a branch that is hardly ever
+// taken), so that O is hardly ever rescaled.  A ring of units in LDS, one barrier for two units.
+constexpr int kRing = 8;
+constexpr float kSlack = 8.f;
+
+__device__ __forceinline__ void in_vector_registers(v16f& a, v16f& b) { asm volatile("" : "+v"(a), "+v"(b)); }
+template <int DT>
+__device__ __forceinline__ unsigned pack2(float a, float b) {
+  typedef Part<DT> p2 __attribute__((ext_vector_type(2)));
+  const p2 x = {(Part<DT>)a, (Part<DT>)b};
+  unsigned w = __builtin_bit_cast(unsigned, x);
+  asm("" : "+v"(w));                       // here, not where the last of eight is known
+  return w;
+}
+// sum + both elements of w (as rounded: what is divided by then is the sum of what is multiplied)
+template <int DT>
+__device__ __forceinline__ float add2(unsigned w, float sum) {
+  if constexpr (DT == MQ_F16) {
+    typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+    const h2 one = {(_Float16)1.f, (_Float16)1.f};
+    return __builtin_amdgcn_fdot2(__builtin_bit_cast(h2, w), one, sum, false);
+  } else {
+    typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+    const b2 one = {(__bf16)1.f, (__bf16)1.f};
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(b2, w), one, sum, false);
+  }
+}
+// Sums of matrix instructions times a factor, from accumulation registers and back.  (The compiler would otherwise take the
+// copies that the vector unit needs out of the branch, into every step.)
+__device__ __forceinline__ void scale_sums(v16f& o, float factor) {
+  asm volatile("" : "+a"(o));
+  o *= factor;
+  asm volatile("" : "+a"(o));
+}
+
+template <int DT, int ND>
+__global__ __launch_bounds__(kW * kWave, 1) void k_prompt_wide(const PromptParams p) {
+  using T = typename Elem<DT>::T;
+  using P8 = Part8<DT>;
+  constexpr unsigned UNIT = 2 * kUnit * 32 * ND * 2, PW = UNIT / 1024 / kW, BM = 2 * kW * kQ;
+  extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
+  const unsigned lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const unsigned col = lane % 32, half = lane / 32, d = p.d;
+  const unsigned per = p.heads / p.kv_heads;
+  const unsigned id = xcd_remap(blockIdx.x, gridDim.x);
+  const unsigned kvh = id / (p.q_slots * per), in = id % (p.q_slots * per);
+  const unsigned slot = p.q_slots - 1 - in / per, head = kvh * per + in % per;
+  const int b = __builtin_amdgcn_readfirstlane(wave_search(p.B, slot, [&](unsigned i) { return first_at(p.q_first, i, p.Tq) / BM + i; }));
+  if (b < 0) return;
+  const unsigned q0 = first_at(p.q_first, b, p.Tq), q1 = first_at(p.q_first, b + 1, p.Tq), nq = q1 > q0 ? q1 - q0 : 0;
+  const unsigned k0 = first_at(p.k_first, b, p.Tk), k1 = first_at(p.k_first, b + 1, p.Tk), nk = k1 > k0 ? k1 - k0 : 0;
+  const unsigned i0 = (slot - (q0 / BM + (unsigned)b)) * BM;
+  if (i0 >= nq) return;
+  const unsigned unit0 = k0 / kUnit + (unsigned)b, units = (nk + kUnit - 1) / kUnit;
+  auto seen_by = [&](unsigned i) -> unsigned {
+    if (!p.causal) return nk;
+    const long long s = (long long)i + 1 + (long long)nk - (long long)nq;
+    return s < 0 ? 0u : s > (long long)nk ? nk : (unsigned)s;
+  };
+  const unsigned iw = i0 + wave * 2 * kQ;
+  unsigned seen[2];
+  P8 qf[2][2 * ND];
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    const unsigned i = iw + c * kQ + col;
+    const bool mine = i < nq;
+    seen[c] = mine ? seen_by(i) : 0u;
+    const T* src = static_cast<const T*>(p.q) + (size_t)(q0 + (mine ? i : i0)) * p.ldq + (size_t)head * d;
+#pragma unroll
+    for (int f = 0; f < 2 * ND; ++f)
+    {
+      float x[8];
+      row8<DT>(src, f * 16 + half * 8, d, p.vec, x);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) qf[c][f][j] = (Part<DT>)(p.negative ? -x[j] : x[j]);   // (the scale's sign: what is masked stays at minus infinity)
     }
+  }
+  const unsigned last = min(i0 + BM, nq) - 1, wave_last = min(iw + 2 * kQ, nq) - 1;
+  const unsigned n_wg = __builtin_amdgcn_readfirstlane((seen_by(last) + kUnit - 1) / kUnit);
+  const unsigned n_wave = iw < nq ? __builtin_amdgcn_readfirstlane((seen_by(wave_last) + kUnit - 1) / kUnit) : 0u;
+  // units before this one are seen whole by every query of the tile
+  unsigned n_whole[2];
+#pragma unroll
+  for (int c = 0; c < 2; ++c)
+    n_whole[c] = iw + (c + 1) * kQ <= nq ? __builtin_amdgcn_readfirstlane(seen_by(iw + c * kQ) / kUnit) : 0u;
+
+  const uint8_t* base = p.units + ((size_t)kvh * p.k_slots + unit0) * UNIT + wave * 1024 + lane * 16;
+  auto fetch = [&](unsigned n) {
+    const uint8_t* src = base + (size_t)(n < units ? n : units - 1) * UNIT;       // past the end: the last one, masked
+    uint8_t* dst = smem + n % kRing * UNIT + wave * 1024;
+#pragma unroll
+    for (unsigned c = 0; c < PW; ++c)
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(src + c * (kW * 1024)),
+                                       (__attribute__((address_space(3))) void*)(dst + c * (kW * 1024)), 16, 0, 0);
+  };
+
+  v16f o[2][ND], sa[2], sb[2];
+  u4 pa[2][2] = {}, pb[2][2] = {};       // probabilities, eight of the type each
+  float last_e[2];
+  float top[2] = {-INFINITY, -INFINITY}, total[2] = {0.f, 0.f};
+  bool poison[2] = {false, false};
+#pragma unroll
+  for (int c = 0; c < 2; ++c)
+#pragma unroll
+    for (int t = 0; t < ND; ++t) o[c][t] = v16f{};
+
+  // what has to be known before the exponentials of unit n: masks, and whether a reference moves.  `held`: probabilities whose
+  // product with V is still to come
+  auto settle = [&](v16f (&s)[2], u4 (&held)[2][2], unsigned n) {
+    float m[2];
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      if (__builtin_expect(n >= n_whole[c], 0))
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (n * kUnit + 8 * (r / 4) + 4 * half + r % 4 >= seen[c]) s[c][r] = -INFINITY;
+      m[c] = s[c][0];
+#pragma unroll
+      for (int r = 1; r < 16; ++r) m[c] = fmaxf(m[c], s[c][r]);
+      m[c] = across32_f(m[c], [](float a, float b) { return fmaxf(a, b); }) * p.scale2;
+    }
+    if (__builtin_expect(__any(m[0] > top[0] + kSlack || m[1] > top[1] + kSlack), 0)) {
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        // (only for the queries concerned: no other query's result depends on theirs)
+        const float now = m[c] > top[c] + kSlack ? m[c] : top[c], keep = now == top[c] ? 1.f : __builtin_amdgcn_exp2f(top[c] - now);
+        top[c] = now;
+        total[c] *= keep;
+#pragma unroll
+        for (int t = 0; t < ND; ++t) scale_sums(o[c][t], keep);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          {
+            P8 x = __builtin_bit_cast(P8, held[c][i]);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = (Part<DT>)((float)x[j] * keep);
+            held[c][i] = __builtin_bit_cast(u4, x);
+          }
+      }
+    }
+  };
+  // exponentials [from, end) of the 32 that a lane has of a unit; two neighbours become a word of the operand
+  auto exponentials = [&](const v16f (&s)[2], u4 (&to)[2][2], int from, int end) {
+#pragma unroll
+    for (int i = from; i < end; ++i) {
+      const int c = i / 16, r = i % 16;
+      last_e[i % 2] = __builtin_amdgcn_exp2f(fmaf(s[c][r], p.scale2, -(top[c] == -INFINITY ? 0.f : top[c])));
+      if (i % 2 == 1) {
+        const unsigned w = pack2<DT>(last_e[0], last_e[1]);
+        to[c][r / 8][r % 8 / 2] = w;
+        total[c] = add2<DT>(w, total[c]);
+      }
+    }
+  };
+  auto scores = [&](unsigned n, v16f (&s)[2]) {
+    const uint8_t* at = smem + n % kRing * UNIT + lane * 16;
+    s[0] = s[1] = v16f{};
+#pragma unroll
+    for (int f = 0; f < 2 * ND; ++f) {
+      const P8 kf = *reinterpret_cast<const P8*>(at + f * 1024);
+      s[0] = mfma(kf, qf[0][f], s[0]);
+      s[1] = mfma(kf, qf[1][f], s[1]);
+    }
+  };
+  // step n, with the scores of unit n + 1 in s and its probabilities to go to `to`, unit n's in `held`, unit n + 2's scores to go
+  // to `next`: 8 ND matrix instructions, each with its share of the exponentials behind it, in this order.  V's pieces are asked
+  // for while K's are multiplied, those of unit n + 3's K while V's are.  (Left to itself, the compiler waits for each as it asks.)
+  P8 kf[2 * ND];
+  auto step = [&](unsigned n, v16f (&s)[2], v16f (&next)[2], u4 (&held)[2][2], u4 (&to)[2][2]) {
+    constexpr int N = 4 * ND;
+    const uint8_t *kat = smem + (n + 3) % kRing * UNIT + lane * 16, *vat = smem + n % kRing * UNIT + 2 * ND * 1024 + lane * 16;
+    P8 vf[2 * ND];
+    settle(s, held, n + 1);
+    next[0] = next[1] = v16f{};
+#pragma unroll
+    for (int i = 0; i < 2 * N; ++i) {
+      const int c = i % 2, f = i / 2 % (2 * ND), t = f % ND, h = f / ND;
+      if (i < 2 * ND) vf[i] = *reinterpret_cast<const P8*>(vat + (2 * (i % ND) + i / ND) * 1024);
+      if (i >= N && i < N + 2 * ND) kf[i - N] = *reinterpret_cast<const P8*>(kat + (i - N) * 1024);
+      if (i < N) next[c] = mfma(kf[f], qf[c][f], next[c]);
+      else o[c][t] = mfma(vf[f], __builtin_bit_cast(P8, held[c][h]), o[c][t]);
+      exponentials(s, to, i * 32 / (2 * N), (i + 1) * 32 / (2 * N));
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    in_vector_registers(next[0], next[1]);
+  };
+  // before steps n and n + 1: units up to n + 4 are there, and nobody reads units n - 2 and n - 1 any more
+  auto arrive = [&](unsigned n) {
+    constexpr unsigned ahead = (kRing - 7) * PW;
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0F70 | (ahead & 15) | (ahead >> 4) << 14);
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    fetch(n + kRing - 2);
+    fetch(n + kRing - 1);
+  };
+  // keys that are not finite, 64 units at a time
+  auto look = [&](unsigned n) {
+    const unsigned at = n + lane < units ? n + lane : units - 1;
+    const unsigned w = p.bad[(size_t)kvh * p.k_slots + unit0 + at];
+    unsigned long long some = __ballot(w != 0 && n + lane < units);
+    while (some != 0) {
+      const int l = __ffsll((long long)some) - 1;
+      some &= some - 1;
+      const unsigned bits = __builtin_amdgcn_readlane((int)w, l), from = (n + l) * kUnit;
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+        if (seen[c] > from) poison[c] |= (seen[c] - from >= 32 ? bits : bits & ((1u << (seen[c] - from)) - 1)) != 0;
+    }
+  };
+
+  if (n_wg > 0) {
+    for (unsigned n = 0; n < n_wg; n += kWave) look(n);
+#pragma unroll
+    for (unsigned n = 0; n + 2 < (unsigned)kRing; ++n) fetch(n);
+    __builtin_amdgcn_s_waitcnt(0x0F70);
+    __syncthreads();
+    scores(0, sa);
+    scores(1, sb);
+#pragma unroll
+    for (int f = 0; f < 2 * ND; ++f) kf[f] = *reinterpret_cast<const P8*>(smem + 2 * UNIT + f * 1024 + lane * 16);
+    settle(sa, pb, 0);
+    exponentials(sa, pa, 0, 32);
+    // (a wave whose queries see fewer units keeps the others company)
+    for (unsigned n = 0; n < n_wg; n += 2) {
+      arrive(n);
+      if (__builtin_expect(n < n_wave, 1)) {
+        step(n, sb, sa, pa, pb);
+        step(n + 1, sa, sb, pb, pa);
+      }
+    }
+  }
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    const unsigned i = iw + c * kQ + col;
+    const float sum = across32_f(total[c], [](float a, float b) { return a + b; });
+    if (i >= nq) continue;
+    const float inv = poison[c] ? NAN : sum == 0.f ? 0.f : __fdiv_rn(1.f, sum);
+    T* dst = static_cast<T*>(p.out) + (size_t)(q0 + i) * p.ldo + (size_t)head * d;
+#pragma unroll
+    for (int t = 0; t < ND; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; r += 4)
+        store4<DT>(dst, o[c][t][r], o[c][t][r + 1], o[c][t][r + 2], o[c][t][r + 3], inv, 32 * t + 2 * r + 4 * half, d, p.vec);
+  }
+}
+
+// ---- short sequences ---------------------------------------------------------------------------------------------------
+// Sentences of a few dozen words: nothing is reused often enough to be worth an order of its own, and a second launch and a walk
+// through LDS cost more than the product.  A wave takes 16 queries of one head and reads keys and values as they are; waves
+// wait for nobody.  The tiles are 16 x 16 (sentences leave half of a 32 x 32 one empty), and binary32 runs on the binary32
+// matrix instruction: splitting operands that are used once costs more vector instructions than it saves matrix ones.
+// Lane l: query (or key) l % 16, place group g = l / 16.  An operand's 8 elements are, for a 16-bit type, the 8 neighbouring
+// contracted places 8 g .. of 32, for binary32 two times four, 4 g .. of 16.
+constexpr int kQShort = 16;
+
+// The column that element j of a lane's n-th 8 stands for.
+template <int DT>
+__device__ __forceinline__ constexpr unsigned column_of(unsigned n, unsigned g, unsigned j) {
+  return DT == MQ_F32 ? 32 * n + 16 * (j / 4) + 4 * g + j % 4 : 32 * n + 8 * g + j;
+}
+
+// A lane's 8 elements of the row at base + row as floats; columns past d repeat the row's first.  VEC: whole 16-byte pieces
+template <int DT, bool VEC>
+__device__ __forceinline__ void load8(const typename Elem<DT>::T* base, unsigned row, unsigned n, unsigned g, unsigned d, float (&x)[8]) {
+  using T = typename Elem<DT>::T;
+  if constexpr (VEC) {
+    constexpr int W = DT == MQ_F32 ? 4 : 8;
+    typedef T tw __attribute__((ext_vector_type(W)));
+#pragma unroll
+    for (int i = 0; i < 8; i += W) {
+      const unsigned c = column_of<DT>(n, g, i);
+      const tw v = *reinterpret_cast<const tw*>(base + (row + (c < d ? c : 0)));
+#pragma unroll
+      for (int j = 0; j < W; ++j) x[i + j] = (float)v[j];
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const unsigned c = column_of<DT>(n, g, j);
+      x[j] = (float)base[row + (c < d ? c : 0)];
+    }
+  }
+}
+
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef __bf16 b4 __attribute__((ext_vector_type(4)));
+typedef _Float16 h4 __attribute__((ext_vector_type(4)));
+// contracts 32 columns
+template <int DT>
+__device__ __forceinline__ v4f mfma_columns(const float (&a)[8], const float (&b)[8], v4f c) {
+  if constexpr (DT == MQ_F32) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[j], b[j], c, 0, 0, 0);
+    return c;
+  } else {
+    Part8<DT> x, y;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      x[j] = (Part<DT>)a[j];
+      y[j] = (Part<DT>)b[j];
+    }
+    if constexpr (DT == MQ_F16) return __builtin_amdgcn_mfma_f32_16x16x32_f16(x, y, c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, c, 0, 0, 0);
+  }
+}
+// contracts 16 keys, of which a lane holds 4 g .. 4 g + 3
+template <int DT>
+__device__ __forceinline__ v4f mfma_keys(const float (&a)[4], const float (&b)[4], v4f c) {
+  if constexpr (DT == MQ_F32) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[j], b[j], c, 0, 0, 0);
+    return c;
+  } else if constexpr (DT == MQ_F16) {
+    const h4 x = {(_Float16)a[0], (_Float16)a[1], (_Float16)a[2], (_Float16)a[3]},
+             y = {(_Float16)b[0], (_Float16)b[1], (_Float16)b[2], (_Float16)b[3]};
+    return __builtin_amdgcn_mfma_f32_16x16x16f16(x, y, c, 0, 0, 0);
+  } else {
+    typedef short s4 __attribute__((ext_vector_type(4)));
+    const b4 x = {(__bf16)a[0], (__bf16)a[1], (__bf16)a[2], (__bf16)a[3]},
+             y = {(__bf16)b[0], (__bf16)b[1], (__bf16)b[2], (__bf16)b[3]};
+    return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s4, x), __builtin_bit_cast(s4, y), c, 0, 0, 0);
+  }
+}
+
+template <int DT, int ND, bool VEC>
+__global__ __launch_bounds__(256, ND <= 2 ? 3 : 2) void k_prompt_short(const PromptParams p) {
+  using T = typename Elem<DT>::T;
+  const unsigned lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const unsigned col = lane % 16, g = lane / 16, d = p.d;
+  const unsigned id = xcd_remap(blockIdx.x, gridDim.x) * 4 + wave, slot = id / p.heads, head = id % p.heads;
+  const unsigned kvh = head / (p.heads / p.kv_heads);
+  const int b = __builtin_amdgcn_readfirstlane(
+      slot < p.q_slots ? wave_search(p.B, slot, [&](unsigned i) { return first_at(p.q_first, i, p.Tq) / kQShort + i; }) : -1);
+  if (b < 0) return;
+  const unsigned q0 = first_at(p.q_first, b, p.Tq), q1 = first_at(p.q_first, b + 1, p.Tq), nq = q1 > q0 ? q1 - q0 : 0;
+  const unsigned k0 = first_at(p.k_first, b, p.Tk), k1 = first_at(p.k_first, b + 1, p.Tk), nk = k1 > k0 ? k1 - k0 : 0;
+  const unsigned i0 = (slot - (q0 / kQShort + (unsigned)b)) * kQShort, i = i0 + col;
+  if (i0 >= nq) return;
+  auto seen_by = [&](unsigned i) -> unsigned {
+    if (!p.causal) return nk;
+    const long long s = (long long)i + 1 + (long long)nk - (long long)nq;
+    return s < 0 ? 0u : s > (long long)nk ? nk : (unsigned)s;
+  };
+  const bool mine = i < nq;
+  const unsigned seen = mine ? seen_by(i) : 0u;
+  const unsigned most = __builtin_amdgcn_readfirstlane(seen_by(nq - i0 < (unsigned)kQShort ? nq - 1 : i0 + kQShort - 1));
+  const T* src = static_cast<const T*>(p.q) + (size_t)(q0 + i0) * p.ldq + (size_t)head * d;
+  const T* kp = static_cast<const T*>(p.k) + (size_t)k0 * p.ldk + (size_t)kvh * d;
+  const T* vp = static_cast<const T*>(p.v) + (size_t)k0 * p.ldv + (size_t)kvh * d;
+  const unsigned ldk = (unsigned)p.ldk, ldv = (unsigned)p.ldv;       // 32 rows are below 2^31 bytes
+  float qx[ND][8];
+#pragma unroll
+  for (int n = 0; n < ND; ++n) {
+    load8<DT, VEC>(src, (mine ? col : 0) * (unsigned)p.ldq, n, g, d, qx[n]);
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (column_of<DT>(n, g, j) >= d) qx[n][j] = 0.f;               // what keys have there then does not count
+  }
+  // keys [j0, j0 + 16) and their values.  Keys past the end repeat the last one: masked below.  Columns past d repeat one that
+  // is there: not stored
+  auto fetch = [&](unsigned j0, float (&kx)[ND][8], float (&vx)[2 * ND][4]) {
+    const T *kj = kp + (size_t)j0 * p.ldk, *vj = vp + (size_t)j0 * p.ldv;
+    const unsigned last = nk - j0 - 1, krow = min(col, last) * ldk;
+#pragma unroll
+    for (int n = 0; n < ND; ++n) load8<DT, VEC>(kj, krow, n, g, d, kx[n]);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const unsigned vrow = min(4 * g + j, last) * ldv;
+#pragma unroll
+      for (int t = 0; t < 2 * ND; ++t) vx[t][j] = (float)vj[vrow + (16 * t + col < d ? 16 * t + col : 0)];
+    }
+  };
+  v4f o[2 * ND];
+#pragma unroll
+  for (int t = 0; t < 2 * ND; ++t) o[t] = v4f{};
+  float top = -INFINITY, total = 0.f;
+  bool poison = false;
+  float kn[ND][8], vn[2 * ND][4];
+  if (most > 0) fetch(0, kn, vn);
+  for (unsigned j0 = 0; j0 < most; j0 += 16) {
+    float kx[ND][8], vx[2 * ND][4];
+    float check = 0.f;                                 // NaN as soon as one of them is not finite
+#pragma unroll
+    for (int n = 0; n < ND; ++n)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        kx[n][j] = kn[n][j];
+        vx[2 * n + j / 4][j % 4] = vn[2 * n + j / 4][j % 4];
+        check = fmaf(kx[n][j], 0.f, fmaf(vx[2 * n + j / 4][j % 4], 0.f, check));
+      }
+    if (j0 + 16 < most) fetch(j0 + 16, kn, vn);
+    if (__any(check != check)) {
+      unsigned bad = 0;                                // keys that are not finite; their elements become zero
+      auto clean = [&](float& x, unsigned key) {
+        const bool fine = fabsf(x) <= 3.402823466e38f;
+        x = fine ? x : 0.f;
+        bad |= fine ? 0u : 1u << key;
+        asm volatile("" : "+v"(bad));                  // one after the other: so many conditions at once do not fit
+      };
+#pragma unroll
+      for (int n = 0; n < ND; ++n)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          clean(kx[n][j], col);
+          clean(vx[2 * n + j / 4][j % 4], 4 * g + j % 4);
+        }
+#pragma unroll
+      for (int off = 32; off >= 1; off >>= 1) bad |= __shfl_xor(bad, off, 64);
+      if (seen > j0) poison |= (seen - j0 >= 16 ? bad : bad & ((1u << (seen - j0)) - 1)) != 0;
+    }
+    v4f s = {};
+#pragma unroll
+    for (int n = 0; n < ND; ++n) s = mfma_columns<DT>(kx[n], qx[n], s);
+    float e[4], m = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      e[j] = j0 + 4 * g + j < seen ? s[j] * p.scale2 : -INFINITY;
+      m = fmaxf(m, e[j]);
+    }
+    auto larger = [](float a, float b) { return fmaxf(a, b); };
+    m = fmaxf(top, across16_f(across32_f(m, larger), larger));
+    const float ref = m == -INFINITY ? 0.f : m, keep = __builtin_amdgcn_exp2f(top - ref);
+    top = m;
+    total *= keep;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      e[j] = __builtin_amdgcn_exp2f(e[j] - ref);
+      total += e[j];
+    }
+#pragma unroll
+    for (int t = 0; t < 2 * ND; ++t) o[t] = mfma_keys<DT>(vx[t], e, o[t] * keep);
+  }
+  auto sum = [](float a, float b) { return a + b; };
+  total = across16_f(across32_f(total, sum), sum);
+  if (!mine) return;
+  const float inv = poison ? NAN : total == 0.f ? 0.f : __fdiv_rn(1.f, total);
+  T* dst = static_cast<T*>(p.out) + (size_t)(q0 + i) * p.ldo + (size_t)head * d;
+#pragma unroll
+  for (int t = 0; t < 2 * ND; ++t) store4<DT>(dst, o[t][0], o[t][1], o[t][2], o[t][3], inv, 16 * t + 4 * g, d, VEC);
 }
 
 }  // namespace
@@ -313,22 +801,68 @@ int launch_prompt_attention(const void* q, size_t ldq, const void* k, size_t ldk
                             const int32_t* q_first, const int32_t* k_first, size_t B, size_t Tq, size_t Tk, int heads,
                             int kv_heads, size_t d, int causal, float scale, void* out, size_t ldo, void* ws, hipStream_t s) {
   const size_t n = k_slots(B, Tk) * (size_t)kv_heads, q_slots = Tq / (kW * kQ) + B, wgs = q_slots * (size_t)heads;
-  if (n >= (size_t)1 << 31 || wgs >= (size_t)1 << 31) return MQ_ERR_SHAPE;
+  if (n >= (size_t)1 << 31 || (Tq / kQShort + B) * (size_t)heads >= (size_t)1 << 31) return MQ_ERR_SHAPE;
+  const bool is_short = d <= 128 && ldq < (size_t)1 << 24 && ldk < (size_t)1 << 24 && ldv < (size_t)1 << 24 && Tq <= 64 * B && Tk <= 64 * B;
+  const bool is_long = d <= 128 && scale != 0.f && Tq >= 256 * B;
+  const size_t per16 = 16 / elem_bytes(dtype);
+  auto whole = [&](const void* x, size_t ld) { return reinterpret_cast<uintptr_t>(x) % 16 == 0 && ld % per16 == 0; };
+  const bool vec = d % 8 == 0 && whole(q, ldq) && whole(k, ldk) && whole(v, ldv) && whole(out, ldo);
   uint8_t* units = static_cast<uint8_t*>(ws);
   PromptParams p{q, k, v, out, q_first, k_first, units,
                  reinterpret_cast<unsigned*>(units + n * unit_bytes((unsigned)d, dtype == MQ_F32 ? 3 : 1)),
                  ldq, ldk, ldv, ldo, (unsigned)B, (unsigned)Tq, (unsigned)Tk, (unsigned)heads, (unsigned)kv_heads, (unsigned)d,
-                 (unsigned)q_slots, causal, scale * 1.44269504088896340736f};
+                 (unsigned)q_slots, (unsigned)k_slots(B, Tk), causal, 0, vec, scale * 1.44269504088896340736f};
   return with_dtype(dtype, [&](auto dt) {
     constexpr int DT = decltype(dt)::value;
+    if (is_short) {
+      p.q_slots = (unsigned)(Tq / kQShort + B);
+      auto go = [&](auto nd) {
+        constexpr int ND = decltype(nd)::value;
+        const unsigned n = (unsigned)(((size_t)p.q_slots * p.heads + 3) / 4);
+        if (vec) hipLaunchKernelGGL((k_prompt_short<DT, ND, true>), dim3(n), dim3(256), 0, s, p);
+        else hipLaunchKernelGGL((k_prompt_short<DT, ND, false>), dim3(n), dim3(256), 0, s, p);
+        return check_hip(hipGetLastError());
+      };
+      switch (padded(p.d) / 32) {
+        case 1: return go(std::integral_constant<int, 1>{});
+        case 2: return go(std::integral_constant<int, 2>{});
+        case 3: return go(std::integral_constant<int, 3>{});
+        default: return go(std::integral_constant<int, 4>{});
+      }
+    }
     hipLaunchKernelGGL((k_prompt_pack<DT>), dim3((unsigned)n), dim3(256), 0, s, p);
     int rc = check_hip(hipGetLastError());
     if (rc != MQ_OK) return rc;
+    if constexpr (DT != MQ_F32) {
+      if (is_long) {
+        p.q_slots = (unsigned)(Tq / (2 * kW * kQ) + B);
+        p.negative = scale < 0.f;
+        p.scale2 = fabsf(p.scale2);
+        auto go = [&](auto nd) {
+          constexpr int ND = decltype(nd)::value;
+          constexpr unsigned lds = kRing * 2 * kUnit * 32 * ND * 2;
+          auto kern = k_prompt_wide<DT, ND>;
+          if (lds > 65536) {
+            const int e = check_hip(hipFuncSetAttribute(reinterpret_cast<const void*>(kern),
+                                                        hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+            if (e != MQ_OK) return e;
+          }
+          hipLaunchKernelGGL(kern, dim3((unsigned)(p.q_slots * (size_t)p.heads)), dim3(kW * kWave), lds, s, p);
+          return check_hip(hipGetLastError());
+        };
+        switch (padded(p.d) / 32) {
+          case 1: return go(std::integral_constant<int, 1>{});
+          case 2: return go(std::integral_constant<int, 2>{});
+          case 3: return go(std::integral_constant<int, 3>{});
+          default: return go(std::integral_constant<int, 4>{});
+        }
+      }
+    }
     auto go = [&](auto nd) {
       constexpr int ND = decltype(nd)::value;
       // two units to a tile and two tiles in LDS where they fit, else one of both
       constexpr unsigned UNIT = 2 * kUnit * 32 * ND * 2 * kParts<DT>;
-      constexpr int NU = 4 * UNIT <= kLds ? 2 : 1, BUF = 2 * NU * UNIT <= kLds ? 2 : 1;
+      constexpr int NU = DT != MQ_F32 && 4 * UNIT <= kLds ? 2 : 1, BUF = 2 * NU * UNIT <= kLds ? 2 : 1;
       auto kern = k_prompt_attention<DT, ND, NU, BUF>;
       constexpr unsigned lds = NU * BUF * UNIT;
       if (lds > 65536) {

@@ -470,6 +470,9 @@ SEQUENCES = [  # queries, keys
     ([200, 300], None),
     ([1, 40, 1, 130], [70, 200, 1, 131]),
     ([50, 33, 3], [20, 0, 1]),                       # more queries than keys: with a causal mask the first see nothing
+    ([1, 31, 32, 33, 0, 64, 65, 7], [3, 31, 40, 33, 0, 64, 65, 100]),       # few of each: the one-launch form
+    ([700, 257], [700, 300]),                        # many of each: two tiles a wave (16-bit types)
+    ([600, 450, 33, 1], [2500, 1, 0, 40]),
 ]
 
 
@@ -500,12 +503,14 @@ def test_prompt_attention(which, heads, hk, dim, dtype, causal):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-def test_prompt_attention_masked_places_never_count(dtype):
+@pytest.mark.parametrize("n,others", [(150, 0), (150, 7), (300, 0)])      # (empty sequences: the one-launch form takes the call)
+def test_prompt_attention_masked_places_never_count(dtype, n, others):
     g = gen(21)
-    heads, hk, dim, n = 2, 1, 64, 150
+    heads, hk, dim = 2, 1, 64
+    ends = [0] + [n] * (1 + others)
     q, k, v = (normal(g, n, h * dim).to(dtype) for h in (heads, hk, hk))
-    want, tol = prompt_reference(q, k, v, [0, n], [0, n], heads, hk, dim, True, 0.125)
-    clean = prompt(q.to(DEV), k.to(DEV), v.to(DEV), [0, n], [0, n], heads, hk, dim, True, 0.125).cpu()
+    want, tol = prompt_reference(q, k, v, ends, ends, heads, hk, dim, True, 0.125)
+    clean = prompt(q.to(DEV), k.to(DEV), v.to(DEV), ends, ends, heads, hk, dim, True, 0.125).cpu()
     for at, kind in ((100, "k"), (70, "v"), (149, "kv"), (96, "v")):
         for bad in (math.nan, math.inf, -math.inf, torch.finfo(dtype).max, torch.finfo(dtype).min):
             kb, vb = k.clone(), v.clone()
@@ -513,19 +518,20 @@ def test_prompt_attention_masked_places_never_count(dtype):
                 kb[at, 3] = bad
             if "v" in kind:
                 vb[at, 5] = bad
-            got = prompt(q.to(DEV), kb.to(DEV), vb.to(DEV), [0, n], [0, n], heads, hk, dim, True, 0.125).cpu()
+            got = prompt(q.to(DEV), kb.to(DEV), vb.to(DEV), ends, ends, heads, hk, dim, True, 0.125).cpu()
             assert torch.equal(got[:at], clean[:at]), (at, kind, bad)
             if not math.isfinite(bad):
                 assert torch.isnan(got[at:]).all(), (at, kind, bad)
     assert ((clean.double() - want).abs() <= tol).all()
     qb = q.clone()
     qb[7, dim + 2] = math.nan                        # a query's own NaN stays with its head
-    got = prompt(qb.to(DEV), k.to(DEV), v.to(DEV), [0, n], [0, n], heads, hk, dim, True, 0.125).cpu()
+    got = prompt(qb.to(DEV), k.to(DEV), v.to(DEV), ends, ends, heads, hk, dim, True, 0.125).cpu()
     assert torch.isnan(got[7, dim:]).all() and torch.equal(got[7, :dim], clean[7, :dim])
     assert torch.equal(got[:7], clean[:7]) and torch.equal(got[8:], clean[8:])
 
 
-def test_prompt_attention_values_of_any_magnitude():
+@pytest.mark.parametrize("others", [0, 3])
+def test_prompt_attention_values_of_any_magnitude(others):
     g = gen(22)
     heads, hk, dim, n = 1, 1, 32, 90
     q, k, v = (normal(g, n, dim) for _ in range(3))
@@ -534,7 +540,8 @@ def test_prompt_attention_values_of_any_magnitude():
     q *= 1e-12
     k *= 1e12
     want, tol = prompt_reference(q, k, v, [0, n], [0, n], heads, hk, dim, True, 0.125)
-    got = prompt(q.to(DEV), k.to(DEV), v.to(DEV), [0, n], [0, n], heads, hk, dim, True, 0.125).cpu().double()
+    ends = [0] + [n] * (1 + others)
+    got = prompt(q.to(DEV), k.to(DEV), v.to(DEV), ends, ends, heads, hk, dim, True, 0.125).cpu().double()
     assert ((got - want).abs() <= tol).all()
     # rows in front of the large ones are as exact as without them
     w2, t2 = prompt_reference(q[:3], k[:3], v[:3], [0, 3], [0, 3], heads, hk, dim, True, 0.125)
