@@ -348,10 +348,20 @@ __global__ __launch_bounds__(kW * kWave) void k_prompt_attention(const PromptPar
 // K and V pieces on their way from LDS a few instructions ahead.
 // The reference m of a query's softmax moves only when a score exceeds it by more than 2^kSlack (a branch that is hardly ever
 // taken), so that O is hardly ever rescaled.  A ring of units in LDS, one barrier for two units.
+#define MQ_INLINE __attribute__((always_inline))
 constexpr int kRing = 8;
 constexpr float kSlack = 8.f;
 
-__device__ __forceinline__ void in_vector_registers(v16f& a, v16f& b) { asm volatile("" : "+v"(a), "+v"(b)); }
+// One result of a matrix instruction, out of its accumulation register at this place.  (The compiler would copy all sixteen as
+// soon as they are there, and wait for that.)  The compiler does not see what is read here, so whoever reads the first result
+// lets the eleven wait states of an 8-pass instruction go by: FIRST.
+template <bool FIRST>
+__device__ __forceinline__ float accumulated(float x) {
+  float y;
+  if constexpr (FIRST) asm volatile("s_nop 10\n\tv_accvgpr_read_b32 %0, %1" : "=v"(y) : "a"(x));
+  else asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(y) : "a"(x));
+  return y;
+}
 template <int DT>
 __device__ __forceinline__ unsigned pack2(float a, float b) {
   typedef Part<DT> p2 __attribute__((ext_vector_type(2)));
@@ -406,6 +416,26 @@ __global__ __launch_bounds__(kW * kWave, 1) void k_prompt_wide(const PromptParam
     return s < 0 ? 0u : s > (long long)nk ? nk : (unsigned)s;
   };
   const unsigned iw = i0 + wave * 2 * kQ;
+  const unsigned last = min(i0 + BM, nq) - 1, wave_last = min(iw + 2 * kQ, nq) - 1;
+  const unsigned n_wg = __builtin_amdgcn_readfirstlane((seen_by(last) + kUnit - 1) / kUnit);
+  const unsigned n_wave = iw < nq ? __builtin_amdgcn_readfirstlane((seen_by(wave_last) + kUnit - 1) / kUnit) : 0u;
+  // units before this one are seen whole by every query of the workgroup
+  const unsigned n_full = __builtin_amdgcn_readfirstlane(seen_by(i0) / kUnit);
+
+  const uint8_t* base = p.units + ((size_t)kvh * p.k_slots + unit0) * UNIT + wave * 1024 + lane * 16;
+  auto fetch = [&](unsigned n) {
+    const uint8_t* src = base + (size_t)(n < units ? n : units - 1) * UNIT;       // past the end: the last one, masked
+    uint8_t* dst = smem + n % kRing * UNIT + wave * 1024;
+#pragma unroll
+    for (unsigned c = 0; c < PW; ++c)
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(src + c * (kW * 1024)),
+                                       (__attribute__((address_space(3))) void*)(dst + c * (kW * 1024)), 16, 0, 0);
+  };
+
+  // (the first units are on their way while the queries come)
+  if (n_wg > 0)
+#pragma unroll
+    for (unsigned n = 0; n + 2 < (unsigned)kRing; ++n) fetch(n);
   unsigned seen[2];
   P8 qf[2][2 * ND];
 #pragma unroll
@@ -423,27 +453,9 @@ __global__ __launch_bounds__(kW * kWave, 1) void k_prompt_wide(const PromptParam
       for (int j = 0; j < 8; ++j) qf[c][f][j] = (Part<DT>)(p.negative ? -x[j] : x[j]);   // (the scale's sign: what is masked stays at minus infinity)
     }
   }
-  const unsigned last = min(i0 + BM, nq) - 1, wave_last = min(iw + 2 * kQ, nq) - 1;
-  const unsigned n_wg = __builtin_amdgcn_readfirstlane((seen_by(last) + kUnit - 1) / kUnit);
-  const unsigned n_wave = iw < nq ? __builtin_amdgcn_readfirstlane((seen_by(wave_last) + kUnit - 1) / kUnit) : 0u;
-  // units before this one are seen whole by every query of the tile
-  unsigned n_whole[2];
-#pragma unroll
-  for (int c = 0; c < 2; ++c)
-    n_whole[c] = iw + (c + 1) * kQ <= nq ? __builtin_amdgcn_readfirstlane(seen_by(iw + c * kQ) / kUnit) : 0u;
-
-  const uint8_t* base = p.units + ((size_t)kvh * p.k_slots + unit0) * UNIT + wave * 1024 + lane * 16;
-  auto fetch = [&](unsigned n) {
-    const uint8_t* src = base + (size_t)(n < units ? n : units - 1) * UNIT;       // past the end: the last one, masked
-    uint8_t* dst = smem + n % kRing * UNIT + wave * 1024;
-#pragma unroll
-    for (unsigned c = 0; c < PW; ++c)
-      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(src + c * (kW * 1024)),
-                                       (__attribute__((address_space(3))) void*)(dst + c * (kW * 1024)), 16, 0, 0);
-  };
-
-  v16f o[2][ND], sa[2], sb[2];
-  u4 pa[2][2] = {}, pb[2][2] = {};       // probabilities, eight of the type each
+  v16f o[2][ND];
+  float sa[2][16], sb[2][16], high_a[2], high_b[2];       // scores of two units, and the largest of a lane's 16
+  u4 pa[2][2] = {}, pb[2][2] = {};                        // probabilities, eight of the type each
   float last_e[2];
   float top[2] = {-INFINITY, -INFINITY}, total[2] = {0.f, 0.f};
   bool poison[2] = {false, false};
@@ -454,18 +466,19 @@ __global__ __launch_bounds__(kW * kWave, 1) void k_prompt_wide(const PromptParam
 
   // what has to be known before the exponentials of unit n: masks, and whether a reference moves.  `held`: probabilities whose
   // product with V is still to come
-  auto settle = [&](v16f (&s)[2], u4 (&held)[2][2], unsigned n) {
+  auto settle = [&](auto masked, float (&s)[2][16], float (&high)[2], u4 (&held)[2][2], unsigned n) MQ_INLINE {
     float m[2];
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
-      if (__builtin_expect(n >= n_whole[c], 0))
+      if constexpr (decltype(masked)::value) {
+        high[c] = -INFINITY;
 #pragma unroll
-        for (int r = 0; r < 16; ++r)
+        for (int r = 0; r < 16; ++r) {
           if (n * kUnit + 8 * (r / 4) + 4 * half + r % 4 >= seen[c]) s[c][r] = -INFINITY;
-      m[c] = s[c][0];
-#pragma unroll
-      for (int r = 1; r < 16; ++r) m[c] = fmaxf(m[c], s[c][r]);
-      m[c] = across32_f(m[c], [](float a, float b) { return fmaxf(a, b); }) * p.scale2;
+          high[c] = fmaxf(high[c], s[c][r]);
+        }
+      }
+      m[c] = across32_f(high[c], [](float a, float b) { return fmaxf(a, b); }) * p.scale2;
     }
     if (__builtin_expect(__any(m[0] > top[0] + kSlack || m[1] > top[1] + kSlack), 0)) {
 #pragma unroll
@@ -477,18 +490,17 @@ __global__ __launch_bounds__(kW * kWave, 1) void k_prompt_wide(const PromptParam
 #pragma unroll
         for (int t = 0; t < ND; ++t) scale_sums(o[c][t], keep);
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-          {
-            P8 x = __builtin_bit_cast(P8, held[c][i]);
+        for (int i = 0; i < 2; ++i) {
+          P8 x = __builtin_bit_cast(P8, held[c][i]);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = (Part<DT>)((float)x[j] * keep);
-            held[c][i] = __builtin_bit_cast(u4, x);
-          }
+          for (int j = 0; j < 8; ++j) x[j] = (Part<DT>)((float)x[j] * keep);
+          held[c][i] = __builtin_bit_cast(u4, x);
+        }
       }
     }
   };
   // exponentials [from, end) of the 32 that a lane has of a unit; two neighbours become a word of the operand
-  auto exponentials = [&](const v16f (&s)[2], u4 (&to)[2][2], int from, int end) {
+  auto exponentials = [&](const float (&s)[2][16], u4 (&to)[2][2], int from, int end) MQ_INLINE {
 #pragma unroll
     for (int i = from; i < end; ++i) {
       const int c = i / 16, r = i % 16;
@@ -500,37 +512,54 @@ __global__ __launch_bounds__(kW * kWave, 1) void k_prompt_wide(const PromptParam
       }
     }
   };
-  auto scores = [&](unsigned n, v16f (&s)[2]) {
+  // scores [from, end) of the 32, out of the matrix instructions' registers
+  auto take = [&](const v16f (&x)[2], float (&s)[2][16], float (&high)[2], int from, int end) MQ_INLINE {
+#pragma unroll
+    for (int i = from; i < end; ++i) {
+      const int c = i / 16, r = i % 16;
+      s[c][r] = i == 0 ? accumulated<true>(x[c][r]) : accumulated<false>(x[c][r]);
+      if (r % 2 == 1) high[c] = r == 1 ? fmaxf(s[c][0], s[c][1]) : fmaxf(fmaxf(high[c], s[c][r - 1]), s[c][r]);
+    }
+  };
+  auto scores = [&](unsigned n, float (&s)[2][16], float (&high)[2]) MQ_INLINE {
     const uint8_t* at = smem + n % kRing * UNIT + lane * 16;
-    s[0] = s[1] = v16f{};
+    v16f x[2] = {};
 #pragma unroll
     for (int f = 0; f < 2 * ND; ++f) {
       const P8 kf = *reinterpret_cast<const P8*>(at + f * 1024);
-      s[0] = mfma(kf, qf[0][f], s[0]);
-      s[1] = mfma(kf, qf[1][f], s[1]);
+      x[0] = mfma(kf, qf[0][f], x[0]);
+      x[1] = mfma(kf, qf[1][f], x[1]);
     }
+    __builtin_amdgcn_sched_barrier(0);                     // (take counts on all of them being issued)
+    take(x, s, high, 0, 32);
   };
   // step n, with the scores of unit n + 1 in s and its probabilities to go to `to`, unit n's in `held`, unit n + 2's scores to go
-  // to `next`: 8 ND matrix instructions, each with its share of the exponentials behind it, in this order.  V's pieces are asked
-  // for while K's are multiplied, those of unit n + 3's K while V's are.  (Left to itself, the compiler waits for each as it asks.)
+  // to `next`: 8 ND matrix instructions, each with its share of the vector ones behind it, in this order.  The exponentials lie
+  // mostly beside K's half, the way of the new scores beside V's.  V's pieces are asked for while K's are multiplied, those of
+  // unit n + 3's K while V's are.  (Left to itself, the compiler waits for each as it asks.)
   P8 kf[2 * ND];
-  auto step = [&](unsigned n, v16f (&s)[2], v16f (&next)[2], u4 (&held)[2][2], u4 (&to)[2][2]) {
-    constexpr int N = 4 * ND;
+  auto step = [&](auto masked, unsigned n, float (&s)[2][16], float (&high)[2], float (&next)[2][16], float (&next_high)[2], u4 (&held)[2][2],
+                  u4 (&to)[2][2]) MQ_INLINE {
+    constexpr int N = 4 * ND, EARLY = 22;                  // exponentials of the first half
     const uint8_t *kat = smem + (n + 3) % kRing * UNIT + lane * 16, *vat = smem + n % kRing * UNIT + 2 * ND * 1024 + lane * 16;
     P8 vf[2 * ND];
-    settle(s, held, n + 1);
-    next[0] = next[1] = v16f{};
+    settle(masked, s, high, held, n + 1);
+    v16f x[2] = {};
 #pragma unroll
     for (int i = 0; i < 2 * N; ++i) {
-      const int c = i % 2, f = i / 2 % (2 * ND), t = f % ND, h = f / ND;
+      const int c = i % 2, f = i / 2 % (2 * ND), t = f % ND, h = f / ND, j = i - N;
       if (i < 2 * ND) vf[i] = *reinterpret_cast<const P8*>(vat + (2 * (i % ND) + i / ND) * 1024);
-      if (i >= N && i < N + 2 * ND) kf[i - N] = *reinterpret_cast<const P8*>(kat + (i - N) * 1024);
-      if (i < N) next[c] = mfma(kf[f], qf[c][f], next[c]);
-      else o[c][t] = mfma(vf[f], __builtin_bit_cast(P8, held[c][h]), o[c][t]);
-      exponentials(s, to, i * 32 / (2 * N), (i + 1) * 32 / (2 * N));
+      if (i >= N && i < N + 2 * ND) kf[j] = *reinterpret_cast<const P8*>(kat + j * 1024);
+      if (i < N) {
+        x[c] = mfma(kf[f], qf[c][f], x[c]);
+        exponentials(s, to, i * EARLY / N, (i + 1) * EARLY / N);
+      } else {
+        o[c][t] = mfma(vf[f], __builtin_bit_cast(P8, held[c][h]), o[c][t]);
+        exponentials(s, to, EARLY + j * (32 - EARLY) / N, EARLY + (j + 1) * (32 - EARLY) / N);
+        if (j >= 2) take(x, next, next_high, (j - 2) * 32 / (N - 2), (j - 1) * 32 / (N - 2));
+      }
       __builtin_amdgcn_sched_barrier(0);
     }
-    in_vector_registers(next[0], next[1]);
   };
   // before steps n and n + 1: units up to n + 4 are there, and nobody reads units n - 2 and n - 1 any more
   auto arrive = [&](unsigned n) {
@@ -558,24 +587,30 @@ __global__ __launch_bounds__(kW * kWave, 1) void k_prompt_wide(const PromptParam
   };
 
   if (n_wg > 0) {
-    for (unsigned n = 0; n < n_wg; n += kWave) look(n);
-#pragma unroll
-    for (unsigned n = 0; n + 2 < (unsigned)kRing; ++n) fetch(n);
+    unsigned any = 0;
+    for (unsigned n = lane; n < min(n_wg, units); n += kWave) any |= p.bad[(size_t)kvh * p.k_slots + unit0 + n];
+    if (__builtin_expect(__any(any != 0), 0))
+      for (unsigned n = 0; n < n_wg; n += kWave) look(n);
     __builtin_amdgcn_s_waitcnt(0x0F70);
     __syncthreads();
-    scores(0, sa);
-    scores(1, sb);
+    scores(0, sa, high_a);
+    scores(1, sb, high_b);
 #pragma unroll
     for (int f = 0; f < 2 * ND; ++f) kf[f] = *reinterpret_cast<const P8*>(smem + 2 * UNIT + f * 1024 + lane * 16);
-    settle(sa, pb, 0);
+    settle(std::true_type{}, sa, high_a, pb, 0);
     exponentials(sa, pa, 0, 32);
-    // (a wave whose queries see fewer units keeps the others company)
-    for (unsigned n = 0; n < n_wg; n += 2) {
+    unsigned n = 0;
+    auto two = [&](auto masked) MQ_INLINE {
+      step(masked, n, sb, high_b, sa, high_a, pa, pb);
+      step(masked, n + 1, sa, high_a, sb, high_b, pb, pa);
+    };
+    for (; n + 2 < n_full; n += 2) {
       arrive(n);
-      if (__builtin_expect(n < n_wave, 1)) {
-        step(n, sb, sa, pa, pb);
-        step(n + 1, sa, sb, pb, pa);
-      }
+      two(std::false_type{});
+    }
+    for (; n < n_wg; n += 2) {
+      arrive(n);
+      if (n < n_wave) two(std::true_type{});     // (a wave whose queries see fewer units keeps the others company)
     }
   }
 #pragma unroll
