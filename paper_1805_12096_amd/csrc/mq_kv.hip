@@ -6,6 +6,12 @@
 // tokens.  Nobody else writes to the block, so there is nothing to wait for and no atomic.  Queries are rotated by workgroups
 // behind those, a wave per token.
 // Bound by bytes for prompts and by the chain of dependent loads (sequence, table, amax) for single tokens.
+//
+// Rows of whole 16-byte pieces (k_kv_append_rows): what a workgroup rotates and quantizes stays in registers between the two
+// maxima and the stores.  A thread has 16 elements of a key, the two groups of 8 that are rotated together, and for the values
+// 4 tokens x 2 columns, whose bytes are one word of a row of the cache each.  256 threads take a block at once; where a call
+// brings few tokens to a block, 64 threads take 8 (4 for wide heads) at a time, sines and cosines formed by all of them in LDS
+// (with more tokens every thread forms its own: a pair is used once).  Other rows: k_kv_append, element by element.
 #include <type_traits>
 
 #include "mq_glue.h"
@@ -27,6 +33,7 @@ struct AppendParams {
   float* amax;
   void *k_out, *q_out;
   unsigned B, T, kv_heads, heads, d, rot, page_wgs;
+  unsigned slot_tokens, slot_more;      // sequence b's slots start at first[b] / slot_tokens + slot_more b
   int interleaved;
 };
 
@@ -125,14 +132,13 @@ __global__ __launch_bounds__(kT) void k_kv_append(const AppendParams p) {
   int b = (int)slot;
   unsigned f0 = slot, n = 1, local = 0;
   if (p.first != nullptr) {
-    // sequence b touches at most n / 64 + 2 blocks; its slots start at first[b] / 64 + 2 b
-    auto base = [&](unsigned i) { return first_at(p.first, i, p.T) / kKvBlock + 2 * i; };
+    auto base = [&](unsigned i) { return first_at(p.first, i, p.T) / p.slot_tokens + p.slot_more * i; };
     b = wave_search(p.B, slot, base);
     if (b < 0) return;
     f0 = first_at(p.first, b, p.T);
     const unsigned f1 = first_at(p.first, b + 1, p.T);
     n = f1 > f0 ? f1 - f0 : 0;
-    local = slot - (f0 / kKvBlock + 2 * (unsigned)b);
+    local = slot - (f0 / p.slot_tokens + p.slot_more * (unsigned)b);
   }
   const long long held = p.held[b];
   // positions [t0, t1) of this block that are new; blocks count from the one the first new token falls into
@@ -227,29 +233,339 @@ __global__ __launch_bounds__(kT) void k_kv_append(const AppendParams p) {
   }
 }
 
+// ---- rows of whole 16-byte pieces --------------------------------------------------------------------------------------
+
+// 8 elements as floats
+template <int DT>
+__device__ __forceinline__ void load8(const typename Elem<DT>::T* at, float* x) {
+  using T = typename Elem<DT>::T;
+  constexpr int W = 16 / sizeof(T);
+  typedef T tw __attribute__((ext_vector_type(W)));
+#pragma unroll
+  for (int i = 0; i < 8; i += W) {
+    const tw v = *reinterpret_cast<const tw*>(at + i);
+#pragma unroll
+    for (int j = 0; j < W; ++j) x[i + j] = (float)v[j];
+  }
+}
+template <int DT>
+__device__ __forceinline__ void store8(typename Elem<DT>::T* at, const float* x) {
+  using T = typename Elem<DT>::T;
+  constexpr int W = 16 / sizeof(T);
+  typedef T tw __attribute__((ext_vector_type(W)));
+#pragma unroll
+  for (int i = 0; i < 8; i += W) {
+    tw v;
+#pragma unroll
+    for (int j = 0; j < W; ++j) v[j] = (T)x[i + j];
+    *reinterpret_cast<tw*>(at + i) = v;
+  }
+}
+// Of the u-th 16 elements of a head: where its two groups of 8 start.  Rotated halves take a group of each half.
+__device__ __forceinline__ void groups_of(unsigned u, unsigned rot, int interleaved, unsigned& one, unsigned& two) {
+  const bool halves = !interleaved && u < rot / 16;
+  one = halves ? 8 * u : 16 * u;
+  two = halves ? 8 * u + rot / 2 : 16 * u + 8;
+}
+// Rotates them; angle(i) is pair i's.
+template <typename Angle>
+__device__ __forceinline__ void rotate16(float (&x)[16], unsigned u, unsigned rot, int interleaved, Angle angle) {
+  if (u >= rot / 16) return;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const SinCos w = angle(8 * u + j);
+    if (interleaved) rotate(x[2 * j], x[2 * j + 1], w);
+    else rotate(x[j], x[8 + j], w);
+  }
+}
+__device__ __forceinline__ unsigned pack4(float a, float b, float c, float d, float s) {
+  return quant8(a, s) | quant8(b, s) << 8 | quant8(c, s) << 16 | quant8(d, s) << 24;
+}
+__device__ __forceinline__ unsigned requant4(unsigned w, float ratio) {
+  return requant8(w, ratio) | requant8(w >> 8, ratio) << 8 | requant8(w >> 16, ratio) << 16 | requant8(w >> 24, ratio) << 24;
+}
+typedef uint32_t w4 __attribute__((ext_vector_type(4)));
+typedef uint32_t w2 __attribute__((ext_vector_type(2)));
+
+// TH threads; KI, VI: a thread's 16 elements of keys and 4 x 2 of values, of a chunk of CG groups of four tokens
+template <int DT, int TH, int KI, int VI>
+__global__ __launch_bounds__(TH) void k_kv_append_rows(const AppendParams p) {
+  using T = typename Elem<DT>::T;
+  constexpr bool kTable = TH == kWave;                // (one wave: no table or maximum crosses waves)
+  constexpr int kTableSize = 512;
+  __shared__ SinCos table[kTable ? kTableSize : 1];
+  __shared__ float red[2][TH / kWave];
+  __shared__ unsigned image[kTable ? 1 : 256 * 17];   // a block of values, rows of 16 words and one of padding
+  const unsigned tid = threadIdx.x, d = p.d, half = p.rot / 2, d16 = d / 16;
+
+  if (blockIdx.x >= p.page_wgs) {
+    // queries: a token per wave
+    const unsigned lane = tid % kWave, t = (blockIdx.x - p.page_wgs) * (TH / kWave) + tid / kWave;
+    __shared__ SinCos turn[TH / kWave][128];
+    int b = -1;
+    unsigned f0 = t;
+    if (t < p.T) {
+      b = (int)t;
+      if (p.first != nullptr) {
+        b = wave_search(p.B + 1, t, [&](unsigned i) { return first_at(p.first, i, p.T); });
+        if (b >= (int)p.B) b = -1;                    // a row that belongs to no sequence
+        if (b >= 0) f0 = first_at(p.first, b, p.T);
+      }
+    }
+    if (b >= 0) {
+      const double pos = (double)((long long)p.held[b] + (long long)(t - f0));
+      for (unsigned i = lane; i < half; i += kWave) turn[tid / kWave][i] = sincos_f64(pos * (double)p.freq[i]);
+    }
+    __syncthreads();
+    if (b < 0) return;
+    const T* src = static_cast<const T*>(p.q) + (size_t)t * p.ldq;
+    T* dst = static_cast<T*>(p.q_out) + (size_t)t * p.heads * d;
+    for (unsigned i = lane; i < p.heads * d16; i += kWave) {
+      const unsigned h = i / d16, u = i % d16;
+      unsigned one, two;
+      groups_of(u, p.rot, p.interleaved, one, two);
+      float x[16];
+      load8<DT>(src + h * d + one, x);
+      load8<DT>(src + h * d + two, x + 8);
+      rotate16(x, u, p.rot, p.interleaved, [&](unsigned j) { return turn[tid / kWave][j]; });
+      store8<DT>(dst + h * d + one, x);
+      store8<DT>(dst + h * d + two, x + 8);
+    }
+    return;
+  }
+
+  const unsigned slot = blockIdx.x / p.kv_heads, h = blockIdx.x % p.kv_heads;
+  int b = (int)slot;
+  unsigned f0 = slot, n = 1, local = 0;
+  if (p.first != nullptr) {
+    auto base = [&](unsigned i) { return first_at(p.first, i, p.T) / p.slot_tokens + p.slot_more * i; };
+    b = wave_search(p.B, slot, base);
+    if (b < 0) return;
+    f0 = first_at(p.first, b, p.T);
+    const unsigned f1 = first_at(p.first, b + 1, p.T);
+    n = f1 > f0 ? f1 - f0 : 0;
+    local = slot - (f0 / p.slot_tokens + p.slot_more * (unsigned)b);
+  }
+  const long long held = p.held[b];
+  const long long page = (held >> 6) + local, p0 = page * kKvBlock;
+  const long long t0 = held > p0 ? held : p0, t1 = held + n < p0 + kKvBlock ? held + n : p0 + kKvBlock;
+  if (t0 >= t1) return;
+  const unsigned lo = (unsigned)(t0 - p0), hi = (unsigned)(t1 - p0), row0 = f0 + (unsigned)(t0 - held);
+  int block = -1;
+  if (page >= 0 && page < (long long)p.table_width) block = p.table[(size_t)b * p.table_width + page];
+  const bool cached = block >= 0 && (size_t)block < p.blocks;
+  const size_t at = (size_t)(cached ? block : 0) * p.kv_heads + h;
+  const float2 had = reinterpret_cast<const float2*>(p.amax)[at];
+
+  const T* kin = static_cast<const T*>(p.k) + (size_t)row0 * p.ldk + (size_t)h * d;
+  const T* vin = static_cast<const T*>(p.v) + (size_t)row0 * p.ldv + (size_t)h * d;
+  T* kout = p.k_out == nullptr ? nullptr : static_cast<T*>(p.k_out) + ((size_t)row0 * p.kv_heads + h) * d;
+  const size_t ko = (size_t)p.kv_heads * d;
+  // chunks of CG groups of four tokens, from the first group with a new token
+  const unsigned CG = kTable ? (d > 128 ? 1 : 2) : 16, g_first = lo / 4, g_end = (hi + 3) / 4, d2 = d / 2;
+  const unsigned chunks = (g_end - g_first + CG - 1) / CG;
+  float kx[KI][16], vx[VI][2][4];
+  // keys [t, end) and value groups of chunk c; `out`: rotated keys leave as well
+  auto bring = [&](unsigned c, bool out) {
+    const unsigned ga = g_first + c * CG, ta = max(lo, 4 * ga), tb = min(hi, 4 * (ga + CG));
+    if constexpr (kTable) {
+      __syncthreads();
+      for (unsigned i = tid; i < (tb - ta) * half; i += TH)
+        table[i] = sincos_f64((double)(p0 + ta + i / half) * (double)p.freq[i % half]);
+      __syncthreads();
+    }
+#pragma unroll
+    for (int i = 0; i < KI; ++i) {
+      const unsigned item = tid + i * TH, t = ta + item / d16, u = item % d16;
+      if (t < tb) {
+        unsigned one, two;
+        groups_of(u, p.rot, p.interleaved, one, two);
+        load8<DT>(kin + (size_t)(t - lo) * p.ldk + one, kx[i]);
+        load8<DT>(kin + (size_t)(t - lo) * p.ldk + two, kx[i] + 8);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < VI; ++i) {
+      const unsigned item = tid + i * TH, g = ga + item / d2, col = item % d2 * 2;
+      if (g < ga + CG && g < g_end)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const unsigned t = min(max(4 * g + j, lo), hi - 1);        // (others' places are not used)
+          typedef T t2 __attribute__((ext_vector_type(2)));
+          const t2 v = *reinterpret_cast<const t2*>(vin + (size_t)(t - lo) * p.ldv + col);
+          vx[i][0][j] = (float)v[0];
+          vx[i][1][j] = (float)v[1];
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < KI; ++i) {
+      const unsigned item = tid + i * TH, t = ta + item / d16, u = item % d16;
+      if (t < tb) {
+        rotate16(kx[i], u, p.rot, p.interleaved, [&](unsigned j) -> SinCos {
+          if constexpr (kTable) return table[(t - ta) * half + j];
+          return sincos_f64((double)(p0 + t) * (double)p.freq[j]);
+        });
+        if (out && kout != nullptr) {
+          unsigned one, two;
+          groups_of(u, p.rot, p.interleaved, one, two);
+          store8<DT>(kout + (size_t)(t - lo) * ko + one, kx[i]);
+          store8<DT>(kout + (size_t)(t - lo) * ko + two, kx[i] + 8);
+        }
+      }
+    }
+  };
+  float mk = 0.f, mv = 0.f;
+  for (unsigned c = 0; c < chunks; ++c) {
+    bring(c, true);
+    const unsigned ga = g_first + c * CG, ta = max(lo, 4 * ga), tb = min(hi, 4 * (ga + CG));
+#pragma unroll
+    for (int i = 0; i < KI; ++i)
+      if (ta + (tid + i * TH) / d16 < tb)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) mk = fmaxf(mk, finite_abs(kx[i][j]));
+#pragma unroll
+    for (int i = 0; i < VI; ++i) {
+      const unsigned g = ga + (tid + i * TH) / d2;
+      if (g < ga + CG && g < g_end)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) mv = fmaxf(mv, fmaxf(finite_abs(vx[i][0][j]), finite_abs(vx[i][1][j])));
+    }
+  }
+  mk = wave_max_f(mk);
+  mv = wave_max_f(mv);
+  if constexpr (TH > kWave) {
+    if (tid % kWave == 0) {
+      red[0][tid / kWave] = mk;
+      red[1][tid / kWave] = mv;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < TH / kWave; ++w) {
+      mk = fmaxf(mk, red[0][w]);
+      mv = fmaxf(mv, red[1][w]);
+    }
+  }
+  if (!cached) return;
+  const bool fresh = lo == 0;
+  if (!fresh) {
+    mk = fmaxf(mk, had.x);
+    mv = fmaxf(mv, had.y);
+  }
+  if (tid == 0) reinterpret_cast<float2*>(p.amax)[at] = make_float2(mk, mv);
+  auto mult = [](float a) { return a > 0.f ? __fdiv_rn(127.f, a) : 1.f; };
+  const float ck = mult(mk), cv = mult(mv);
+  const unsigned dk = kv_dk(d), kwords4 = kKvBlock * dk / 16, vwords4 = d * kKvBlock / 16;      // (kv_dv(d) is d)
+  int8_t* keys = p.keys + at * kKvBlock * dk;
+  unsigned* values = reinterpret_cast<unsigned*>(p.values) + at * d * (kKvBlock / 4);
+  // a block that starts anew is zero but for the new tokens; one whose maximum grew is requantized
+  const bool whole = hi - lo == (unsigned)kKvBlock, by_image = !kTable && fresh;
+  if (fresh) {
+    if (!whole || dk != d)
+      for (unsigned i = tid; i < kwords4; i += TH) reinterpret_cast<w4*>(keys)[i] = w4{};
+    if (by_image) {
+      if (!whole)
+        for (unsigned i = tid; i < d * 17; i += TH) image[i] = 0;
+    } else {
+      for (unsigned i = tid; i < vwords4; i += TH) reinterpret_cast<w4*>(values)[i] = w4{};
+    }
+  } else {
+    auto again = [&](w4* at, unsigned count, float ratio) {
+      for (unsigned i = tid; i < count; i += TH) {
+        w4 w = at[i];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = requant4(w[j], ratio);
+        at[i] = w;
+      }
+    };
+    if (mk > had.x) again(reinterpret_cast<w4*>(keys), kwords4, __fdiv_rn(had.x, mk));
+    if (mv > had.y) again(reinterpret_cast<w4*>(values), vwords4, __fdiv_rn(had.y, mv));
+  }
+  __syncthreads();                                    // before the new tokens' places are written
+  for (unsigned c = 0; c < chunks; ++c) {
+    if (chunks > 1) bring(c, false);
+    const unsigned ga = g_first + c * CG, ta = max(lo, 4 * ga), tb = min(hi, 4 * (ga + CG));
+#pragma unroll
+    for (int i = 0; i < KI; ++i) {
+      const unsigned item = tid + i * TH, t = ta + item / d16;
+      if (t < tb) {
+        unsigned one, two;
+        groups_of(item % d16, p.rot, p.interleaved, one, two);
+        const float (&x)[16] = kx[i];
+        const w2 a = {pack4(x[0], x[1], x[2], x[3], ck), pack4(x[4], x[5], x[6], x[7], ck)},
+                 b2 = {pack4(x[8], x[9], x[10], x[11], ck), pack4(x[12], x[13], x[14], x[15], ck)};
+        *reinterpret_cast<w2*>(keys + t * dk + one) = a;
+        *reinterpret_cast<w2*>(keys + t * dk + two) = b2;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < VI; ++i) {
+      const unsigned item = tid + i * TH, g = ga + item / d2, col = item % d2 * 2, word = kv_place(4 * g) / 4;
+      if (g < ga + CG && g < g_end) {
+        // bytes of the word that are new
+        const unsigned from = 4 * g < lo ? lo - 4 * g : 0, end = 4 * g + 4 > hi ? hi - 4 * g : 4;
+        const unsigned mask = (end == 4 ? 0xFFFFFFFFu : (1u << (8 * end)) - 1) & ~((1u << (8 * from)) - 1);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const unsigned w = pack4(vx[i][j][0], vx[i][j][1], vx[i][j][2], vx[i][j][3], cv) & mask;
+          if (by_image) {
+            image[(col + j) * 17 + word] = w;
+          } else {
+            unsigned* to = values + (col + j) * (kKvBlock / 4) + word;
+            *to = mask == 0xFFFFFFFFu || fresh ? w : (*to & ~mask) | w;
+          }
+        }
+      }
+    }
+  }
+  if (by_image) {
+    __syncthreads();
+    for (unsigned i = tid; i < vwords4; i += TH) {
+      const unsigned* from = image + i / 4 * 17 + i % 4 * 4;
+      reinterpret_cast<w4*>(values)[i] = w4{from[0], from[1], from[2], from[3]};
+    }
+  }
+}
+
 }  // namespace
 
 int launch_kv_append(const mq_kv_cache& cache, const int32_t* table, size_t table_width, const int32_t* first,
                      const int32_t* held, size_t B, size_t T, const void* k, size_t ldk, const void* v, size_t ldv,
                      const void* q, size_t ldq, int heads, int dtype, const float* freq, size_t rot, int interleaved,
                      void* k_out, void* q_out, hipStream_t s) {
-  const size_t slots = first == nullptr ? B : T / kKvBlock + 2 * B;
-  const size_t page_wgs = slots * (size_t)cache.kv_heads;
-  const size_t q_wgs = q == nullptr ? 0 : (T + kTokensPerWg - 1) / kTokensPerWg;
+  // A sequence of n tokens touches at most n / 64 + 2 blocks, and no more than n: slots by whichever is fewer in all.  The
+  // latter means few tokens to a block.
+  const bool few = first == nullptr || T < T / kKvBlock + 2 * B;
+  const size_t slots = first == nullptr ? B : few ? T : T / kKvBlock + 2 * B;
+  const size_t page_wgs = slots * (size_t)cache.kv_heads, d = cache.head_dim;
+  const size_t piece = 16 / elem_bytes(dtype);
+  auto whole = [&](const void* x, size_t ld) { return reinterpret_cast<uintptr_t>(x) % 16 == 0 && ld % piece == 0; };
+  const bool rows = d % 16 == 0 && rot % 16 == 0 && whole(k, ldk) && whole(v, ldv) && whole(k_out, 0) &&
+                    (q == nullptr || (whole(q, ldq) && whole(q_out, 0)));
+  const size_t q_tokens = rows && few ? 1 : kTokensPerWg, q_wgs = q == nullptr ? 0 : (T + q_tokens - 1) / q_tokens;
   if (page_wgs + q_wgs >= (size_t)1 << 31) return MQ_ERR_SHAPE;
-  AppendParams p{k, v, q, table, first, held, freq, ldk, ldv, ldq, table_width, cache.blocks, cache.keys, cache.values,
-                 cache.amax, k_out, q_out, (unsigned)B, (unsigned)T, (unsigned)cache.kv_heads, (unsigned)heads,
-                 (unsigned)cache.head_dim, (unsigned)rot, (unsigned)page_wgs, interleaved};
-  const size_t tokens = first == nullptr ? 1 : T < (size_t)kKvBlock ? T : (size_t)kKvBlock;      // of one block, at most
-  const size_t lds = 2 * tokens * (cache.head_dim + 1) * sizeof(float);
+  const AppendParams p{k, v, q, table, first, held, freq, ldk, ldv, ldq, table_width, cache.blocks, cache.keys, cache.values,
+                       cache.amax, k_out, q_out, (unsigned)B, (unsigned)T, (unsigned)cache.kv_heads, (unsigned)heads,
+                       (unsigned)d, (unsigned)rot, (unsigned)page_wgs, few ? 1u : (unsigned)kKvBlock, few ? 0u : 2u, interleaved};
+  const unsigned wgs = (unsigned)(page_wgs + q_wgs);
   return with_dtype(dtype, [&](auto dt) {
-    auto kern = k_kv_append<decltype(dt)::value>;
+    constexpr int DT = decltype(dt)::value;
+    if (rows) {
+      auto go = [&](auto kern, int threads) { hipLaunchKernelGGL(kern, dim3(wgs), dim3(threads), 0, s, p); };
+      if (few) go(k_kv_append_rows<DT, 64, 1, 2>, 64);
+      else if (d <= 64) go(k_kv_append_rows<DT, 256, 1, 2>, 256);
+      else if (d <= 128) go(k_kv_append_rows<DT, 256, 2, 4>, 256);
+      else go(k_kv_append_rows<DT, 256, 4, 8>, 256);
+      return check_hip(hipGetLastError());
+    }
+    const size_t tokens = first == nullptr ? 1 : T < (size_t)kKvBlock ? T : (size_t)kKvBlock;      // of one block, at most
+    const size_t lds = 2 * tokens * (d + 1) * sizeof(float);
+    auto kern = k_kv_append<DT>;
     if (lds > 65536) {
       const int rc = check_hip(hipFuncSetAttribute(reinterpret_cast<const void*>(kern),
                                                    hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
       if (rc != MQ_OK) return rc;
     }
-    hipLaunchKernelGGL(kern, dim3((unsigned)(page_wgs + q_wgs)), dim3(kT), lds, s, p);
+    hipLaunchKernelGGL(kern, dim3(wgs), dim3(kT), lds, s, p);
     return check_hip(hipGetLastError());
   });
 }
