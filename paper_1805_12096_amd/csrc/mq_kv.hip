@@ -337,7 +337,8 @@ __global__ __launch_bounds__(TH) void k_kv_append_rows(const AppendParams p) {
   const unsigned slot = blockIdx.x / p.kv_heads, h = blockIdx.x % p.kv_heads;
   int b = (int)slot;
   unsigned f0 = slot, n = 1, local = 0;
-  if (p.first != nullptr) {
+  long long held = p.held[min(slot, p.B - 1)];        // (right where every sequence in front has one token: no search then)
+  if (p.first != nullptr && !(kTable && slot < p.B && first_at(p.first, slot, p.T) == slot && first_at(p.first, slot + 1, p.T) == slot + 1)) {
     auto base = [&](unsigned i) { return first_at(p.first, i, p.T) / p.slot_tokens + p.slot_more * i; };
     b = wave_search(p.B, slot, base);
     if (b < 0) return;
@@ -345,18 +346,14 @@ __global__ __launch_bounds__(TH) void k_kv_append_rows(const AppendParams p) {
     const unsigned f1 = first_at(p.first, b + 1, p.T);
     n = f1 > f0 ? f1 - f0 : 0;
     local = slot - (f0 / p.slot_tokens + p.slot_more * (unsigned)b);
+    held = p.held[b];
   }
-  const long long held = p.held[b];
   const long long page = (held >> 6) + local, p0 = page * kKvBlock;
   const long long t0 = held > p0 ? held : p0, t1 = held + n < p0 + kKvBlock ? held + n : p0 + kKvBlock;
   if (t0 >= t1) return;
   const unsigned lo = (unsigned)(t0 - p0), hi = (unsigned)(t1 - p0), row0 = f0 + (unsigned)(t0 - held);
   int block = -1;
   if (page >= 0 && page < (long long)p.table_width) block = p.table[(size_t)b * p.table_width + page];
-  const bool cached = block >= 0 && (size_t)block < p.blocks;
-  const size_t at = (size_t)(cached ? block : 0) * p.kv_heads + h;
-  const float2 had = reinterpret_cast<const float2*>(p.amax)[at];
-
   const T* kin = static_cast<const T*>(p.k) + (size_t)row0 * p.ldk + (size_t)h * d;
   const T* vin = static_cast<const T*>(p.v) + (size_t)row0 * p.ldv + (size_t)h * d;
   T* kout = p.k_out == nullptr ? nullptr : static_cast<T*>(p.k_out) + ((size_t)row0 * p.kv_heads + h) * d;
@@ -415,8 +412,28 @@ __global__ __launch_bounds__(TH) void k_kv_append_rows(const AppendParams p) {
     }
   };
   float mk = 0.f, mv = 0.f;
+  bring(0, true);
+  // (the block's number is on its way meanwhile)
+  const bool cached = block >= 0 && (size_t)block < p.blocks, fresh = lo == 0;
+  const size_t at = (size_t)(cached ? block : 0) * p.kv_heads + h;
+  const float2 had = reinterpret_cast<const float2*>(p.amax)[at];
+  const unsigned dk = kv_dk(d), kwords4 = kKvBlock * dk / 16, vwords4 = d * kKvBlock / 16;      // (kv_dv(d) is d)
+  int8_t* keys = p.keys + at * kKvBlock * dk;
+  unsigned* values = reinterpret_cast<unsigned*>(p.values) + at * d * (kKvBlock / 4);
+  // the words of values that the first chunk's tokens share with others
+  unsigned old[VI][2] = {};
+  if (!fresh)
+#pragma unroll
+    for (int i = 0; i < VI; ++i) {
+      if (kTable) {
+        const unsigned g = g_first + (tid + i * TH) / d2, col = (tid + i * TH) % d2 * 2;
+        const bool some = g < g_first + CG && g < g_end;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) old[i][j] = values[((some ? col : 0) + j) * (kKvBlock / 4) + (some ? kv_place(4 * g) / 4 : 0)];
+      }
+    }
   for (unsigned c = 0; c < chunks; ++c) {
-    bring(c, true);
+    if (c > 0) bring(c, true);
     const unsigned ga = g_first + c * CG, ta = max(lo, 4 * ga), tb = min(hi, 4 * (ga + CG));
 #pragma unroll
     for (int i = 0; i < KI; ++i)
@@ -446,7 +463,6 @@ __global__ __launch_bounds__(TH) void k_kv_append_rows(const AppendParams p) {
     }
   }
   if (!cached) return;
-  const bool fresh = lo == 0;
   if (!fresh) {
     mk = fmaxf(mk, had.x);
     mv = fmaxf(mv, had.y);
@@ -454,9 +470,6 @@ __global__ __launch_bounds__(TH) void k_kv_append_rows(const AppendParams p) {
   if (tid == 0) reinterpret_cast<float2*>(p.amax)[at] = make_float2(mk, mv);
   auto mult = [](float a) { return a > 0.f ? __fdiv_rn(127.f, a) : 1.f; };
   const float ck = mult(mk), cv = mult(mv);
-  const unsigned dk = kv_dk(d), kwords4 = kKvBlock * dk / 16, vwords4 = d * kKvBlock / 16;      // (kv_dv(d) is d)
-  int8_t* keys = p.keys + at * kKvBlock * dk;
-  unsigned* values = reinterpret_cast<unsigned*>(p.values) + at * d * (kKvBlock / 4);
   // a block that starts anew is zero but for the new tokens; one whose maximum grew is requantized
   const bool whole = hi - lo == (unsigned)kKvBlock, by_image = !kTable && fresh;
   if (fresh) {
@@ -511,7 +524,8 @@ __global__ __launch_bounds__(TH) void k_kv_append_rows(const AppendParams p) {
             image[(col + j) * 17 + word] = w;
           } else {
             unsigned* to = values + (col + j) * (kKvBlock / 4) + word;
-            *to = mask == 0xFFFFFFFFu || fresh ? w : (*to & ~mask) | w;
+            const bool kept = kTable && chunks == 1 && !(mv > had.y);        // (what was read early still holds)
+            *to = mask == 0xFFFFFFFFu || fresh ? w : ((kept ? old[i][j] : *to) & ~mask) | w;
           }
         }
       }

@@ -124,12 +124,17 @@ CASES = [  # heads, kv heads, dim, rot, interleaved, new tokens, held
     (2, 1, 33, 8, True, [17, 90], [40, 3]),
     (2, 2, 256, 256, False, [64, 65, 1], [0, 10, 2]),
     (16, 4, 80, 40, False, [9] * 70, list(range(70))),
+    (8, 4, 128, 64, True, [1] * 30 + [40, 1, 0, 3], list(range(25, 59))),       # few tokens to a block, but for one
+    (4, 2, 256, 256, False, [1, 1, 7, 1, 20], [63, 64, 60, 127, 50]),
+    (2, 2, 48, 16, False, [64, 128, 1], [0, 32, 5]),
+    (4, 2, 160, 32, True, [100, 33], [0, 64]),
 ]
 
 
+@pytest.mark.parametrize("extra", [5, 16])           # rows of any alignment, and of whole 16-byte pieces
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("case", CASES)
-def test_append_is_the_rule_bit_for_bit(case, dtype):
+def test_append_is_the_rule_bit_for_bit(case, dtype, extra):
     heads, hk, dim, rot, inter, new, held = case
     g = gen(sum(new) + dim)
     B, rounds = len(new), 3
@@ -147,7 +152,7 @@ def test_append_is_the_rule_bit_for_bit(case, dtype):
     freq = torch.tensor(10000.0 ** (-np.arange(0, rot, 2) / max(rot, 1)), dtype=F32)
     # front and back rows that belong to nobody, and columns of one wide product
     front, back = 2, 3
-    width_all = (heads + 2 * hk) * dim + 5
+    width_all = (heads + 2 * hk) * dim + extra
     at = list(held)
     for step in range(rounds):
         T = sum(new) + front + back
