@@ -10,8 +10,7 @@
 // Rows of whole 16-byte pieces (k_kv_append_rows): what a workgroup rotates and quantizes stays in registers between the two
 // maxima and the stores.  A thread has 16 elements of a key, the two groups of 8 that are rotated together, and for the values
 // 4 tokens x 2 columns, whose bytes are one word of a row of the cache each.  256 threads take a block at once; where a call
-// brings few tokens to a block, 64 threads take 8 (4 for wide heads) at a time, sines and cosines formed by all of them in LDS
-// (with more tokens every thread forms its own: a pair is used once).  Other rows: k_kv_append, element by element.
+// brings few tokens to a block, 64 threads take 8 (4 for wide heads) at a time, sines and cosines formed by all of them in LDS.  Other rows: k_kv_append, element by element.
 #include <type_traits>
 
 #include "mq_glue.h"
@@ -292,8 +291,9 @@ template <int DT, int TH, int KI, int VI>
 __global__ __launch_bounds__(TH) void k_kv_append_rows(const AppendParams p) {
   using T = typename Elem<DT>::T;
   constexpr bool kTable = TH == kWave;                // (one wave: no table or maximum crosses waves)
-  constexpr int kTableSize = 512;
-  __shared__ SinCos table[kTable ? kTableSize : 1];
+  // sines and cosines: of a chunk's tokens, or of every eighth position of the block and of 0 .. 7, whose products are all
+  // (angles are exact: 24 bits of frequency times 29 of position)
+  extern __shared__ SinCos table[];
   __shared__ float red[2][TH / kWave];
   __shared__ unsigned image[kTable ? 1 : 256 * 17];   // a block of values, rows of 16 words and one of padding
   const unsigned tid = threadIdx.x, d = p.d, half = p.rot / 2, d16 = d / 16;
@@ -320,16 +320,28 @@ __global__ __launch_bounds__(TH) void k_kv_append_rows(const AppendParams p) {
     if (b < 0) return;
     const T* src = static_cast<const T*>(p.q) + (size_t)t * p.ldq;
     T* dst = static_cast<T*>(p.q_out) + (size_t)t * p.heads * d;
-    for (unsigned i = lane; i < p.heads * d16; i += kWave) {
-      const unsigned h = i / d16, u = i % d16;
-      unsigned one, two;
-      groups_of(u, p.rot, p.interleaved, one, two);
-      float x[16];
-      load8<DT>(src + h * d + one, x);
-      load8<DT>(src + h * d + two, x + 8);
-      rotate16(x, u, p.rot, p.interleaved, [&](unsigned j) { return turn[tid / kWave][j]; });
-      store8<DT>(dst + h * d + one, x);
-      store8<DT>(dst + h * d + two, x + 8);
+    constexpr int F = 4;                              // in flight
+    const unsigned items = p.heads * d16;
+    for (unsigned i0 = lane; i0 < items; i0 += F * kWave) {
+      float x[F][16];
+      unsigned one[F], two[F], u[F];
+#pragma unroll
+      for (int f = 0; f < F; ++f) {
+        const unsigned i = min(i0 + f * kWave, items - 1);
+        u[f] = i % d16;
+        groups_of(u[f], p.rot, p.interleaved, one[f], two[f]);
+        one[f] += i / d16 * d;
+        two[f] += i / d16 * d;
+        load8<DT>(src + one[f], x[f]);
+        load8<DT>(src + two[f], x[f] + 8);
+      }
+#pragma unroll
+      for (int f = 0; f < F; ++f) {
+        if (i0 + f * kWave >= items) break;
+        rotate16(x[f], u[f], p.rot, p.interleaved, [&](unsigned j) { return turn[tid / kWave][j]; });
+        store8<DT>(dst + one[f], x[f]);
+        store8<DT>(dst + two[f], x[f] + 8);
+      }
     }
     return;
   }
@@ -370,6 +382,12 @@ __global__ __launch_bounds__(TH) void k_kv_append_rows(const AppendParams p) {
       for (unsigned i = tid; i < (tb - ta) * half; i += TH)
         table[i] = sincos_f64((double)(p0 + ta + i / half) * (double)p.freq[i % half]);
       __syncthreads();
+    } else {
+      const double eighth = (double)p0;
+      for (unsigned i = tid; i < 16 * half; i += TH) {
+        const unsigned k = i / half;
+        table[i] = sincos_f64((k < 8 ? eighth + 8 * k : (double)(k - 8)) * (double)p.freq[i % half]);
+      }
     }
 #pragma unroll
     for (int i = 0; i < KI; ++i) {
@@ -394,13 +412,15 @@ __global__ __launch_bounds__(TH) void k_kv_append_rows(const AppendParams p) {
           vx[i][1][j] = (float)v[1];
         }
     }
+    if constexpr (!kTable) __syncthreads();
 #pragma unroll
     for (int i = 0; i < KI; ++i) {
       const unsigned item = tid + i * TH, t = ta + item / d16, u = item % d16;
       if (t < tb) {
         rotate16(kx[i], u, p.rot, p.interleaved, [&](unsigned j) -> SinCos {
           if constexpr (kTable) return table[(t - ta) * half + j];
-          return sincos_f64((double)(p0 + t) * (double)p.freq[j]);
+          const SinCos a = table[t / 8 * half + j], b = table[(8 + t % 8) * half + j];
+          return {a.sin * b.cos + a.cos * b.sin, a.cos * b.cos - a.sin * b.sin};
         });
         if (out && kout != nullptr) {
           unsigned one, two;
@@ -564,7 +584,8 @@ int launch_kv_append(const mq_kv_cache& cache, const int32_t* table, size_t tabl
   return with_dtype(dtype, [&](auto dt) {
     constexpr int DT = decltype(dt)::value;
     if (rows) {
-      auto go = [&](auto kern, int threads) { hipLaunchKernelGGL(kern, dim3(wgs), dim3(threads), 0, s, p); };
+      const size_t table = few ? 512 * sizeof(SinCos) : 16 * (rot / 2) * sizeof(SinCos);
+      auto go = [&](auto kern, int threads) { hipLaunchKernelGGL(kern, dim3(wgs), dim3(threads), table, s, p); };
       if (few) go(k_kv_append_rows<DT, 64, 1, 2>, 64);
       else if (d <= 64) go(k_kv_append_rows<DT, 256, 1, 2>, 256);
       else if (d <= 128) go(k_kv_append_rows<DT, 256, 2, 4>, 256);
