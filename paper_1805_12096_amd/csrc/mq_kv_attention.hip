@@ -12,8 +12,10 @@
 //     maximum: a long run of small probabilities keeps its bits.)
 //   * the sums of a block are exact integers; block scales, the rescaling of the softmax and the digits' weights are one
 //     multiply-add per element of the 16 x dv result.
-// No LDS and no exchange between lanes inside the loop but the maximum over four lane groups.  A wave takes every W-th block of
-// a sequence; the four waves of a workgroup join in LDS, the workgroups of a split sequence through the workspace.
+// No LDS and no exchange between lanes inside the loop but the maximum over four lane groups.  The next block's keys are asked for
+// as soon as this one's are multiplied, its values likewise; which blocks they are a wave reads 64 at a time.  A workgroup takes
+// `run` neighbouring blocks of a sequence, its waves in turn; they join in LDS, the workgroups of a sequence through the
+// workspace.  Runs are equally long whatever the sequences' lengths, so that long and short ones keep the chip busy to the end.
 #include <type_traits>
 
 #include "mq_gemm_common.h"
@@ -24,7 +26,7 @@ namespace mq {
 
 namespace {
 
-constexpr int kW = 4;                 // waves of a workgroup
+constexpr int kW = 4;                 // waves of a workgroup, at most
 constexpr int kRows = 16;             // query rows of a wave
 
 struct CachedParams {
@@ -33,25 +35,46 @@ struct CachedParams {
   const int32_t *table, *lens;
   const void* q;
   void* out;
-  float* part;                        // [B][heads][splits][dv + 2]: sums, maximum, total
+  float* part;                        // [B][heads][splits][dv + 2]: sums, maximum, total; splits runs of `run` blocks
   size_t ldq, ldo, table_width, blocks;
-  unsigned max_len, kv_heads, heads, d, splits;
+  unsigned max_len, kv_heads, heads, d, splits, run;
   float scale2;                       // scale log2(e)
+  int vec;                            // rows of queries are whole 16-byte pieces
 };
 
 // the largest sum of digits 256^i that NP signed bytes hold whatever the lower ones are
 template <int NP>
 constexpr float kDigits = NP == 2 ? 127.f * 256.f : 127.f * 65536.f;
 
-// digits of n, least significant first, one byte each into byte `at` of w[0 .. NP)
+// Byte i of four words, for i < NP, as the four bytes of w[i].
 template <int NP>
-__device__ __forceinline__ void put_digits(int n, int at, unsigned (&w)[NP]) {
+__device__ __forceinline__ void gather_bytes(const unsigned (&x)[4], unsigned (&w)[NP]) {
+  const unsigned a = __builtin_amdgcn_perm(x[1], x[0], 0x05010400u), b = __builtin_amdgcn_perm(x[3], x[2], 0x05010400u);
+  w[0] = __builtin_amdgcn_perm(b, a, 0x05040100u);
+  w[1] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+  if constexpr (NP == 3)
+    w[2] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(x[3], x[2], 0x0C0C0602u), __builtin_amdgcn_perm(x[1], x[0], 0x0C0C0602u), 0x05040100u);
+}
+// Signed digits of four integers: adding 128 at every place makes the bytes the digits plus 128.
+template <int NP>
+__device__ __forceinline__ void digits_of(const int (&n)[4], unsigned (&w)[NP]) {
+  unsigned x[4];
 #pragma unroll
-  for (int i = 0; i < NP; ++i) {
-    const int low = i + 1 < NP ? (int)(int8_t)n : n;
-    w[i] |= ((unsigned)low & 255u) << (8 * at);
-    n = (n - low) >> 8;
-  }
+  for (int j = 0; j < 4; ++j) x[j] = (unsigned)n[j] + (NP == 3 ? 0x808080u : 0x8080u);
+  gather_bytes<NP>(x, w);
+#pragma unroll
+  for (int i = 0; i < NP; ++i) w[i] ^= 0x80808080u;
+}
+// The same of e kDigits, 0 <= e <= 1, rounded: the sum with 2^23 and the 128s has units as its last place, so the multiply-add
+// rounds and the bytes of its result are the digits plus 128 (the third, whose 128 is 2^23 itself, is the digit).
+template <int NP>
+__device__ __forceinline__ void digits_of_share(const float (&e)[4], unsigned (&w)[NP]) {
+  unsigned x[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) x[j] = __float_as_uint(fmaf(e[j], kDigits<NP>, NP == 3 ? 8421504.f : 8388608.f + 32896.f));
+  gather_bytes<NP>(x, w);
+  w[0] ^= 0x80808080u;
+  w[1] ^= 0x80808080u;
 }
 template <int NP>
 __device__ __forceinline__ float join_digits(const v4i (&a)[NP], int r) {
@@ -73,9 +96,10 @@ __global__ __launch_bounds__(kW * kWave) void k_cached_attention(const CachedPar
   using T = typename Elem<DT>::T;
   constexpr int NP = DT == MQ_F32 ? 3 : 2;
   constexpr int ND = 4 * DC;          // 16-column pieces of a value row, at most
-  __shared__ float sums[kW][kRows][ND * 16 + 1];
-  __shared__ float stat[kW][2][kRows];
-  const unsigned lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  extern __shared__ float lds[];      // [waves][kRows][ND 16 + 1] sums, [waves][2][kRows] maxima and totals
+  const unsigned lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), waves = blockDim.x / kWave;
+  auto sums = [&](unsigned w, unsigned row, unsigned c) -> float& { return lds[(w * kRows + row) * (ND * 16 + 1) + c]; };
+  auto stat = [&](unsigned w, unsigned i, unsigned row) -> float& { return lds[waves * kRows * (ND * 16 + 1) + (w * 2 + i) * kRows + row]; };
   const unsigned col = lane % 16, grp = lane / 16;
   const unsigned split = blockIdx.x % p.splits, kvh = blockIdx.x / p.splits % p.kv_heads;
   const unsigned per = p.heads / p.kv_heads, tiles = (per + kRows - 1) / kRows;
@@ -85,20 +109,83 @@ __global__ __launch_bounds__(kW * kWave) void k_cached_attention(const CachedPar
   const unsigned len = len_any < 0 ? 0u : min((unsigned)len_any, p.max_len), nblocks = (len + kKvBlock - 1) / kKvBlock;
   const unsigned dk = kv_dk(d), dv = kv_dv(d), nd = dv / 16;
   const int32_t* table = p.table + (size_t)b * p.table_width;
+  // this workgroup's blocks [start, end), this wave's every waves-th of them
+  const unsigned start = split * p.run, end = min(start + p.run, nblocks);
+  if (split > 0 && start >= nblocks) return;           // (the first run answers for an empty sequence)
+  const unsigned mine = end > start + wave ? __builtin_amdgcn_readfirstlane((end - start - wave + waves - 1) / waves) : 0u;
+  int ids = 0;
+  auto look = [&](unsigned i) {                        // 64 of the wave's blocks, from its i-th on
+    const unsigned pg = start + wave + (i + lane) * waves;
+    ids = i + lane < mine ? table[pg] : 0;
+  };
+  if (mine > 0) look(0);
 
+  float acc[ND][4];
+  float top = -INFINITY, total = 0.f;
+#pragma unroll
+  for (int t = 0; t < ND; ++t)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) acc[t][r] = 0.f;
+  u4 kf[4][DC], vf[ND];
+  float2 am, am_next;
+  bool there, there_next;                              // whether the block is one
+  size_t at_next;
+  auto find = [&](unsigned i) {                        // the wave's i-th block
+    if (i % kWave == 0 && i > 0) look(i);
+    const int block = __builtin_amdgcn_readlane(ids, i % kWave);
+    there_next = block >= 0 && (size_t)block < p.blocks;
+    at_next = (size_t)(there_next ? block : 0) * p.kv_heads + kvh;
+  };
+  auto bring_keys = [&] {
+    const int8_t* kp = p.keys + at_next * kKvBlock * dk + col * dk + grp * 16;
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int c = 0; c < DC; ++c) kf[t][c] = *reinterpret_cast<const u4*>(kp + (size_t)t * 16 * dk + c * 64);
+    am_next = reinterpret_cast<const float2*>(p.amax)[at_next];
+  };
+  auto bring_values = [&] {                            // lane l of piece t: row 16 t + l % 16, bytes 16 (l / 16) ..
+    const int8_t* vp = p.values + at_next * dv * kKvBlock + col * kKvBlock + grp * 16;
+#pragma unroll
+    for (int t = 0; t < ND; ++t)
+      if (t < (int)nd) vf[t] = *reinterpret_cast<const u4*>(vp + t * 16 * kKvBlock);
+  };
+  if (mine > 0) {
+    find(0);
+    bring_keys();
+    bring_values();
+  }
   // the query row of this lane's column, in digits
   v4i qd[DC][NP];
   float qscale;
   {
-    const T* src = static_cast<const T*>(p.q) + (size_t)b * p.ldq + (size_t)(head0 + col) * d;
+    const T* src = static_cast<const T*>(p.q) + (size_t)b * p.ldq + (size_t)(head0 + (col < rows ? col : 0)) * d;
     float x[DC][16], m = 0.f;
     bool bad = false;
+    // (loads in front of every choice: a load behind a condition is waited for on its own)
+    if (p.vec) {
+      constexpr int W = 16 / sizeof(T);
+      typedef T tw __attribute__((ext_vector_type(W)));
+#pragma unroll
+      for (int c = 0; c < DC; ++c)
+#pragma unroll
+        for (int j = 0; j < 16; j += W) {
+          const unsigned i = c * 64 + grp * 16 + j;
+          const tw v = *reinterpret_cast<const tw*>(src + (i < d ? i : 0));
+#pragma unroll
+          for (int k = 0; k < W; ++k) x[c][j + k] = (float)v[k];
+        }
+    } else {
+#pragma unroll
+      for (int c = 0; c < DC; ++c)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) x[c][j] = (float)src[c * 64 + grp * 16 + j < d ? c * 64 + grp * 16 + j : 0];
+    }
 #pragma unroll
     for (int c = 0; c < DC; ++c)
 #pragma unroll
       for (int j = 0; j < 16; ++j) {
-        const unsigned i = c * 64 + grp * 16 + j;
-        x[c][j] = col < rows && i < d ? (float)src[i] : 0.f;
+        if (col >= rows || c * 64 + grp * 16 + j >= d) x[c][j] = 0.f;
         bad |= !(fabsf(x[c][j]) <= 3.402823466e38f);
         m = fmaxf(m, fabsf(x[c][j]));
       }
@@ -111,35 +198,21 @@ __global__ __launch_bounds__(kW * kWave) void k_cached_attention(const CachedPar
     for (int c = 0; c < DC; ++c)
 #pragma unroll
       for (int w4 = 0; w4 < 4; ++w4) {
-        unsigned w[NP] = {};
+        unsigned w[NP];
+        int n[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) put_digits<NP>(m < INFINITY && fits ? (int)rintf(x[c][4 * w4 + j] * s) : 0, j, w);
+        for (int j = 0; j < 4; ++j) n[j] = m < INFINITY && fits ? (int)rintf(x[c][4 * w4 + j] * s) : 0;
+        digits_of<NP>(n, w);
 #pragma unroll
         for (int i = 0; i < NP; ++i) qd[c][i][w4] = (int)w[i];
       }
   }
 
-  float acc[ND][4];
-  float top = -INFINITY, total = 0.f;
-#pragma unroll
-  for (int t = 0; t < ND; ++t)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) acc[t][r] = 0.f;
-  for (unsigned pg = split * kW + wave; pg < nblocks; pg += p.splits * kW) {
-    const int block = table[pg];
-    if (block < 0 || (size_t)block >= p.blocks) continue;
-    const size_t at = (size_t)block * p.kv_heads + kvh;
-    const int8_t* kp = p.keys + at * kKvBlock * dk + col * dk + grp * 16;
-    const int8_t* vp = p.values + at * dv * kKvBlock + lane * 16;
-    const float2 am = reinterpret_cast<const float2*>(p.amax)[at];
-    u4 vf[ND];
-#pragma unroll
-    for (int t = 0; t < ND; ++t)
-      if (t < (int)nd) {
-        // lane l of piece t: row 16 t + l % 16, bytes 16 (l / 16) ..
-        vf[t] = *reinterpret_cast<const u4*>(p.values + at * dv * kKvBlock + (size_t)(16 * t + col) * kKvBlock + grp * 16);
-      }
-    (void)vp;
+  for (unsigned i = 0; i < mine; ++i) {
+    const unsigned pg = start + wave + i * waves;
+    am = am_next;
+    there = there_next;
+    if (i + 1 < mine) find(i + 1);
     float sc[4][4];
     float mt = -INFINITY;
     const float f = qscale * (am.x * (1.f / 127.f));
@@ -148,32 +221,41 @@ __global__ __launch_bounds__(kW * kWave) void k_cached_attention(const CachedPar
       v4i a[NP] = {};
 #pragma unroll
       for (int c = 0; c < DC; ++c) {
-        const u4 kf = *reinterpret_cast<const u4*>(kp + (size_t)t * 16 * dk + c * 64);
 #pragma unroll
-        for (int i = 0; i < NP; ++i) a[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(as_v4i(kf), qd[c][i], a[i], 0, 0, 0);
+        for (int j = 0; j < NP; ++j) a[j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(as_v4i(kf[t][c]), qd[c][j], a[j], 0, 0, 0);
       }
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const float x = join_digits<NP>(a, r) * f;
-        sc[t][r] = pg * kKvBlock + t * 16 + grp * 4 + r < len ? x : -INFINITY;
-        mt = fmaxf(mt, sc[t][r]);
+        sc[t][r] = join_digits<NP>(a, r) * f;
       }
     }
+    if (!there || (pg + 1) * kKvBlock > len)
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (!there || pg * kKvBlock + t * 16 + grp * 4 + r >= len) sc[t][r] = -INFINITY;
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) mt = fmaxf(mt, sc[t][r]);
+    if (i + 1 < mine) bring_keys();
     mt = groups_f(mt, fmax2);
     const float base = finite_or_0(mt);
     float lt = 0.f;
     v4i pd[NP];
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-      unsigned w[NP] = {};
+      unsigned w[NP];
+      float e[4];
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const float e = __builtin_amdgcn_exp2f(sc[t][r] - base);
-        lt += e;
-        put_digits<NP>((int)rintf(e * kDigits<NP>), r, w);
+        e[r] = __builtin_amdgcn_exp2f(sc[t][r] - base);
+        lt += e[r];
       }
+      digits_of_share<NP>(e, w);
 #pragma unroll
-      for (int i = 0; i < NP; ++i) pd[i][t] = (int)w[i];
+      for (int j = 0; j < NP; ++j) pd[j][t] = (int)w[j];
     }
     const float now = fmaxf(top, mt), keep = __builtin_amdgcn_exp2f(top - finite_or_0(now)),
                 in = __builtin_amdgcn_exp2f(mt - finite_or_0(now));
@@ -185,35 +267,34 @@ __global__ __launch_bounds__(kW * kWave) void k_cached_attention(const CachedPar
       if (t < (int)nd) {
         v4i a[NP] = {};
 #pragma unroll
-        for (int i = 0; i < NP; ++i) a[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(as_v4i(vf[t]), pd[i], a[i], 0, 0, 0);
+        for (int j = 0; j < NP; ++j) a[j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(as_v4i(vf[t]), pd[j], a[j], 0, 0, 0);
 #pragma unroll
         for (int r = 0; r < 4; ++r) acc[t][r] = fmaf(acc[t][r], keep, join_digits<NP>(a, r) * fv);
       }
+    if (i + 1 < mine) bring_values();
   }
   total = groups_f(total, fadd2);
 
-  // the four waves
+  // the waves
 #pragma unroll
   for (int t = 0; t < ND; ++t)
     if (t < (int)nd)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) sums[wave][col][16 * t + 4 * grp + r] = acc[t][r];
+      for (int r = 0; r < 4; ++r) sums(wave, col, 16 * t + 4 * grp + r) = acc[t][r];
   if (grp == 0) {
-    stat[wave][0][col] = top;
-    stat[wave][1][col] = total;
+    stat(wave, 0, col) = top;
+    stat(wave, 1, col) = total;
   }
   __syncthreads();
-  for (unsigned i = threadIdx.x; i < rows * dv; i += kW * kWave) {
+  for (unsigned i = threadIdx.x; i < rows * dv; i += blockDim.x) {
     const unsigned r = i / dv, c = i % dv;
     float m = -INFINITY, l = 0.f, x = 0.f;
-#pragma unroll
-    for (int w = 0; w < kW; ++w) m = fmaxf(m, stat[w][0][r]);
+    for (unsigned w = 0; w < waves; ++w) m = fmaxf(m, stat(w, 0, r));
     const float base = finite_or_0(m);
-#pragma unroll
-    for (int w = 0; w < kW; ++w) {
-      const float e = __builtin_amdgcn_exp2f(stat[w][0][r] - base);
-      l = fmaf(e, stat[w][1][r], l);
-      x = fmaf(e, sums[w][r][c], x);
+    for (unsigned w = 0; w < waves; ++w) {
+      const float e = __builtin_amdgcn_exp2f(stat(w, 0, r) - base);
+      l = fmaf(e, stat(w, 1, r), l);
+      x = fmaf(e, sums(w, r, c), x);
     }
     if (p.splits == 1) {
       if (c < d) static_cast<T*>(p.out)[(size_t)b * p.ldo + (size_t)(head0 + r) * d + c] = (T)(l == 0.f ? 0.f : __fdiv_rn(x, l));
@@ -235,10 +316,14 @@ __global__ __launch_bounds__(256) void k_cached_join(const CachedParams p) {
   const unsigned dv = kv_dv(p.d), c = threadIdx.x, b = blockIdx.x / p.heads, h = blockIdx.x % p.heads;
   if (c >= p.d) return;
   const float* part = p.part + (size_t)blockIdx.x * p.splits * (dv + 2);
+  // the runs that the sequence has
+  const int len_any = p.lens[b];
+  const unsigned len = len_any < 0 ? 0u : min((unsigned)len_any, p.max_len), tokens = p.run * kKvBlock;
+  const unsigned runs = max(1u, (len + tokens - 1) / tokens);
   float m = -INFINITY, l = 0.f, x = 0.f;
-  for (unsigned s = 0; s < p.splits; ++s) m = fmaxf(m, part[s * (dv + 2) + dv]);
+  for (unsigned s = 0; s < runs; ++s) m = fmaxf(m, part[s * (dv + 2) + dv]);
   const float base = finite_or_0(m);
-  for (unsigned s = 0; s < p.splits; ++s) {
+  for (unsigned s = 0; s < runs; ++s) {
     const float e = __builtin_amdgcn_exp2f(part[s * (dv + 2) + dv] - base);
     l = fmaf(e, part[s * (dv + 2) + dv + 1], l);
     x = fmaf(e, part[s * (dv + 2) + c], x);
@@ -246,40 +331,59 @@ __global__ __launch_bounds__(256) void k_cached_join(const CachedParams p) {
   static_cast<T*>(p.out)[(size_t)b * p.ldo + (size_t)h * p.d + c] = (T)(l == 0.f ? 0.f : __fdiv_rn(x, l));
 }
 
-// Workgroups that share a sequence: as many as it takes to give every compute unit two, while each wave still has a block.
-unsigned splits_of(size_t B, size_t max_len, int heads, int kv_heads) {
+// Blocks to a run, runs of the longest sequence, waves of a workgroup.  As many runs as fill the chip's 512 places for
+// workgroups once where all sequences are as long as they may be, while a wave still has a block: 32 sequences of 4000 .. 32000
+// tokens, 8 kv heads of 128, take 209 us with that many, 224 with twice as many and 247 with four times (a workgroup's start and
+// end), 311 with half.  One wave where two blocks are all there is.
+struct Split {
+  unsigned run, splits, waves;
+};
+Split split_of(size_t B, size_t max_len, int heads, int kv_heads) {
   const size_t per = (size_t)(heads / kv_heads), wgs = B * (size_t)kv_heads * ((per + kRows - 1) / kRows);
-  const size_t want = (512 + wgs - 1) / wgs, most = (max_len + kW * kKvBlock - 1) / (kW * kKvBlock);
-  return (unsigned)(want < most ? want : most);
+  const size_t blocks = (max_len + kKvBlock - 1) / kKvBlock, want = (512 + wgs - 1) / wgs;
+  size_t run = (blocks + want - 1) / want;
+  if (run < (size_t)kW) run = kW;
+  if (run > blocks) run = blocks;
+  return {(unsigned)run, (unsigned)((blocks + run - 1) / run), (unsigned)(run <= 2 ? 1 : run < (size_t)kW ? run : kW)};
 }
 
 }  // namespace
 
 size_t cached_attention_ws_bytes(size_t B, size_t max_len, int heads, int kv_heads, size_t d) {
-  const unsigned splits = splits_of(B, max_len, heads, kv_heads);
+  const unsigned splits = split_of(B, max_len, heads, kv_heads).splits;
   return splits == 1 ? 16 : B * (size_t)heads * splits * (kv_dv((unsigned)d) + 2) * sizeof(float);
 }
 
 int launch_cached_attention(const mq_kv_cache& cache, const int32_t* table, size_t table_width, const int32_t* lens, size_t B,
                             size_t max_len, const void* q, size_t ldq, int heads, int dtype, float scale, void* out,
                             size_t ldo, void* ws, hipStream_t s) {
-  const unsigned splits = splits_of(B, max_len, heads, cache.kv_heads);
+  const Split split = split_of(B, max_len, heads, cache.kv_heads);
+  const unsigned splits = split.splits;
   const size_t per = (size_t)(heads / cache.kv_heads);
   const size_t wgs = B * (size_t)cache.kv_heads * ((per + kRows - 1) / kRows) * splits;
   if (wgs >= (size_t)1 << 31 || B * (size_t)heads >= (size_t)1 << 31) return MQ_ERR_SHAPE;
+  const size_t piece = 16 / elem_bytes(dtype);
+  const int vec = cache.head_dim % piece == 0 && ldq % piece == 0 && reinterpret_cast<uintptr_t>(q) % 16 == 0;
   const CachedParams p{cache.keys, cache.values, cache.amax, table, lens, q, out, static_cast<float*>(ws), ldq, ldo,
                        table_width, cache.blocks, (unsigned)max_len, (unsigned)cache.kv_heads, (unsigned)heads,
-                       (unsigned)cache.head_dim, splits, scale * 1.44269504088896340736f};
+                       (unsigned)cache.head_dim, splits, split.run, scale * 1.44269504088896340736f, vec};
   return with_dtype(dtype, [&](auto dt) {
     constexpr int DT = decltype(dt)::value;
-    auto go = [&](auto kern) { hipLaunchKernelGGL(kern, dim3((unsigned)wgs), dim3(kW * kWave), 0, s, p); };
-    switch (kv_dk(p.d) / 64) {
+    const unsigned pieces = kv_dk(p.d) / 64;
+    const size_t lds = split.waves * kRows * (pieces * 64 + 1 + 2) * sizeof(float);
+    int rc = MQ_OK;
+    auto go = [&](auto kern) {
+      if (lds > 65536)
+        rc = check_hip(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+      if (rc == MQ_OK) hipLaunchKernelGGL(kern, dim3((unsigned)wgs), dim3(split.waves * kWave), lds, s, p);
+    };
+    switch (pieces) {
       case 1: go(k_cached_attention<DT, 1>); break;
       case 2: go(k_cached_attention<DT, 2>); break;
       case 3: go(k_cached_attention<DT, 3>); break;
       default: go(k_cached_attention<DT, 4>); break;
     }
-    int rc = check_hip(hipGetLastError());
+    if (rc == MQ_OK) rc = check_hip(hipGetLastError());
     if (rc != MQ_OK || splits == 1) return rc;
     hipLaunchKernelGGL((k_cached_join<DT>), dim3((unsigned)(B * (size_t)heads)), dim3(256), 0, s, p);
     return check_hip(hipGetLastError());
