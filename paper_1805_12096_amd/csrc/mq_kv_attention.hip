@@ -26,7 +26,9 @@ namespace mq {
 
 namespace {
 
-constexpr int kW = 4;                 // waves of a workgroup, at most
+constexpr int kW = 4;                 // waves of a workgroup of a split sequence
+// waves of a workgroup at most, by what a wave's registers leave room for (DC: 64-column pieces of a key)
+constexpr int most_waves(int dc) { return dc == 1 ? 16 : dc == 2 ? 8 : 4; }
 constexpr int kRows = 16;             // query rows of a wave
 
 struct CachedParams {
@@ -92,19 +94,19 @@ __device__ __forceinline__ float fadd2(float a, float b) { return a + b; }
 __device__ __forceinline__ float finite_or_0(float m) { return m == -INFINITY ? 0.f : m; }
 
 template <int DT, int DC>             // DC: 64-column pieces of a key
-__global__ __launch_bounds__(kW * kWave) void k_cached_attention(const CachedParams p) {
+__global__ __launch_bounds__(most_waves(DC) * kWave) void k_cached_attention(const CachedParams p) {
   using T = typename Elem<DT>::T;
   constexpr int NP = DT == MQ_F32 ? 3 : 2;
   constexpr int ND = 4 * DC;          // 16-column pieces of a value row, at most
-  extern __shared__ float lds[];      // [waves][kRows][ND 16 + 1] sums, [waves][2][kRows] maxima and totals
+  extern __shared__ float lds[];      // [waves][rows][ND 16 + 1] sums, [waves][2][rows] maxima and totals
   const unsigned lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), waves = blockDim.x / kWave;
-  auto sums = [&](unsigned w, unsigned row, unsigned c) -> float& { return lds[(w * kRows + row) * (ND * 16 + 1) + c]; };
-  auto stat = [&](unsigned w, unsigned i, unsigned row) -> float& { return lds[waves * kRows * (ND * 16 + 1) + (w * 2 + i) * kRows + row]; };
   const unsigned col = lane % 16, grp = lane / 16;
   const unsigned split = blockIdx.x % p.splits, kvh = blockIdx.x / p.splits % p.kv_heads;
   const unsigned per = p.heads / p.kv_heads, tiles = (per + kRows - 1) / kRows;
   const unsigned tile = blockIdx.x / (p.splits * p.kv_heads) % tiles, b = blockIdx.x / (p.splits * p.kv_heads * tiles);
   const unsigned rows = min(per - tile * kRows, (unsigned)kRows), head0 = kvh * per + tile * kRows, d = p.d;
+  auto sums = [&](unsigned w, unsigned row, unsigned c) -> float& { return lds[(w * rows + row) * (ND * 16 + 1) + c]; };
+  auto stat = [&](unsigned w, unsigned i, unsigned row) -> float& { return lds[waves * rows * (ND * 16 + 1) + (w * 2 + i) * rows + row]; };
   const int len_any = p.lens[b];
   const unsigned len = len_any < 0 ? 0u : min((unsigned)len_any, p.max_len), nblocks = (len + kKvBlock - 1) / kKvBlock;
   const unsigned dk = kv_dk(d), dv = kv_dv(d), nd = dv / 16;
@@ -113,12 +115,11 @@ __global__ __launch_bounds__(kW * kWave) void k_cached_attention(const CachedPar
   const unsigned start = split * p.run, end = min(start + p.run, nblocks);
   if (split > 0 && start >= nblocks) return;           // (the first run answers for an empty sequence)
   const unsigned mine = end > start + wave ? __builtin_amdgcn_readfirstlane((end - start - wave + waves - 1) / waves) : 0u;
-  int ids = 0;
   auto look = [&](unsigned i) {                        // 64 of the wave's blocks, from its i-th on
-    const unsigned pg = start + wave + (i + lane) * waves;
-    ids = i + lane < mine ? table[pg] : 0;
+    const size_t pg = start + wave + (size_t)(i + lane) * waves;
+    return table[pg < p.table_width ? pg : p.table_width - 1];
   };
-  if (mine > 0) look(0);
+  int ids = look(0);                                   // (does not wait for the length)
 
   float acc[ND][4];
   float top = -INFINITY, total = 0.f;
@@ -131,7 +132,7 @@ __global__ __launch_bounds__(kW * kWave) void k_cached_attention(const CachedPar
   bool there, there_next;                              // whether the block is one
   size_t at_next;
   auto find = [&](unsigned i) {                        // the wave's i-th block
-    if (i % kWave == 0 && i > 0) look(i);
+    if (i % kWave == 0 && i > 0) ids = look(i);
     const int block = __builtin_amdgcn_readlane(ids, i % kWave);
     there_next = block >= 0 && (size_t)block < p.blocks;
     at_next = (size_t)(there_next ? block : 0) * p.kv_heads + kvh;
@@ -276,12 +277,13 @@ __global__ __launch_bounds__(kW * kWave) void k_cached_attention(const CachedPar
   total = groups_f(total, fadd2);
 
   // the waves
+  if (col < rows)
 #pragma unroll
-  for (int t = 0; t < ND; ++t)
-    if (t < (int)nd)
+    for (int t = 0; t < ND; ++t)
+      if (t < (int)nd)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) sums(wave, col, 16 * t + 4 * grp + r) = acc[t][r];
-  if (grp == 0) {
+        for (int r = 0; r < 4; ++r) sums(wave, col, 16 * t + 4 * grp + r) = acc[t][r];
+  if (grp == 0 && col < rows) {
     stat(wave, 0, col) = top;
     stat(wave, 1, col) = total;
   }
@@ -335,29 +337,38 @@ __global__ __launch_bounds__(256) void k_cached_join(const CachedParams p) {
 // workgroups once where all sequences are as long as they may be, while a wave still has a block: 32 sequences of 4000 .. 32000
 // tokens, 8 kv heads of 128, take 209 us with that many, 224 with twice as many and 247 with four times (a workgroup's start and
 // end), 311 with half.  One wave where two blocks are all there is.
+constexpr size_t kFull = 1024;
 struct Split {
   unsigned run, splits, waves;
 };
-Split split_of(size_t B, size_t max_len, int heads, int kv_heads) {
+Split split_of(size_t B, size_t max_len, int heads, int kv_heads, size_t d) {
   const size_t per = (size_t)(heads / kv_heads), wgs = B * (size_t)kv_heads * ((per + kRows - 1) / kRows);
   const size_t blocks = (max_len + kKvBlock - 1) / kKvBlock, want = (512 + wgs - 1) / wgs;
+  // one workgroup for a sequence of few blocks: no second launch.  As many waves as there are blocks while the chip has room
+  const size_t rows = per < (size_t)kRows ? per : kRows, dc = kv_dk((unsigned)d) / 64;
+  size_t waves = most_waves((int)dc);
+  while (waves > 1 && waves * rows * (dc * 64 + 3) * sizeof(float) > 65536) waves /= 2;
+  if (blocks <= 2 * waves) {
+    const size_t room = wgs >= kFull ? (blocks + 1) / 2 : blocks;
+    return {(unsigned)blocks, 1u, (unsigned)(room < waves ? room : waves)};
+  }
   size_t run = (blocks + want - 1) / want;
   if (run < (size_t)kW) run = kW;
-  if (run > blocks) run = blocks;
-  return {(unsigned)run, (unsigned)((blocks + run - 1) / run), (unsigned)(run <= 2 ? 1 : run < (size_t)kW ? run : kW)};
+  waves = waves < (size_t)kW ? waves : kW;
+  return {(unsigned)run, (unsigned)((blocks + run - 1) / run), (unsigned)waves};
 }
 
 }  // namespace
 
 size_t cached_attention_ws_bytes(size_t B, size_t max_len, int heads, int kv_heads, size_t d) {
-  const unsigned splits = split_of(B, max_len, heads, kv_heads).splits;
+  const unsigned splits = split_of(B, max_len, heads, kv_heads, d).splits;
   return splits == 1 ? 16 : B * (size_t)heads * splits * (kv_dv((unsigned)d) + 2) * sizeof(float);
 }
 
 int launch_cached_attention(const mq_kv_cache& cache, const int32_t* table, size_t table_width, const int32_t* lens, size_t B,
                             size_t max_len, const void* q, size_t ldq, int heads, int dtype, float scale, void* out,
                             size_t ldo, void* ws, hipStream_t s) {
-  const Split split = split_of(B, max_len, heads, cache.kv_heads);
+  const Split split = split_of(B, max_len, heads, cache.kv_heads, cache.head_dim);
   const unsigned splits = split.splits;
   const size_t per = (size_t)(heads / cache.kv_heads);
   const size_t wgs = B * (size_t)cache.kv_heads * ((per + kRows - 1) / kRows) * splits;
@@ -370,7 +381,7 @@ int launch_cached_attention(const mq_kv_cache& cache, const int32_t* table, size
   return with_dtype(dtype, [&](auto dt) {
     constexpr int DT = decltype(dt)::value;
     const unsigned pieces = kv_dk(p.d) / 64;
-    const size_t lds = split.waves * kRows * (pieces * 64 + 1 + 2) * sizeof(float);
+    const size_t lds = split.waves * (per < (size_t)kRows ? per : kRows) * (pieces * 64 + 1 + 2) * sizeof(float);
     int rc = MQ_OK;
     auto go = [&](auto kern) {
       if (lds > 65536)
