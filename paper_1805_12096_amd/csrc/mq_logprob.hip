@@ -22,15 +22,18 @@ namespace mq {
 
 namespace {
 
-constexpr int kWaves = 8;
+// waves of a workgroup at most, by what a wave's registers leave room for (kf: pieces of K held)
+constexpr int most_waves(int kf) { return kf <= 16 ? 16 : 8; }
+constexpr unsigned kMostColumns = 256;
+constexpr size_t kLdsBytes = 144 * 1024;
 constexpr int kTagBits = 7, kUnitsPerList = 8;
 constexpr int kNone = -2147483647 - 1;          // below every key: sums are above -2^24
 
 struct LogprobParams {
   const uint8_t *packedA, *packedW;
-  unsigned M, N, K, kfrags;
-  unsigned columns, row_waves;          // workgroups that share the words; waves of a workgroup that share the rows
-  float4* stat;                         // [M][columns words groups]: c, l, t
+  unsigned M, N, kfrags;
+  unsigned columns, row_waves, ring;    // workgroups that share the words; waves of one that share the rows; stages in LDS
+  float4* stat;                         // [M][columns]: c, l, t, whether there are words
   unsigned long long* list;             // the same, NB keys each
   const float *sA, *sW;
   const int32_t* target;
@@ -74,175 +77,211 @@ __device__ __forceinline__ void join_stats(float& c, float& l, float& t, float c
   c = low;
 }
 
-// KF: 32-element pieces of K held, CT: 32-row tiles of a wave, NB: length of the list of best words (0: none)
-template <int KF, int CT, int NB>
-__global__ __launch_bounds__(kWaves * kWave) void k_logprob_stream(const LogprobParams p) {
+// Waits until at most n loads of this wave are on their way (fewer where n is none of the steps).
+__device__ __forceinline__ void wait_loads(unsigned n) {
+  asm volatile("" ::: "memory");
+#define MQ_WAIT(N) __builtin_amdgcn_s_waitcnt(((N) & 15) | ((N) >> 4) << 14 | 0x0F70)
+  if (n >= 32) MQ_WAIT(32);
+  else if (n >= 24) MQ_WAIT(24);
+  else if (n >= 16) MQ_WAIT(16);
+  else if (n >= 12) MQ_WAIT(12);
+  else if (n >= 8) MQ_WAIT(8);
+  else if (n >= 6) MQ_WAIT(6);
+  else if (n >= 4) MQ_WAIT(4);
+  else if (n >= 2) MQ_WAIT(2);
+  else MQ_WAIT(0);
+#undef MQ_WAIT
+}
+
+// KF: 32-element pieces of K held, NB: length of the list of best words (0: none)
+template <int KF, int NB>
+__global__ __launch_bounds__(most_waves(KF) * kWave) void k_logprob_stream(const LogprobParams p) {
+  constexpr int NL = NB > 0 ? NB : 1;
   extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
-  const unsigned lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const unsigned wr = wave % p.row_waves, wn = wave / p.row_waves, word_waves = kWaves / p.row_waves;
+  const unsigned lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), waves = blockDim.x / kWave;
+  const unsigned wr = wave % p.row_waves, wn = wave / p.row_waves, word_waves = waves / p.row_waves;
   const unsigned column = blockIdx.x % p.columns, chunk = blockIdx.x / p.columns;
-  const unsigned tile0 = (chunk * p.row_waves + wr) * CT, tiles = (p.M + 31) / 32;
+  const unsigned tile = chunk * p.row_waves + wr, tiles = (p.M + 31) / 32;
   const unsigned units = (p.N + 31) / 32, stages = (units + word_waves - 1) / word_waves;
   const unsigned kf = p.kfrags, unit_bytes = kf * kFragBytes, stage_bytes = word_waves * unit_bytes;
-  const float u2 = __fmul_rn(__fdiv_rn(1.0f, __fmul_rn(*p.sA, *p.sW)), 1.44269504088896340736f);
+  const unsigned pieces = word_waves * kf, each = (pieces + waves - 1) / waves;      // 1 KB pieces of a stage, loads of a wave
+  const unsigned mine = column < stages ? (stages - column + p.columns - 1) / p.columns : 0u;      // this workgroup's stages
 
-  v4i h[CT][KF];
-#pragma unroll
-  for (int i = 0; i < CT; ++i) {
-    const unsigned t = tile0 + i < tiles ? tile0 + i : tiles - 1;
-#pragma unroll
-    for (int f = 0; f < KF; ++f)
-      h[i][f] = f < (int)kf ? *reinterpret_cast<const v4i*>(p.packedA + ((size_t)t * kf + f) * kFragBytes + lane * 16) : v4i{};
-  }
-  float c[CT], l[CT], t[CT];
-  int ref[CT];
-  int best[CT][NB > 0 ? NB : 1];
-  u64 top[CT][NB > 0 ? NB : 1];
-#pragma unroll
-  for (int i = 0; i < CT; ++i) {
-    ref[i] = kNone;
-    c[i] = 0.f;
-    l[i] = t[i] = 0.f;
-#pragma unroll
-    for (int j = 0; j < (NB > 0 ? NB : 1); ++j) {
-      best[i][j] = kNone;
-      top[i][j] = 0;
-    }
-  }
-  auto fetch = [&](unsigned stage, unsigned buf) {
-    const unsigned u0 = stage * word_waves;
-    for (unsigned piece = wave; piece < word_waves * kf; piece += kWaves) {
-      const unsigned u = u0 + piece / kf < units ? u0 + piece / kf : units - 1;
+  // every wave issues the same number of loads for a stage (a piece may come twice), past the last stage as well: how many are
+  // on their way at a given point does not depend on anything
+  auto fetch = [&](unsigned i) {
+    const unsigned stage = column + min(i, mine - 1) * p.columns, u0 = stage * word_waves, buf = i % p.ring;
+    for (unsigned j = 0; j < each; ++j) {
+      const unsigned piece = min(wave + j * waves, pieces - 1), u = min(u0 + piece / kf, units - 1);
       __builtin_amdgcn_global_load_lds(
           (const __attribute__((address_space(1))) void*)(p.packedW + ((size_t)u * kf + piece % kf) * kFragBytes + lane * 16),
           (__attribute__((address_space(3))) void*)(smem + buf * stage_bytes + piece * kFragBytes), 16, 0, 0);
     }
   };
-  unsigned held = 0, list_unit = 0;              // units in the 32-bit lists, and the first of them
+  if (mine > 0)
+    for (unsigned i = 0; i + 1 < p.ring; ++i) fetch(i);
+  const float u2 = __fmul_rn(__fdiv_rn(1.0f, __fmul_rn(*p.sA, *p.sW)), 1.44269504088896340736f);
+  v4i h[KF];
+  const uint8_t* rows = p.packedA + (size_t)(tile < tiles ? tile : tiles - 1) * kf * kFragBytes + lane * 16;
+#pragma unroll
+  for (int f = 0; f < KF; ++f) h[f] = *reinterpret_cast<const v4i*>(rows + (f < (int)kf ? f : 0) * kFragBytes);
+  float c = 0.f, l = 0.f, t = 0.f;
+  int ref = kNone;
+  int best[NL];
+  u64 top[NL];
+#pragma unroll
+  for (int j = 0; j < NL; ++j) {
+    best[j] = kNone;
+    top[j] = 0;
+  }
+  unsigned held = 0, list_unit = 0;              // units in the 32-bit list, and the first of them
   const unsigned unit_step = p.columns * word_waves;
-  auto flush = [&]() {
+  auto flush = [&] {
     if constexpr (NB > 0) {
+      u64 keys[NB];
 #pragma unroll
-      for (int i = 0; i < CT; ++i) {
-        u64 keys[NB];
-#pragma unroll
-        for (int j = 0; j < NB; ++j) {
-          const unsigned place = 127u - ((unsigned)best[i][j] & 127u), r = place % 16;
-          const unsigned word = (list_unit + place / 16 * unit_step) * 32 + 8 * (r / 4) + 4 * (lane / 32) + r % 4;
-          keys[j] = best[i][j] == kNone ? 0 : key_of(best[i][j] >> kTagBits, word);
-          best[i][j] = kNone;
-        }
-        merge_lists<NB>(top[i], keys);
+      for (int j = 0; j < NB; ++j) {
+        const unsigned place = 127u - ((unsigned)best[j] & 127u), r = place % 16;
+        const unsigned word = (list_unit + place / 16 * unit_step) * 32 + 8 * (r / 4) + 4 * (lane / 32) + r % 4;
+        keys[j] = best[j] == kNone ? 0 : key_of(best[j] >> kTagBits, word);
+        best[j] = kNone;
       }
+      merge_lists<NB>(top, keys);
     }
     held = 0;
   };
-  unsigned buf = 0;
-  if (column < stages) fetch(column, 0);
-  for (unsigned stage = column; stage < stages; stage += p.columns) {
-    __builtin_amdgcn_s_waitcnt(0x0F70);
-    __syncthreads();
-    if (stage + p.columns < stages) fetch(stage + p.columns, buf ^ 1);
-    const unsigned unit = stage * word_waves + wn;
-    const uint8_t* at = smem + buf * stage_bytes + wn * unit_bytes + lane * 16;
-    buf ^= 1;
-    if (unit >= units || tile0 >= tiles) continue;
-    v16i acc[CT];
+  // the 16 words of a unit that a lane has; the vocabulary's last unit may have fewer
+  auto take = [&](const v16i& acc, unsigned unit, auto whole) {
+    auto there = [&](int r) { return decltype(whole)::value || unit * 32 + 4 * (lane / 32) + 8 * (r / 4) + r % 4 < p.N; };
+    int most = kNone;
 #pragma unroll
-    for (int i = 0; i < CT; ++i) acc[i] = v16i{};
+    for (int r = 0; r < 16; ++r) most = max(most, there(r) ? acc[r] : kNone);
+    if (__any(most > ref)) {
+      const int now = max(most, ref);
+      const float cn = now == kNone ? 0.f : -(float)now * u2, D = l > 0.f ? c - cn : 0.f, e = __builtin_amdgcn_exp2f(-D);
+      t = e * (t - D * l);
+      l *= e;
+      c = cn;
+      ref = now;
+    }
+    const int tag = 127 - (int)(held * 16);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const float z = fmaf((float)acc[r], u2, c), e = there(r) ? __builtin_amdgcn_exp2f(z) : 0.f;
+      l += e;
+      t = fmaf(e, z, t);
+      if constexpr (NB > 0) {
+        const int key = there(r) ? (acc[r] << kTagBits) + (tag - r) : kNone;
+#pragma unroll
+        for (int j = NB - 1; j > 0; --j) best[j] = median3(best[j - 1], best[j], key);
+        best[0] = max(best[0], key);
+      }
+    }
+  };
+  for (unsigned i = 0; i < mine; ++i) {
+    wait_loads((p.ring - 2) * each);
+    __builtin_amdgcn_s_barrier();                // stage i is there, and nobody reads the one before
+    asm volatile("" ::: "memory");
+    fetch(i + p.ring - 1);
+    const unsigned unit = (column + i * p.columns) * word_waves + wn;
+    if (unit >= units || tile >= tiles) continue;
+    const uint8_t* at = smem + i % p.ring * stage_bytes + wn * unit_bytes + lane * 16;
+    v16i acc = {};
 #pragma unroll
     for (int f = 0; f < KF; ++f)
-      if (f < (int)kf) {
-        const v4i w = *reinterpret_cast<const v4i*>(at + f * kFragBytes);
-#pragma unroll
-        for (int i = 0; i < CT; ++i) acc[i] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w, h[i][f], acc[i], 0, 0, 0);
-      }
+      if (f < (int)kf) acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(*reinterpret_cast<const v4i*>(at + f * kFragBytes), h[f], acc, 0, 0, 0);
     if (held == 0) list_unit = unit;
-    const unsigned n0 = unit * 32 + 4 * (lane / 32);
-    const bool whole = unit * 32 + 32 <= p.N;
-#pragma unroll
-    for (int i = 0; i < CT; ++i) {
-      auto there = [&](int r) { return whole || n0 + 8 * (r / 4) + r % 4 < p.N; };
-      int most = kNone;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) most = max(most, there(r) ? acc[i][r] : kNone);
-      if (__any(most > ref[i])) {
-        const int now = max(most, ref[i]);
-        const float cn = now == kNone ? 0.f : -(float)now * u2, D = l[i] > 0.f ? c[i] - cn : 0.f, e = __builtin_amdgcn_exp2f(-D);
-        t[i] = e * (t[i] - D * l[i]);
-        l[i] *= e;
-        c[i] = cn;
-        ref[i] = now;
-      }
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const float z = fmaf((float)acc[i][r], u2, c[i]), e = there(r) ? __builtin_amdgcn_exp2f(z) : 0.f;
-        l[i] += e;
-        t[i] = fmaf(e, z, t[i]);
-        if constexpr (NB > 0) {
-          const int key = there(r) ? (acc[i][r] << kTagBits) | (127 - (int)(held * 16 + r)) : kNone;
-#pragma unroll
-          for (int j = NB - 1; j > 0; --j) best[i][j] = median3(best[i][j - 1], best[i][j], key);
-          best[i][0] = max(best[i][0], key);
-        }
-      }
-    }
+    if (unit * 32 + 32 <= p.N) take(acc, unit, std::true_type{});
+    else take(acc, unit, std::false_type{});
     if (++held == kUnitsPerList) flush();
   }
-  if (tile0 >= tiles) return;
   flush();
-  const unsigned groups = p.columns * word_waves, group = column * word_waves + wn;
+  // the two lanes of a row.  A lane without words has l = 0 and must not set the reference
+  const float c2 = __shfl_xor(c, 32, 64), l2 = __shfl_xor(l, 32, 64), t2 = __shfl_xor(t, 32, 64);
+  const int ref2 = __shfl_xor(ref, 32, 64);
+  if (ref == kNone) {
+    c = c2;
+    l = l2;
+    t = t2;
+  } else if (ref2 != kNone) {
+    join_stats(c, l, t, c2, l2, t2);
+  }
+  bool any = ref != kNone || ref2 != kNone;
+  if constexpr (NB > 0) {
+    u64 other[NB];
 #pragma unroll
-  for (int i = 0; i < CT; ++i) {
-    const unsigned m = (tile0 + i) * 32 + lane % 32;
-    // the two lanes of a row.  A lane without words has l = 0 and must not set the reference
-    const float c2 = __shfl_xor(c[i], 32, 64), l2 = __shfl_xor(l[i], 32, 64), t2 = __shfl_xor(t[i], 32, 64);
-    const int ref2 = __shfl_xor(ref[i], 32, 64);
-    if (ref[i] == kNone) {
-      c[i] = c2;
-      l[i] = l2;
-      t[i] = t2;
-    } else if (ref2 != kNone) {
-      join_stats(c[i], l[i], t[i], c2, l2, t2);
-    }
-    const bool any = ref[i] != kNone || ref2 != kNone;
-    if constexpr (NB > 0) {
-      u64 other[NB];
-#pragma unroll
-      for (int j = 0; j < NB; ++j) other[j] = __shfl_xor(top[i][j], 32, 64);
-      merge_lists<NB>(top[i], other);
-    }
-    if (lane < 32 && tile0 + i < tiles && m < p.M) {
-      p.stat[(size_t)m * groups + group] = make_float4(c[i], l[i], t[i], any ? 1.f : 0.f);
+    for (int j = 0; j < NB; ++j) other[j] = __shfl_xor(top[j], 32, 64);
+    merge_lists<NB>(top, other);
+  }
+  // the waves that shared the words of a row, through LDS
+  if (word_waves > 1) {
+    __builtin_amdgcn_s_waitcnt(0x0F70);          // (loads for stages that are not there land in LDS too)
+    __syncthreads();
+    float4* stat = reinterpret_cast<float4*>(smem);
+    u64* list = reinterpret_cast<u64*>(smem + waves * 32 * sizeof(float4));
+    if (wn > 0 && lane < 32) {
+      stat[wave * 32 + lane] = make_float4(c, l, t, any ? 1.f : 0.f);
       if constexpr (NB > 0)
 #pragma unroll
-        for (int j = 0; j < NB; ++j) p.list[((size_t)m * groups + group) * NB + j] = top[i][j];
+        for (int j = 0; j < NB; ++j) list[(wave * 32 + lane) * NB + j] = top[j];
     }
+    __syncthreads();
+    if (wn > 0) return;
+    for (unsigned w = 1; w < word_waves; ++w) {
+      const unsigned at = (w * p.row_waves + wr) * 32 + lane % 32;
+      const float4 s = stat[at];
+      if (s.w != 0.f) {
+        if (any) join_stats(c, l, t, s.x, s.y, s.z);
+        else { c = s.x; l = s.y; t = s.z; }
+        any = true;
+      }
+      if constexpr (NB > 0) {
+        u64 other[NB];
+#pragma unroll
+        for (int j = 0; j < NB; ++j) other[j] = list[at * NB + j];
+        merge_lists<NB>(top, other);
+      }
+    }
+  }
+  const unsigned m = tile * 32 + lane;
+  if (lane < 32 && tile < tiles && m < p.M) {
+    p.stat[(size_t)m * p.columns + column] = make_float4(c, l, t, any ? 1.f : 0.f);
+    if constexpr (NB > 0)
+#pragma unroll
+      for (int j = 0; j < NB; ++j) p.list[((size_t)m * p.columns + column) * NB + j] = top[j];
   }
 }
 
 // A wave per row.
 template <int NB>
-__global__ __launch_bounds__(256) void k_logprob_join(const LogprobParams p, unsigned groups) {
+__global__ __launch_bounds__(256) void k_logprob_join(const LogprobParams p) {
   const unsigned lane = threadIdx.x % kWave, m = blockIdx.x * (256 / kWave) + threadIdx.x / kWave;
   if (m >= p.M) return;
+  const int word = p.target[m];
   const float u2 = __fmul_rn(__fdiv_rn(1.0f, __fmul_rn(*p.sA, *p.sW)), 1.44269504088896340736f);
   float c = 0.f, l = 0.f, t = 0.f;
   bool any = false;
   u64 top[NB > 0 ? NB : 1] = {};
-  for (unsigned g = lane; g < groups; g += kWave) {
-    const float4 s = p.stat[(size_t)m * groups + g];
-    if (s.w != 0.f) {
-      if (any) join_stats(c, l, t, s.x, s.y, s.z);
-      else { c = s.x; l = s.y; t = s.z; }
+  // up to four parts a lane, all asked for at once
+  float4 stat[kMostColumns / kWave];
+  u64 list[kMostColumns / kWave][NB > 0 ? NB : 1];
+#pragma unroll
+  for (int i = 0; i < kMostColumns / kWave; ++i) {
+    const size_t at = (size_t)m * p.columns + min(lane + i * kWave, p.columns - 1);
+    stat[i] = p.stat[at];
+    if constexpr (NB > 0)
+#pragma unroll
+      for (int j = 0; j < NB; ++j) list[i][j] = p.list[at * NB + j];
+  }
+#pragma unroll
+  for (int i = 0; i < kMostColumns / kWave; ++i) {
+    if (lane + i * kWave >= p.columns) break;
+    if (stat[i].w != 0.f) {
+      if (any) join_stats(c, l, t, stat[i].x, stat[i].y, stat[i].z);
+      else { c = stat[i].x; l = stat[i].y; t = stat[i].z; }
       any = true;
     }
-    if constexpr (NB > 0) {
-      u64 other[NB];
-#pragma unroll
-      for (int j = 0; j < NB; ++j) other[j] = p.list[((size_t)m * groups + g) * NB + j];
-      merge_lists<NB>(top, other);
-    }
+    if constexpr (NB > 0) merge_lists<NB>(top, list[i]);
   }
 #pragma unroll
   for (int off = 32; off >= 1; off >>= 1) {
@@ -259,7 +298,6 @@ __global__ __launch_bounds__(256) void k_logprob_join(const LogprobParams p, uns
     }
   }
   // the given word's sum: 16 elements of K per lane, element k of row n in piece k / 32, half (k / 16) % 2
-  const int word = p.target[m];
   const bool given = word >= 0 && (unsigned)word < p.N;
   int sum = 0;
   if (given)
@@ -289,21 +327,28 @@ __global__ __launch_bounds__(256) void k_logprob_join(const LogprobParams p, uns
       }
 }
 
+// How the product is dealt.  A workgroup's waves share its rows, 32 each, and, where there are few of them, the words of a stage;
+// as many columns of workgroups as fill the chip once.
 struct Shape {
-  unsigned row_waves, ct, chunks, columns, groups;
+  unsigned row_waves, word_waves, chunks, columns, ring;
 };
-Shape shape_of(size_t M, size_t N, bool wide) {
+Shape shape_of(size_t M, size_t N, unsigned kf) {
   Shape s;
-  const size_t tiles = (M + 31) / 32, units = (N + 31) / 32;
-  s.ct = !wide && tiles > 8 ? 2 : 1;
-  const size_t waves = (tiles + s.ct - 1) / s.ct;
-  s.row_waves = wide ? 4 : 2;           // (so that two stages fit LDS)
-  while (s.row_waves < 8 && s.row_waves < waves) s.row_waves *= 2;
-  s.chunks = (unsigned)((waves + s.row_waves - 1) / s.row_waves);
-  const size_t stages = (units + kWaves / s.row_waves - 1) / (kWaves / s.row_waves);
-  const size_t want = s.chunks >= 256 ? 1 : 256 / s.chunks;
+  const size_t tiles = (M + 31) / 32, units = (N + 31) / 32, most = most_waves(kf > 16 ? 32 : 16);
+  s.chunks = (unsigned)((tiles + most - 1) / most);
+  s.row_waves = (unsigned)((tiles + s.chunks - 1) / s.chunks);
+  const size_t want = s.chunks >= kMostColumns ? 1 : kMostColumns / s.chunks;
+  // units of a stage: as many waves as there are, as one round of the columns needs, and as LDS holds twice
+  size_t words = most / s.row_waves;
+  const size_t needed = (units + want - 1) / want, fit = kLdsBytes / 2 / (kf * kFragBytes);
+  words = words < needed ? words : needed;
+  words = words < fit ? words : fit;
+  s.word_waves = (unsigned)(words > 1 ? words : 1);
+  const size_t stages = (units + s.word_waves - 1) / s.word_waves;
   s.columns = (unsigned)(want < stages ? want : stages);
-  s.groups = s.columns * (kWaves / s.row_waves);
+  const size_t ring = kLdsBytes / (s.word_waves * kf * kFragBytes), each = (stages + s.columns - 1) / s.columns + 1;
+  s.ring = (unsigned)(ring < 2 ? 2 : ring < each ? ring : each < 2 ? 2 : each);
+  if (s.ring > 8) s.ring = 8;
   return s;
 }
 int list_length(int k) { return k == 0 ? 0 : k <= 4 ? 4 : 8; }
@@ -311,47 +356,43 @@ int list_length(int k) { return k == 0 ? 0 : k <= 4 ? 4 : 8; }
 }  // namespace
 
 size_t token_logprob_ws_bytes(size_t M, size_t N, int k) {
-  size_t most = 0;
-  for (int wide = 0; wide < 2; ++wide) {
-    const size_t n = M * shape_of(M, N, wide != 0).groups * (sizeof(float4) + list_length(k) * sizeof(u64));
-    if (n > most) most = n;
-  }
-  return most;
+  return M * kMostColumns * (sizeof(float4) + list_length(k) * sizeof(u64));
 }
 
 int launch_token_logprob(const void* packedA, const void* packedW, size_t M, size_t N, size_t K, const float* sA,
                          const float* sW, const int32_t* target, int k, float* logprob, float* entropy, int32_t* tok,
                          float* alt, void* ws, hipStream_t s) {
   const unsigned kf = (unsigned)PackedDims(8, N, K).kfrags;
-  const Shape sh = shape_of(M, N, kf > 16);
+  const Shape sh = shape_of(M, N, kf);
   LogprobParams p{static_cast<const uint8_t*>(packedA), static_cast<const uint8_t*>(packedW), (unsigned)M, (unsigned)N,
-                  (unsigned)K, kf, sh.columns, sh.row_waves, static_cast<float4*>(ws),
-                  reinterpret_cast<u64*>(static_cast<float4*>(ws) + M * sh.groups), sA, sW, target, k, logprob, entropy, alt, tok};
-  auto go = [&](auto kfc, auto ctc, auto nbc) {
+                  kf, sh.columns, sh.row_waves, sh.ring, static_cast<float4*>(ws),
+                  reinterpret_cast<u64*>(static_cast<float4*>(ws) + M * sh.columns), sA, sW, target, k, logprob, entropy, alt, tok};
+  auto go = [&](auto kfc, auto nbc) {
     constexpr int NB = decltype(nbc)::value;
-    auto kern = k_logprob_stream<decltype(kfc)::value, decltype(ctc)::value, NB>;
-    const unsigned lds = 2 * kWaves / sh.row_waves * kf * kFragBytes;
+    auto kern = k_logprob_stream<decltype(kfc)::value, NB>;
+    const unsigned waves = sh.row_waves * sh.word_waves;
+    const size_t ring = (size_t)sh.ring * sh.word_waves * kf * kFragBytes, join = waves * 32 * (sizeof(float4) + NB * sizeof(u64));
+    const size_t lds = sh.word_waves > 1 && join > ring ? join : ring;
     if (lds > 65536) {
       const int e = check_hip(hipFuncSetAttribute(reinterpret_cast<const void*>(kern),
                                                   hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
       if (e != MQ_OK) return e;
     }
-    hipLaunchKernelGGL(kern, dim3(sh.columns * sh.chunks), dim3(kWaves * kWave), lds, s, p);
+    hipLaunchKernelGGL(kern, dim3(sh.columns * sh.chunks), dim3(waves * kWave), lds, s, p);
     const int rc = check_hip(hipGetLastError());
     if (rc != MQ_OK) return rc;
-    hipLaunchKernelGGL((k_logprob_join<NB>), dim3((unsigned)((M + 3) / 4)), dim3(256), 0, s, p, sh.groups);
+    hipLaunchKernelGGL((k_logprob_join<NB>), dim3((unsigned)((M + 3) / 4)), dim3(256), 0, s, p);
     return check_hip(hipGetLastError());
   };
-  auto with_list = [&](auto kfc, auto ctc) {
+  auto with_list = [&](auto kfc) {
     switch (list_length(k)) {
-      case 0: return go(kfc, ctc, std::integral_constant<int, 0>{});
-      case 4: return go(kfc, ctc, std::integral_constant<int, 4>{});
-      default: return go(kfc, ctc, std::integral_constant<int, 8>{});
+      case 0: return go(kfc, std::integral_constant<int, 0>{});
+      case 4: return go(kfc, std::integral_constant<int, 4>{});
+      default: return go(kfc, std::integral_constant<int, 8>{});
     }
   };
-  if (kf > 16) return with_list(std::integral_constant<int, 32>{}, std::integral_constant<int, 1>{});
-  if (sh.ct == 2) return with_list(std::integral_constant<int, 16>{}, std::integral_constant<int, 2>{});
-  return with_list(std::integral_constant<int, 16>{}, std::integral_constant<int, 1>{});
+  if (kf > 16) return with_list(std::integral_constant<int, 32>{});
+  return with_list(std::integral_constant<int, 16>{});
 }
 
 }  // namespace mq
