@@ -164,7 +164,7 @@ __global__ __launch_bounds__(most_waves(KF) * kWave) void k_logprob_stream(const
       c = cn;
       ref = now;
     }
-    const int tag = 127 - (int)(held * 16);
+    const int tag = __builtin_amdgcn_readfirstlane(127 - (int)(held * 16));
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       const float z = fmaf((float)acc[r], u2, c), e = there(r) ? __builtin_amdgcn_exp2f(z) : 0.f;
@@ -187,9 +187,16 @@ __global__ __launch_bounds__(most_waves(KF) * kWave) void k_logprob_stream(const
     if (unit >= units || tile >= tiles) continue;
     const uint8_t* at = smem + i % p.ring * stage_bytes + wn * unit_bytes + lane * 16;
     v16i acc = {};
+    if (kf == KF) {                              // (a check for each piece would have each wait for LDS on its own)
 #pragma unroll
-    for (int f = 0; f < KF; ++f)
-      if (f < (int)kf) acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(*reinterpret_cast<const v4i*>(at + f * kFragBytes), h[f], acc, 0, 0, 0);
+      for (int f = 0; f < KF; ++f)
+        acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(*reinterpret_cast<const v4i*>(at + f * kFragBytes), h[f], acc, 0, 0, 0);
+    } else {
+#pragma unroll
+      for (int f = 0; f < KF; ++f)
+        if (f < (int)kf)
+          acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(*reinterpret_cast<const v4i*>(at + f * kFragBytes), h[f], acc, 0, 0, 0);
+    }
     if (held == 0) list_unit = unit;
     if (unit * 32 + 32 <= p.N) take(acc, unit, std::true_type{});
     else take(acc, unit, std::false_type{});
