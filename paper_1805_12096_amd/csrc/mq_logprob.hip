@@ -22,10 +22,11 @@ namespace mq {
 
 namespace {
 
-// waves of a workgroup at most, by what a wave's registers leave room for (kf: pieces of K held)
-constexpr int most_waves(int kf) { return kf <= 16 ? 16 : 8; }
+// waves of a workgroup at most, by what a wave's registers leave room for (KF: pieces of K held, CT: tiles of 32 rows)
+constexpr int most_waves(int KF, int CT) { return KF == 16 ? (CT == 1 ? 12 : 8) : CT == 1 ? 8 : 4; }
 constexpr unsigned kMostColumns = 256;
 constexpr size_t kLdsBytes = 144 * 1024;
+#define MQ_INLINE __attribute__((always_inline))
 constexpr int kTagBits = 7, kUnitsPerList = 8;
 constexpr int kNone = -2147483647 - 1;          // below every key: sums are above -2^24
 
@@ -93,116 +94,12 @@ __device__ __forceinline__ void wait_loads(unsigned n) {
 #undef MQ_WAIT
 }
 
-// KF: 32-element pieces of K held, NB: length of the list of best words (0: none)
-template <int KF, int NB>
-__global__ __launch_bounds__(most_waves(KF) * kWave) void k_logprob_stream(const LogprobParams p) {
-  constexpr int NL = NB > 0 ? NB : 1;
-  extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
-  const unsigned lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), waves = blockDim.x / kWave;
-  const unsigned wr = wave % p.row_waves, wn = wave / p.row_waves, word_waves = waves / p.row_waves;
-  const unsigned column = blockIdx.x % p.columns, chunk = blockIdx.x / p.columns;
-  const unsigned tile = chunk * p.row_waves + wr, tiles = (p.M + 31) / 32;
-  const unsigned units = (p.N + 31) / 32, stages = (units + word_waves - 1) / word_waves;
-  const unsigned kf = p.kfrags, unit_bytes = kf * kFragBytes, stage_bytes = word_waves * unit_bytes;
-  const unsigned pieces = word_waves * kf, each = (pieces + waves - 1) / waves;      // 1 KB pieces of a stage, loads of a wave
-  const unsigned mine = column < stages ? (stages - column + p.columns - 1) / p.columns : 0u;      // this workgroup's stages
-
-  // every wave issues the same number of loads for a stage (a piece may come twice), past the last stage as well: how many are
-  // on their way at a given point does not depend on anything
-  auto fetch = [&](unsigned i) {
-    const unsigned stage = column + min(i, mine - 1) * p.columns, u0 = stage * word_waves, buf = i % p.ring;
-    for (unsigned j = 0; j < each; ++j) {
-      const unsigned piece = min(wave + j * waves, pieces - 1), u = min(u0 + piece / kf, units - 1);
-      __builtin_amdgcn_global_load_lds(
-          (const __attribute__((address_space(1))) void*)(p.packedW + ((size_t)u * kf + piece % kf) * kFragBytes + lane * 16),
-          (__attribute__((address_space(3))) void*)(smem + buf * stage_bytes + piece * kFragBytes), 16, 0, 0);
-    }
-  };
-  if (mine > 0)
-    for (unsigned i = 0; i + 1 < p.ring; ++i) fetch(i);
-  const float u2 = __fmul_rn(__fdiv_rn(1.0f, __fmul_rn(*p.sA, *p.sW)), 1.44269504088896340736f);
-  v4i h[KF];
-  const uint8_t* rows = p.packedA + (size_t)(tile < tiles ? tile : tiles - 1) * kf * kFragBytes + lane * 16;
-#pragma unroll
-  for (int f = 0; f < KF; ++f) h[f] = *reinterpret_cast<const v4i*>(rows + (f < (int)kf ? f : 0) * kFragBytes);
-  float c = 0.f, l = 0.f, t = 0.f;
-  int ref = kNone;
-  int best[NL];
-  u64 top[NL];
-#pragma unroll
-  for (int j = 0; j < NL; ++j) {
-    best[j] = kNone;
-    top[j] = 0;
-  }
-  unsigned held = 0, list_unit = 0;              // units in the 32-bit list, and the first of them
-  const unsigned unit_step = p.columns * word_waves;
-  auto flush = [&] {
-    if constexpr (NB > 0) {
-      u64 keys[NB];
-#pragma unroll
-      for (int j = 0; j < NB; ++j) {
-        const unsigned place = 127u - ((unsigned)best[j] & 127u), r = place % 16;
-        const unsigned word = (list_unit + place / 16 * unit_step) * 32 + 8 * (r / 4) + 4 * (lane / 32) + r % 4;
-        keys[j] = best[j] == kNone ? 0 : key_of(best[j] >> kTagBits, word);
-        best[j] = kNone;
-      }
-      merge_lists<NB>(top, keys);
-    }
-    held = 0;
-  };
-  // the 16 words of a unit that a lane has; the vocabulary's last unit may have fewer
-  auto take = [&](const v16i& acc, unsigned unit, auto whole) {
-    auto there = [&](int r) { return decltype(whole)::value || unit * 32 + 4 * (lane / 32) + 8 * (r / 4) + r % 4 < p.N; };
-    int most = kNone;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) most = max(most, there(r) ? acc[r] : kNone);
-    if (__any(most > ref)) {
-      const int now = max(most, ref);
-      const float cn = now == kNone ? 0.f : -(float)now * u2, D = l > 0.f ? c - cn : 0.f, e = __builtin_amdgcn_exp2f(-D);
-      t = e * (t - D * l);
-      l *= e;
-      c = cn;
-      ref = now;
-    }
-    const int tag = __builtin_amdgcn_readfirstlane(127 - (int)(held * 16));
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const float z = fmaf((float)acc[r], u2, c), e = there(r) ? __builtin_amdgcn_exp2f(z) : 0.f;
-      l += e;
-      t = fmaf(e, z, t);
-      if constexpr (NB > 0) {
-        const int key = there(r) ? (acc[r] << kTagBits) + (tag - r) : kNone;
-#pragma unroll
-        for (int j = NB - 1; j > 0; --j) best[j] = median3(best[j - 1], best[j], key);
-        best[0] = max(best[0], key);
-      }
-    }
-  };
-  for (unsigned i = 0; i < mine; ++i) {
-    wait_loads((p.ring - 2) * each);
-    __builtin_amdgcn_s_barrier();                // stage i is there, and nobody reads the one before
-    asm volatile("" ::: "memory");
-    fetch(i + p.ring - 1);
-    const unsigned unit = (column + i * p.columns) * word_waves + wn;
-    if (unit >= units || tile >= tiles) continue;
-    const uint8_t* at = smem + i % p.ring * stage_bytes + wn * unit_bytes + lane * 16;
-    v16i acc = {};
-    if (kf == KF) {                              // (a check for each piece would have each wait for LDS on its own)
-#pragma unroll
-      for (int f = 0; f < KF; ++f)
-        acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(*reinterpret_cast<const v4i*>(at + f * kFragBytes), h[f], acc, 0, 0, 0);
-    } else {
-#pragma unroll
-      for (int f = 0; f < KF; ++f)
-        if (f < (int)kf)
-          acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(*reinterpret_cast<const v4i*>(at + f * kFragBytes), h[f], acc, 0, 0, 0);
-    }
-    if (held == 0) list_unit = unit;
-    if (unit * 32 + 32 <= p.N) take(acc, unit, std::true_type{});
-    else take(acc, unit, std::false_type{});
-    if (++held == kUnitsPerList) flush();
-  }
-  flush();
+// A wave's statistics and list of a tile, joined over the two lanes of a row and over the waves that shared its words, to the
+// workspace.
+template <int NB, int CT>
+__device__ __forceinline__ void finish(const LogprobParams& p, uint8_t* smem, int x, unsigned tile, unsigned tiles, unsigned column,
+                                       unsigned wave, unsigned wr, unsigned wn, unsigned word_waves, unsigned waves, unsigned lane,
+                                       int ref, float c, float l, float t, u64 (&top)[NB > 0 ? NB : 1]) {
   // the two lanes of a row.  A lane without words has l = 0 and must not set the reference
   const float c2 = __shfl_xor(c, 32, 64), l2 = __shfl_xor(l, 32, 64), t2 = __shfl_xor(t, 32, 64);
   const int ref2 = __shfl_xor(ref, 32, 64);
@@ -233,8 +130,7 @@ __global__ __launch_bounds__(most_waves(KF) * kWave) void k_logprob_stream(const
         for (int j = 0; j < NB; ++j) list[(wave * 32 + lane) * NB + j] = top[j];
     }
     __syncthreads();
-    if (wn > 0) return;
-    for (unsigned w = 1; w < word_waves; ++w) {
+    for (unsigned w = 1; w < word_waves && wn == 0; ++w) {
       const unsigned at = (w * p.row_waves + wr) * 32 + lane % 32;
       const float4 s = stat[at];
       if (s.w != 0.f) {
@@ -251,12 +147,205 @@ __global__ __launch_bounds__(most_waves(KF) * kWave) void k_logprob_stream(const
     }
   }
   const unsigned m = tile * 32 + lane;
-  if (lane < 32 && tile < tiles && m < p.M) {
+  if (wn == 0 && lane < 32 && tile < tiles && m < p.M) {
     p.stat[(size_t)m * p.columns + column] = make_float4(c, l, t, any ? 1.f : 0.f);
     if constexpr (NB > 0)
 #pragma unroll
       for (int j = 0; j < NB; ++j) p.list[((size_t)m * p.columns + column) * NB + j] = top[j];
   }
+}
+
+// KF: 32-element pieces of K held, CT: tiles of 32 rows, NB: length of the list of best words (0: none)
+// A unit's matrix instructions stand beside the vector ones of the unit before (all of K held: K of 512 or 1024 elements; other
+// widths one after the other).  Pieces are asked of LDS three ahead.
+template <int KF, int CT, int NB>
+__global__ __launch_bounds__(most_waves(KF, CT) * kWave, 1) void k_logprob_stream(const LogprobParams p) {
+  constexpr int NL = NB > 0 ? NB : 1;
+  extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
+  const unsigned lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), waves = blockDim.x / kWave;
+  const unsigned wr = wave % p.row_waves, wn = wave / p.row_waves, word_waves = waves / p.row_waves;
+  const unsigned column = blockIdx.x % p.columns, chunk = blockIdx.x / p.columns;
+  const unsigned tile = (chunk * p.row_waves + wr) * CT, tiles = (p.M + 31) / 32;
+  const unsigned units = (p.N + 31) / 32, stages = (units + word_waves - 1) / word_waves;
+  const unsigned kf = p.kfrags, unit_bytes = kf * kFragBytes, stage_bytes = word_waves * unit_bytes;
+  const unsigned pieces = word_waves * kf, each = (pieces + waves - 1) / waves;      // 1 KB pieces of a stage, loads of a wave
+  const unsigned mine = column < stages ? (stages - column + p.columns - 1) / p.columns : 0u;      // this workgroup's stages
+
+  // every wave issues the same number of loads for a stage (a piece may come twice), past the last stage as well: how many are
+  // on their way at a given point does not depend on anything
+  auto fetch = [&](unsigned i) {
+    const unsigned stage = column + min(i, mine - 1) * p.columns, u0 = stage * word_waves, buf = i % p.ring;
+    for (unsigned j = 0; j < each; ++j) {
+      const unsigned piece = min(wave + j * waves, pieces - 1), u = min(u0 + piece / kf, units - 1);
+      __builtin_amdgcn_global_load_lds(
+          (const __attribute__((address_space(1))) void*)(p.packedW + ((size_t)u * kf + piece % kf) * kFragBytes + lane * 16),
+          (__attribute__((address_space(3))) void*)(smem + buf * stage_bytes + piece * kFragBytes), 16, 0, 0);
+    }
+  };
+  if (mine > 0)
+    for (unsigned i = 0; i + 1 < p.ring; ++i) fetch(i);
+  const float u2 = __fmul_rn(__fdiv_rn(1.0f, __fmul_rn(*p.sA, *p.sW)), 1.44269504088896340736f);
+  v4i h[CT][KF];
+#pragma unroll
+  for (int x = 0; x < CT; ++x) {
+    const uint8_t* rows = p.packedA + (size_t)min(tile + x, tiles - 1) * kf * kFragBytes + lane * 16;
+#pragma unroll
+    for (int f = 0; f < KF; ++f) h[x][f] = *reinterpret_cast<const v4i*>(rows + (f < (int)kf ? f : 0) * kFragBytes);
+  }
+  float c[CT], l[CT], t[CT];
+  int ref[CT], best[CT][NL];
+  u64 top[CT][NL];
+#pragma unroll
+  for (int x = 0; x < CT; ++x) {
+    c[x] = l[x] = t[x] = 0.f;
+    ref[x] = kNone;
+#pragma unroll
+    for (int j = 0; j < NL; ++j) {
+      best[x][j] = kNone;
+      top[x][j] = 0;
+    }
+  }
+  unsigned held = 0, list_unit = 0;              // units in the 32-bit lists, and the first of them
+  const unsigned unit_step = p.columns * word_waves;
+  auto flush = [&]() MQ_INLINE {
+    if constexpr (NB > 0)
+#pragma unroll
+      for (int x = 0; x < CT; ++x) {
+        u64 keys[NB];
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+          const unsigned place = 127u - ((unsigned)best[x][j] & 127u), r = place % 16;
+          const unsigned word = (list_unit + place / 16 * unit_step) * 32 + 8 * (r / 4) + 4 * (lane / 32) + r % 4;
+          keys[j] = best[x][j] == kNone ? 0 : key_of(best[x][j] >> kTagBits, word);
+          best[x][j] = kNone;
+        }
+        merge_lists<NB>(top[x], keys);
+      }
+    held = 0;
+  };
+  int sums[CT][16];                              // of unit `unit`, whose turn with the vector unit is next
+  unsigned unit = 0;
+  // the vocabulary's last unit may have fewer than 32 words; a wave has it last
+  auto there = [&](auto whole, int r) MQ_INLINE {
+    return decltype(whole)::value || unit * 32 + 4 * (lane / 32) + 8 * (r / 4) + r % 4 < p.N;
+  };
+  auto settle = [&](auto whole) MQ_INLINE {
+    if (held == 0) list_unit = unit;
+#pragma unroll
+    for (int x = 0; x < CT; ++x) {
+      int most = kNone;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) most = max(most, there(whole, r) ? sums[x][r] : kNone);
+      if (__builtin_expect(__any(most > ref[x]), 0)) {
+        const int now = max(most, ref[x]);
+        const float cn = now == kNone ? 0.f : -(float)now * u2, D = l[x] > 0.f ? c[x] - cn : 0.f, e = __builtin_amdgcn_exp2f(-D);
+        t[x] = e * (t[x] - D * l[x]);
+        l[x] *= e;
+        c[x] = cn;
+        ref[x] = now;
+      }
+    }
+  };
+  // words [from, end) of the CT 16
+  auto take = [&](auto whole, int tag, int from, int end) MQ_INLINE {
+#pragma unroll
+    for (int i = from; i < end; ++i) {
+      const int x = i / 16, r = i % 16;
+      const float z = fmaf((float)sums[x][r], u2, c[x]), e = there(whole, r) ? __builtin_amdgcn_exp2f(z) : 0.f;
+      l[x] += e;
+      t[x] = fmaf(e, z, t[x]);
+      if constexpr (NB > 0) {
+        const int key = there(whole, r) ? (sums[x][r] << kTagBits) + (tag - r) : kNone;
+#pragma unroll
+        for (int j = NB - 1; j > 0; --j) best[x][j] = median3(best[x][j - 1], best[x][j], key);
+        best[x][0] = max(best[x][0], key);
+      }
+    }
+  };
+  auto tag = [&]() MQ_INLINE { return __builtin_amdgcn_readfirstlane(127 - (int)(held * 16)); };
+  auto counted = [&]() MQ_INLINE { if (++held == kUnitsPerList) flush(); };
+  auto arrive = [&](unsigned i) MQ_INLINE {
+    wait_loads((p.ring - 2) * each);
+    __builtin_amdgcn_s_barrier();                // stage i is there, and nobody reads the one before
+    asm volatile("" ::: "memory");
+    fetch(i + p.ring - 1);
+  };
+  // unit's sums; `beside`: the words of the unit before, settled already
+  auto multiply = [&](const uint8_t* at, auto beside) MQ_INLINE {
+    constexpr int AHEAD = 3;
+    v4i piece[AHEAD + 1];
+    auto read = [&](int f) MQ_INLINE { piece[f % (AHEAD + 1)] = *reinterpret_cast<const v4i*>(at + f * kFragBytes); };
+#pragma unroll
+    for (int f = 0; f < AHEAD; ++f) read(f);
+    if constexpr (decltype(beside)::value) settle(std::true_type{});
+    const int from = tag();
+    v16i acc[CT] = {};
+#pragma unroll
+    for (int f = 0; f < KF; ++f) {
+      if (f + AHEAD < KF) read(f + AHEAD);
+#pragma unroll
+      for (int x = 0; x < CT; ++x) acc[x] = __builtin_amdgcn_mfma_i32_32x32x32_i8(piece[f % (AHEAD + 1)], h[x][f], acc[x], 0, 0, 0);
+      if constexpr (decltype(beside)::value) take(std::true_type{}, from, f * 16 * CT / KF, (f + 1) * 16 * CT / KF);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int x = 0; x < CT; ++x)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sums[x][r] = acc[x][r];
+  };
+  const unsigned first = column * word_waves + wn;
+  // this wave's units: stages [0, count)
+  const unsigned count = tile < tiles && first < units ? (units - first + unit_step - 1) / unit_step : 0u;
+  auto place = [&](unsigned i) MQ_INLINE { return smem + i % p.ring * stage_bytes + wn * unit_bytes + lane * 16; };
+  auto last = [&]() MQ_INLINE {
+    if (unit * 32 + 32 <= p.N) {
+      settle(std::true_type{});
+      take(std::true_type{}, tag(), 0, 16 * CT);
+    } else {
+      settle(std::false_type{});
+      take(std::false_type{}, tag(), 0, 16 * CT);
+    }
+    counted();
+  };
+  if (kf == KF) {
+    if (mine > 0) {
+      arrive(0);
+      if (count > 0) {
+        unit = first;
+        multiply(place(0), std::false_type{});
+      }
+    }
+    for (unsigned i = 1; i < mine; ++i) {
+      arrive(i);
+      if (i >= count) continue;
+      multiply(place(i), std::true_type{});
+      counted();
+      unit += unit_step;
+    }
+    if (count > 0) last();
+  } else {
+    for (unsigned i = 0; i < mine; ++i) {
+      arrive(i);
+      if (i >= count) continue;
+      unit = first + i * unit_step;
+      v16i acc[CT] = {};
+#pragma unroll
+      for (int f = 0; f < KF; ++f)
+        if (f < (int)kf) {
+          const v4i w = *reinterpret_cast<const v4i*>(place(i) + f * kFragBytes);
+#pragma unroll
+          for (int x = 0; x < CT; ++x) acc[x] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w, h[x][f], acc[x], 0, 0, 0);
+        }
+#pragma unroll
+      for (int x = 0; x < CT; ++x)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sums[x][r] = acc[x][r];
+      last();
+    }
+  }
+  flush();
+#pragma unroll
+  for (int x = 0; x < CT; ++x) finish<NB, CT>(p, smem, x, tile + x, tiles, column, wave, wr, wn, word_waves, waves, lane, ref[x], c[x], l[x], t[x], top[x]);
 }
 
 // A wave per row.
@@ -336,12 +425,15 @@ __global__ __launch_bounds__(256) void k_logprob_join(const LogprobParams p) {
 
 // How the product is dealt.  A workgroup's waves share its rows, 32 each, and, where there are few of them, the words of a stage;
 // as many columns of workgroups as fill the chip once.
+inline bool two_tiles(size_t M, unsigned kf) { return M > (kf > 16 ? 256u : 384u); }
 struct Shape {
-  unsigned row_waves, word_waves, chunks, columns, ring;
+  unsigned ct, row_waves, word_waves, chunks, columns, ring;
 };
 Shape shape_of(size_t M, size_t N, unsigned kf) {
   Shape s;
-  const size_t tiles = (M + 31) / 32, units = (N + 31) / 32, most = most_waves(kf > 16 ? 32 : 16);
+  // two tiles a wave halve what it reads from LDS, where there are rows for more workgroups than one tile each would fill
+  s.ct = two_tiles(M, kf) ? 2 : 1;
+  const size_t tiles = ((M + 31) / 32 + s.ct - 1) / s.ct, units = (N + 31) / 32, most = most_waves(kf > 16 ? 32 : 16, (int)s.ct);
   s.chunks = (unsigned)((tiles + most - 1) / most);
   s.row_waves = (unsigned)((tiles + s.chunks - 1) / s.chunks);
   const size_t want = s.chunks >= kMostColumns ? 1 : kMostColumns / s.chunks;
@@ -374,9 +466,9 @@ int launch_token_logprob(const void* packedA, const void* packedW, size_t M, siz
   LogprobParams p{static_cast<const uint8_t*>(packedA), static_cast<const uint8_t*>(packedW), (unsigned)M, (unsigned)N,
                   kf, sh.columns, sh.row_waves, sh.ring, static_cast<float4*>(ws),
                   reinterpret_cast<u64*>(static_cast<float4*>(ws) + M * sh.columns), sA, sW, target, k, logprob, entropy, alt, tok};
-  auto go = [&](auto kfc, auto nbc) {
+  auto go = [&](auto kfc, auto ctc, auto nbc) {
     constexpr int NB = decltype(nbc)::value;
-    auto kern = k_logprob_stream<decltype(kfc)::value, NB>;
+    auto kern = k_logprob_stream<decltype(kfc)::value, decltype(ctc)::value, NB>;
     const unsigned waves = sh.row_waves * sh.word_waves;
     const size_t ring = (size_t)sh.ring * sh.word_waves * kf * kFragBytes, join = waves * 32 * (sizeof(float4) + NB * sizeof(u64));
     const size_t lds = sh.word_waves > 1 && join > ring ? join : ring;
@@ -391,15 +483,17 @@ int launch_token_logprob(const void* packedA, const void* packedW, size_t M, siz
     hipLaunchKernelGGL((k_logprob_join<NB>), dim3((unsigned)((M + 3) / 4)), dim3(256), 0, s, p);
     return check_hip(hipGetLastError());
   };
-  auto with_list = [&](auto kfc) {
+  auto with_list = [&](auto kfc, auto ctc) {
     switch (list_length(k)) {
-      case 0: return go(kfc, std::integral_constant<int, 0>{});
-      case 4: return go(kfc, std::integral_constant<int, 4>{});
-      default: return go(kfc, std::integral_constant<int, 8>{});
+      case 0: return go(kfc, ctc, std::integral_constant<int, 0>{});
+      case 4: return go(kfc, ctc, std::integral_constant<int, 4>{});
+      default: return go(kfc, ctc, std::integral_constant<int, 8>{});
     }
   };
-  if (kf > 16) return with_list(std::integral_constant<int, 32>{});
-  return with_list(std::integral_constant<int, 16>{});
+  constexpr std::integral_constant<int, 1> one;
+  constexpr std::integral_constant<int, 2> two;
+  if (kf > 16) return sh.ct == 2 ? with_list(std::integral_constant<int, 32>{}, two) : with_list(std::integral_constant<int, 32>{}, one);
+  return sh.ct == 2 ? with_list(std::integral_constant<int, 16>{}, two) : with_list(std::integral_constant<int, 16>{}, one);
 }
 
 }  // namespace mq
