@@ -22,8 +22,8 @@ namespace mq {
 
 namespace {
 
-// waves of a workgroup at most, by what a wave's registers leave room for (KF: pieces of K held, CT: tiles of 32 rows)
-constexpr int most_waves(int KF, int CT) { return KF == 16 ? (CT == 1 ? 12 : 8) : CT == 1 ? 8 : 4; }
+// waves of a workgroup at most, by what a wave's registers leave room for (KF: pieces of K held, CT: tiles of 32 rows, NB: list)
+constexpr int most_waves(int KF, int CT, int NB) { return KF == 16 ? (CT == 1 ? 12 : NB == 0 ? 8 : 4) : CT == 1 ? 8 : 4; }
 constexpr unsigned kMostColumns = 256;
 constexpr size_t kLdsBytes = 144 * 1024;
 #define MQ_INLINE __attribute__((always_inline))
@@ -159,7 +159,7 @@ __device__ __forceinline__ void finish(const LogprobParams& p, uint8_t* smem, in
 // A unit's matrix instructions stand beside the vector ones of the unit before (all of K held: K of 512 or 1024 elements; other
 // widths one after the other).  Pieces are asked of LDS three ahead.
 template <int KF, int CT, int NB>
-__global__ __launch_bounds__(most_waves(KF, CT) * kWave, 1) void k_logprob_stream(const LogprobParams p) {
+__global__ __launch_bounds__(most_waves(KF, CT, NB) * kWave, 1) void k_logprob_stream(const LogprobParams p) {
   constexpr int NL = NB > 0 ? NB : 1;
   extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
   const unsigned lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), waves = blockDim.x / kWave;
@@ -173,17 +173,26 @@ __global__ __launch_bounds__(most_waves(KF, CT) * kWave, 1) void k_logprob_strea
 
   // every wave issues the same number of loads for a stage (a piece may come twice), past the last stage as well: how many are
   // on their way at a given point does not depend on anything
-  auto fetch = [&](unsigned i) {
-    const unsigned stage = column + min(i, mine - 1) * p.columns, u0 = stage * word_waves, buf = i % p.ring;
+  // (a stage's units lie next to each other; slots and places by addition, a division would stand in front of every stage)
+  const size_t step = (size_t)p.columns * pieces, all = (size_t)units * kf;
+  size_t next = (size_t)column * pieces;         // first piece of the stage that is fetched next
+  unsigned next_left = mine, next_slot = 0, slot = 0;
+  const unsigned ring_bytes = p.ring * stage_bytes;
+  auto fetch = [&]() MQ_INLINE {
     for (unsigned j = 0; j < each; ++j) {
-      const unsigned piece = min(wave + j * waves, pieces - 1), u = min(u0 + piece / kf, units - 1);
-      __builtin_amdgcn_global_load_lds(
-          (const __attribute__((address_space(1))) void*)(p.packedW + ((size_t)u * kf + piece % kf) * kFragBytes + lane * 16),
-          (__attribute__((address_space(3))) void*)(smem + buf * stage_bytes + piece * kFragBytes), 16, 0, 0);
+      const unsigned piece = min(wave + j * waves, pieces - 1);
+      const size_t at = next + piece < all ? next + piece : all - 1;
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(p.packedW + at * kFragBytes + lane * 16),
+                                       (__attribute__((address_space(3))) void*)(smem + next_slot + piece * kFragBytes), 16, 0, 0);
     }
+    if (next_left > 1) {
+      --next_left;
+      next += step;
+    }
+    next_slot = next_slot + stage_bytes == ring_bytes ? 0 : next_slot + stage_bytes;
   };
   if (mine > 0)
-    for (unsigned i = 0; i + 1 < p.ring; ++i) fetch(i);
+    for (unsigned i = 0; i + 1 < p.ring; ++i) fetch();
   const float u2 = __fmul_rn(__fdiv_rn(1.0f, __fmul_rn(*p.sA, *p.sW)), 1.44269504088896340736f);
   v4i h[CT][KF];
 #pragma unroll
@@ -264,11 +273,14 @@ __global__ __launch_bounds__(most_waves(KF, CT) * kWave, 1) void k_logprob_strea
   };
   auto tag = [&]() MQ_INLINE { return __builtin_amdgcn_readfirstlane(127 - (int)(held * 16)); };
   auto counted = [&]() MQ_INLINE { if (++held == kUnitsPerList) flush(); };
-  auto arrive = [&](unsigned i) MQ_INLINE {
+  const uint8_t* here = nullptr;                 // this wave's unit of the stage
+  auto arrive = [&]() MQ_INLINE {
     wait_loads((p.ring - 2) * each);
-    __builtin_amdgcn_s_barrier();                // stage i is there, and nobody reads the one before
+    __builtin_amdgcn_s_barrier();                // the next stage is there, and nobody reads the one before
     asm volatile("" ::: "memory");
-    fetch(i + p.ring - 1);
+    fetch();
+    here = smem + slot + wn * unit_bytes + lane * 16;
+    slot = slot + stage_bytes == ring_bytes ? 0 : slot + stage_bytes;
   };
   // unit's sums; `beside`: the words of the unit before, settled already
   auto multiply = [&](const uint8_t* at, auto beside) MQ_INLINE {
@@ -296,7 +308,6 @@ __global__ __launch_bounds__(most_waves(KF, CT) * kWave, 1) void k_logprob_strea
   const unsigned first = column * word_waves + wn;
   // this wave's units: stages [0, count)
   const unsigned count = tile < tiles && first < units ? (units - first + unit_step - 1) / unit_step : 0u;
-  auto place = [&](unsigned i) MQ_INLINE { return smem + i % p.ring * stage_bytes + wn * unit_bytes + lane * 16; };
   auto last = [&]() MQ_INLINE {
     if (unit * 32 + 32 <= p.N) {
       settle(std::true_type{});
@@ -309,30 +320,30 @@ __global__ __launch_bounds__(most_waves(KF, CT) * kWave, 1) void k_logprob_strea
   };
   if (kf == KF) {
     if (mine > 0) {
-      arrive(0);
+      arrive();
       if (count > 0) {
         unit = first;
-        multiply(place(0), std::false_type{});
+        multiply(here, std::false_type{});
       }
     }
     for (unsigned i = 1; i < mine; ++i) {
-      arrive(i);
+      arrive();
       if (i >= count) continue;
-      multiply(place(i), std::true_type{});
+      multiply(here, std::true_type{});
       counted();
       unit += unit_step;
     }
     if (count > 0) last();
   } else {
     for (unsigned i = 0; i < mine; ++i) {
-      arrive(i);
+      arrive();
       if (i >= count) continue;
       unit = first + i * unit_step;
       v16i acc[CT] = {};
 #pragma unroll
       for (int f = 0; f < KF; ++f)
         if (f < (int)kf) {
-          const v4i w = *reinterpret_cast<const v4i*>(place(i) + f * kFragBytes);
+          const v4i w = *reinterpret_cast<const v4i*>(here + f * kFragBytes);
 #pragma unroll
           for (int x = 0; x < CT; ++x) acc[x] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w, h[x][f], acc[x], 0, 0, 0);
         }
@@ -429,11 +440,11 @@ inline bool two_tiles(size_t M, unsigned kf) { return M > (kf > 16 ? 256u : 384u
 struct Shape {
   unsigned ct, row_waves, word_waves, chunks, columns, ring;
 };
-Shape shape_of(size_t M, size_t N, unsigned kf) {
+Shape shape_of(size_t M, size_t N, unsigned kf, int nb) {
   Shape s;
   // two tiles a wave halve what it reads from LDS, where there are rows for more workgroups than one tile each would fill
   s.ct = two_tiles(M, kf) ? 2 : 1;
-  const size_t tiles = ((M + 31) / 32 + s.ct - 1) / s.ct, units = (N + 31) / 32, most = most_waves(kf > 16 ? 32 : 16, (int)s.ct);
+  const size_t tiles = ((M + 31) / 32 + s.ct - 1) / s.ct, units = (N + 31) / 32, most = most_waves(kf > 16 ? 32 : 16, (int)s.ct, nb);
   s.chunks = (unsigned)((tiles + most - 1) / most);
   s.row_waves = (unsigned)((tiles + s.chunks - 1) / s.chunks);
   const size_t want = s.chunks >= kMostColumns ? 1 : kMostColumns / s.chunks;
@@ -462,7 +473,7 @@ int launch_token_logprob(const void* packedA, const void* packedW, size_t M, siz
                          const float* sW, const int32_t* target, int k, float* logprob, float* entropy, int32_t* tok,
                          float* alt, void* ws, hipStream_t s) {
   const unsigned kf = (unsigned)PackedDims(8, N, K).kfrags;
-  const Shape sh = shape_of(M, N, kf);
+  const Shape sh = shape_of(M, N, kf, list_length(k));
   LogprobParams p{static_cast<const uint8_t*>(packedA), static_cast<const uint8_t*>(packedW), (unsigned)M, (unsigned)N,
                   kf, sh.columns, sh.row_waves, sh.ring, static_cast<float4*>(ws),
                   reinterpret_cast<u64*>(static_cast<float4*>(ws) + M * sh.columns), sA, sW, target, k, logprob, entropy, alt, tok};
