@@ -25,7 +25,7 @@ namespace {
 // waves of a workgroup at most, by what a wave's registers leave room for (KF: pieces of K held, CT: tiles of 32 rows, NB: list)
 constexpr int most_waves(int KF, int CT, int NB) { return KF == 16 ? (CT == 1 ? 12 : NB == 0 ? 8 : 4) : CT == 1 ? 8 : 4; }
 constexpr unsigned kMostColumns = 256;
-constexpr size_t kLdsBytes = 144 * 1024;
+constexpr size_t kLdsBytes = 160 * 1024;
 #define MQ_INLINE __attribute__((always_inline))
 constexpr int kTagBits = 7, kUnitsPerList = 8;
 constexpr int kNone = -2147483647 - 1;          // below every key: sums are above -2^24
