@@ -170,6 +170,13 @@ __device__ __forceinline__ v16f mfma_parts(const P8 (&a)[NP], const P8 (&b)[NP],
   return c;
 }
 
+// Slot of queries and head of a workgroup: the last queries of a sequence, which see most, first, and neighbouring heads, which
+// share keys and values, on one XCD (exactly where the heads are a multiple of eight), whose L2 then holds their units.
+__device__ __forceinline__ void which(const PromptParams& p, unsigned& slot, unsigned& head) {
+  slot = p.q_slots - 1 - blockIdx.x / p.heads;
+  head = xcd_remap(blockIdx.x % p.heads, p.heads);
+}
+
 // Four neighbouring columns of an output row, times inv.  vec: rows are whole 16-byte pieces.
 template <int DT>
 __device__ __forceinline__ void store4(typename Elem<DT>::T* row, float a, float b, float c, float e, float inv, unsigned at,
@@ -186,21 +193,22 @@ __device__ __forceinline__ void store4(typename Elem<DT>::T* row, float a, float
   }
 }
 
-// ND: 32-column pieces of a head.  NU: units of a tile.  BUF: tiles in LDS.
-template <int DT, int ND, int NU, int BUF>
-__global__ __launch_bounds__(kW * kWave) void k_prompt_attention(const PromptParams p) {
+// ND: 32-column pieces of a head.  NU: units of a tile.  BUF: tiles in LDS.  KS: groups of waves that take the tiles in turn and
+// join at the end (a workgroup's way through a long sequence is what a call of few sequences waits for).
+template <int DT, int ND, int NU, int BUF, int KS>
+__global__ __launch_bounds__(KS * kW * kWave) void k_prompt_attention(const PromptParams p) {
   using T = typename Elem<DT>::T;
   using P8 = Part8<DT>;
   constexpr int NP = kParts<DT>;
   constexpr unsigned UNIT = 2 * kUnit * 32 * ND * 2 * NP, TILE = NU * UNIT;
   extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
-  const unsigned lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const unsigned lane = threadIdx.x % kWave, any_wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const unsigned wave = any_wave % kW, group = any_wave / kW;
   const unsigned col = lane % 32, half = lane / 32, d = p.d;
   const unsigned per = p.heads / p.kv_heads;
-  // one kv head's workgroups next to each other on an XCD, whose L2 then holds its units; the last queries, which see most, first
-  const unsigned id = xcd_remap(blockIdx.x, gridDim.x);
-  const unsigned kvh = id / (p.q_slots * per), in = id % (p.q_slots * per);
-  const unsigned slot = p.q_slots - 1 - in / per, head = kvh * per + in % per;
+  unsigned slot, head;
+  which(p, slot, head);
+  const unsigned kvh = head / per;
   constexpr unsigned BM = kW * kQ;
   const int b = wave_search(p.B, slot, [&](unsigned i) { return first_at(p.q_first, i, p.Tq) / BM + i; });
   if (b < 0) return;
@@ -223,16 +231,6 @@ __global__ __launch_bounds__(kW * kWave) void k_prompt_attention(const PromptPar
   const unsigned wave_last = iw < nq ? seen_by(nq - iw < (unsigned)kQ ? nq - 1 : iw + kQ - 1) : 0u;   // most keys of this wave
   const unsigned wave_least = iw + kQ <= nq ? seen_by(iw) : 0u;                                        // fewest
 
-  P8 qf[2 * ND][NP];
-  {
-    const T* src = static_cast<const T*>(p.q) + (size_t)(q0 + (mine ? i : i0)) * p.ldq + (size_t)head * d;
-#pragma unroll
-    for (int f = 0; f < 2 * ND; ++f) {
-      float x[8];
-      row8<DT>(src, f * 16 + half * 8, d, p.vec, x);
-      split_parts<DT>(x, qf[f]);
-    }
-  }
   const unsigned units = (nk + kUnit - 1) / kUnit;          // that the sequence has
   const uint8_t* base = p.units + ((size_t)kvh * p.k_slots + unit0) * UNIT;
   auto fetch = [&](unsigned tile, unsigned buf) {
@@ -240,7 +238,7 @@ __global__ __launch_bounds__(kW * kWave) void k_prompt_attention(const PromptPar
     for (unsigned u = 0; u < NU; ++u) {
       const unsigned n = tile * NU + u < units ? tile * NU + u : units - 1;      // past the end: the last one, masked
       const uint8_t* src = base + (size_t)n * UNIT + lane * 16;
-      uint8_t* dst = smem + buf * TILE + u * UNIT;
+      uint8_t* dst = smem + (buf * KS + group) * TILE + u * UNIT;
 #pragma unroll
       for (unsigned c = 0; c < UNIT / 1024 / kW; ++c) {
         const unsigned piece = c * kW + wave;
@@ -251,24 +249,39 @@ __global__ __launch_bounds__(kW * kWave) void k_prompt_attention(const PromptPar
   };
   static_assert(UNIT % (1024 * kW) == 0, "pieces of a unit");
 
+  if (tiles > 0 && BUF == 2) fetch(group, 0);              // (on its way while the queries come)
+  P8 qf[2 * ND][NP];
+  {
+    const T* src = static_cast<const T*>(p.q) + (size_t)(q0 + (mine ? i : i0)) * p.ldq + (size_t)head * d;
+#pragma unroll
+    for (int f = 0; f < 2 * ND; ++f) {
+      float x[8];
+      row8<DT>(src, f * 16 + half * 8, d, p.vec, x);
+      split_parts<DT>(x, qf[f]);
+    }
+  }
   v16f o[ND];
 #pragma unroll
   for (int t = 0; t < ND; ++t) o[t] = v16f{};
   float top = -INFINITY, total = 0.f;
   bool poison = false;
-  if (tiles > 0 && BUF == 2) fetch(0, 0);
-  for (unsigned tile = 0; tile < tiles; ++tile) {
-    const unsigned buf = BUF == 2 ? tile & 1 : 0;
+  // (looked at in front of the loop: in it, this load would be waited for behind the next tile's)
+  unsigned any = 0;
+  for (unsigned n = lane; n < units; n += kWave) any |= p.bad[(size_t)kvh * p.k_slots + unit0 + n];
+  const bool some_bad = __any(any != 0);
+  const unsigned steps = (tiles + KS - 1) / KS;            // (past the end: keys that nobody sees)
+  for (unsigned step = 0; step < steps; ++step) {
+    const unsigned buf = BUF == 2 ? step & 1 : 0, tile = step * KS + group;
     if (BUF == 1) {
       __syncthreads();                       // everybody is done with the tile before
       fetch(tile, 0);
     }
     __builtin_amdgcn_s_waitcnt(0x0F70);      // this wave's pieces are in LDS
     __syncthreads();
-    if (BUF == 2 && tile + 1 < tiles) fetch(tile + 1, buf ^ 1);
+    if (BUF == 2 && step + 1 < steps) fetch(tile + KS, buf ^ 1);
     const unsigned j0 = tile * NU * kUnit;
     if (j0 >= wave_last) continue;
-    const uint8_t* at = smem + buf * TILE + lane * 16;
+    const uint8_t* at = smem + (buf * KS + group) * TILE + lane * 16;
     v16f s[NU];
 #pragma unroll
     for (int u = 0; u < NU; ++u) {
@@ -291,6 +304,7 @@ __global__ __launch_bounds__(kW * kWave) void k_prompt_attention(const PromptPar
         s[u][r] = whole || j < seen ? s[u][r] * p.scale2 : -INFINITY;
         m = fmaxf(m, s[u][r]);
       }
+    if (__builtin_expect(some_bad, 0))
 #pragma unroll
     for (int u = 0; u < NU; ++u) {
       const unsigned n = tile * NU + u;
@@ -309,11 +323,11 @@ __global__ __launch_bounds__(kW * kWave) void k_prompt_attention(const PromptPar
 #pragma unroll
     for (int u = 0; u < NU; ++u)
 #pragma unroll
-      for (int step = 0; step < 2; ++step) {
+      for (int part = 0; part < 2; ++part) {
         float e[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          e[j] = __builtin_amdgcn_exp2f(s[u][8 * step + j] - ref);
+          e[j] = __builtin_amdgcn_exp2f(s[u][8 * part + j] - ref);
           total += e[j];
         }
         P8 pf[NP];
@@ -323,10 +337,36 @@ __global__ __launch_bounds__(kW * kWave) void k_prompt_attention(const PromptPar
           P8 vf[NP];
 #pragma unroll
           for (int n = 0; n < NP; ++n)
-            vf[n] = *reinterpret_cast<const P8*>(at + u * UNIT + ((2 * ND + 2 * t + step) * NP + n) * 1024);
+            vf[n] = *reinterpret_cast<const P8*>(at + u * UNIT + ((2 * ND + 2 * t + part) * NP + n) * 1024);
           o[t] = mfma_parts<NP>(vf, pf, o[t]);
         }
       }
+  }
+  if constexpr (KS == 2) {
+    // the second group's sums to the first, wave by wave; a lane's piece next to its neighbours'
+    constexpr int ROWS = 16 * ND + 3;
+    static_assert(kW * ROWS * kWave * 4 <= KS * BUF * TILE, "the sums of a group");
+    float* box = reinterpret_cast<float*>(smem) + wave * ROWS * kWave + lane;
+    __syncthreads();
+    if (group == 1) {
+#pragma unroll
+      for (int t = 0; t < ND; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) box[(16 * t + r) * kWave] = o[t][r];
+      box[16 * ND * kWave] = top;
+      box[(16 * ND + 1) * kWave] = total;
+      box[(16 * ND + 2) * kWave] = poison ? 1.f : 0.f;
+    }
+    __syncthreads();
+    if (group == 1) return;
+    const float other = box[16 * ND * kWave], m = fmaxf(top, other), ref = m == -INFINITY ? 0.f : m;
+    const float a = __builtin_amdgcn_exp2f(top - ref), b = __builtin_amdgcn_exp2f(other - ref);
+    total = total * a + box[(16 * ND + 1) * kWave] * b;
+    poison |= box[(16 * ND + 2) * kWave] != 0.f;
+#pragma unroll
+    for (int t = 0; t < ND; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[t][r] = o[t][r] * a + box[(16 * t + r) * kWave] * b;
   }
   total = across32_f(total, [](float a, float b) { return a + b; });
   if (!mine) return;
@@ -400,9 +440,9 @@ __global__ __launch_bounds__(kW * kWave, 1) void k_prompt_wide(const PromptParam
   const unsigned lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const unsigned col = lane % 32, half = lane / 32, d = p.d;
   const unsigned per = p.heads / p.kv_heads;
-  const unsigned id = xcd_remap(blockIdx.x, gridDim.x);
-  const unsigned kvh = id / (p.q_slots * per), in = id % (p.q_slots * per);
-  const unsigned slot = p.q_slots - 1 - in / per, head = kvh * per + in % per;
+  unsigned slot, head;
+  which(p, slot, head);
+  const unsigned kvh = head / per;
   const int b = __builtin_amdgcn_readfirstlane(wave_search(p.B, slot, [&](unsigned i) { return first_at(p.q_first, i, p.Tq) / BM + i; }));
   if (b < 0) return;
   const unsigned q0 = first_at(p.q_first, b, p.Tq), q1 = first_at(p.q_first, b + 1, p.Tq), nq = q1 > q0 ? q1 - q0 : 0;
@@ -835,7 +875,7 @@ size_t prompt_attention_ws_bytes(int dtype, size_t B, size_t Tk, int kv_heads, s
 int launch_prompt_attention(const void* q, size_t ldq, const void* k, size_t ldk, const void* v, size_t ldv, int dtype,
                             const int32_t* q_first, const int32_t* k_first, size_t B, size_t Tq, size_t Tk, int heads,
                             int kv_heads, size_t d, int causal, float scale, void* out, size_t ldo, void* ws, hipStream_t s) {
-  const size_t n = k_slots(B, Tk) * (size_t)kv_heads, q_slots = Tq / (kW * kQ) + B, wgs = q_slots * (size_t)heads;
+  const size_t n = k_slots(B, Tk) * (size_t)kv_heads, q_slots = Tq / (kW * kQ) + B;
   if (n >= (size_t)1 << 31 || (Tq / kQShort + B) * (size_t)heads >= (size_t)1 << 31) return MQ_ERR_SHAPE;
   const bool is_short = d <= 128 && ldq < (size_t)1 << 24 && ldk < (size_t)1 << 24 && ldv < (size_t)1 << 24 && Tq <= 64 * B && Tk <= 64 * B;
   const bool is_long = d <= 128 && scale != 0.f && Tq >= 256 * B;
@@ -898,14 +938,16 @@ int launch_prompt_attention(const void* q, size_t ldq, const void* k, size_t ldk
       // two units to a tile and two tiles in LDS where they fit, else one of both
       constexpr unsigned UNIT = 2 * kUnit * 32 * ND * 2 * kParts<DT>;
       constexpr int NU = DT != MQ_F32 && 4 * UNIT <= kLds ? 2 : 1, BUF = 2 * NU * UNIT <= kLds ? 2 : 1;
-      auto kern = k_prompt_attention<DT, ND, NU, BUF>;
-      constexpr unsigned lds = NU * BUF * UNIT;
+      // and two groups of waves, where LDS holds as much for each
+      constexpr int KS = DT == MQ_F32 && 2 * NU * BUF * UNIT <= kLds ? 2 : 1;
+      auto kern = k_prompt_attention<DT, ND, NU, BUF, KS>;
+      constexpr unsigned lds = NU * BUF * KS * UNIT;
       if (lds > 65536) {
         const int e = check_hip(hipFuncSetAttribute(reinterpret_cast<const void*>(kern),
                                                     hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
         if (e != MQ_OK) return e;
       }
-      hipLaunchKernelGGL(kern, dim3((unsigned)wgs), dim3(kW * kWave), lds, s, p);
+      hipLaunchKernelGGL(kern, dim3((unsigned)(p.q_slots * (size_t)heads)), dim3(KS * kW * kWave), lds, s, p);
       return check_hip(hipGetLastError());
     };
     switch (padded((unsigned)d) / 32) {
