@@ -12,13 +12,13 @@
  * `stream` and return an mq_status, arguments checked before anything is enqueued.  No call here waits inside a kernel for
  * other workgroups, none needs a prepared workspace, and none keeps anything from one call to the next; a workspace's
  * contents are irrelevant on entry and undefined on return, so calls that may overlap in time (two streams, two captured
- * graphs) need one each.  Results do not depend on what else runs: no atomics.
+ * graphs) need one each.  Results depend neither on what else runs nor on an order of atomics.
  *
  * Types.  Queries, keys, values and outputs are of one type, an mq_dtype.  Arithmetic is binary32 or better whatever the
  * type; a result is rounded to the type once.
- * Rows.  A "token row" holds heads x head_dim elements, head after head; rows are `ld` elements apart (ld >= heads head_dim),
- * so that queries, keys and values may be columns of one product's result.  Base pointers and ld need the alignment of one
- * element only (out, q, k, v aligned to 16 bytes with ld a multiple of 16 bytes load faster).
+ * Rows.  A "token row" holds heads x head_dim neighbouring elements, head after head; rows are `ld` elements apart
+ * (ld >= heads head_dim), so that queries, keys and values may be columns of one product's result.  Base pointers and ld need
+ * the alignment of one element only (rows and heads that start on 16 bytes load faster).
  * Heads.  Queries have `heads` heads, keys and values kv_heads; heads is a multiple of kv_heads and query head h reads
  * kv head h / (heads / kv_heads).  1 <= head_dim <= 256, heads <= 1024.
  * Packed sequences.  `first` is a device int32 [B + 1], ascending, first[0] >= 0: sequence b has token rows first[b] ..
@@ -87,7 +87,7 @@ int mq_kv_append(const mq_kv_cache* cache, const int32_t* table, size_t table_wi
  *   out[b] = sum_t p_t V[t],  p = softmax over t < lens[b] of scale (q[b] . K[t]),  per head;
  * zeros where nothing is there to attend to.
  *   lens: device int32 [B]; values above max_len count as max_len, negative ones as 0.  max_len <= 64 table_width.
- *   q: token rows [B] of `heads` heads, out likewise (it may be q itself).
+ *   q: token rows [B] of `heads` heads, out likewise (it may be q itself, with ldo = ldq).
  * Queries and probabilities enter the integer products with a scale of their own for each row, binary32 ones as 24-bit
  * values, 16-bit types as 16-bit values; sums are exact, the softmax statistics binary32.
  * ws: device, 16-byte aligned, mq_cached_attention_ws_bytes (0 for invalid arguments).  One launch, two where a sequence is
@@ -103,10 +103,11 @@ int mq_cached_attention(const mq_kv_cache* cache, const int32_t* table, size_t t
  *   out[i] = sum_j p_j v[j],  p = softmax over the keys seen of scale (q[i] . k[j]),  per head.
  * What lies at places a query does not see never counts, whatever it holds.  A key position with a NaN or an infinity in its
  * key or its value turns the whole output (of that head) of every query that sees it into NaN.
- * Binary32 operands enter the matrix products as two binary16 halves with a power-of-two scale for each tile (22 bits);
- * sums are binary32.
+ * Binary32 operands are multiplied as binary32, or as three bfloat16 parts that hold all of their 24 bits; probabilities of
+ * 16-bit types are rounded to the type.  Sums and softmax statistics are binary32.
  * ws: device, 256-byte aligned, mq_prompt_attention_ws_bytes (0 for invalid arguments): keys and values in the order the
- * products read them.  Two launches.  out must not overlap k or v; it may be q itself. */
+ * products read them.  Two launches; one where the sequences have up to 64 queries and keys on average and head_dim <= 128.
+ * out must not overlap k or v; it may be q itself, with ldo = ldq. */
 size_t mq_prompt_attention_ws_bytes(int dtype, size_t B, size_t Tk, int kv_heads, size_t head_dim);
 int mq_prompt_attention(const void* q, size_t ldq, const void* k, size_t ldk, const void* v, size_t ldv, int dtype,
                         const int32_t* q_first, const int32_t* k_first, size_t B, size_t Tq, size_t Tk, int heads,

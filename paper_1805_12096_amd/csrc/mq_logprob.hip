@@ -244,7 +244,8 @@ __global__ __launch_bounds__(most_waves(KF, CT, NB) * kWave, 1) void k_logprob_s
     for (int x = 0; x < CT; ++x) {
       int most = kNone;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) most = max(most, there(whole, r) ? sums[x][r] : kNone);
+      for (int r = 0; r < 16; r += 2)
+        most = max(max(most, there(whole, r) ? sums[x][r] : kNone), there(whole, r + 1) ? sums[x][r + 1] : kNone);
       if (__builtin_expect(__any(most > ref[x]), 0)) {
         const int now = max(most, ref[x]);
         const float cn = now == kNone ? 0.f : -(float)now * u2, D = l[x] > 0.f ? c[x] - cn : 0.f, e = __builtin_amdgcn_exp2f(-D);
@@ -438,7 +439,7 @@ __global__ __launch_bounds__(256) void k_logprob_join(const LogprobParams p) {
 // as many columns of workgroups as fill the chip once.
 inline bool two_tiles(size_t M, unsigned kf) { return M > (kf > 16 ? 256u : 384u); }
 struct Shape {
-  unsigned ct, row_waves, word_waves, chunks, columns, ring;
+  unsigned ct, row_waves, word_waves, chunks, columns, ring, most_columns;     // (columns whatever K is)
 };
 Shape shape_of(size_t M, size_t N, unsigned kf, int nb) {
   Shape s;
@@ -448,6 +449,7 @@ Shape shape_of(size_t M, size_t N, unsigned kf, int nb) {
   s.chunks = (unsigned)((tiles + most - 1) / most);
   s.row_waves = (unsigned)((tiles + s.chunks - 1) / s.chunks);
   const size_t want = s.chunks >= kMostColumns ? 1 : kMostColumns / s.chunks;
+  s.most_columns = (unsigned)want;
   // units of a stage: as many waves as there are, as one round of the columns needs, and as LDS holds twice
   size_t words = most / s.row_waves;
   const size_t needed = (units + want - 1) / want, fit = kLdsBytes / 2 / (kf * kFragBytes);
@@ -466,7 +468,10 @@ int list_length(int k) { return k == 0 ? 0 : k <= 4 ? 4 : 8; }
 }  // namespace
 
 size_t token_logprob_ws_bytes(size_t M, size_t N, int k) {
-  return M * kMostColumns * (sizeof(float4) + list_length(k) * sizeof(u64));
+  // (K is not known here: the wider layout has more chunks of rows, but may hold one tile a wave where the other has two)
+  const int nb = list_length(k);
+  const size_t a = shape_of(M, N, 16, nb).most_columns, b = shape_of(M, N, 32, nb).most_columns;
+  return M * (a > b ? a : b) * (sizeof(float4) + nb * sizeof(u64));
 }
 
 int launch_token_logprob(const void* packedA, const void* packedW, size_t M, size_t N, size_t K, const float* sA,

@@ -57,15 +57,19 @@ def _lib():
     return lib
 
 
-def _p(t):
+def _current() -> int:
+    """The current device's number (without building an object for it: a decode-sized call's host time shows)."""
+    return binding._device() if binding._device is not None else torch.cuda.current_device()
+
+
+def _p(t, current=None):
     """Device address of a tensor on the current device (None -> NULL); raw ints pass through."""
     if t is None or isinstance(t, int):
         return t
     if not t.is_cuda:
         raise ValueError(f"a tensor on {t.device} was passed: the library takes device memory")
-    current = binding._device() if binding._device is not None else torch.cuda.current_device()
-    if t.get_device() != current:
-        raise ValueError(f"a tensor on {t.device} was passed while the current device is cuda:{current}")
+    if t.get_device() != (_current() if current is None else current):
+        raise ValueError(f"a tensor on {t.device} was passed while the current device is another")
     return t.data_ptr()
 
 
@@ -89,6 +93,7 @@ class KvCache:
             raise ValueError("tensors do not have the sizes of a cache of that many blocks and heads")
         self.keys, self.values, self.amax = keys, values, amax
         self.blocks, self.kv_heads, self.head_dim = blocks, kv_heads, head_dim
+        self.device = keys.get_device() if keys.is_cuda and values.device == keys.device == amax.device else -1
         self.c = _CKvCache(keys.data_ptr(), values.data_ptr(), amax.data_ptr(), blocks, kv_heads, head_dim)
 
 
@@ -100,10 +105,15 @@ def kv_cache(blocks: int, kv_heads: int, head_dim: int, device="cuda") -> KvCach
                    torch.zeros((blocks, kv_heads, 2), dtype=torch.float32, device=device), blocks, kv_heads, head_dim)
 
 
-def _cache(cache):
-    for t in (cache.keys, cache.values, cache.amax):
-        _p(t)
+def _cache(cache, current):
+    if cache.device != current:
+        raise ValueError("a cache that is not on the current device")
     return ctypes.byref(cache.c)
+
+
+def _here():
+    """The current device, or none that a tensor could be on while nothing has touched a device yet."""
+    return _current() if torch.cuda.is_initialized() else -2
 
 
 def mq_kv_key_bytes(blocks, kv_heads, head_dim) -> int:
@@ -117,9 +127,10 @@ def mq_kv_value_bytes(blocks, kv_heads, head_dim) -> int:
 def mq_kv_append(cache, table, table_width, first, held, B, T, k, ldk, v, ldv, q, ldq, heads, dtype, freq, rot, interleaved,
                  k_out=None, q_out=None, stream=None):
     """cache: a KvCache; everything else as in include/mq_seq.h."""
-    _check(_lib().mq_kv_append(_cache(cache), _p(table), table_width, _p(first), _p(held), B, T, _p(k), ldk, _p(v), ldv, _p(q),
-                               ldq, heads, dtype, _p(freq), rot, int(interleaved), _p(k_out), _p(q_out), _stream(stream)),
-           "mq_kv_append")
+    c = _here()
+    _check(_lib().mq_kv_append(_cache(cache, c), _p(table, c), table_width, _p(first, c), _p(held, c), B, T, _p(k, c), ldk,
+                               _p(v, c), ldv, _p(q, c), ldq, heads, dtype, _p(freq, c), rot, int(interleaved), _p(k_out, c),
+                               _p(q_out, c), _stream(stream)), "mq_kv_append")
 
 
 def mq_cached_attention_ws_bytes(B, max_len, heads, kv_heads, head_dim) -> int:
@@ -129,8 +140,10 @@ def mq_cached_attention_ws_bytes(B, max_len, heads, kv_heads, head_dim) -> int:
 def mq_cached_attention(cache, table, table_width, lens, B, max_len, q, ldq, heads, dtype, scale, out, ldo, ws, ws_bytes,
                         stream=None):
     """cache: a KvCache; everything else as in include/mq_seq.h."""
-    _check(_lib().mq_cached_attention(_cache(cache), _p(table), table_width, _p(lens), B, max_len, _p(q), ldq, heads, dtype,
-                                      scale, _p(out), ldo, _p(ws), ws_bytes, _stream(stream)), "mq_cached_attention")
+    c = _here()
+    _check(_lib().mq_cached_attention(_cache(cache, c), _p(table, c), table_width, _p(lens, c), B, max_len, _p(q, c), ldq, heads,
+                                      dtype, scale, _p(out, c), ldo, _p(ws, c), ws_bytes, _stream(stream)),
+           "mq_cached_attention")
 
 
 def mq_prompt_attention_ws_bytes(dtype, B, Tk, kv_heads, head_dim) -> int:
@@ -139,9 +152,10 @@ def mq_prompt_attention_ws_bytes(dtype, B, Tk, kv_heads, head_dim) -> int:
 
 def mq_prompt_attention(q, ldq, k, ldk, v, ldv, dtype, q_first, k_first, B, Tq, Tk, heads, kv_heads, head_dim, causal, scale,
                         out, ldo, ws, ws_bytes, stream=None):
-    _check(_lib().mq_prompt_attention(_p(q), ldq, _p(k), ldk, _p(v), ldv, dtype, _p(q_first), _p(k_first), B, Tq, Tk, heads,
-                                      kv_heads, head_dim, int(causal), scale, _p(out), ldo, _p(ws), ws_bytes, _stream(stream)),
-           "mq_prompt_attention")
+    c = _here()
+    _check(_lib().mq_prompt_attention(_p(q, c), ldq, _p(k, c), ldk, _p(v, c), ldv, dtype, _p(q_first, c), _p(k_first, c), B, Tq,
+                                      Tk, heads, kv_heads, head_dim, int(causal), scale, _p(out, c), ldo, _p(ws, c), ws_bytes,
+                                      _stream(stream)), "mq_prompt_attention")
 
 
 def mq_token_logprob_ws_bytes(M, N, k) -> int:
@@ -150,6 +164,7 @@ def mq_token_logprob_ws_bytes(M, N, k) -> int:
 
 def mq_gemm_token_logprob_packed(packedA, packedW, M, N, K, sA, sW, target, k, logprob, entropy, tok, alt_logprob, ws, ws_bytes,
                                  stream=None):
-    _check(_lib().mq_gemm_token_logprob_packed(_p(packedA), _p(packedW), M, N, K, _p(sA), _p(sW), _p(target), int(k),
-                                               _p(logprob), _p(entropy), _p(tok), _p(alt_logprob), _p(ws), ws_bytes,
-                                               _stream(stream)), "mq_gemm_token_logprob_packed")
+    c = _here()
+    _check(_lib().mq_gemm_token_logprob_packed(_p(packedA, c), _p(packedW, c), M, N, K, _p(sA, c), _p(sW, c), _p(target, c),
+                                               int(k), _p(logprob, c), _p(entropy, c), _p(tok, c), _p(alt_logprob, c), _p(ws, c),
+                                               ws_bytes, _stream(stream)), "mq_gemm_token_logprob_packed")
