@@ -22,8 +22,8 @@ namespace mq {
 
 namespace {
 
-// waves of a workgroup at most, by what a wave's registers leave room for (KF: pieces of K held, CT: tiles of 32 rows, NB: list)
-constexpr int most_waves(int KF, int CT, int NB) { return KF == 16 ? (CT == 1 ? 12 : NB == 0 ? 8 : 4) : CT == 1 ? 8 : 4; }
+// waves of a workgroup at most, by what a wave's registers leave room for (KF: pieces of K held, CT: tiles of 32 rows)
+constexpr int most_waves(int KF, int CT) { return KF == 16 && CT == 1 ? 12 : 8; }
 constexpr unsigned kMostColumns = 256;
 constexpr size_t kLdsBytes = 160 * 1024;
 #define MQ_INLINE __attribute__((always_inline))
@@ -159,7 +159,7 @@ __device__ __forceinline__ void finish(const LogprobParams& p, uint8_t* smem, in
 // A unit's matrix instructions stand beside the vector ones of the unit before (all of K held: K of 512 or 1024 elements; other
 // widths one after the other).  Pieces are asked of LDS three ahead.
 template <int KF, int CT, int NB>
-__global__ __launch_bounds__(most_waves(KF, CT, NB) * kWave, 1) void k_logprob_stream(const LogprobParams p) {
+__global__ __launch_bounds__(most_waves(KF, CT) * kWave, 1) void k_logprob_stream(const LogprobParams p) {
   constexpr int NL = NB > 0 ? NB : 1;
   extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
   const unsigned lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), waves = blockDim.x / kWave;
@@ -437,15 +437,17 @@ __global__ __launch_bounds__(256) void k_logprob_join(const LogprobParams p) {
 
 // How the product is dealt.  A workgroup's waves share its rows, 32 each, and, where there are few of them, the words of a stage;
 // as many columns of workgroups as fill the chip once.
-inline bool two_tiles(size_t M, unsigned kf) { return M > (kf > 16 ? 256u : 384u); }
+// Two tiles of rows a wave halve what it reads from LDS, and take twice its registers, so half the waves.  Measured over 36000
+// words, one tile / two (us): K = 512 without a list 768 rows 27 / 30, 1024 rows 36 / 31, 4096 rows 91 / 84, 8192 rows 170 / 156;
+// with 4 best words 1024 rows 42 / 43, 8192 rows 217 / 246; K = 1024 8192 rows 292 / 290 without a list, 326 / 349 with.
+inline bool two_tiles(size_t M, unsigned kf, int nb) { return kf <= 16 && nb == 0 && M > 896; }
 struct Shape {
   unsigned ct, row_waves, word_waves, chunks, columns, ring, most_columns;     // (columns whatever K is)
 };
 Shape shape_of(size_t M, size_t N, unsigned kf, int nb) {
   Shape s;
-  // two tiles a wave halve what it reads from LDS, where there are rows for more workgroups than one tile each would fill
-  s.ct = two_tiles(M, kf) ? 2 : 1;
-  const size_t tiles = ((M + 31) / 32 + s.ct - 1) / s.ct, units = (N + 31) / 32, most = most_waves(kf > 16 ? 32 : 16, (int)s.ct, nb);
+  s.ct = two_tiles(M, kf, nb) ? 2 : 1;
+  const size_t tiles = ((M + 31) / 32 + s.ct - 1) / s.ct, units = (N + 31) / 32, most = most_waves(kf > 16 ? 32 : 16, (int)s.ct);
   s.chunks = (unsigned)((tiles + most - 1) / most);
   s.row_waves = (unsigned)((tiles + s.chunks - 1) / s.chunks);
   const size_t want = s.chunks >= kMostColumns ? 1 : kMostColumns / s.chunks;
@@ -499,17 +501,18 @@ int launch_token_logprob(const void* packedA, const void* packedW, size_t M, siz
     hipLaunchKernelGGL((k_logprob_join<NB>), dim3((unsigned)((M + 3) / 4)), dim3(256), 0, s, p);
     return check_hip(hipGetLastError());
   };
-  auto with_list = [&](auto kfc, auto ctc) {
-    switch (list_length(k)) {
-      case 0: return go(kfc, ctc, std::integral_constant<int, 0>{});
-      case 4: return go(kfc, ctc, std::integral_constant<int, 4>{});
-      default: return go(kfc, ctc, std::integral_constant<int, 8>{});
-    }
-  };
   constexpr std::integral_constant<int, 1> one;
   constexpr std::integral_constant<int, 2> two;
-  if (kf > 16) return sh.ct == 2 ? with_list(std::integral_constant<int, 32>{}, two) : with_list(std::integral_constant<int, 32>{}, one);
-  return sh.ct == 2 ? with_list(std::integral_constant<int, 16>{}, two) : with_list(std::integral_constant<int, 16>{}, one);
+  auto with_list = [&](auto kfc) {
+    switch (list_length(k)) {
+      case 0: return go(kfc, one, std::integral_constant<int, 0>{});
+      case 4: return go(kfc, one, std::integral_constant<int, 4>{});
+      default: return go(kfc, one, std::integral_constant<int, 8>{});
+    }
+  };
+  if (kf > 16) return with_list(std::integral_constant<int, 32>{});
+  if (sh.ct == 2) return go(std::integral_constant<int, 16>{}, two, std::integral_constant<int, 0>{});
+  return with_list(std::integral_constant<int, 16>{});
 }
 
 }  // namespace mq

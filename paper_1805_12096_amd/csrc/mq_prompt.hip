@@ -865,6 +865,16 @@ __global__ __launch_bounds__(256, ND <= 2 ? 3 : 2) void k_prompt_short(const Pro
 
 }  // namespace
 
+// Which kernel: by the mean length, the only one known without reading the lists.  Measured (us, causal, sequences x length,
+// d = 64 with 8 heads | d = 128 with 16 heads over 4):
+//   binary32, pack + attention / short: 64 x 96 41 / 19 | 75 / 62, 32 x 192 37 / 32 | 98 / 99, 32 x 256 52 / 51 | 120 / 155,
+//     8 x 800 72 / 96
+//   bfloat16, pack + attention / short: 64 x 96 18 / 13 | 39 / 39, 64 x 128 25 / 17 | 58 / 55, 32 x 192 19 / 20 | 39 / 57,
+//     16 x 400 25 / 34 | 54 / 98
+//   bfloat16, pack + attention / pack + wide: 8 x 1100 52 / 60 | 100 / 116, 16 x 1500 110 / 104 | 277 / 286,
+//     4 x 2000 72 / 64 | 142 / 131, 3 x 3000 90 / 89 | 199 / 184, 2 x 8000 296 / 289 | 701 / 566
+constexpr size_t kShortMean32 = 192, kShortMean16 = 128, kLongMean = 1536;
+
 static size_t k_slots(size_t B, size_t Tk) { return Tk / kUnit + B; }
 
 size_t prompt_attention_ws_bytes(int dtype, size_t B, size_t Tk, int kv_heads, size_t d) {
@@ -877,8 +887,9 @@ int launch_prompt_attention(const void* q, size_t ldq, const void* k, size_t ldk
                             int kv_heads, size_t d, int causal, float scale, void* out, size_t ldo, void* ws, hipStream_t s) {
   const size_t n = k_slots(B, Tk) * (size_t)kv_heads, q_slots = Tq / (kW * kQ) + B;
   if (n >= (size_t)1 << 31 || (Tq / kQShort + B) * (size_t)heads >= (size_t)1 << 31) return MQ_ERR_SHAPE;
-  const bool is_short = d <= 128 && ldq < (size_t)1 << 24 && ldk < (size_t)1 << 24 && ldv < (size_t)1 << 24 && Tq <= 64 * B && Tk <= 64 * B;
-  const bool is_long = d <= 128 && scale != 0.f && Tq >= 256 * B;
+  const size_t few = (dtype == MQ_F32 ? kShortMean32 : kShortMean16) * B;
+  const bool is_short = d <= 128 && ldq < (size_t)1 << 24 && ldk < (size_t)1 << 24 && ldv < (size_t)1 << 24 && Tq <= few && Tk <= few;
+  const bool is_long = d <= 128 && scale != 0.f && Tq >= kLongMean * B;
   const size_t per16 = 16 / elem_bytes(dtype);
   auto whole = [&](const void* x, size_t ld) { return reinterpret_cast<uintptr_t>(x) % 16 == 0 && ld % per16 == 0; };
   const bool vec = d % 8 == 0 && whole(q, ldq) && whole(k, ldk) && whole(v, ldv) && whole(out, ldo);

@@ -476,8 +476,11 @@ SEQUENCES = [  # queries, keys
     ([1, 40, 1, 130], [70, 200, 1, 131]),
     ([50, 33, 3], [20, 0, 1]),                       # more queries than keys: with a causal mask the first see nothing
     ([1, 31, 32, 33, 0, 64, 65, 7], [3, 31, 40, 33, 0, 64, 65, 100]),       # few of each: the one-launch form
-    ([700, 257], [700, 300]),                        # many of each: two tiles a wave (16-bit types)
+    ([700, 257], [700, 300]),
     ([600, 450, 33, 1], [2500, 1, 0, 40]),
+    ([1, 31, 32, 33, 0, 64, 65, 127, 128, 129, 5, 1501, 700], None),       # short ones beside long ones
+    ([1700, 1500], [1700, 1601]),                    # many of each: two tiles a wave (16-bit types)
+    ([1601, 1473], [33, 2000]),
 ]
 
 
@@ -508,7 +511,7 @@ def test_prompt_attention(which, heads, hk, dim, dtype, causal):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("n,others", [(150, 0), (150, 7), (300, 0)])      # (empty sequences: the one-launch form takes the call)
+@pytest.mark.parametrize("n,others", [(150, 0), (150, 7), (300, 0), (1600, 0)])      # (empty sequences: the one-launch form takes the call)
 def test_prompt_attention_masked_places_never_count(dtype, n, others):
     g = gen(21)
     heads, hk, dim = 2, 1, 64
@@ -533,6 +536,18 @@ def test_prompt_attention_masked_places_never_count(dtype, n, others):
     got = prompt(qb.to(DEV), k.to(DEV), v.to(DEV), ends, ends, heads, hk, dim, True, 0.125).cpu()
     assert torch.isnan(got[7, dim:]).all() and torch.equal(got[7, :dim], clean[7, :dim])
     assert torch.equal(got[:7], clean[:7]) and torch.equal(got[8:], clean[8:])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("scale", [-0.125, 0.0])
+@pytest.mark.parametrize("n", [70, 300, 1600])
+def test_prompt_attention_scales_that_are_not_positive(n, scale, dtype):
+    g = gen(25)
+    heads, hk, dim = 2, 1, 64
+    q, k, v = (normal(g, n, h * dim).to(dtype) for h in (heads, hk, hk))
+    want, tol = prompt_reference(q, k, v, [0, n], [0, n], heads, hk, dim, True, scale)
+    got = prompt(q.to(DEV), k.to(DEV), v.to(DEV), [0, n], [0, n], heads, hk, dim, True, scale).cpu().double()
+    assert ((got - want).abs() <= tol).all()
 
 
 @pytest.mark.parametrize("others", [0, 3])
@@ -637,7 +652,8 @@ def ints(g, rows, cols, most=127):
 @pytest.mark.parametrize("M,N,K,k", [
     (1, 1, 1, 1), (1, 36000, 512, 4), (7, 36000, 512, 4), (7, 1000, 1024, 8), (32, 33, 64, 8), (33, 31, 100, 5), (65, 5000, 512, 0),
     (100, 2049, 777, 3), (300, 4000, 512, 4), (384, 4000, 513, 4), (600, 3001, 512, 8), (600, 3001, 1000, 1), (2100, 1500, 512, 4),
-    (2100, 1500, 1024, 0), (31, 255, 32, 2), (129, 8, 48, 8), (520, 36000, 960, 4)])
+    (2100, 1500, 1024, 0), (31, 255, 32, 2), (129, 8, 48, 8), (520, 36000, 960, 4), (2100, 1500, 512, 0), (900, 33000, 300, 0),
+    (897, 31, 40, 0), (2500, 4000, 512, 8)])
 def test_token_logprob(M, N, K, k):
     g = gen(M + N + K)
     target = torch.randint(-2, N + 2, (M,), generator=g, dtype=torch.int32)
