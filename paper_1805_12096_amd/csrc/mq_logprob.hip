@@ -10,6 +10,9 @@
 //   * best words: sums are below 2^24, so sum << 7 | 127 - place is a 32-bit key that orders by sum, then by earlier place, for
 //     128 places of a lane (8 units of 32 words); a sorted list takes a key with one maximum and medians of three.  After 8
 //     units the list is decoded and merged into one of 64-bit keys (sum, word).
+// Bound by the matrix instructions where there are many rows (8192 x 36000 x 1024: 290 us, 2.08 POP/s with the join), and by the twelve
+// vector instructions that a word with a list costs else (384 x 36000 x 512 with 4 best words: 21 + 5 us, a third of it matrix
+// instructions); a unit of 32 words has both side by side.
 // Every (row, workgroup column) leaves its statistics and list in the workspace; a second kernel joins them, a wave per row,
 // and forms the given word's sum itself (one dot product of K bytes).
 #include <type_traits>
