@@ -57,20 +57,24 @@ def _lib():
     return lib
 
 
-def _current() -> int:
-    """The current device's number (without building an object for it: a decode-sized call's host time shows)."""
-    return binding._device() if binding._device is not None else torch.cuda.current_device()
-
-
-def _p(t, current=None):
+def _p(t, current=-2):
     """Device address of a tensor on the current device (None -> NULL); raw ints pass through."""
     if t is None or isinstance(t, int):
         return t
-    if not t.is_cuda:
-        raise ValueError(f"a tensor on {t.device} was passed: the library takes device memory")
-    if t.get_device() != (_current() if current is None else current):
-        raise ValueError(f"a tensor on {t.device} was passed while the current device is another")
+    if t.get_device() != current:                    # (-1 for host memory)
+        raise ValueError(f"a tensor on {t.device} was passed: the library takes memory of the current device")
     return t.data_ptr()
+
+
+def _here(stream):
+    """The current device (-2, where no tensor is, while nothing has touched a device yet) and the stream's handle, asked for
+    once a call: a decode-sized call's host time shows."""
+    if not torch.cuda.is_initialized():
+        return -2, 0 if stream is None else _stream(stream)
+    if binding._device is None or binding._raw_stream is None:
+        return torch.cuda.current_device(), _stream(stream)
+    current = binding._device()
+    return current, binding._raw_stream(current) if stream is None else _stream(stream)
 
 
 def dtype_code(dtype: torch.dtype) -> int:
@@ -111,11 +115,6 @@ def _cache(cache, current):
     return ctypes.byref(cache.c)
 
 
-def _here():
-    """The current device, or none that a tensor could be on while nothing has touched a device yet."""
-    return _current() if torch.cuda.is_initialized() else -2
-
-
 def mq_kv_key_bytes(blocks, kv_heads, head_dim) -> int:
     return int(_lib().mq_kv_key_bytes(blocks, kv_heads, head_dim))
 
@@ -127,10 +126,10 @@ def mq_kv_value_bytes(blocks, kv_heads, head_dim) -> int:
 def mq_kv_append(cache, table, table_width, first, held, B, T, k, ldk, v, ldv, q, ldq, heads, dtype, freq, rot, interleaved,
                  k_out=None, q_out=None, stream=None):
     """cache: a KvCache; everything else as in include/mq_seq.h."""
-    c = _here()
+    c, at = _here(stream)
     _check(_lib().mq_kv_append(_cache(cache, c), _p(table, c), table_width, _p(first, c), _p(held, c), B, T, _p(k, c), ldk,
                                _p(v, c), ldv, _p(q, c), ldq, heads, dtype, _p(freq, c), rot, int(interleaved), _p(k_out, c),
-                               _p(q_out, c), _stream(stream)), "mq_kv_append")
+                               _p(q_out, c), at), "mq_kv_append")
 
 
 def mq_cached_attention_ws_bytes(B, max_len, heads, kv_heads, head_dim) -> int:
@@ -140,9 +139,9 @@ def mq_cached_attention_ws_bytes(B, max_len, heads, kv_heads, head_dim) -> int:
 def mq_cached_attention(cache, table, table_width, lens, B, max_len, q, ldq, heads, dtype, scale, out, ldo, ws, ws_bytes,
                         stream=None):
     """cache: a KvCache; everything else as in include/mq_seq.h."""
-    c = _here()
+    c, at = _here(stream)
     _check(_lib().mq_cached_attention(_cache(cache, c), _p(table, c), table_width, _p(lens, c), B, max_len, _p(q, c), ldq, heads,
-                                      dtype, scale, _p(out, c), ldo, _p(ws, c), ws_bytes, _stream(stream)),
+                                      dtype, scale, _p(out, c), ldo, _p(ws, c), ws_bytes, at),
            "mq_cached_attention")
 
 
@@ -152,10 +151,10 @@ def mq_prompt_attention_ws_bytes(dtype, B, Tk, kv_heads, head_dim) -> int:
 
 def mq_prompt_attention(q, ldq, k, ldk, v, ldv, dtype, q_first, k_first, B, Tq, Tk, heads, kv_heads, head_dim, causal, scale,
                         out, ldo, ws, ws_bytes, stream=None):
-    c = _here()
+    c, at = _here(stream)
     _check(_lib().mq_prompt_attention(_p(q, c), ldq, _p(k, c), ldk, _p(v, c), ldv, dtype, _p(q_first, c), _p(k_first, c), B, Tq,
                                       Tk, heads, kv_heads, head_dim, int(causal), scale, _p(out, c), ldo, _p(ws, c), ws_bytes,
-                                      _stream(stream)), "mq_prompt_attention")
+                                      at), "mq_prompt_attention")
 
 
 def mq_token_logprob_ws_bytes(M, N, k) -> int:
@@ -164,7 +163,7 @@ def mq_token_logprob_ws_bytes(M, N, k) -> int:
 
 def mq_gemm_token_logprob_packed(packedA, packedW, M, N, K, sA, sW, target, k, logprob, entropy, tok, alt_logprob, ws, ws_bytes,
                                  stream=None):
-    c = _here()
+    c, at = _here(stream)
     _check(_lib().mq_gemm_token_logprob_packed(_p(packedA, c), _p(packedW, c), M, N, K, _p(sA, c), _p(sW, c), _p(target, c),
                                                int(k), _p(logprob, c), _p(entropy, c), _p(tok, c), _p(alt_logprob, c), _p(ws, c),
-                                               ws_bytes, _stream(stream)), "mq_gemm_token_logprob_packed")
+                                               ws_bytes, at), "mq_gemm_token_logprob_packed")
