@@ -384,6 +384,12 @@ __global__ __launch_bounds__(256) void k_logprob_join(const LogprobParams p) {
 #pragma unroll
       for (int j = 0; j < NB; ++j) list[i][j] = p.list[at * NB + j];
   }
+  // the given word's: 16 elements of K per lane, element k of row n in piece k / 32, half (k / 16) % 2 (2 kfrags <= 64)
+  const bool given = word >= 0 && (unsigned)word < p.N;
+  const unsigned i0 = min(lane, p.kfrags * 2 - 1), n0 = given ? (unsigned)word : 0u;
+  const size_t in = (size_t)(i0 / 2) * kFragBytes + (i0 % 2) * 512;
+  const v4i pa = *reinterpret_cast<const v4i*>(p.packedA + (size_t)(m / 32) * p.kfrags * kFragBytes + in + m % 32 * 16);
+  const v4i pw = *reinterpret_cast<const v4i*>(p.packedW + (size_t)(n0 / 32) * p.kfrags * kFragBytes + in + n0 % 32 * 16);
 #pragma unroll
   for (int i = 0; i < kMostColumns / kWave; ++i) {
     if (lane + i * kWave >= p.columns) break;
@@ -408,17 +414,10 @@ __global__ __launch_bounds__(256) void k_logprob_join(const LogprobParams p) {
       merge_lists<NB>(top, other);
     }
   }
-  // the given word's sum: 16 elements of K per lane, element k of row n in piece k / 32, half (k / 16) % 2
-  const bool given = word >= 0 && (unsigned)word < p.N;
   int sum = 0;
-  if (given)
-    for (unsigned i = lane; i < p.kfrags * 2; i += kWave) {
-      const size_t in = (size_t)(i / 2) * kFragBytes + (i % 2) * 512;
-      const v4i a = *reinterpret_cast<const v4i*>(p.packedA + (size_t)(m / 32) * p.kfrags * kFragBytes + in + m % 32 * 16);
-      const v4i w = *reinterpret_cast<const v4i*>(p.packedW + (size_t)(word / 32) * p.kfrags * kFragBytes + in + word % 32 * 16);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) sum = __builtin_amdgcn_sdot4(a[j], w[j], sum, false);
-    }
+  for (int j = 0; j < 4; ++j) sum = __builtin_amdgcn_sdot4(pa[j], pw[j], sum, false);
+  if (lane >= p.kfrags * 2) sum = 0;
 #pragma unroll
   for (int off = 32; off >= 1; off >>= 1) sum += __shfl_xor(sum, off, 64);
   const float norm = log2f(l), ln2 = 0.69314718055994530942f;
