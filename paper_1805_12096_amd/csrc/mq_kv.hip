@@ -23,6 +23,8 @@ namespace {
 
 constexpr int kT = 256;
 constexpr int kTokensPerWg = kT / kWave;      // of the query rotation
+// pieces of 16 elements of a token's queries, a wave at a time (about 250 tokens of 128 heads of 256: 27 us, a wave per token 124)
+constexpr int kQPieces = 256;
 
 struct AppendParams {
   const void *k, *v, *q;
@@ -34,6 +36,7 @@ struct AppendParams {
   void *k_out, *q_out;
   unsigned B, T, kv_heads, heads, d, rot, page_wgs;
   unsigned slot_tokens, slot_more;      // sequence b's slots start at first[b] / slot_tokens + slot_more b
+  unsigned q_parts;                     // waves of a token of queries
   int interleaved;
 };
 
@@ -300,8 +303,8 @@ __global__ __launch_bounds__(TH) void k_kv_append_rows(const AppendParams p) {
   const unsigned tid = threadIdx.x, d = p.d, half = p.rot / 2, d16 = d / 16;
 
   if (blockIdx.x >= p.page_wgs) {
-    // queries: a token per wave
-    const unsigned lane = tid % kWave, t = (blockIdx.x - p.page_wgs) * (TH / kWave) + tid / kWave;
+    // queries: a wave per token and F kWave pieces of 16 elements
+    const unsigned lane = tid % kWave, wg = blockIdx.x - p.page_wgs, t = wg / p.q_parts * (TH / kWave) + tid / kWave;
     __shared__ SinCos turn[TH / kWave][128];
     int b = -1;
     unsigned f0 = t;
@@ -321,28 +324,26 @@ __global__ __launch_bounds__(TH) void k_kv_append_rows(const AppendParams p) {
     if (b < 0) return;
     const T* src = static_cast<const T*>(p.q) + (size_t)t * p.ldq;
     T* dst = static_cast<T*>(p.q_out) + (size_t)t * p.heads * d;
-    constexpr int F = 4;                              // in flight
-    const unsigned items = p.heads * d16;
-    for (unsigned i0 = lane; i0 < items; i0 += F * kWave) {
-      float x[F][16];
-      unsigned one[F], two[F], u[F];
+    constexpr int F = kQPieces / kWave;               // in flight
+    const unsigned items = p.heads * d16, i0 = wg % p.q_parts * kQPieces + lane;
+    float x[F][16];
+    unsigned one[F], two[F], u[F];
 #pragma unroll
-      for (int f = 0; f < F; ++f) {
-        const unsigned i = min(i0 + f * kWave, items - 1);
-        u[f] = i % d16;
-        groups_of(u[f], p.rot, p.interleaved, one[f], two[f]);
-        one[f] += i / d16 * d;
-        two[f] += i / d16 * d;
-        load8<DT>(src + one[f], x[f]);
-        load8<DT>(src + two[f], x[f] + 8);
-      }
+    for (int f = 0; f < F; ++f) {
+      const unsigned i = min(i0 + f * kWave, items - 1);
+      u[f] = i % d16;
+      groups_of(u[f], p.rot, p.interleaved, one[f], two[f]);
+      one[f] += i / d16 * d;
+      two[f] += i / d16 * d;
+      load8<DT>(src + one[f], x[f]);
+      load8<DT>(src + two[f], x[f] + 8);
+    }
 #pragma unroll
-      for (int f = 0; f < F; ++f) {
-        if (i0 + f * kWave >= items) break;
-        rotate16(x[f], u[f], p.rot, p.interleaved, [&](unsigned j) { return turn[tid / kWave][j]; });
-        store8<DT>(dst + one[f], x[f]);
-        store8<DT>(dst + two[f], x[f] + 8);
-      }
+    for (int f = 0; f < F; ++f) {
+      if (i0 + f * kWave >= items) break;
+      rotate16(x[f], u[f], p.rot, p.interleaved, [&](unsigned j) { return turn[tid / kWave][j]; });
+      store8<DT>(dst + one[f], x[f]);
+      store8<DT>(dst + two[f], x[f] + 8);
     }
     return;
   }
@@ -351,7 +352,7 @@ __global__ __launch_bounds__(TH) void k_kv_append_rows(const AppendParams p) {
   int b = (int)slot;
   unsigned f0 = slot, n = 1, local = 0;
   long long held = p.held[min(slot, p.B - 1)];        // (right where every sequence in front has one token: no search then)
-  if (p.first != nullptr && !(kTable && slot < p.B && first_at(p.first, slot, p.T) == slot && first_at(p.first, slot + 1, p.T) == slot + 1)) {
+  if (p.first != nullptr && !(kTable && p.slot_more == 0 && slot < p.B && first_at(p.first, slot, p.T) == slot && first_at(p.first, slot + 1, p.T) == slot + 1)) {
     auto base = [&](unsigned i) { return first_at(p.first, i, p.T) / p.slot_tokens + p.slot_more * i; };
     b = wave_search(p.B, slot, base);
     if (b < 0) return;
@@ -576,18 +577,23 @@ int launch_kv_append(const mq_kv_cache& cache, const int32_t* table, size_t tabl
   auto whole = [&](const void* x, size_t ld) { return reinterpret_cast<uintptr_t>(x) % 16 == 0 && ld % piece == 0; };
   const bool rows = d % 16 == 0 && rot % 16 == 0 && whole(k, ldk) && whole(v, ldv) && whole(k_out, 0) &&
                     (q == nullptr || (whole(q, ldq) && whole(q_out, 0)));
-  const size_t q_tokens = rows && few ? 1 : kTokensPerWg, q_wgs = q == nullptr ? 0 : (T + q_tokens - 1) / q_tokens;
+  // One wave to a block where a sequence's tokens are one chunk of its: 200 sequences, 8 heads of 64, binary32, 3 tokens each 16 us with
+  // four waves and 9 with one, 8 tokens 16 and 10 (13 behind others); 100 sequences, 8 heads of 128 and 32 of queries, bfloat16, 3
+  // tokens 20 and 10, 8 tokens 23 and 15 (22 behind others).
+  const bool narrow = T <= 8 * B;
+  const size_t q_tokens = rows && narrow ? 1 : kTokensPerWg, q_parts = rows && q != nullptr ? ((size_t)heads * (d / 16) + kQPieces - 1) / kQPieces : 1;
+  const size_t q_wgs = q == nullptr ? 0 : (T + q_tokens - 1) / q_tokens * q_parts;
   if (page_wgs + q_wgs >= (size_t)1 << 31) return MQ_ERR_SHAPE;
   const AppendParams p{k, v, q, table, first, held, freq, ldk, ldv, ldq, table_width, cache.blocks, cache.keys, cache.values,
                        cache.amax, k_out, q_out, (unsigned)B, (unsigned)T, (unsigned)cache.kv_heads, (unsigned)heads,
-                       (unsigned)d, (unsigned)rot, (unsigned)page_wgs, few ? 1u : (unsigned)kKvBlock, few ? 0u : 2u, interleaved};
+                       (unsigned)d, (unsigned)rot, (unsigned)page_wgs, few ? 1u : (unsigned)kKvBlock, few ? 0u : 2u, (unsigned)q_parts, interleaved};
   const unsigned wgs = (unsigned)(page_wgs + q_wgs);
   return with_dtype(dtype, [&](auto dt) {
     constexpr int DT = decltype(dt)::value;
     if (rows) {
-      const size_t table = few ? 512 * sizeof(SinCos) : 16 * (rot / 2) * sizeof(SinCos);
+      const size_t table = narrow ? 512 * sizeof(SinCos) : 16 * (rot / 2) * sizeof(SinCos);
       auto go = [&](auto kern, int threads) { hipLaunchKernelGGL(kern, dim3(wgs), dim3(threads), table, s, p); };
-      if (few) go(k_kv_append_rows<DT, 64, 1, 2>, 64);
+      if (narrow) go(k_kv_append_rows<DT, 64, 1, 2>, 64);
       else if (d <= 64) go(k_kv_append_rows<DT, 256, 1, 2>, 256);
       else if (d <= 128) go(k_kv_append_rows<DT, 256, 2, 4>, 256);
       else go(k_kv_append_rows<DT, 256, 4, 8>, 256);

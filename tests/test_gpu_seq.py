@@ -128,6 +128,9 @@ CASES = [  # heads, kv heads, dim, rot, interleaved, new tokens, held
     (4, 2, 256, 256, False, [1, 1, 7, 1, 20], [63, 64, 60, 127, 50]),
     (2, 2, 48, 16, False, [64, 128, 1], [0, 32, 5]),
     (4, 2, 160, 32, True, [100, 33], [0, 64]),
+    (66, 2, 128, 128, True, [1] * 20 + [5, 1], list(range(50, 72))),            # several waves to a token's queries
+    (40, 8, 128, 128, False, [90, 3], [5, 60]),
+    (4, 4, 64, 64, False, [8, 1, 8, 3, 8, 8, 0, 4], [0, 60, 61, 64, 3, 59, 9, 0]),       # several to a block, but few
 ]
 
 
@@ -321,7 +324,7 @@ def cached(c, table, lens, max_len, q, heads, scale, ldo=None, stream=None, ws=N
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("heads,hk,dim", [(8, 8, 64), (8, 2, 128), (16, 1, 80), (40, 2, 33), (4, 4, 256), (3, 1, 192), (5, 5, 1), (64, 1, 16)])
-@pytest.mark.parametrize("lens", [[0, 1, 2, 63, 64, 65, 129, 700], [1500], [33] * 40])
+@pytest.mark.parametrize("lens", [[0, 1, 2, 63, 64, 65, 129, 700], [1500], [33] * 40, [9000, 0, 64, 4097]])
 def test_cached_attention(heads, hk, dim, dtype, lens):
     g = gen(heads * dim + len(lens))
     B = len(lens)
