@@ -106,8 +106,8 @@ int mq_cached_attention(const mq_kv_cache* cache, const int32_t* table, size_t t
  * Binary32 operands are multiplied as binary32, or as three bfloat16 parts that hold all of their 24 bits; probabilities of
  * 16-bit types are rounded to the type.  Sums and softmax statistics are binary32.
  * ws: device, 256-byte aligned, mq_prompt_attention_ws_bytes (0 for invalid arguments): keys and values in the order the
- * products read them.  Two launches; one where head_dim <= 128 and the sequences have up to 192 queries and keys on
- * average (16-bit types: 128).
+ * products read them.  Two launches; one where the sequences have up to 192 queries and keys on average, 16-bit
+ * types 128 (128 and 48 where head_dim > 128).
  * out must not overlap k or v; it may be q itself, with ldo = ldq. */
 size_t mq_prompt_attention_ws_bytes(int dtype, size_t B, size_t Tk, int kv_heads, size_t head_dim);
 int mq_prompt_attention(const void* q, size_t ldq, const void* k, size_t ldk, const void* v, size_t ldv, int dtype,

@@ -756,7 +756,7 @@ __device__ __forceinline__ v4f mfma_keys(const float (&a)[4], const float (&b)[4
 }
 
 template <int DT, int ND, bool VEC>
-__global__ __launch_bounds__(256, ND <= 2 ? 3 : 2) void k_prompt_short(const PromptParams p) {
+__global__ __launch_bounds__(256, ND <= 2 ? 3 : ND <= 4 ? 2 : 1) void k_prompt_short(const PromptParams p) {
   using T = typename Elem<DT>::T;
   const unsigned lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const unsigned col = lane % 16, g = lane / 16, d = p.d;
@@ -882,7 +882,10 @@ __global__ __launch_bounds__(256, ND <= 2 ? 3 : 2) void k_prompt_short(const Pro
 //     16 x 400 25 / 34 | 54 / 98
 //   bfloat16, pack + attention / pack + wide: 8 x 1100 52 / 60 | 100 / 116, 16 x 1500 110 / 104 | 277 / 286,
 //     4 x 2000 72 / 64 | 142 / 131, 3 x 3000 90 / 89 | 199 / 184, 2 x 8000 296 / 289 | 701 / 566
-constexpr size_t kShortMean32 = 192, kShortMean16 = 128, kLongMean = 1536;
+// d = 256 with 4 heads | d = 192 with 16 heads over 4, pack + attention / short:
+//   binary32: 256 x 2 84 / 11 | 182 / 26, 64 x 64 59 / 34 | 83 / 67, 32 x 128 59 / 55 | 119 / 99, 32 x 192 97 / 111 | 147 / 188
+//   bfloat16: 256 x 2 61 / 11 | 156 / 30, 100 x 32 37 / 23 | 78 / 53, 64 x 64 36 / 28 | 50 / 66, 64 x 96 46 / 51 | 71 / 105
+constexpr size_t kShortMean32 = 192, kShortMean16 = 128, kShortMeanWide32 = 128, kShortMeanWide16 = 48, kLongMean = 1536;
 
 static size_t k_slots(size_t B, size_t Tk) { return Tk / kUnit + B; }
 
@@ -896,8 +899,8 @@ int launch_prompt_attention(const void* q, size_t ldq, const void* k, size_t ldk
                             int kv_heads, size_t d, int causal, float scale, void* out, size_t ldo, void* ws, hipStream_t s) {
   const size_t n = k_slots(B, Tk) * (size_t)kv_heads, q_slots = Tq / (kW * kQ) + B;
   if (n >= (size_t)1 << 31 || (Tq / kQShort + B) * (size_t)heads >= (size_t)1 << 31) return MQ_ERR_SHAPE;
-  const size_t few = (dtype == MQ_F32 ? kShortMean32 : kShortMean16) * B;
-  const bool is_short = d <= 128 && ldq < (size_t)1 << 24 && ldk < (size_t)1 << 24 && ldv < (size_t)1 << 24 && Tq <= few && Tk <= few;
+  const size_t few = (dtype == MQ_F32 ? d <= 128 ? kShortMean32 : kShortMeanWide32 : d <= 128 ? kShortMean16 : kShortMeanWide16) * B;
+  const bool is_short = ldq < (size_t)1 << 24 && ldk < (size_t)1 << 24 && ldv < (size_t)1 << 24 && Tq <= few && Tk <= few;
   const bool is_long = d <= 128 && scale != 0.f && Tq >= kLongMean * B;
   const size_t per16 = 16 / elem_bytes(dtype);
   auto whole = [&](const void* x, size_t ld) { return reinterpret_cast<uintptr_t>(x) % 16 == 0 && ld % per16 == 0; };
@@ -922,7 +925,10 @@ int launch_prompt_attention(const void* q, size_t ldq, const void* k, size_t ldk
         case 1: return go(std::integral_constant<int, 1>{});
         case 2: return go(std::integral_constant<int, 2>{});
         case 3: return go(std::integral_constant<int, 3>{});
-        default: return go(std::integral_constant<int, 4>{});
+        case 4: return go(std::integral_constant<int, 4>{});
+        case 5:
+        case 6: return go(std::integral_constant<int, 6>{});
+        default: return go(std::integral_constant<int, 8>{});
       }
     }
     hipLaunchKernelGGL((k_prompt_pack<DT>), dim3((unsigned)n), dim3(256), 0, s, p);

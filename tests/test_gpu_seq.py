@@ -514,10 +514,10 @@ def test_prompt_attention(which, heads, hk, dim, dtype, causal):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("n,others", [(150, 0), (150, 7), (300, 0), (1600, 0)])      # (empty sequences: the one-launch form takes the call)
-def test_prompt_attention_masked_places_never_count(dtype, n, others):
+@pytest.mark.parametrize("n,others,dim", [(150, 0, 64), (150, 7, 64), (300, 0, 64), (1600, 0, 64), (150, 7, 256), (150, 0, 192)])      # (empty sequences: the one-launch form takes the call)
+def test_prompt_attention_masked_places_never_count(dtype, n, others, dim):
     g = gen(21)
-    heads, hk, dim = 2, 1, 64
+    heads, hk = 2, 1
     ends = [0] + [n] * (1 + others)
     q, k, v = (normal(g, n, h * dim).to(dtype) for h in (heads, hk, hk))
     want, tol = prompt_reference(q, k, v, ends, ends, heads, hk, dim, True, 0.125)
