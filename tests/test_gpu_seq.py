@@ -830,6 +830,42 @@ def test_captured_steps_replay_beside_eager_ones():
                 assert torch.equal(x, y)
 
 
+def test_two_streams_at_once():
+    # buffers and workspaces of their own: neither call sees the other
+    steps = [Step(), Step()]
+    for s in steps:
+        s.run()
+    torch.cuda.synchronize()
+    want = steps[0].results()
+    for s in steps:
+        for x in (s.o, s.lp, s.ent, s.alt, s.o1, s.kr, s.qr, s.kr1, s.qr1):
+            x.fill_(math.nan)
+        for x in (s.wp, s.wc, s.ws):
+            x.fill_(255)
+        s.cache.keys.zero_(), s.cache.values.zero_(), s.cache.amax.zero_()
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(4):
+        for s, at in zip(steps, streams):
+            D, hk, d, h, T, B, width = 256, s.hk, s.dim, s.heads, s.x.shape[0], 4, s.qkv.shape[1]
+            for x, first, held, kr, qr in ((s.qkv, s.first, s.zero, s.kr, s.qr), (s.qkv1, None, s.held, s.kr1, s.qr1)):
+                q, k, v = x[:, :D], x[:, D:D + hk * d], x[:, D + hk * d:]
+                mq.mq_kv_append(s.cache, s.table, 3, first, held, B, len(x), k, width, v, width, q, width, h, 0, s.freq, d, False,
+                                kr, qr, stream=at)
+                if first is None:
+                    mq.mq_cached_attention(s.cache, s.table, 3, s.after, B, 192, qr, D, h, 0, d ** -0.5, s.o1, D, s.wc, s.wc.numel(),
+                                           stream=at)
+                else:
+                    mq.mq_prompt_attention(qr, D, kr, hk * d, v, width, 0, first, first, B, T, T, h, hk, d, True, d ** -0.5, s.o, D,
+                                           s.wp, s.wp.numel(), stream=at)
+                    mq.mq_gemm_token_logprob_packed(s.pa, s.pe.packed, T, s.N, D, s.sa, s.pe.scale, s.target, 3, s.lp, s.ent, s.tok,
+                                                    s.alt, s.ws, s.ws.numel(), stream=at)
+    torch.cuda.synchronize()
+    for s in steps:
+        for x, y in zip(s.results(), want):
+            assert torch.equal(x, y)
+
+
 def test_another_stream():
     s, want = Step(), Step()
     want.run()
