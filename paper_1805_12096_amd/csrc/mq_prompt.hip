@@ -401,11 +401,12 @@ constexpr float kSlack = 8.f;
 
 // One result of a matrix instruction, out of its accumulation register at this place.  (The compiler would copy all sixteen as
 // soon as they are there, and wait for that.)  The compiler does not see what is read here, so whoever reads the first result
-// lets the eleven wait states of an 8-pass instruction go by: FIRST.
+// lets the twelve wait states go by that an 8-pass instruction needs on gfx950: FIRST.  (It may belong to the product issued
+// last: the compiler puts two tiles' last products in either order.  The other tile's first read is sixteen behind it.)
 template <bool FIRST>
 __device__ __forceinline__ float accumulated(float x) {
   float y;
-  if constexpr (FIRST) asm volatile("s_nop 10\n\tv_accvgpr_read_b32 %0, %1" : "=v"(y) : "a"(x));
+  if constexpr (FIRST) asm volatile("s_nop 11\n\tv_accvgpr_read_b32 %0, %1" : "=v"(y) : "a"(x));
   else asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(y) : "a"(x));
   return y;
 }
