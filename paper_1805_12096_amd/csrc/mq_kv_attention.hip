@@ -262,7 +262,8 @@ __global__ __launch_bounds__(most_waves(DC) * kWave) void k_cached_attention(con
                 in = __builtin_amdgcn_exp2f(mt - finite_or_0(now));
     total = fmaf(total, keep, lt * in);
     top = now;
-    const float fv = in * (am.y * (1.f / (127.f * kDigits<NP>)));
+    // (where there is no block, block 0 was read, whose maximum may be anything: 0 times that must not get in)
+    const float fv = there ? in * (am.y * (1.f / (127.f * kDigits<NP>))) : 0.f;
 #pragma unroll
     for (int t = 0; t < ND; ++t)
       if (t < (int)nd) {
