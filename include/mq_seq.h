@@ -85,7 +85,7 @@ int mq_kv_append(const mq_kv_cache* cache, const int32_t* table, size_t table_wi
 
 /* Attention of one query per sequence over the first lens[b] tokens of its cache:
  *   out[b] = sum_t p_t V[t],  p = softmax over t < lens[b] of scale (q[b] . K[t]),  per head;
- * zeros where nothing is there to attend to.
+ * zeros where nothing is there to attend to, else NaN where the query holds a NaN or an infinity.
  *   lens: device int32 [B]; values above max_len count as max_len, negative ones as 0.  max_len <= 64 table_width.
  *   q: token rows [B] of `heads` heads, out likewise (it may be q itself, with ldo = ldq).
  * Queries and probabilities enter the integer products with a scale of their own for each row, binary32 ones as 24-bit
@@ -102,7 +102,8 @@ int mq_cached_attention(const mq_kv_cache* cache, const int32_t* table, size_t t
  * j <= i + m - n (the last query sees all; queries that see none give zeros).
  *   out[i] = sum_j p_j v[j],  p = softmax over the keys seen of scale (q[i] . k[j]),  per head.
  * What lies at places a query does not see never counts, whatever it holds.  A key position with a NaN or an infinity in its
- * key or its value turns the whole output (of that head) of every query that sees it into NaN.
+ * key or its value turns the whole output (of that head) of every query that sees it into NaN; a query with a NaN or an
+ * infinity that sees any key gives NaN.
  * Binary32 operands are multiplied as binary32, or as three bfloat16 parts that hold all of their 24 bits; probabilities of
  * 16-bit types are rounded to the type.  Sums and softmax statistics are binary32.
  * ws: device, 256-byte aligned, mq_prompt_attention_ws_bytes (0 for invalid arguments): keys and values in the order the

@@ -182,6 +182,13 @@ __device__ __forceinline__ void which(const PromptParams& p, unsigned& slot, uns
   head = xcd_remap(blockIdx.x % p.heads, p.heads);
 }
 
+// What a query's sums are multiplied by.  Where keys are seen but nothing was summed, all scores were minus infinity (an infinite
+// element of the query): there is no softmax, and the row is NaN, as with any other infinite score.
+__device__ __forceinline__ float inverse_of(float total, bool poison, unsigned seen) {
+  if (total == 0.f) return poison || seen > 0 ? NAN : 0.f;
+  return poison ? NAN : __fdiv_rn(1.f, total);
+}
+
 // Four neighbouring columns of an output row, times inv.  vec: rows are whole 16-byte pieces.
 template <int DT>
 __device__ __forceinline__ void store4(typename Elem<DT>::T* row, float a, float b, float c, float e, float inv, unsigned at,
@@ -375,7 +382,7 @@ __global__ __launch_bounds__(KS * kW * kWave) void k_prompt_attention(const Prom
   }
   total = across32_f(total, [](float a, float b) { return a + b; });
   if (!mine) return;
-  const float inv = poison ? NAN : total == 0.f ? 0.f : __fdiv_rn(1.f, total);
+  const float inv = inverse_of(total, poison, seen);
   T* dst = static_cast<T*>(p.out) + (size_t)(q0 + i) * p.ldo + (size_t)head * d;
 #pragma unroll
   for (int t = 0; t < ND; ++t)
@@ -666,7 +673,7 @@ __global__ __launch_bounds__(kW * kWave, 1) void k_prompt_wide(const PromptParam
     const unsigned i = iw + c * kQ + col;
     const float sum = across32_f(total[c], [](float a, float b) { return a + b; });
     if (i >= nq) continue;
-    const float inv = poison[c] ? NAN : sum == 0.f ? 0.f : __fdiv_rn(1.f, sum);
+    const float inv = inverse_of(sum, poison[c], seen[c]);
     T* dst = static_cast<T*>(p.out) + (size_t)(q0 + i) * p.ldo + (size_t)head * d;
 #pragma unroll
     for (int t = 0; t < ND; ++t)
@@ -867,7 +874,7 @@ __global__ __launch_bounds__(256, ND <= 2 ? 3 : ND <= 4 ? 2 : 1) void k_prompt_s
   auto sum = [](float a, float b) { return a + b; };
   total = across16_f(across32_f(total, sum), sum);
   if (!mine) return;
-  const float inv = poison ? NAN : total == 0.f ? 0.f : __fdiv_rn(1.f, total);
+  const float inv = inverse_of(total, poison, seen);
   T* dst = static_cast<T*>(p.out) + (size_t)(q0 + i) * p.ldo + (size_t)head * d;
 #pragma unroll
   for (int t = 0; t < 2 * ND; ++t) store4<DT>(dst, o[t][0], o[t][1], o[t][2], o[t][3], inv, 16 * t + 4 * g, d, VEC);

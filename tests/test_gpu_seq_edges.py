@@ -55,6 +55,30 @@ def test_cached_attention_reads_nothing_of_blocks_that_are_not_there(lens, heads
 FORMS = [(150, 7), (300, 0), (1600, 0)]          # queries and keys, empty sequences behind: one launch, packed, long
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,others", FORMS)
+@pytest.mark.parametrize("scale", [0.125, -0.125])
+def test_prompt_attention_of_infinite_queries_is_nan(n, others, scale, dtype):
+    # an infinite element makes every score infinite; scores of which all are minus infinity have no softmax either
+    g = base.gen(51)
+    heads, hk, dim = 2, 1, 64
+    q, k, v = (base.normal(g, n, h * dim).to(dtype) for h in (heads, hk, hk))
+    k[:, 3] = k[:, 3].abs() + 1
+    for row, x in ((0, math.inf), (20, -math.inf), (n - 1, -math.inf), (n - 2, math.inf)):
+        q[row, 3] = x
+    ends = [0] + [n] * (1 + others)
+    for causal in (True, False):
+        got = base.prompt(q.to(DEV), k.to(DEV), v.to(DEV), ends, ends, heads, hk, dim, causal, scale).cpu()
+        for row in (0, 20, n - 1, n - 2):
+            assert torch.isnan(got[row, :dim]).all(), (row, causal)
+            assert torch.isfinite(got[row, dim:]).all()
+        assert torch.isfinite(got[1:20]).all() and torch.isfinite(got[21:n - 2]).all()
+    # queries that see nothing give zeros, whatever they hold
+    kends = [0] + [n - 30] * (1 + others)
+    got = base.prompt(q.to(DEV), k.to(DEV), v.to(DEV), ends, kends, heads, hk, dim, True, scale).cpu()
+    assert (got[:30] == 0).all() and torch.isnan(got[n - 2:, :dim]).all()
+
+
 def grown(g, n, dim, jumps, dtype):
     """Queries, keys and values [n, dim] whose scores move by whole steps of about 8 (natural logarithm) at the units of 32
     keys named by `jumps`, up for some queries, down for others, hardly for the rest."""
