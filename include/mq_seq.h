@@ -25,6 +25,8 @@
  * first[b + 1] - 1.  Empty sequences are allowed; rows in front of first[0] and from first[B] on belong to nobody: nothing of
  * theirs is read or written.  Values outside [0, rows] are taken as the nearest bound, and a sequence whose end lies before
  * its start is empty: a bad list gives wrong results, never a read or write outside the buffers.
+ * Sizes.  Rows, sequences and table columns are 1 .. 2^30 each; a call that would take a launch of 2^32 threads or more (some
+ * 2^23 sequences x 8 heads, some 2^26 rows to score) is refused with MQ_ERR_SHAPE.
  */
 #ifndef MQ_SEQ_H_
 #define MQ_SEQ_H_

@@ -583,7 +583,7 @@ int launch_kv_append(const mq_kv_cache& cache, const int32_t* table, size_t tabl
   const bool narrow = T <= 8 * B;
   const size_t q_tokens = rows && narrow ? 1 : kTokensPerWg, q_parts = rows && q != nullptr ? ((size_t)heads * (d / 16) + kQPieces - 1) / kQPieces : 1;
   const size_t q_wgs = q == nullptr ? 0 : (T + q_tokens - 1) / q_tokens * q_parts;
-  if (page_wgs + q_wgs >= (size_t)1 << 31) return MQ_ERR_SHAPE;
+  if (!launchable(page_wgs + q_wgs, rows && narrow ? kWave : kT)) return MQ_ERR_SHAPE;
   const AppendParams p{k, v, q, table, first, held, freq, ldk, ldv, ldq, table_width, cache.blocks, cache.keys, cache.values,
                        cache.amax, k_out, q_out, (unsigned)B, (unsigned)T, (unsigned)cache.kv_heads, (unsigned)heads,
                        (unsigned)d, (unsigned)rot, (unsigned)page_wgs, few ? 1u : (unsigned)kKvBlock, few ? 0u : 2u, (unsigned)q_parts, interleaved};

@@ -408,7 +408,7 @@ int launch_cached_attention(const mq_kv_cache& cache, const int32_t* table, size
   const unsigned splits = split.splits;
   const size_t per = (size_t)(heads / cache.kv_heads);
   const size_t wgs = B * (size_t)cache.kv_heads * ((per + kRows - 1) / kRows) * splits;
-  if (wgs >= (size_t)1 << 31 || B * (size_t)heads >= (size_t)1 << 31) return MQ_ERR_SHAPE;
+  if (!launchable(wgs, split.waves * kWave) || (splits > 1 && !launchable(B * (size_t)heads, kJoin))) return MQ_ERR_SHAPE;
   const size_t piece = 16 / elem_bytes(dtype);
   const int vec = cache.head_dim % piece == 0 && ldq % piece == 0 && reinterpret_cast<uintptr_t>(q) % 16 == 0;
   const CachedParams p{cache.keys, cache.values, cache.amax, table, lens, q, out, static_cast<float*>(ws), ldq, ldo,

@@ -486,6 +486,7 @@ int launch_token_logprob(const void* packedA, const void* packedW, size_t M, siz
   LogprobParams p{static_cast<const uint8_t*>(packedA), static_cast<const uint8_t*>(packedW), (unsigned)M, (unsigned)N,
                   kf, sh.columns, sh.row_waves, sh.ring, static_cast<float4*>(ws),
                   reinterpret_cast<u64*>(static_cast<float4*>(ws) + M * sh.columns), sA, sW, target, k, logprob, entropy, alt, tok};
+  if (!launchable((size_t)sh.columns * sh.chunks, sh.row_waves * sh.word_waves * kWave) || !launchable((M + 3) / 4, 256)) return MQ_ERR_SHAPE;
   auto go = [&](auto kfc, auto ctc, auto nbc) {
     constexpr int NB = decltype(nbc)::value;
     auto kern = k_logprob_stream<decltype(kfc)::value, decltype(ctc)::value, NB>;

@@ -906,10 +906,14 @@ int launch_prompt_attention(const void* q, size_t ldq, const void* k, size_t ldk
                             const int32_t* q_first, const int32_t* k_first, size_t B, size_t Tq, size_t Tk, int heads,
                             int kv_heads, size_t d, int causal, float scale, void* out, size_t ldo, void* ws, hipStream_t s) {
   const size_t n = k_slots(B, Tk) * (size_t)kv_heads, q_slots = Tq / (kW * kQ) + B;
-  if (n >= (size_t)1 << 31 || (Tq / kQShort + B) * (size_t)heads >= (size_t)1 << 31) return MQ_ERR_SHAPE;
   const size_t few = (dtype == MQ_F32 ? d <= 128 ? kShortMean32 : kShortMeanWide32 : d <= 128 ? kShortMean16 : kShortMeanWide16) * B;
   const bool is_short = ldq < (size_t)1 << 24 && ldk < (size_t)1 << 24 && ldv < (size_t)1 << 24 && Tq <= few && Tk <= few;
   const bool is_long = d <= 128 && scale != 0.f && Tq >= kLongMean * B;
+  // every launch of the call, before the first
+  const size_t h = (size_t)heads;
+  if (is_short ? !launchable(((Tq / kQShort + B) * h + 3) / 4, 256)
+               : !launchable(n, 256) || !launchable(q_slots * h, dtype == MQ_F32 ? 2 * kW * kWave : kW * kWave))
+    return MQ_ERR_SHAPE;
   const size_t per16 = 16 / elem_bytes(dtype);
   auto whole = [&](const void* x, size_t ld) { return reinterpret_cast<uintptr_t>(x) % 16 == 0 && ld % per16 == 0; };
   const bool vec = d % 8 == 0 && whole(q, ldq) && whole(k, ldk) && whole(v, ldv) && whole(out, ldo);

@@ -71,6 +71,9 @@ __device__ __forceinline__ int wave_search(unsigned n, unsigned x, Key key) {
   return (int)(lo + c) - 1;
 }
 
+// Whether a launch of that many workgroups is one: a grid has fewer than 2^32 threads.
+inline bool launchable(size_t workgroups, size_t threads) { return workgroups < ((size_t)1 << 32) / threads; }
+
 int launch_kv_append(const mq_kv_cache& cache, const int32_t* table, size_t table_width, const int32_t* first,
                      const int32_t* held, size_t B, size_t T, const void* k, size_t ldk, const void* v, size_t ldv,
                      const void* q, size_t ldq, int heads, int dtype, const float* freq, size_t rot, int interleaved,
