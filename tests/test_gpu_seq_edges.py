@@ -50,6 +50,37 @@ def test_cached_attention_reads_nothing_of_blocks_that_are_not_there(lens, heads
         assert (got[2] == 0).all()
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+def test_cached_attention_of_more_blocks_than_a_wave_reads_at_once(dtype):
+    # many sequences of which one is long: it stays in one run, and a wave of it has more than 64 blocks
+    g = base.gen(71)
+    B, hk, dim, n = 520, 1, 64, 20_000
+    lens = [3] * B
+    lens[300], lens[301], lens[302] = n, n - 1, 64 * 256 + 1
+    c = base.filled_cache(g, 400, hk, dim)
+    table = torch.randint(0, 400, (B, -(-n // BLOCK)), generator=g, dtype=torch.int32)
+    q = base.normal(g, B, 2 * dim).to(dtype)
+    want, tol = base.cached_reference(c, table, lens, n, q, 2, dim ** -0.5)
+    got = base.cached(c, table.to(DEV), base.i32(lens), n, q.to(DEV), 2, dim ** -0.5).cpu().double()
+    assert ((got - want).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("lens", [[100, 0, 64], [9000, 33]])       # one launch, two
+def test_cached_attention_in_place(lens):
+    g = base.gen(72)
+    heads, hk, dim = 20, 1, 128
+    blocks = 160
+    c = base.filled_cache(g, blocks, hk, dim)
+    table = torch.randint(0, blocks, (len(lens), -(-max(lens) // BLOCK)), generator=g, dtype=torch.int32)
+    q = base.normal(g, len(lens), heads * dim)
+    want, tol = base.cached_reference(c, table, lens, max(lens), q, heads, 0.1)
+    qd, ld = q.to(DEV), heads * dim
+    n = mq.mq_cached_attention_ws_bytes(len(lens), max(lens), heads, hk, dim)
+    ws = torch.full((n,), 255, dtype=torch.uint8, device=DEV)
+    mq.mq_cached_attention(c, table.to(DEV), table.shape[1], base.i32(lens), len(lens), max(lens), qd, ld, heads, 0, 0.1, qd, ld, ws, n)
+    assert ((qd.cpu().double() - want).abs() <= tol).all()
+
+
 # ---- packed sequences ---------------------------------------------------------------------------------------------------
 
 FORMS = [(150, 7), (300, 0), (1600, 0)]          # queries and keys, empty sequences behind: one launch, packed, long
