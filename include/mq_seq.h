@@ -14,8 +14,10 @@
  * contents are irrelevant on entry and undefined on return, so calls that may overlap in time (two streams, two captured
  * graphs) need one each.  Results depend neither on what else runs nor on an order of atomics.
  *
- * Types.  Queries, keys, values and outputs are of one type, an mq_dtype.  Arithmetic is binary32 or better whatever the
- * type; a result is rounded to the type once.
+ * Types.  Queries, keys, values and outputs are of one type, an mq_dtype.  Sums, softmax statistics and angles are binary32 or
+ * better whatever the type, and a result is rounded to the type once; what enters a product with fewer bits (probabilities, and
+ * queries of the cache) stands with each call.  Softmax sums of values are formed before they are divided, so values within a
+ * factor of 256 times the number of keys of the largest binary32 value may overflow.
  * Rows.  A "token row" holds heads x head_dim neighbouring elements, head after head; rows are `ld` elements apart
  * (ld >= heads head_dim), so that queries, keys and values may be columns of one product's result.  Base pointers and ld need
  * the alignment of one element only (rows and heads that start on 16 bytes load faster).
@@ -106,8 +108,9 @@ int mq_cached_attention(const mq_kv_cache* cache, const int32_t* table, size_t t
  * What lies at places a query does not see never counts, whatever it holds.  A key position with a NaN or an infinity in its
  * key or its value turns the whole output (of that head) of every query that sees it into NaN; a query with a NaN or an
  * infinity that sees any key gives NaN.
- * Binary32 operands are multiplied as binary32, or as three bfloat16 parts that hold all of their 24 bits; probabilities of
- * 16-bit types are rounded to the type.  Sums and softmax statistics are binary32.
+ * Binary32 operands are multiplied as binary32, or as three bfloat16 parts that hold all of their 24 bits (of magnitudes below
+ * 2^-100 the last ones may be lost); probabilities of 16-bit types are rounded to the type.  Sums and softmax statistics are
+ * binary32.
  * ws: device, 256-byte aligned, mq_prompt_attention_ws_bytes (0 for invalid arguments): keys and values in the order the
  * products read them.  Two launches; one where the sequences have up to 192 queries and keys on average, 16-bit
  * types 128 (128 and 48 where head_dim > 128).

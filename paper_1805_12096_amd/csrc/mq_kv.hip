@@ -11,7 +11,10 @@
 // Rows of whole 16-byte pieces (k_kv_append_rows): what a workgroup rotates and quantizes stays in registers between the two
 // maxima and the stores.  A thread has 16 elements of a key, the two groups of 8 that are rotated together, and for the values
 // 4 tokens x 2 columns, whose bytes are one word of a row of the cache each.  256 threads take a block at once; where a call
-// brings few tokens to a block, 64 threads take 8 (4 for wide heads) at a time, sines and cosines formed by all of them in LDS.  Other rows: k_kv_append, element by element.
+// brings few tokens to a block, 64 threads take 8 (4 for wide heads) at a time, sines and cosines formed by all of them in LDS.
+// Vector instructions take half of the clocks in which a prompt's compute units are busy, and 184 registers leave two waves a SIMD.
+// Other rows, and rotations that are not a multiple of 16 elements: k_kv_append, element by element (12 prompts of 2000, 32 heads
+// of 80 over 8, bfloat16: 380 us with 40 elements rotated, 150 with 80).
 #include <type_traits>
 
 #include "mq_glue.h"
@@ -352,7 +355,9 @@ __global__ __launch_bounds__(TH) void k_kv_append_rows(const AppendParams p) {
   int b = (int)slot;
   unsigned f0 = slot, n = 1, local = 0;
   long long held = p.held[min(slot, p.B - 1)];        // (right where every sequence in front has one token: no search then)
-  if (p.first != nullptr && !(kTable && p.slot_more == 0 && slot < p.B && first_at(p.first, slot, p.T) == slot && first_at(p.first, slot + 1, p.T) == slot + 1)) {
+  const bool alone = kTable && p.slot_more == 0 && slot < p.B && p.first != nullptr && first_at(p.first, slot, p.T) == slot &&
+                     first_at(p.first, slot + 1, p.T) == slot + 1;
+  if (p.first != nullptr && !alone) {
     auto base = [&](unsigned i) { return first_at(p.first, i, p.T) / p.slot_tokens + p.slot_more * i; };
     b = wave_search(p.B, slot, base);
     if (b < 0) return;
@@ -577,16 +582,19 @@ int launch_kv_append(const mq_kv_cache& cache, const int32_t* table, size_t tabl
   auto whole = [&](const void* x, size_t ld) { return reinterpret_cast<uintptr_t>(x) % 16 == 0 && ld % piece == 0; };
   const bool rows = d % 16 == 0 && rot % 16 == 0 && whole(k, ldk) && whole(v, ldv) && whole(k_out, 0) &&
                     (q == nullptr || (whole(q, ldq) && whole(q_out, 0)));
-  // One wave to a block where a sequence's tokens are one chunk of its: 200 sequences, 8 heads of 64, binary32, 3 tokens each 16 us with
-  // four waves and 9 with one, 8 tokens 16 and 10 (13 behind others); 100 sequences, 8 heads of 128 and 32 of queries, bfloat16, 3
-  // tokens 20 and 10, 8 tokens 23 and 15 (22 behind others).
+  // One wave to a block where a sequence's tokens are one chunk of its: 200 sequences, 8 heads of 64, binary32, 3 tokens each
+  // 16 us with four waves and 9 with one, 8 tokens 16 and 10 (13 behind others); 100 sequences, 8 heads of 128 and 32 of queries,
+  // bfloat16, 3 tokens 20 and 10, 8 tokens 23 and 15 (22 behind others).  With four, 64 sequences of the latter heads take 18 us
+  // for 9 tokens each, 20 for 16, 27 for 32.
   const bool narrow = T <= 8 * B;
-  const size_t q_tokens = rows && narrow ? 1 : kTokensPerWg, q_parts = rows && q != nullptr ? ((size_t)heads * (d / 16) + kQPieces - 1) / kQPieces : 1;
+  const size_t q_tokens = rows && narrow ? 1 : kTokensPerWg;
+  const size_t q_parts = rows && q != nullptr ? ((size_t)heads * (d / 16) + kQPieces - 1) / kQPieces : 1;
   const size_t q_wgs = q == nullptr ? 0 : (T + q_tokens - 1) / q_tokens * q_parts;
   if (!launchable(page_wgs + q_wgs, rows && narrow ? kWave : kT)) return MQ_ERR_SHAPE;
   const AppendParams p{k, v, q, table, first, held, freq, ldk, ldv, ldq, table_width, cache.blocks, cache.keys, cache.values,
                        cache.amax, k_out, q_out, (unsigned)B, (unsigned)T, (unsigned)cache.kv_heads, (unsigned)heads,
-                       (unsigned)d, (unsigned)rot, (unsigned)page_wgs, few ? 1u : (unsigned)kKvBlock, few ? 0u : 2u, (unsigned)q_parts, interleaved};
+                       (unsigned)d, (unsigned)rot, (unsigned)page_wgs, few ? 1u : (unsigned)kKvBlock, few ? 0u : 2u,
+                       (unsigned)q_parts, interleaved};
   const unsigned wgs = (unsigned)(page_wgs + q_wgs);
   return with_dtype(dtype, [&](auto dt) {
     constexpr int DT = decltype(dt)::value;

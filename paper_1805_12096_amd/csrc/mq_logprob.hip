@@ -10,9 +10,13 @@
 //   * best words: sums are below 2^24, so sum << 7 | 127 - place is a 32-bit key that orders by sum, then by earlier place, for
 //     128 places of a lane (8 units of 32 words); a sorted list takes a key with one maximum and medians of three.  After 8
 //     units the list is decoded and merged into one of 64-bit keys (sum, word).
-// Bound by the matrix instructions where there are many rows (8192 x 36000 x 1024: 290 us, 2.08 POP/s with the join), and by the twelve
-// vector instructions that a word with a list costs else (384 x 36000 x 512 with 4 best words: 21 + 5 us, a third of it matrix
-// instructions); a unit of 32 words has both side by side.
+// Bound by the matrix instructions where there are many rows (8192 x 36000 x 1024: 292 .. 300 us with the join, 2.0 POP/s; they
+// take 53 % of the clocks in which the compute units are busy, vector ones 36 %).  With 384 rows (36000 x 512, 4 best words,
+// 24.5 us with the join) a compute unit is busy for 37 000 clocks, about 16 us, of which vector instructions, twelve for a word with a
+// list, take half and matrix instructions 18 %; a wave waits a third of its time, for the start, where every workgroup fetches its
+// rows' hidden states, and for the end, after four or five stages.
+// u2 is rounded once more than 1 / (sA sW) and a lane adds up its words one after the other: 2.2e-7 off the result in 64 bits
+// (8192 rows; 6.8e-8 with a sum over the whole row at once).
 // Every (row, workgroup column) leaves its statistics and list in the workspace; a second kernel joins them, a wave per row,
 // and forms the given word's sum itself (one dot product of K bytes).
 #include <type_traits>
@@ -322,6 +326,10 @@ __global__ __launch_bounds__(most_waves(KF, CT) * kWave, 1) void k_logprob_strea
     }
     counted();
   };
+  // Overlapped only where all of K held is there (449 .. 512 and 961 .. 1024 elements): with a check for each piece the order
+  // cannot be kept.  8192 rows x 36000, overlapped / not, us: K = 512 156 / 260, with 4 best words 216 / 249; K = 1024 292 / 335,
+  // 326 / 399.  384 rows with 4 best words: 24.7 / 26.3, 32.3 / 38.6.  Widths in between take the other loop, and longer than the
+  // next whole one: 448 240, 640 282, 768 303, 960 331 (8192 rows).
   if (kf == KF) {
     if (mine > 0) {
       arrive();
@@ -360,7 +368,8 @@ __global__ __launch_bounds__(most_waves(KF, CT) * kWave, 1) void k_logprob_strea
   }
   flush();
 #pragma unroll
-  for (int x = 0; x < CT; ++x) finish<NB, CT>(p, smem, x, tile + x, tiles, column, wave, wr, wn, word_waves, waves, lane, ref[x], c[x], l[x], t[x], top[x]);
+  for (int x = 0; x < CT; ++x)
+    finish<NB, CT>(p, smem, x, tile + x, tiles, column, wave, wr, wn, word_waves, waves, lane, ref[x], c[x], l[x], t[x], top[x]);
 }
 
 // A wave per row.
@@ -486,7 +495,8 @@ int launch_token_logprob(const void* packedA, const void* packedW, size_t M, siz
   LogprobParams p{static_cast<const uint8_t*>(packedA), static_cast<const uint8_t*>(packedW), (unsigned)M, (unsigned)N,
                   kf, sh.columns, sh.row_waves, sh.ring, static_cast<float4*>(ws),
                   reinterpret_cast<u64*>(static_cast<float4*>(ws) + M * sh.columns), sA, sW, target, k, logprob, entropy, alt, tok};
-  if (!launchable((size_t)sh.columns * sh.chunks, sh.row_waves * sh.word_waves * kWave) || !launchable((M + 3) / 4, 256)) return MQ_ERR_SHAPE;
+  if (!launchable((size_t)sh.columns * sh.chunks, sh.row_waves * sh.word_waves * kWave) || !launchable((M + 3) / 4, 256))
+    return MQ_ERR_SHAPE;
   auto go = [&](auto kfc, auto ctc, auto nbc) {
     constexpr int NB = decltype(nbc)::value;
     auto kern = k_logprob_stream<decltype(kfc)::value, decltype(ctc)::value, NB>;

@@ -8,13 +8,17 @@
 // leaving their lane.  Odd widths and lengths are padded with zeros here, strides and alignment are dealt with here, and what is
 // not finite becomes zero and is noted (a bit for each key), so that it cannot reach queries that do not see it.
 // The second kernel streams the units through LDS, two tiles of keys in turn where they fit, for 32 queries of one head per wave.
-// 16-bit types are multiplied as they are.  Binary32 becomes three bfloat16 parts (8 + 8 + 8 bits: all of it, at any
-// magnitude), and a product the six of part i with part j, i + j <= 2; what is left out is below 2^-24 of the factors' product.
+// 16-bit types are multiplied as they are, and probabilities are rounded to the type, because the matrix instructions take both
+// operands of one type and two parts of each probability would double the second product.  3 sequences of
+// 4500 .. 8190 in bfloat16 are 2.0e-3 off the result in 64 bits, with binary32 probabilities 1.5e-3 (the result's own rounding).
+// Binary32 becomes three bfloat16 parts (8 + 8 + 8 bits: all of it, from 2^-100 up, where the third is above bfloat16's
+// subnormals), and a product the six of part i with part j, i + j <= 2; what is left out is below 2^-24 of the factors' product.
 // (Six bfloat16 products take 0.75 of the time of one on the binary32 matrix instruction, 1236 / 6 against 154 TFLOP/s, and
 // leave it its lanes' layout.)
 // Bound by matrix and vector instructions, which overlap in part only: 10 documents of 333 .. 1900 tokens, 16 heads of 64,
-// binary32, causal, take 180 us behind 34 us of the first kernel, of which 92 us are matrix instructions at the rate that they hold
-// here and 56 us vector ones.
+// binary32, causal, take 188 us, about 40 of them the first kernel (43 us with an attention of no queries behind it); while the
+// second's compute units are busy, 40 % of the clocks have a matrix instruction and 40 % a vector one, and a wave waits a third
+// of its time.
 #include <type_traits>
 
 #include "mq_gemm_common.h"
@@ -175,6 +179,13 @@ __device__ __forceinline__ v16f mfma_parts(const P8 (&a)[NP], const P8 (&b)[NP],
   return c;
 }
 
+// Keys [0, this) are seen by query i of a sequence.
+__device__ __forceinline__ unsigned keys_seen(const PromptParams& p, unsigned i, unsigned nq, unsigned nk) {
+  if (!p.causal) return nk;
+  const long long s = (long long)i + 1 + (long long)nk - (long long)nq;
+  return s < 0 ? 0u : s > (long long)nk ? nk : (unsigned)s;
+}
+
 // Slot of queries and head of a workgroup: the last queries of a sequence, which see most, first, and neighbouring heads, which
 // share keys and values, on one XCD (exactly where the heads are a multiple of eight), whose L2 then holds their units.
 __device__ __forceinline__ void which(const PromptParams& p, unsigned& slot, unsigned& head) {
@@ -229,12 +240,7 @@ __global__ __launch_bounds__(KS * kW * kWave) void k_prompt_attention(const Prom
   const unsigned i0 = (slot - (q0 / BM + (unsigned)b)) * BM;
   if (i0 >= nq) return;
   const unsigned unit0 = __builtin_amdgcn_readfirstlane(k0 / kUnit + (unsigned)b);
-  // keys [0, seen) are seen by query i
-  auto seen_by = [&](unsigned i) -> unsigned {
-    if (!p.causal) return nk;
-    const long long s = (long long)i + 1 + (long long)nk - (long long)nq;
-    return s < 0 ? 0u : s > (long long)nk ? nk : (unsigned)s;
-  };
+  auto seen_by = [&](unsigned i) { return keys_seen(p, i, nq, nk); };
   const unsigned iw = i0 + wave * kQ, i = iw + col;
   const bool mine = i < nq;
   const unsigned seen = mine ? seen_by(i) : 0u;
@@ -398,10 +404,11 @@ __global__ __launch_bounds__(KS * kW * kWave) void k_prompt_attention(const Prom
 // on three units at a time, so that nothing in a step waits for anything else in it:
 //   S = K Q^T of unit n + 2 and O += V P of unit n (matrix)   beside   P = exp2(S - m) of unit n + 1 (vector),
 // K and V pieces on their way from LDS a few instructions ahead.
-// The reference m of a query's softmax moves only when a score exceeds it by more than 2^kSlack (a branch that is hardly ever
-// taken), so that O is hardly ever rescaled.  A ring of units in LDS, one barrier for two units.
-// 3 sequences of 4500 .. 8190 bfloat16 tokens, 32 heads of 128 over 8, causal: 1.33 ms, 880 TFLOP/s (1.86 in the first form: one tile
-// a wave, one step after the other).  969 us are the matrix instructions themselves at the rate that they hold under this load.
+// The reference m of a query's softmax moves only when a score exceeds it by more than kSlack, in powers of two (a branch that
+// is hardly ever taken), so that O is hardly ever rescaled.  A ring of units in LDS, one barrier for two units.
+// 3 sequences of 4500 .. 8190 bfloat16 tokens, 32 heads of 128 over 8, causal: 1.28 .. 1.32 ms with the packing kernel from card
+// to card, 880 .. 910 TFLOP/s (the first form, one tile a wave, one step after the other: 1.86).  Matrix instructions take 43 % of
+// the busy clocks, vector ones 44 %; a wave, alone on its SIMD, waits for a quarter of them.
 #define MQ_INLINE __attribute__((always_inline))
 constexpr int kRing = 8;
 constexpr float kSlack = 8.f;
@@ -465,11 +472,7 @@ __global__ __launch_bounds__(kW * kWave, 1) void k_prompt_wide(const PromptParam
   const unsigned i0 = (slot - (q0 / BM + (unsigned)b)) * BM;
   if (i0 >= nq) return;
   const unsigned unit0 = k0 / kUnit + (unsigned)b, units = (nk + kUnit - 1) / kUnit;
-  auto seen_by = [&](unsigned i) -> unsigned {
-    if (!p.causal) return nk;
-    const long long s = (long long)i + 1 + (long long)nk - (long long)nq;
-    return s < 0 ? 0u : s > (long long)nk ? nk : (unsigned)s;
-  };
+  auto seen_by = [&](unsigned i) { return keys_seen(p, i, nq, nk); };
   const unsigned iw = i0 + wave * 2 * kQ;
   const unsigned last = min(i0 + BM, nq) - 1, wave_last = min(iw + 2 * kQ, nq) - 1;
   const unsigned n_wg = __builtin_amdgcn_readfirstlane((seen_by(last) + kUnit - 1) / kUnit);
@@ -691,7 +694,9 @@ __global__ __launch_bounds__(kW * kWave, 1) void k_prompt_wide(const PromptParam
 // Lane l: query (or key) l % 16, place group g = l / 16.  An operand's 8 elements are, for a 16-bit type, the 8 neighbouring
 // contracted places 8 g .. of 32, for binary32 two times four, 4 g .. of 16.
 // 300 sentences of 2 .. 60 binary32 words, 8 heads of 64: 19 us, 9.6 of them bytes.  What bounds it is the longest sentences' chain
-// of loads and products, and the load units (a key is read by every 16 queries of every head that it serves).
+// of loads and products, and the load units (a key is read by every 16 queries of every head that it serves).  Operands are kept
+// as binary32 also for 16-bit types: heads of more than 128 leave one wave a SIMD, and rows that are not whole 16-byte pieces
+// spill at 97 .. 128 and above 192.
 constexpr int kQShort = 16;
 
 // The column that element j of a lane's n-th 8 stands for.
@@ -777,11 +782,7 @@ __global__ __launch_bounds__(256, ND <= 2 ? 3 : ND <= 4 ? 2 : 1) void k_prompt_s
   const unsigned k0 = first_at(p.k_first, b, p.Tk), k1 = first_at(p.k_first, b + 1, p.Tk), nk = k1 > k0 ? k1 - k0 : 0;
   const unsigned i0 = (slot - (q0 / kQShort + (unsigned)b)) * kQShort, i = i0 + col;
   if (i0 >= nq) return;
-  auto seen_by = [&](unsigned i) -> unsigned {
-    if (!p.causal) return nk;
-    const long long s = (long long)i + 1 + (long long)nk - (long long)nq;
-    return s < 0 ? 0u : s > (long long)nk ? nk : (unsigned)s;
-  };
+  auto seen_by = [&](unsigned i) { return keys_seen(p, i, nq, nk); };
   const bool mine = i < nq;
   const unsigned seen = mine ? seen_by(i) : 0u;
   const unsigned most = __builtin_amdgcn_readfirstlane(seen_by(nq - i0 < (unsigned)kQShort ? nq - 1 : i0 + kQShort - 1));
@@ -882,7 +883,9 @@ __global__ __launch_bounds__(256, ND <= 2 ? 3 : ND <= 4 ? 2 : 1) void k_prompt_s
 
 }  // namespace
 
-// Which kernel: by the mean length, the only one known without reading the lists.  Measured (us, causal, sequences x length,
+// Which kernel: by the mean length, the only one known without reading the lists.  (Where one sequence is far longer than
+// the mean that is the wrong one: one of 8000 among 63 of 1, 32 heads of 128 over 8, bfloat16, takes 6.6 ms in the short form;
+// and 512 queries on 8000 keys, which are not many queries, 263 us in the form between.)  Measured (us, causal, sequences x length,
 // d = 64 with 8 heads | d = 128 with 16 heads over 4):
 //   binary32, pack + attention / short: 64 x 96 41 / 19 | 75 / 62, 32 x 192 37 / 32 | 98 / 99, 32 x 256 52 / 51 | 120 / 155,
 //     8 x 800 72 / 96
