@@ -6,7 +6,9 @@
 // tokens.  Nobody else writes to the block, so there is nothing to wait for and no atomic.  Queries are rotated by workgroups
 // behind those, a wave per token.
 // Bound by bytes for prompts (449 MB in 128 us, 3.5 TB/s; element by element 508) and by the chain of dependent loads (sequence,
-// table, amax) for single tokens (64 sequences, 32 heads of 128 over 8: 7 us; element by element 16).
+// table, amax) for single tokens (64 sequences, 32 heads of 128 over 8: 7 us; element by element 16).  Where the maximum of every
+// block grows and all of it is requantized, single tokens take 13 us instead of 6 (the same) and 15 instead of 7 (300 sequences,
+// 8 heads of 64, binary32).
 //
 // Rows of whole 16-byte pieces (k_kv_append_rows): what a workgroup rotates and quantizes stays in registers between the two
 // maxima and the stores.  A thread has 16 elements of a key, the two groups of 8 that are rotated together, and for the values
