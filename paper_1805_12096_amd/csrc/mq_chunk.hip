@@ -19,6 +19,9 @@ namespace {
 
 constexpr int kRows = 32;             // query rows of a tile
 constexpr int kWaves = 4;             // of a workgroup, at most
+// How far (as a power of two) a row's scores may rise over the reference that its sums are relative to before they are
+// rescaled: exponentials up to 2^8 lose nothing in a binary format, and a maximum that rises a little does not cost anything.
+constexpr float kSlack = 8.f;
 
 struct ChunkParams {
   const int8_t *keys, *values;
@@ -26,13 +29,22 @@ struct ChunkParams {
   const int32_t *table, *first, *lens;
   const void* q;
   void* out;
-  float* part;                        // [T][heads][splits][dv + 2]: sums, maximum, total; splits runs of `run` blocks
+  float* part;                        // [T][heads][splits][dv + 4]: sums, reference, total; splits runs of `run` blocks
   size_t ldq, ldo, table_width, blocks;
   unsigned B, T, max_len, kv_heads, heads, d, splits, run;
   float scale2;                       // scale log2(e)
   int causal;
 };
 
+// Exponent of the power of two taken off a row whose largest magnitude is m.
+__device__ __forceinline__ int row_exponent(float m) {
+  return m > 0.f && m < INFINITY ? max((int)(__float_as_uint(m) >> 23) - 127, -126) : 0;
+}
+// The same number, and nothing that the compiler keeps comparisons with: dozens of kept masks do not fit the scalar registers.
+__device__ __forceinline__ unsigned again(unsigned x) {
+  asm volatile("" : "+s"(x));
+  return x;
+}
 __device__ __forceinline__ float finite_or_0(float m) { return m == -INFINITY ? 0.f : m; }
 __device__ __forceinline__ float fmax2(float a, float b) { return fmaxf(a, b); }
 __device__ __forceinline__ float fadd2(float a, float b) { return a + b; }
@@ -42,16 +54,17 @@ struct Tile {
   int b;                              // sequence, -1: no such tile
   unsigned first, n, row0, rows, len; // its first token row and new tokens, the tile's first row and rows, tokens in the cache
 };
-// Tiles of sequence b lie from tile number first[b] per / 32 + b on: enough for each, whatever the lengths.
+// Tiles of sequence b lie from tile number first[b] per / ROWS + b on: enough for each, whatever the lengths.
+template <unsigned ROWS>
 __device__ __forceinline__ Tile find_tile(const ChunkParams& p, unsigned slot, unsigned per) {
-  auto start = [&](unsigned i) { return first_at(p.first, i, p.T) * per / kRows + i; };
+  auto start = [&](unsigned i) { return first_at(p.first, i, p.T) * per / ROWS + i; };
   const int b = __builtin_amdgcn_readfirstlane(wave_search(p.B, slot, start));
   if (b < 0) return {-1, 0, 0, 0, 0, 0};
   const unsigned f = first_at(p.first, b, p.T), e = first_at(p.first, b + 1, p.T), n = e > f ? e - f : 0;
-  const unsigned row0 = (slot - start(b)) * kRows;
+  const unsigned row0 = (slot - start(b)) * ROWS;
   if (row0 >= n * per) return {-1, 0, 0, 0, 0, 0};
   const int len = p.lens[b];
-  return {b, f, n, row0, min(n * per - row0, (unsigned)kRows), len < 0 ? 0u : min((unsigned)len, p.max_len)};
+  return {b, f, n, row0, min(n * per - row0, ROWS), len < 0 ? 0u : min((unsigned)len, p.max_len)};
 }
 // Tokens that query i of n sees.
 __device__ __forceinline__ unsigned seen_by(const ChunkParams& p, const Tile& t, unsigned i) {
@@ -73,7 +86,7 @@ __global__ __launch_bounds__(kWaves * kWave) void k_chunk_attention(const ChunkP
   const unsigned col = lane % 32, grp = lane / 32;
   const unsigned split = blockIdx.x % p.splits, kvh = blockIdx.x / p.splits % p.kv_heads, slot = blockIdx.x / (p.splits * p.kv_heads);
   const unsigned per = p.heads / p.kv_heads, d = p.d, dk = kv_dk(d), dv = kv_dv(d);
-  const Tile tile = find_tile(p, slot, per);
+  const Tile tile = find_tile<kRows>(p, slot, per);
   if (tile.b < 0) return;
   auto row_at = [&](unsigned r) {              // element offset of row r's queries in q, without the row pitch: token, head
     const unsigned i = tile.row0 + r;
@@ -88,7 +101,7 @@ __global__ __launch_bounds__(kWaves * kWave) void k_chunk_attention(const ChunkP
 
   // queries: a power of two off each row, so that its largest element is 1 .. 2, then parts in operand order
   {
-    const unsigned r = threadIdx.x / 8 % kRows, j0 = threadIdx.x % 8, step = blockDim.x / 8;
+    const unsigned j0 = threadIdx.x % 8, step = blockDim.x / 8;
     for (unsigned rr = threadIdx.x / 8; rr < kRows; rr += step) {
       float m = 0.f;
       if (rr < tile.rows) {
@@ -104,12 +117,11 @@ __global__ __launch_bounds__(kWaves * kWave) void k_chunk_attention(const ChunkP
       for (int off = 4; off >= 1; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, 8));
       if (j0 == 0) fac[rr] = m;
     }
-    (void)r;
     __syncthreads();
     for (unsigned u = threadIdx.x; u < NK * 2 * kWave; u += blockDim.x) {
       const unsigned l = u % kWave, c = u / (2 * kWave), s = u / kWave % 2, rr = l % 32, k = 32 * c + 16 * (l / 32) + 8 * s;
       const float m = fac[rr];
-      const int e = m > 0.f && m < INFINITY ? max((int)(__float_as_uint(m) >> 23) - 127, -126) : 0;
+      const int e = row_exponent(m);
       const float mul = __uint_as_float((unsigned)(127 - e) << 23);          // 2^-e
       bf8 part[NP];
       const uint2 at = row_at(rr < tile.rows ? rr : 0);
@@ -130,9 +142,7 @@ __global__ __launch_bounds__(kWaves * kWave) void k_chunk_attention(const ChunkP
   }
   float qscale;
   {
-    const float m = fac[col];
-    const int e = m > 0.f && m < INFINITY ? max((int)(__float_as_uint(m) >> 23) - 127, -126) : 0;
-    qscale = ldexpf(p.scale2, e);
+    qscale = ldexpf(p.scale2, row_exponent(fac[col]));
   }
 
   float acc_top = -INFINITY, total = 0.f;      // of row l % 32; the total of this lane's tokens
@@ -188,14 +198,17 @@ __global__ __launch_bounds__(kWaves * kWave) void k_chunk_attention(const ChunkP
 #pragma unroll
       for (int r = 0; r < 16; ++r) mt = fmaxf(mt, sc[t][r]);
     mt = across32_f(mt, fmax2);
-    const float now = fmaxf(acc_top, mt), base = finite_or_0(now), keep = __builtin_amdgcn_exp2f(acc_top - base);
-    acc_top = now;
-    total *= keep;
-    if (__any(keep != 1.f))
+    if (__any(mt > acc_top + kSlack)) {
+      // (only for the rows concerned: no other row's result depends on theirs)
+      const float now = mt > acc_top + kSlack ? mt : acc_top, keep = now == acc_top ? 1.f : __builtin_amdgcn_exp2f(acc_top - now);
+      acc_top = now;
+      total *= keep;
 #pragma unroll
       for (int t = 0; t < ND; ++t)
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[t][r] *= keep;
+    }
+    const float base = finite_or_0(acc_top);
     const float fv = am.y * (1.f / 127.f);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -251,7 +264,7 @@ __global__ __launch_bounds__(kWaves * kWave) void k_chunk_attention(const ChunkP
     if (p.splits == 1) {
       if (c < d) static_cast<T*>(p.out)[(size_t)at.x * p.ldo + (size_t)at.y * d + c] = (T)(l == 0.f ? 0.f : __fdiv_rn(x, l));
     } else {
-      float* to = p.part + (((size_t)at.x * p.heads + at.y) * p.splits + split) * (dv + 2);
+      float* to = p.part + (((size_t)at.x * p.heads + at.y) * p.splits + split) * (dv + 4);
       to[c] = x;
       if (c == 0) {
         to[dv] = mm;
@@ -261,11 +274,361 @@ __global__ __launch_bounds__(kWaves * kWave) void k_chunk_attention(const ChunkP
   }
 }
 
+// ---- many rows ----------------------------------------------------------------------------------------------------------
+//
+// A workgroup's four waves have 32 CT rows each and go through the same blocks, which they bring into LDS together, converted to
+// bfloat16 once, in operand order.  Scores are 32 tokens ahead: their products stand beside the exponentials of the 32 tokens
+// before, and the conversions of blocks to come beside the products of the values.  One barrier a block: keys have three places
+// in LDS, since the next block's are read while this one's values still are.
+
+// Sums of matrix instructions times a factor, from accumulation registers and back.  (The compiler would otherwise take the
+// copies that the vector unit needs out of the branch, into every step.)
+__device__ __forceinline__ void scale_sums(v16f& o, float factor) {
+  asm volatile("" : "+a"(o));
+  o *= factor;
+  asm volatile("" : "+a"(o));
+}
+
+template <int DT, int DC>
+struct TileForm {
+  static constexpr int NP = kParts<DT>, CT = NP == 1 && DC <= 2 ? 2 : 1, kRowsOfWg = 4 * 32 * CT;
+  static constexpr int kUnits = 8 * DC;                    // 1 KB pieces of a block's keys, and of its values
+  static constexpr size_t kLds = 5 * (size_t)kUnits * 1024;       // three blocks of keys, two of values
+};
+
+template <int DT, int DC>
+__global__ __launch_bounds__(kWaves * kWave, 1) void k_chunk_tiles(const ChunkParams p, int vec) {
+  using T = typename Elem<DT>::T;
+  using Form = TileForm<DT, DC>;
+  constexpr int NP = Form::NP, CT = Form::CT, NK = 2 * DC, ND = 2 * DC, KU = Form::kUnits;
+  extern __shared__ __attribute__((aligned(16))) bf8 tile_lds[];                 // keys [3][KU][64], values [2][KU][64]
+  bf8 *const kl = tile_lds, *const vl = tile_lds + 3 * KU * kWave;
+  const unsigned lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), col = lane % 32, grp = lane / 32;
+  // workgroups of a kv head on neighbouring places of one XCD where there are eight: they read the same blocks
+  const unsigned kvh = blockIdx.x % p.kv_heads, split = blockIdx.x / p.kv_heads % p.splits, slot = blockIdx.x / (p.kv_heads * p.splits);
+  const unsigned per = p.heads / p.kv_heads, d = p.d, dk = kv_dk(d), dv = kv_dv(d);
+  const Tile tile = find_tile<Form::kRowsOfWg>(p, slot, per);
+  if (tile.b < 0) return;
+  const unsigned nblocks = (seen_by(p, tile, (tile.row0 + tile.rows - 1) / per) + kKvBlock - 1) / kKvBlock;
+  const unsigned start = split * p.run, end = min(start + p.run, nblocks);
+  if (split > 0 && start >= nblocks) return;
+  const unsigned count = end > start ? end - start : 0;
+  // this wave's rows; past the tile's end they repeat its last and are not stored
+  unsigned mine_sees[CT], least = 0xffffffffu;
+  uint2 at[CT];
+  bool stored[CT];
+#pragma unroll
+  for (int x = 0; x < CT; ++x) {
+    const unsigned r = (wave * CT + x) * 32 + col, i = tile.row0 + min(r, tile.rows - 1);
+    stored[x] = r < tile.rows;
+    at[x] = make_uint2(tile.first + i / per, kvh * per + i % per);
+    mine_sees[x] = seen_by(p, tile, i / per);
+  }
+  least = __builtin_amdgcn_readfirstlane(mine_sees[0]);    // (ascends along the rows)
+
+  // what a wave brings: keys piece n: units 2 i, 2 i + 1 with i = wave + 4 n = t NK + c: token 32 t + col, bytes 32 c + 16 grp ..
+  // values: tile of columns wave + 4 n, both 16-byte pieces of row 32 tile + col that hold lane group grp's tokens
+  constexpr int KP = DC, VP = (ND + 3) / 4;
+  const int32_t* table = p.table + (size_t)tile.b * p.table_width;
+  auto look = [&](unsigned i) {
+    const size_t pg = start + (size_t)i + lane;
+    return table[pg < p.table_width ? pg : p.table_width - 1];
+  };
+  u4 rk[KP], rv[VP][2];
+  float ak = 0.f, av = 0.f;                                // scales of the blocks that rk and rv hold
+  int ids_k = look(0), ids_v = ids_k;
+  auto block_of = [&](int& ids, unsigned i, bool& there) {
+    if (i % kWave == 0 && i > 0) ids = look(i);
+    const int block = __builtin_amdgcn_readlane(ids, i % kWave);
+    there = block >= 0 && (size_t)block < p.blocks;
+    return (size_t)(there ? block : 0) * p.kv_heads + kvh;
+  };
+  bool there_k = true, there_v = true;
+  auto fetch_keys = [&](unsigned i) {
+    if (i >= count) return;
+    const size_t b = block_of(ids_k, i, there_k);
+    const int8_t* kp = p.keys + b * kKvBlock * dk + (size_t)col * dk + grp * 16;
+#pragma unroll
+    for (int n = 0; n < KP; ++n) {
+      const unsigned u = wave + 4 * n;
+      rk[n] = *reinterpret_cast<const u4*>(kp + (size_t)(u / NK) * 32 * dk + u % NK * 32);
+    }
+    ak = p.amax[2 * b];
+  };
+  auto fetch_values = [&](unsigned i) {
+    if (i >= count) return;
+    const size_t b = block_of(ids_v, i, there_v);
+    const int8_t* vp = p.values + b * dv * kKvBlock + grp * 16;
+#pragma unroll
+    for (int n = 0; n < VP; ++n)
+      if (4 * n + 4 <= ND || wave + 4 * n < ND) {
+        const int8_t* row = vp + (size_t)min(32 * (wave + 4 * n) + col, dv - 1) * kKvBlock;
+        rv[n][0] = *reinterpret_cast<const u4*>(row);
+        rv[n][1] = *reinterpret_cast<const u4*>(row + 32);
+      }
+    av = p.amax[2 * b + 1];
+  };
+  auto put_key = [&](unsigned buf, int n, int s) {
+    kl[(buf * KU + 2 * (wave + 4 * n) + s) * kWave + lane] = bf16_of_bytes(rk[n][2 * s], rk[n][2 * s + 1]);
+  };
+  auto put_value = [&](unsigned buf, int n, int j) {
+    if (4 * n + 4 <= ND || wave + 4 * n < ND) vl[(buf * KU + 4 * (wave + 4 * n) + j) * kWave + lane] = bf16_of_bytes(rv[n][0][j], rv[n][1][j]);
+  };
+  auto put_keys = [&](unsigned buf) {
+#pragma unroll
+    for (int n = 0; n < KP; ++n)
+#pragma unroll
+      for (int s = 0; s < 2; ++s) put_key(buf, n, s);
+  };
+  auto put_values = [&](unsigned buf) {
+#pragma unroll
+    for (int n = 0; n < VP; ++n)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) put_value(buf, n, j);
+  };
+  fetch_keys(0);
+
+  // queries in operand order, a power of two off each row
+  bf8 qf[CT][NP][NK * 2];
+  float qscale[CT];
+#pragma unroll
+  for (int x = 0; x < CT; ++x) {
+    const T* src = static_cast<const T*>(p.q) + (size_t)at[x].x * p.ldq + (size_t)at[x].y * d;
+    float m = 0.f;
+    auto piece = [&](int u, float (&v)[8]) {
+      const unsigned k = 32 * (u / 2) + 16 * grp + 8 * (u % 2), d = again(p.d);
+      if (vec & 1) {
+        constexpr int W = 16 / sizeof(T);
+        typedef T tw __attribute__((ext_vector_type(W)));
+#pragma unroll
+        for (int j = 0; j < 8; j += W) {
+          tw w = {};
+          if (k + j < d) w = *reinterpret_cast<const tw*>(src + k + j);
+#pragma unroll
+          for (int i = 0; i < W; ++i) v[j + i] = (float)w[i];
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = k + j < d ? (float)src[k + j] : 0.f;
+      }
+    };
+#pragma unroll
+    for (int u = 0; u < NK * 2; ++u) {
+      float v[8];
+      piece(u, v);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) m = fabsf(v[j]) <= 3.402823466e38f ? fmaxf(m, fabsf(v[j])) : INFINITY;
+    }
+    m = across32_f(m, fmax2);
+    const int e = row_exponent(m);
+    const float mul = __uint_as_float((unsigned)(127 - e) << 23) * (p.scale2 < 0.f ? -1.f : 1.f);
+    qscale[x] = ldexpf(fabsf(p.scale2), e) * (1.f / 127.f);
+#pragma unroll
+    for (int u = 0; u < NK * 2; ++u) {
+      float v[8];
+      piece(u, v);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        __bf16 b[NP];
+        split_bf16<NP>(m == INFINITY ? NAN : v[j] * mul, b);
+#pragma unroll
+        for (int i = 0; i < NP; ++i) qf[x][i][u][j] = b[i];
+      }
+    }
+  }
+
+  float ref[CT], total[CT];
+  v16f acc[CT][ND] = {}, sc[2][CT];            // sums; scores of a block's two halves
+#pragma unroll
+  for (int x = 0; x < CT; ++x) {
+    ref[x] = -INFINITY;
+    total[x] = 0.f;
+  }
+  constexpr int STEPS = NK * 2;
+  // one step of the scores of half t of the block that `ku` holds
+  auto score_step = [&](const bf8* ku, auto half, int u) __attribute__((always_inline)) {
+    constexpr int t = decltype(half)::value;
+    const bf8 a = ku[(2 * (t * NK + u / 2) + u % 2) * kWave];
+#pragma unroll
+    for (int k = NP - 1; k >= 0; --k)
+#pragma unroll
+      for (int x = 0; x < CT; ++x)
+        sc[t][x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[x][k][u], u == 0 && k == NP - 1 ? v16f{} : sc[t][x], 0, 0, 0);
+  };
+  // scales and presence of the block in turn and the next
+  float ak_at[2] = {}, av_now = 0.f;
+  bool th_at[2] = {true, true};
+  if (count > 0) {
+    put_keys(0);
+    ak_at[0] = ak;
+    th_at[0] = there_k;
+    fetch_keys(1);
+    fetch_values(0);
+    put_keys(1);
+    ak_at[1] = ak;
+    th_at[1] = there_k;
+    fetch_keys(2);
+    put_values(0);
+    av_now = av;
+    fetch_values(1);
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < STEPS; ++u) score_step(kl + lane, std::integral_constant<int, 0>{}, u);
+  }
+  unsigned now = 0, next = 1, after = 2;       // places of the keys of blocks i, i + 1, i + 2
+  for (unsigned i = 0; i < count; ++i) {
+    const unsigned pg = start + i, odd = i % 2;
+    const bool there = th_at[0];
+    float f[CT];
+#pragma unroll
+    for (int x = 0; x < CT; ++x) {
+      f[x] = there ? qscale[x] * ak_at[0] : 0.f;
+      f[x] = f[x] == 0.f ? 1e-30f : f[x];      // (0 times a masked score would be NaN; others are below 2^24)
+    }
+    // (where there is no block, block 0 was read, whose maxima may be anything)
+    const float fv = there ? av_now * (1.f / 127.f) : 0.f;
+    const bool masks = !there || (pg + 1) * kKvBlock > least;
+    const bf8* vu = vl + (size_t)odd * KU * kWave + lane;
+    auto half = [&](auto which, const bf8* ku) __attribute__((always_inline)) {
+      constexpr int t = decltype(which)::value;
+      if (masks) {
+#pragma unroll
+        for (int x = 0; x < CT; ++x) {
+          const long long room = (long long)mine_sees[x] - (long long)pg * kKvBlock - 4 * (int)grp;
+          const int limit = !there || room < 0 ? 0 : room > kKvBlock ? kKvBlock : (int)room;
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if (limit <= 32 * t + 8 * (r / 4) + r % 4) sc[t][x][r] = -INFINITY;
+        }
+      }
+      float base[CT], mt[CT];
+      bool rises = false;
+#pragma unroll
+      for (int x = 0; x < CT; ++x) {
+        float m = -INFINITY;
+#pragma unroll
+        for (int r = 0; r < 16; r += 2) m = fmaxf(m, fmaxf(sc[t][x][r], sc[t][x][r + 1]));
+        mt[x] = across32_f(m, fmax2) * f[x];
+        rises |= mt[x] > ref[x] + kSlack;
+      }
+      if (__builtin_expect(__any(rises), 0)) {
+#pragma unroll
+        for (int x = 0; x < CT; ++x) {
+          // (only for the rows concerned: no other row's result depends on theirs)
+          const float top = mt[x] > ref[x] + kSlack ? mt[x] : ref[x];
+          const float keep = top == ref[x] ? 1.f : __builtin_amdgcn_exp2f(ref[x] - top);
+          ref[x] = top;
+          total[x] *= keep;
+#pragma unroll
+          for (int c = 0; c < ND; ++c) scale_sums(acc[x][c], keep);
+        }
+      }
+#pragma unroll
+      for (int x = 0; x < CT; ++x) base[x] = finite_or_0(ref[x]);
+      bf8 pr[CT][NP][2];
+      constexpr int EACH = (16 + STEPS - 1) / STEPS;       // scores of a row to a step
+#pragma unroll
+      for (int u = 0; u < STEPS; ++u) {
+        score_step(ku, std::integral_constant<int, 1 - t>{}, u);
+#pragma unroll
+        for (int x = 0; x < CT; ++x)
+#pragma unroll
+          for (int n = u * EACH; n < (u + 1) * EACH; ++n) {
+            if (n >= 16) continue;
+            const float e = __builtin_amdgcn_exp2f(fmaf(sc[t][x][n], f[x], -base[x]));
+            total[x] += e;
+            __bf16 b[NP];
+            split_bf16<NP>(e * fv, b);
+#pragma unroll
+            for (int k = 0; k < NP; ++k) pr[x][k][n / 8][n % 8] = b[k];
+          }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+#pragma unroll
+        for (int c = 0; c < ND; ++c) {
+          const bf8 a = vu[(4 * c + 2 * t + j) * kWave];
+#pragma unroll
+          for (int k = NP - 1; k >= 0; --k)
+#pragma unroll
+            for (int x = 0; x < CT; ++x) acc[x][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, pr[x][k][j], acc[x][c], 0, 0, 0);
+        }
+        if constexpr (t == 0) {
+#pragma unroll
+          for (int n = 0; n < KP; ++n) put_key(after, n, j);
+        } else {
+#pragma unroll
+          for (int n = 0; n < VP; ++n) {
+            put_value(1 - odd, n, 2 * j);
+            put_value(1 - odd, n, 2 * j + 1);
+          }
+        }
+      }
+    };
+    half(std::integral_constant<int, 0>{}, kl + (size_t)now * KU * kWave + lane);
+    ak_at[0] = ak_at[1];
+    th_at[0] = th_at[1];
+    ak_at[1] = ak;
+    th_at[1] = there_k;
+    fetch_keys(i + 3);
+    half(std::integral_constant<int, 1>{}, kl + (size_t)next * KU * kWave + lane);
+    av_now = av;
+    fetch_values(i + 2);
+    const unsigned free = now;
+    now = next;
+    next = after;
+    after = free;
+    __syncthreads();
+  }
+
+  // every lane has four neighbouring columns of its row at a time
+#pragma unroll
+  for (int x = 0; x < CT; ++x) {
+    const float l = across32_f(total[x], fadd2);
+    if (!stored[x]) continue;
+    if (p.splits == 1) {
+      const bool whole = vec & 2;
+      T* to = static_cast<T*>(p.out) + (size_t)at[x].x * p.ldo + (size_t)at[x].y * d;
+#pragma unroll
+      for (int t = 0; t < ND; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+          const unsigned c = 32 * t + 2 * r + 4 * grp, end = again(p.d);
+          T v[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) v[j] = (T)(l == 0.f ? 0.f : __fdiv_rn(acc[x][t][r + j], l));
+          if (whole && c < end) {
+            typedef T t4 __attribute__((ext_vector_type(4)));
+            *reinterpret_cast<t4*>(to + c) = t4{v[0], v[1], v[2], v[3]};
+          } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              if (c + j < end) to[c + j] = v[j];
+          }
+        }
+    } else {
+      float* to = p.part + (((size_t)at[x].x * p.heads + at[x].y) * p.splits + split) * (dv + 4);
+#pragma unroll
+      for (int t = 0; t < ND; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const unsigned c = 32 * t + 8 * r + 4 * grp;
+          if (c < dv) *reinterpret_cast<v4f*>(to + c) = v4f{acc[x][t][4 * r], acc[x][t][4 * r + 1], acc[x][t][4 * r + 2], acc[x][t][4 * r + 3]};
+        }
+      if (grp == 0) {
+        to[dv] = ref[x];
+        to[dv + 1] = l;
+      }
+    }
+  }
+}
+
 // The parts of split sequences: a wave per (token, head).
 template <int DT>
-__global__ __launch_bounds__(256) void k_chunk_join(const ChunkParams p) {
+__global__ __launch_bounds__(256) void k_chunk_join(const ChunkParams p, unsigned tile_rows) {
   using T = typename Elem<DT>::T;
-  const unsigned lane = threadIdx.x % kWave, dv = kv_dv(p.d), pitch = dv + 2, per = p.heads / p.kv_heads;
+  const unsigned lane = threadIdx.x % kWave, dv = kv_dv(p.d), pitch = dv + 4, per = p.heads / p.kv_heads;
   const unsigned rows = (unsigned)(blockIdx.x * (256 / kWave) + threadIdx.x / kWave), t = rows / p.heads, h = rows % p.heads;
   if (t >= p.T) return;
   const int b = __builtin_amdgcn_readfirstlane(wave_search(p.B, t, [&](unsigned i) { return first_at(p.first, i, p.T); }));
@@ -276,7 +639,7 @@ __global__ __launch_bounds__(256) void k_chunk_join(const ChunkParams p) {
   Tile tile{b, f, e - f, 0, 0, 0};
   const int len = p.lens[b];
   tile.len = len < 0 ? 0u : min((unsigned)len, p.max_len);
-  const unsigned row = (t - f) * per + h % per, last = min(row / kRows * kRows + kRows, tile.n * per) - 1;
+  const unsigned row = (t - f) * per + h % per, last = min(row / tile_rows * tile_rows + tile_rows, tile.n * per) - 1;
   const unsigned tokens = p.run * kKvBlock, runs = max(1u, (seen_by(p, tile, last / per) + tokens - 1) / tokens);
   const float* part = p.part + ((size_t)t * p.heads + h) * p.splits * pitch;
   float m = -INFINITY;
@@ -297,53 +660,98 @@ __global__ __launch_bounds__(256) void k_chunk_join(const ChunkParams p) {
 }
 
 struct Split {
-  unsigned run, splits, waves;
+  unsigned run, splits, waves, tile_rows;
+  bool tiles;
   size_t slots;
 };
-Split split_of(size_t B, size_t T, size_t max_len, int heads, int kv_heads) {
-  const size_t per = (size_t)(heads / kv_heads), slots = T * per / kRows + B, wgs = slots * (size_t)kv_heads;
-  const size_t blocks = (max_len + kKvBlock - 1) / kKvBlock, want = (512 + wgs - 1) / wgs;
-  if (blocks <= 2 * kWaves) return {(unsigned)blocks, 1u, (unsigned)(blocks < kWaves ? blocks : kWaves), slots};
+// rows of a workgroup of the form for many rows
+unsigned tile_rows(int dtype, size_t d) { return dtype == MQ_BF16 && d <= 128 ? 256 : 128; }
+constexpr size_t kManyRows = 96;      // rows of a sequence on average from which on they share blocks through LDS
+Split split_of(int dtype, size_t B, size_t T, size_t max_len, int heads, int kv_heads, size_t d) {
+  const size_t per = (size_t)(heads / kv_heads), blocks = (max_len + kKvBlock - 1) / kKvBlock;
+  Split s{};
+  // binary32 queries of wide heads do not fit beside the sums
+  s.tiles = T * per / B >= kManyRows && !(dtype == MQ_F32 && d > 128);
+  s.tile_rows = s.tiles ? tile_rows(dtype, d) : kRows;
+  s.slots = T * per / s.tile_rows + B;
+  const size_t wgs = s.slots * (size_t)kv_heads;
+  if (s.tiles) {
+    const size_t want = (1024 + wgs - 1) / wgs;
+    size_t run = (blocks + want - 1) / want;
+    if (run < 32) run = 32;
+    s.run = (unsigned)run;
+    s.splits = (unsigned)((blocks + run - 1) / run);
+    s.waves = kWaves;
+    return s;
+  }
+  const size_t want = (512 + wgs - 1) / wgs;
+  if (blocks <= 2 * kWaves) {
+    s.run = (unsigned)blocks;
+    s.splits = 1;
+    s.waves = (unsigned)(blocks < kWaves ? blocks : kWaves);
+    return s;
+  }
   size_t run = (blocks + want - 1) / want;
   if (run < (size_t)kWaves) run = kWaves;
-  return {(unsigned)run, (unsigned)((blocks + run - 1) / run), kWaves, slots};
+  s.run = (unsigned)run;
+  s.splits = (unsigned)((blocks + run - 1) / run);
+  s.waves = kWaves;
+  return s;
 }
 
 }  // namespace
 
 size_t chunk_attention_ws_bytes(size_t B, size_t T, size_t max_len, int heads, int kv_heads, size_t d) {
-  const unsigned splits = split_of(B, T, max_len, heads, kv_heads).splits;
-  return splits == 1 ? 16 : T * (size_t)heads * splits * (kv_dv((unsigned)d) + 2) * sizeof(float);
+  unsigned splits = 1;                // (whatever the type)
+  for (int dtype : {MQ_F32, MQ_F16, MQ_BF16}) {
+    const unsigned n = split_of(dtype, B, T, max_len, heads, kv_heads, d).splits;
+    splits = n > splits ? n : splits;
+  }
+  return splits == 1 ? 16 : T * (size_t)heads * splits * (kv_dv((unsigned)d) + 4) * sizeof(float);
 }
 
 int launch_chunk_attention(const mq_kv_cache& cache, const int32_t* table, size_t table_width, const int32_t* first,
                            const int32_t* lens, size_t B, size_t T, size_t max_len, int causal, const void* q, size_t ldq,
                            int heads, int dtype, float scale, void* out, size_t ldo, void* ws, hipStream_t s) {
-  const Split split = split_of(B, T, max_len, heads, cache.kv_heads);
+  const Split split = split_of(dtype, B, T, max_len, heads, cache.kv_heads, cache.head_dim);
   const size_t wgs = split.slots * (size_t)cache.kv_heads * split.splits;
   const size_t joins = (T * (size_t)heads + 3) / 4;
   if (!launchable(wgs, kWaves * kWave) || (split.splits > 1 && !launchable(joins, 256))) return MQ_ERR_SHAPE;
   const ChunkParams p{cache.keys, cache.values, cache.amax, table, first, lens, q, out, static_cast<float*>(ws), ldq, ldo,
                       table_width, cache.blocks, (unsigned)B, (unsigned)T, (unsigned)max_len, (unsigned)cache.kv_heads,
                       (unsigned)heads, (unsigned)cache.head_dim, split.splits, split.run, scale * 1.44269504088896340736f, causal};
+  const size_t piece = 16 / elem_bytes(dtype);
+  // whole 16-byte pieces of queries, four neighbouring results at once
+  const int vec = (cache.head_dim % piece == 0 && ldq % piece == 0 && reinterpret_cast<uintptr_t>(q) % 16 == 0 ? 1 : 0) |
+                  (cache.head_dim % 4 == 0 && ldo % 4 == 0 && reinterpret_cast<uintptr_t>(out) % (4 * elem_bytes(dtype)) == 0 ? 2 : 0);
   return with_dtype(dtype, [&](auto dt) {
     constexpr int DT = decltype(dt)::value;
-    const size_t pieces = kv_dk(p.d) / 64;
-    const size_t ql = kParts<DT> * pieces * 4 * kWave * 16, sums = kRows * (pieces * 64 + 1) * sizeof(float);
-    const size_t lds = ql > sums ? ql : sums;
-    auto go = [&](auto kern) {
-      hipLaunchKernelGGL(kern, dim3((unsigned)wgs), dim3(split.waves * kWave), lds, s, p);
-      return check_hip(hipGetLastError());
+    int rc = MQ_OK;
+    auto sized = [&](auto dc) {
+      constexpr int DC = decltype(dc)::value;
+      if (split.tiles) {
+        if constexpr (!(DT == MQ_F32 && DC > 2)) {
+          using Form = TileForm<DT, DC>;
+          auto kern = k_chunk_tiles<DT, DC>;
+          if (Form::kLds > 65536)
+            rc = check_hip(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)Form::kLds));
+          if (rc != MQ_OK) return;
+          hipLaunchKernelGGL(kern, dim3((unsigned)wgs), dim3(kWaves * kWave), Form::kLds, s, p, vec);
+        }
+      } else {
+        const size_t ql = kParts<DT> * DC * 4 * kWave * 16, sums = kRows * (DC * 64 + 1) * sizeof(float);
+        hipLaunchKernelGGL((k_chunk_attention<DT, DC>), dim3((unsigned)wgs), dim3(split.waves * kWave), ql > sums ? ql : sums, s, p);
+      }
+      rc = check_hip(hipGetLastError());
     };
-    int rc;
-    switch (pieces) {
-      case 1: rc = go(k_chunk_attention<DT, 1>); break;
-      case 2: rc = go(k_chunk_attention<DT, 2>); break;
-      case 3: rc = go(k_chunk_attention<DT, 3>); break;
-      default: rc = go(k_chunk_attention<DT, 4>); break;
+    switch (kv_dk(p.d) / 64) {
+      case 1: sized(std::integral_constant<int, 1>{}); break;
+      case 2: sized(std::integral_constant<int, 2>{}); break;
+      case 3: sized(std::integral_constant<int, 3>{}); break;
+      default: sized(std::integral_constant<int, 4>{}); break;
     }
     if (rc != MQ_OK || split.splits == 1) return rc;
-    hipLaunchKernelGGL(k_chunk_join<DT>, dim3((unsigned)joins), dim3(256), 0, s, p);
+    hipLaunchKernelGGL(k_chunk_join<DT>, dim3((unsigned)joins), dim3(256), 0, s, p, split.tile_rows);
     return check_hip(hipGetLastError());
   });
 }

@@ -142,6 +142,12 @@ CHUNKS = [
     ([40, 1], [41, 190], 5, 5, 160),
     ([130, 257, 1], [700, 257, 3], 12, 3, 96),
     ([1, 1, 1], [4500, 33, 0], 7, 1, 64),
+    # many rows: whole tiles and ragged ends, several runs of blocks
+    ([300, 0, 77], [300, 10, 2500], 4, 2, 64),
+    ([513, 70], [5000, 90], 4, 1, 128),
+    ([200], [4400], 3, 3, 192),
+    ([129, 260], [131, 2300], 2, 1, 250),
+    ([64], [64], 16, 2, 40),
 ]
 
 
