@@ -196,7 +196,7 @@ __global__ __launch_bounds__(kWaves * kWave) void k_chunk_attention(const ChunkP
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) mt = fmaxf(mt, sc[t][r]);
+      for (int r = 0; r < 16; r += 2) mt = max3(mt, sc[t][r], sc[t][r + 1]);
     mt = across32_f(mt, fmax2);
     if (__any(mt > acc_top + kSlack)) {
       // (only for the rows concerned: no other row's result depends on theirs)
@@ -278,8 +278,10 @@ __global__ __launch_bounds__(kWaves * kWave) void k_chunk_attention(const ChunkP
 //
 // A workgroup's four waves have 32 CT rows each and go through the same blocks, which they bring into LDS together, converted to
 // bfloat16 once, in operand order.  Scores are 32 tokens ahead: their products stand beside the exponentials of the 32 tokens
-// before, and the conversions of blocks to come beside the products of the values.  One barrier a block: keys have three places
-// in LDS, since the next block's are read while this one's values still are.
+// before, and the conversions of blocks to come beside the products of the values.  One barrier a block, two places in LDS for a
+// block's keys and for its values.
+// The scale of a block's values goes into the exponent (for binary32, whose 24 bits the logarithm would cost some, into a
+// product), and the probabilities are summed by a product with ones, so that what is divided by is the sum of what is multiplied.
 
 // Sums of matrix instructions times a factor, from accumulation registers and back.  (The compiler would otherwise take the
 // copies that the vector unit needs out of the branch, into every step.)
@@ -291,18 +293,20 @@ __device__ __forceinline__ void scale_sums(v16f& o, float factor) {
 
 template <int DT, int DC>
 struct TileForm {
-  static constexpr int NP = kParts<DT>, CT = NP == 1 && DC <= 2 ? 2 : 1, kRowsOfWg = 4 * 32 * CT;
+  // two waves a SIMD where their registers fit
+  static constexpr int NP = kParts<DT>, CT = 1, W = NP * DC <= 2 ? 8 : 4, kRowsOfWg = W * 32 * CT;
   static constexpr int kUnits = 8 * DC;                    // 1 KB pieces of a block's keys, and of its values
-  static constexpr size_t kLds = 5 * (size_t)kUnits * 1024;       // three blocks of keys, two of values
+  static constexpr size_t kLds = 4 * (size_t)kUnits * 1024;       // two blocks of each
+  static constexpr bool kFold = NP < 3;
 };
 
 template <int DT, int DC>
-__global__ __launch_bounds__(kWaves * kWave, 1) void k_chunk_tiles(const ChunkParams p, int vec) {
+__global__ __launch_bounds__((TileForm<DT, DC>::W) * kWave, 1) void k_chunk_tiles(const ChunkParams p, int vec) {
   using T = typename Elem<DT>::T;
   using Form = TileForm<DT, DC>;
-  constexpr int NP = Form::NP, CT = Form::CT, NK = 2 * DC, ND = 2 * DC, KU = Form::kUnits;
-  extern __shared__ __attribute__((aligned(16))) bf8 tile_lds[];                 // keys [3][KU][64], values [2][KU][64]
-  bf8 *const kl = tile_lds, *const vl = tile_lds + 3 * KU * kWave;
+  constexpr int NP = Form::NP, CT = Form::CT, W = Form::W, NK = 2 * DC, ND = 2 * DC, KU = Form::kUnits;
+  extern __shared__ __attribute__((aligned(16))) bf8 tile_lds[];                 // keys [2][KU][64], values [2][KU][64]
+  bf8 *const kl = tile_lds, *const vl = tile_lds + 2 * KU * kWave;
   const unsigned lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), col = lane % 32, grp = lane / 32;
   // workgroups of a kv head on neighbouring places of one XCD where there are eight: they read the same blocks
   const unsigned kvh = blockIdx.x % p.kv_heads, split = blockIdx.x / p.kv_heads % p.splits, slot = blockIdx.x / (p.kv_heads * p.splits);
@@ -326,9 +330,9 @@ __global__ __launch_bounds__(kWaves * kWave, 1) void k_chunk_tiles(const ChunkPa
   }
   least = __builtin_amdgcn_readfirstlane(mine_sees[0]);    // (ascends along the rows)
 
-  // what a wave brings: keys piece n: units 2 i, 2 i + 1 with i = wave + 4 n = t NK + c: token 32 t + col, bytes 32 c + 16 grp ..
-  // values: tile of columns wave + 4 n, both 16-byte pieces of row 32 tile + col that hold lane group grp's tokens
-  constexpr int KP = DC, VP = (ND + 3) / 4;
+  // what a wave brings: keys piece n: units 2 i, 2 i + 1 with i = wave + W n = t NK + c: token 32 t + col, bytes 32 c + 16 grp ..
+  // values: tile of columns wave + W n, both 16-byte pieces of row 32 tile + col that hold lane group grp's tokens
+  constexpr int KP = (2 * NK + W - 1) / W, VP = (ND + W - 1) / W;
   const int32_t* table = p.table + (size_t)tile.b * p.table_width;
   auto look = [&](unsigned i) {
     const size_t pg = start + (size_t)i + lane;
@@ -350,8 +354,8 @@ __global__ __launch_bounds__(kWaves * kWave, 1) void k_chunk_tiles(const ChunkPa
     const int8_t* kp = p.keys + b * kKvBlock * dk + (size_t)col * dk + grp * 16;
 #pragma unroll
     for (int n = 0; n < KP; ++n) {
-      const unsigned u = wave + 4 * n;
-      rk[n] = *reinterpret_cast<const u4*>(kp + (size_t)(u / NK) * 32 * dk + u % NK * 32);
+      const unsigned u = wave + W * n;
+      if (W * n + W <= 2 * NK || u < 2 * NK) rk[n] = *reinterpret_cast<const u4*>(kp + (size_t)(u / NK) * 32 * dk + u % NK * 32);
     }
     ak = p.amax[2 * b];
   };
@@ -361,18 +365,23 @@ __global__ __launch_bounds__(kWaves * kWave, 1) void k_chunk_tiles(const ChunkPa
     const int8_t* vp = p.values + b * dv * kKvBlock + grp * 16;
 #pragma unroll
     for (int n = 0; n < VP; ++n)
-      if (4 * n + 4 <= ND || wave + 4 * n < ND) {
-        const int8_t* row = vp + (size_t)min(32 * (wave + 4 * n) + col, dv - 1) * kKvBlock;
+      if (W * n + W <= ND || wave + W * n < ND) {
+        const int8_t* row = vp + (size_t)min(32 * (wave + W * n) + col, dv - 1) * kKvBlock;
         rv[n][0] = *reinterpret_cast<const u4*>(row);
         rv[n][1] = *reinterpret_cast<const u4*>(row + 32);
       }
     av = p.amax[2 * b + 1];
   };
+  // values that are all zero (or below any normal number): their scale has no logarithm
+  auto no_values = [&](float a) { return Form::kFold && a * (1.f / 127.f) < 1.2e-38f; };
   auto put_key = [&](unsigned buf, int n, int s) {
-    kl[(buf * KU + 2 * (wave + 4 * n) + s) * kWave + lane] = bf16_of_bytes(rk[n][2 * s], rk[n][2 * s + 1]);
+    if (W * n + W <= 2 * NK || wave + W * n < 2 * NK)
+      kl[(buf * KU + 2 * (wave + W * n) + s) * kWave + lane] = bf16_of_bytes(rk[n][2 * s], rk[n][2 * s + 1]);
   };
   auto put_value = [&](unsigned buf, int n, int j) {
-    if (4 * n + 4 <= ND || wave + 4 * n < ND) vl[(buf * KU + 4 * (wave + 4 * n) + j) * kWave + lane] = bf16_of_bytes(rv[n][0][j], rv[n][1][j]);
+    const unsigned any = no_values(av) ? 0u : ~0u;
+    if (W * n + W <= ND || wave + W * n < ND)
+      vl[(buf * KU + 4 * (wave + W * n) + j) * kWave + lane] = bf16_of_bytes(rv[n][0][j] & any, rv[n][1][j] & any);
   };
   auto put_keys = [&](unsigned buf) {
 #pragma unroll
@@ -444,16 +453,22 @@ __global__ __launch_bounds__(kWaves * kWave, 1) void k_chunk_tiles(const ChunkPa
     ref[x] = -INFINITY;
     total[x] = 0.f;
   }
+  // a half block's scores take STEPS products a row tile and part, its sums of values as many: pieces of the one are asked for
+  // from LDS beside the products of the other
   constexpr int STEPS = NK * 2;
-  // one step of the scores of half t of the block that `ku` holds
-  auto score_step = [&](const bf8* ku, auto half, int u) __attribute__((always_inline)) {
+  static_assert(STEPS == 2 * ND, "");
+  bf8 kf[STEPS], vf[STEPS];
+  auto read_key = [&](const bf8* ku, auto half, int u) __attribute__((always_inline)) {
     constexpr int t = decltype(half)::value;
-    const bf8 a = ku[(2 * (t * NK + u / 2) + u % 2) * kWave];
+    kf[u] = ku[(2 * (t * NK + u / 2) + u % 2) * kWave];
+  };
+  auto score_step = [&](auto half, int u) __attribute__((always_inline)) {
+    constexpr int t = decltype(half)::value;
 #pragma unroll
     for (int k = NP - 1; k >= 0; --k)
 #pragma unroll
       for (int x = 0; x < CT; ++x)
-        sc[t][x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[x][k][u], u == 0 && k == NP - 1 ? v16f{} : sc[t][x], 0, 0, 0);
+        sc[t][x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[u], qf[x][k][u], u == 0 && k == NP - 1 ? v16f{} : sc[t][x], 0, 0, 0);
   };
   // scales and presence of the block in turn and the next
   float ak_at[2] = {}, av_now = 0.f;
@@ -473,9 +488,18 @@ __global__ __launch_bounds__(kWaves * kWave, 1) void k_chunk_tiles(const ChunkPa
     fetch_values(1);
     __syncthreads();
 #pragma unroll
-    for (int u = 0; u < STEPS; ++u) score_step(kl + lane, std::integral_constant<int, 0>{}, u);
+    for (int u = 0; u < STEPS; ++u) read_key(kl + lane, std::integral_constant<int, 0>{}, u);
+#pragma unroll
+    for (int u = 0; u < STEPS; ++u) score_step(std::integral_constant<int, 0>{}, u);
+#pragma unroll
+    for (int u = 0; u < STEPS; ++u) read_key(kl + lane, std::integral_constant<int, 1>{}, u);
+    __syncthreads();
   }
-  unsigned now = 0, next = 1, after = 2;       // places of the keys of blocks i, i + 1, i + 2
+  constexpr bool FOLD = Form::kFold;
+  const u4 one = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
+  const bf8 ones = __builtin_bit_cast(bf8, one);
+  v16f sum[CT] = {};                           // of a half block's probabilities times the values' scale, in every register
+  float inverse = 0.f;                         // of that scale
   for (unsigned i = 0; i < count; ++i) {
     const unsigned pg = start + i, odd = i % 2;
     const bool there = th_at[0];
@@ -487,6 +511,8 @@ __global__ __launch_bounds__(kWaves * kWave, 1) void k_chunk_tiles(const ChunkPa
     }
     // (where there is no block, block 0 was read, whose maxima may be anything)
     const float fv = there ? av_now * (1.f / 127.f) : 0.f;
+    const bool nothing = !there || no_values(av_now);
+    const float lift = nothing ? 0.f : __builtin_amdgcn_logf(fv), inverse_now = nothing ? 1.f : __fdiv_rn(1.f, fv);
     const bool masks = !there || (pg + 1) * kKvBlock > least;
     const bf8* vu = vl + (size_t)odd * KU * kWave + lane;
     auto half = [&](auto which, const bf8* ku) __attribute__((always_inline)) {
@@ -501,13 +527,18 @@ __global__ __launch_bounds__(kWaves * kWave, 1) void k_chunk_tiles(const ChunkPa
             if (limit <= 32 * t + 8 * (r / 4) + r % 4) sc[t][x][r] = -INFINITY;
         }
       }
+      if constexpr (FOLD) {
+#pragma unroll
+        for (int x = 0; x < CT; ++x) total[x] = fmaf(sum[x][0], inverse, total[x]);
+        inverse = inverse_now;
+      }
       float base[CT], mt[CT];
       bool rises = false;
 #pragma unroll
       for (int x = 0; x < CT; ++x) {
         float m = -INFINITY;
 #pragma unroll
-        for (int r = 0; r < 16; r += 2) m = fmaxf(m, fmaxf(sc[t][x][r], sc[t][x][r + 1]));
+        for (int r = 0; r < 16; r += 2) m = max3(m, sc[t][x][r], sc[t][x][r + 1]);
         mt[x] = across32_f(m, fmax2) * f[x];
         rises |= mt[x] > ref[x] + kSlack;
       }
@@ -524,68 +555,75 @@ __global__ __launch_bounds__(kWaves * kWave, 1) void k_chunk_tiles(const ChunkPa
         }
       }
 #pragma unroll
-      for (int x = 0; x < CT; ++x) base[x] = finite_or_0(ref[x]);
+      for (int x = 0; x < CT; ++x) base[x] = FOLD ? lift - finite_or_0(ref[x]) : -finite_or_0(ref[x]);
       bf8 pr[CT][NP][2];
-      constexpr int EACH = (16 + STEPS - 1) / STEPS;       // scores of a row to a step
-#pragma unroll
-      for (int u = 0; u < STEPS; ++u) {
-        score_step(ku, std::integral_constant<int, 1 - t>{}, u);
+      // exponentials [from, end) of the 16 that a lane has of each row
+      auto exponentials = [&](int from, int end) __attribute__((always_inline)) {
 #pragma unroll
         for (int x = 0; x < CT; ++x)
 #pragma unroll
-          for (int n = u * EACH; n < (u + 1) * EACH; ++n) {
-            if (n >= 16) continue;
-            const float e = __builtin_amdgcn_exp2f(fmaf(sc[t][x][n], f[x], -base[x]));
-            total[x] += e;
+          for (int n = from; n < end; ++n) {
+            const float e = __builtin_amdgcn_exp2f(fmaf(sc[t][x][n], f[x], base[x]));
+            if (!FOLD) total[x] += e;
             __bf16 b[NP];
-            split_bf16<NP>(e * fv, b);
+            split_bf16<NP>(FOLD ? e : e * fv, b);
 #pragma unroll
             for (int k = 0; k < NP; ++k) pr[x][k][n / 8][n % 8] = b[k];
           }
+      };
+      constexpr int EARLY = 12;                // (the others beside the first half of the sums of values)
+#pragma unroll
+      for (int u = 0; u < STEPS; ++u) {
+        score_step(std::integral_constant<int, 1 - t>{}, u);
+        vf[u] = vu[(4 * (u % ND) + 2 * t + u / ND) * kWave];         // (in the registers of the key's piece)
+        exponentials(u * EARLY / STEPS, (u + 1) * EARLY / STEPS);
         __builtin_amdgcn_sched_barrier(0);
       }
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
+      for (int u = 0; u < STEPS; ++u) {
+        const int j = u / ND, c = u % ND;
 #pragma unroll
-        for (int c = 0; c < ND; ++c) {
-          const bf8 a = vu[(4 * c + 2 * t + j) * kWave];
+        for (int k = NP - 1; k >= 0; --k)
+#pragma unroll
+          for (int x = 0; x < CT; ++x) acc[x][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[u], pr[x][k][j], acc[x][c], 0, 0, 0);
+        read_key(ku, std::integral_constant<int, t>{}, u);
+        if (FOLD && c == ND - 1) {
 #pragma unroll
           for (int k = NP - 1; k >= 0; --k)
 #pragma unroll
-            for (int x = 0; x < CT; ++x) acc[x][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, pr[x][k][j], acc[x][c], 0, 0, 0);
+            for (int x = 0; x < CT; ++x)
+              sum[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ones, pr[x][k][j], j == 0 && k == NP - 1 ? v16f{} : sum[x], 0, 0, 0);
         }
+        if (j == 0) exponentials(EARLY + c * (16 - EARLY) / ND, EARLY + (c + 1) * (16 - EARLY) / ND);
         if constexpr (t == 0) {
 #pragma unroll
-          for (int n = 0; n < KP; ++n) put_key(after, n, j);
+          for (int n = 0; n < 2 * KP; ++n)
+            if (n * STEPS / (2 * KP) == u) put_key(odd, n / 2, n % 2);
         } else {
 #pragma unroll
-          for (int n = 0; n < VP; ++n) {
-            put_value(1 - odd, n, 2 * j);
-            put_value(1 - odd, n, 2 * j + 1);
-          }
+          for (int n = 0; n < 4 * VP; ++n)
+            if (n * STEPS / (4 * VP) == u) put_value(1 - odd, n / 4, n % 4);
         }
+        __builtin_amdgcn_sched_barrier(0);
       }
     };
-    half(std::integral_constant<int, 0>{}, kl + (size_t)now * KU * kWave + lane);
+    const bf8* ku = kl + (size_t)(1 - odd) * KU * kWave + lane;       // (what is read ahead is the next block's: half t beside half t's values)
+    half(std::integral_constant<int, 0>{}, ku);
     ak_at[0] = ak_at[1];
     th_at[0] = th_at[1];
     ak_at[1] = ak;
     th_at[1] = there_k;
     fetch_keys(i + 3);
-    half(std::integral_constant<int, 1>{}, kl + (size_t)next * KU * kWave + lane);
+    half(std::integral_constant<int, 1>{}, ku);
     av_now = av;
     fetch_values(i + 2);
-    const unsigned free = now;
-    now = next;
-    next = after;
-    after = free;
     __syncthreads();
   }
 
   // every lane has four neighbouring columns of its row at a time
 #pragma unroll
   for (int x = 0; x < CT; ++x) {
-    const float l = across32_f(total[x], fadd2);
+    const float l = FOLD ? fmaf(sum[x][0], inverse, total[x]) : across32_f(total[x], fadd2);
     if (!stored[x]) continue;
     if (p.splits == 1) {
       const bool whole = vec & 2;
@@ -665,7 +703,7 @@ struct Split {
   size_t slots;
 };
 // rows of a workgroup of the form for many rows
-unsigned tile_rows(int dtype, size_t d) { return dtype == MQ_BF16 && d <= 128 ? 256 : 128; }
+unsigned tile_rows(int dtype, size_t d) { return (dtype == MQ_BF16 && d <= 128) || (dtype == MQ_F16 && d <= 64) ? 256 : 128; }
 constexpr size_t kManyRows = 96;      // rows of a sequence on average from which on they share blocks through LDS
 Split split_of(int dtype, size_t B, size_t T, size_t max_len, int heads, int kv_heads, size_t d) {
   const size_t per = (size_t)(heads / kv_heads), blocks = (max_len + kKvBlock - 1) / kKvBlock;
@@ -716,7 +754,7 @@ int launch_chunk_attention(const mq_kv_cache& cache, const int32_t* table, size_
   const Split split = split_of(dtype, B, T, max_len, heads, cache.kv_heads, cache.head_dim);
   const size_t wgs = split.slots * (size_t)cache.kv_heads * split.splits;
   const size_t joins = (T * (size_t)heads + 3) / 4;
-  if (!launchable(wgs, kWaves * kWave) || (split.splits > 1 && !launchable(joins, 256))) return MQ_ERR_SHAPE;
+  if (!launchable(wgs, 2 * kWaves * kWave) || (split.splits > 1 && !launchable(joins, 256))) return MQ_ERR_SHAPE;
   const ChunkParams p{cache.keys, cache.values, cache.amax, table, first, lens, q, out, static_cast<float*>(ws), ldq, ldo,
                       table_width, cache.blocks, (unsigned)B, (unsigned)T, (unsigned)max_len, (unsigned)cache.kv_heads,
                       (unsigned)heads, (unsigned)cache.head_dim, split.splits, split.run, scale * 1.44269504088896340736f, causal};
@@ -736,7 +774,7 @@ int launch_chunk_attention(const mq_kv_cache& cache, const int32_t* table, size_
           if (Form::kLds > 65536)
             rc = check_hip(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)Form::kLds));
           if (rc != MQ_OK) return;
-          hipLaunchKernelGGL(kern, dim3((unsigned)wgs), dim3(kWaves * kWave), Form::kLds, s, p, vec);
+          hipLaunchKernelGGL(kern, dim3((unsigned)wgs), dim3(Form::W * kWave), Form::kLds, s, p, vec);
         }
       } else {
         const size_t ql = kParts<DT> * DC * 4 * kWave * 16, sums = kRows * (DC * 64 + 1) * sizeof(float);

@@ -25,16 +25,28 @@ __device__ __forceinline__ void split_bf16(float x, __bf16 (&part)[NP]) {
   }
 }
 
+// Byte I of a word, signed, as binary32: one instruction (the compiler takes up to three).
+template <int I>
+__device__ __forceinline__ float f32_of_byte(unsigned x) {
+  float y;
+  if constexpr (I == 0) asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_0" : "=v"(y) : "v"(x));
+  else if constexpr (I == 1) asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_1" : "=v"(y) : "v"(x));
+  else if constexpr (I == 2) asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_2" : "=v"(y) : "v"(x));
+  else asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_3" : "=v"(y) : "v"(x));
+  return y;
+}
 // Eight signed bytes as bfloat16 values (8 bits: exact): the upper halves of their binary32 values.
 __device__ __forceinline__ bf8 bf16_of_bytes(unsigned lo, unsigned hi) {
-  u4 w;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const unsigned x = i < 2 ? lo : hi;
-    const float a = (float)(int8_t)(x >> (16 * (i % 2))), b = (float)(int8_t)(x >> (16 * (i % 2) + 8));
-    w[i] = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
-  }
+  auto upper = [](float a, float b) { return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u); };
+  const u4 w = {upper(f32_of_byte<0>(lo), f32_of_byte<1>(lo)), upper(f32_of_byte<2>(lo), f32_of_byte<3>(lo)),
+                upper(f32_of_byte<0>(hi), f32_of_byte<1>(hi)), upper(f32_of_byte<2>(hi), f32_of_byte<3>(hi))};
   return __builtin_bit_cast(bf8, w);
+}
+// The largest of three, NaNs left out (fmaxf would quiet each operand in an instruction of its own).
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float y;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(y) : "v"(a), "v"(b), "v"(c));
+  return y;
 }
 
 __device__ __forceinline__ void store_as(void* y, int type, size_t at, float v) {
