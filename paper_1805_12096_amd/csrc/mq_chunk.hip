@@ -34,6 +34,8 @@ struct ChunkParams {
   unsigned B, T, max_len, kv_heads, heads, d, splits, run;
   float scale2;                       // scale log2(e)
   int causal;
+  unsigned* plan;                     // many rows: [slots + 1] blocks of the tiles in front of each tile
+  unsigned slots;
 };
 
 // Exponent of the power of two taken off a row whose largest magnitude is m.
@@ -56,15 +58,18 @@ struct Tile {
 };
 // Tiles of sequence b lie from tile number first[b] per / ROWS + b on: enough for each, whatever the lengths.
 template <unsigned ROWS>
-__device__ __forceinline__ Tile find_tile(const ChunkParams& p, unsigned slot, unsigned per) {
-  auto start = [&](unsigned i) { return first_at(p.first, i, p.T) * per / ROWS + i; };
-  const int b = __builtin_amdgcn_readfirstlane(wave_search(p.B, slot, start));
+__device__ __forceinline__ Tile tile_of(const ChunkParams& p, int b, unsigned slot, unsigned per) {
   if (b < 0) return {-1, 0, 0, 0, 0, 0};
   const unsigned f = first_at(p.first, b, p.T), e = first_at(p.first, b + 1, p.T), n = e > f ? e - f : 0;
-  const unsigned row0 = (slot - start(b)) * ROWS;
+  const unsigned row0 = (slot - (f * per / ROWS + b)) * ROWS;
   if (row0 >= n * per) return {-1, 0, 0, 0, 0, 0};
   const int len = p.lens[b];
   return {b, f, n, row0, min(n * per - row0, ROWS), len < 0 ? 0u : min((unsigned)len, p.max_len)};
+}
+template <unsigned ROWS>
+__device__ __forceinline__ Tile find_tile(const ChunkParams& p, unsigned slot, unsigned per) {
+  auto start = [&](unsigned i) { return first_at(p.first, i, p.T) * per / ROWS + i; };
+  return tile_of<ROWS>(p, __builtin_amdgcn_readfirstlane(wave_search(p.B, slot, start)), slot, per);
 }
 // Tokens that query i of n sees.
 __device__ __forceinline__ unsigned seen_by(const ChunkParams& p, const Tile& t, unsigned i) {
@@ -278,8 +283,11 @@ __global__ __launch_bounds__(kWaves * kWave) void k_chunk_attention(const ChunkP
 //
 // A workgroup's four waves have 32 CT rows each and go through the same blocks, which they bring into LDS together, converted to
 // bfloat16 once, in operand order.  Scores are 32 tokens ahead: their products stand beside the exponentials of the 32 tokens
-// before, and the conversions of blocks to come beside the products of the values.  One barrier a block, two places in LDS for a
-// block's keys and for its values.
+// before, and the conversions of blocks to come beside the products of the values.  One barrier a block; three places in
+// LDS for keys, since this block's and the next one's are read while those of the one after come, two for values.
+// Lengths are known on the device only, so a first small launch sums up the blocks that each tile of rows sees.  The workgroups,
+// as many as run at once, share the blocks of all tiles and kv heads in one line equally: each has some tiles whole, and parts of
+// the tiles at its two ends, which go to the workspace and are joined.
 // The scale of a block's values goes into the exponent (for binary32, whose 24 bits the logarithm would cost some, into a
 // product), and the probabilities are summed by a product with ones, so that what is divided by is the sum of what is multiplied.
 
@@ -296,27 +304,89 @@ struct TileForm {
   // two waves a SIMD where their registers fit
   static constexpr int NP = kParts<DT>, CT = 1, W = NP * DC <= 2 ? 8 : 4, kRowsOfWg = W * 32 * CT;
   static constexpr int kUnits = 8 * DC;                    // 1 KB pieces of a block's keys, and of its values
-  static constexpr size_t kLds = 4 * (size_t)kUnits * 1024;       // two blocks of each
+  static constexpr size_t kLds = 5 * (size_t)kUnits * 1024;       // three blocks of keys, two of values
   static constexpr bool kFold = NP < 3;
 };
+
+constexpr int kPlan = 1024;           // threads of the workgroup that plans
+constexpr unsigned kLeast = 8;        // blocks that a workgroup takes at least
+
+// Blocks that a tile's last row sees, one at least: every tile belongs to somebody.
+__device__ __forceinline__ unsigned tile_blocks(const ChunkParams& p, const Tile& t, unsigned per) {
+  return t.b < 0 ? 0u : max(1u, (seen_by(p, t, (t.row0 + t.rows - 1) / per) + kKvBlock - 1) / kKvBlock);
+}
+
+template <unsigned ROWS>
+__global__ __launch_bounds__(kPlan) void k_chunk_plan(const ChunkParams p) {
+  __shared__ unsigned box[kPlan / kWave];
+  const unsigned lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, per = p.heads / p.kv_heads;
+  unsigned ahead = 0;
+  for (unsigned at = 0; at < p.slots; at += kPlan) {
+    const unsigned slot = at + threadIdx.x;
+    // a thread's own search: tiles of sequence b start at first[b] per / ROWS + b
+    unsigned lo = 0, hi = p.B;
+    while (hi - lo > 1) {
+      const unsigned mid = (lo + hi) / 2;
+      if (first_at(p.first, mid, p.T) * per / ROWS + mid <= slot) lo = mid;
+      else hi = mid;
+    }
+    unsigned n = 0;
+    if (slot < p.slots) n = tile_blocks(p, tile_of<ROWS>(p, (int)lo, slot, per), per);
+    unsigned x = n;
+#pragma unroll
+    for (int off = 1; off < kWave; off <<= 1) {
+      const unsigned y = __shfl_up(x, off, kWave);
+      if (lane >= (unsigned)off) x += y;
+    }
+    __syncthreads();
+    if (lane == kWave - 1) box[wave] = x;
+    __syncthreads();
+    unsigned before = ahead + x - n;
+#pragma unroll
+    for (int w = 0; w < kPlan / kWave; ++w) {
+      if (w < (int)wave) before += box[w];
+      ahead += box[w];
+    }
+    if (slot < p.slots) p.plan[slot] = before;
+  }
+  if (threadIdx.x == 0) p.plan[p.slots] = ahead;
+}
+
+// Blocks of the line that a workgroup has.
+__device__ __forceinline__ unsigned long long share_of(const ChunkParams& p, unsigned groups) {
+  const unsigned long long all = (unsigned long long)p.plan[p.slots] * p.kv_heads;
+  return max((unsigned long long)kLeast, (all + groups - 1) / groups);
+}
 
 template <int DT, int DC>
 __global__ __launch_bounds__((TileForm<DT, DC>::W) * kWave, 1) void k_chunk_tiles(const ChunkParams p, int vec) {
   using T = typename Elem<DT>::T;
   using Form = TileForm<DT, DC>;
   constexpr int NP = Form::NP, CT = Form::CT, W = Form::W, NK = 2 * DC, ND = 2 * DC, KU = Form::kUnits;
-  extern __shared__ __attribute__((aligned(16))) bf8 tile_lds[];                 // keys [2][KU][64], values [2][KU][64]
-  bf8 *const kl = tile_lds, *const vl = tile_lds + 2 * KU * kWave;
-  const unsigned lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), col = lane % 32, grp = lane / 32;
-  // workgroups of a kv head on neighbouring places of one XCD where there are eight: they read the same blocks
-  const unsigned kvh = blockIdx.x % p.kv_heads, split = blockIdx.x / p.kv_heads % p.splits, slot = blockIdx.x / (p.kv_heads * p.splits);
-  const unsigned per = p.heads / p.kv_heads, d = p.d, dk = kv_dk(d), dv = kv_dv(d);
+  extern __shared__ __attribute__((aligned(16))) bf8 tile_lds[];                 // keys [3][KU][64], values [2][KU][64]
+  bf8 *const kl = tile_lds, *const vl = tile_lds + 3 * KU * kWave;
+  const unsigned per = p.heads / p.kv_heads;
+  // this workgroup's part of the line: an eighth of it for each XCD, whose workgroups then read the same heads' blocks
+  const unsigned me = blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8, line = p.plan[p.slots];
+  const unsigned long long share = share_of(p, gridDim.x), line_end = (unsigned long long)line * p.kv_heads;
+  const unsigned long long from = me * share, to_end = min(from + share, line_end);
+  unsigned segment = 0;
+  for (unsigned long long at_block = from; at_block < to_end; ++segment) {
+  // (unknown to the compiler to be the same each time: it would keep dozens of places and masks from one part to the next)
+  unsigned lane = threadIdx.x % kWave, d = p.d;
+  asm volatile("" : "+v"(lane), "+s"(d));
+  const unsigned wave = __builtin_amdgcn_readfirstlane((threadIdx.x - threadIdx.x % kWave + lane) / kWave), col = lane % 32, grp = lane / 32;
+  const unsigned dk = kv_dk(d), dv = kv_dv(d);
+  const unsigned kvh = __builtin_amdgcn_readfirstlane((unsigned)(at_block / line)), place = (unsigned)(at_block - (unsigned long long)kvh * line);
+  const unsigned slot = (unsigned)__builtin_amdgcn_readfirstlane(wave_search(p.slots, place, [&](unsigned i) { return p.plan[i]; }));
+  const unsigned tile_start = p.plan[slot], tile_end = p.plan[slot + 1], start = place - tile_start;
+  const unsigned long long left = to_end - at_block;
+  const unsigned end = (unsigned)min((unsigned long long)(tile_end - tile_start), start + left);
+  const bool whole_tile = start == 0 && end == tile_end - tile_start;
+  at_block += end - start;
   const Tile tile = find_tile<Form::kRowsOfWg>(p, slot, per);
-  if (tile.b < 0) return;
   const unsigned nblocks = (seen_by(p, tile, (tile.row0 + tile.rows - 1) / per) + kKvBlock - 1) / kKvBlock;
-  const unsigned start = split * p.run, end = min(start + p.run, nblocks);
-  if (split > 0 && start >= nblocks) return;
-  const unsigned count = end > start ? end - start : 0;
+  const unsigned count = min(end, nblocks) > start ? min(end, nblocks) - start : 0;
   // this wave's rows; past the tile's end they repeat its last and are not stored
   unsigned mine_sees[CT], least = 0xffffffffu;
   uint2 at[CT];
@@ -331,14 +401,16 @@ __global__ __launch_bounds__((TileForm<DT, DC>::W) * kWave, 1) void k_chunk_tile
   least = __builtin_amdgcn_readfirstlane(mine_sees[0]);    // (ascends along the rows)
 
   // what a wave brings: keys piece n: units 2 i, 2 i + 1 with i = wave + W n = t NK + c: token 32 t + col, bytes 32 c + 16 grp ..
-  // values: tile of columns wave + W n, both 16-byte pieces of row 32 tile + col that hold lane group grp's tokens
-  constexpr int KP = (2 * NK + W - 1) / W, VP = (ND + W - 1) / W;
+  // values piece n: units 2 i, 2 i + 1 with i = wave + W n = 2 tile + half: row 32 tile + col, 8 bytes of either 16 that hold lane
+  // group grp's tokens
+  constexpr int KP = (2 * NK + W - 1) / W, VP = (2 * ND + W - 1) / W;
   const int32_t* table = p.table + (size_t)tile.b * p.table_width;
   auto look = [&](unsigned i) {
     const size_t pg = start + (size_t)i + lane;
     return table[pg < p.table_width ? pg : p.table_width - 1];
   };
-  u4 rk[KP], rv[VP][2];
+  u4 rk[KP];
+  uint2 rv[VP][2];
   float ak = 0.f, av = 0.f;                                // scales of the blocks that rk and rv hold
   int ids_k = look(0), ids_v = ids_k;
   auto block_of = [&](int& ids, unsigned i, bool& there) {
@@ -365,10 +437,11 @@ __global__ __launch_bounds__((TileForm<DT, DC>::W) * kWave, 1) void k_chunk_tile
     const int8_t* vp = p.values + b * dv * kKvBlock + grp * 16;
 #pragma unroll
     for (int n = 0; n < VP; ++n)
-      if (W * n + W <= ND || wave + W * n < ND) {
-        const int8_t* row = vp + (size_t)min(32 * (wave + W * n) + col, dv - 1) * kKvBlock;
-        rv[n][0] = *reinterpret_cast<const u4*>(row);
-        rv[n][1] = *reinterpret_cast<const u4*>(row + 32);
+      if (W * n + W <= 2 * ND || wave + W * n < 2 * ND) {
+        const unsigned u = wave + W * n;
+        const int8_t* row = vp + (size_t)min(32 * (u / 2) + col, dv - 1) * kKvBlock + u % 2 * 8;
+        rv[n][0] = *reinterpret_cast<const uint2*>(row);
+        rv[n][1] = *reinterpret_cast<const uint2*>(row + 32);
       }
     av = p.amax[2 * b + 1];
   };
@@ -380,8 +453,9 @@ __global__ __launch_bounds__((TileForm<DT, DC>::W) * kWave, 1) void k_chunk_tile
   };
   auto put_value = [&](unsigned buf, int n, int j) {
     const unsigned any = no_values(av) ? 0u : ~0u;
-    if (W * n + W <= ND || wave + W * n < ND)
-      vl[(buf * KU + 4 * (wave + W * n) + j) * kWave + lane] = bf16_of_bytes(rv[n][0][j] & any, rv[n][1][j] & any);
+    if (W * n + W <= 2 * ND || wave + W * n < 2 * ND)
+      vl[(buf * KU + 2 * (wave + W * n) + j) * kWave + lane] =
+          bf16_of_bytes((j ? rv[n][0].y : rv[n][0].x) & any, (j ? rv[n][1].y : rv[n][1].x) & any);
   };
   auto put_keys = [&](unsigned buf) {
 #pragma unroll
@@ -393,7 +467,7 @@ __global__ __launch_bounds__((TileForm<DT, DC>::W) * kWave, 1) void k_chunk_tile
 #pragma unroll
     for (int n = 0; n < VP; ++n)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) put_value(buf, n, j);
+      for (int j = 0; j < 2; ++j) put_value(buf, n, j);
   };
   fetch_keys(0);
 
@@ -453,14 +527,14 @@ __global__ __launch_bounds__((TileForm<DT, DC>::W) * kWave, 1) void k_chunk_tile
     ref[x] = -INFINITY;
     total[x] = 0.f;
   }
-  // a half block's scores take STEPS products a row tile and part, its sums of values as many: pieces of the one are asked for
-  // from LDS beside the products of the other
-  constexpr int STEPS = NK * 2;
-  static_assert(STEPS == 2 * ND, "");
-  bf8 kf[STEPS], vf[STEPS];
+  // a half block's scores take STEPS products a row tile and part, its sums of values as many: their pieces are asked for from
+  // LDS four products ahead
+  constexpr int STEPS = NK * 2, AHEAD = 4;
+  static_assert(STEPS == 2 * ND && STEPS % AHEAD == 0, "");
+  bf8 piece[AHEAD];
   auto read_key = [&](const bf8* ku, auto half, int u) __attribute__((always_inline)) {
     constexpr int t = decltype(half)::value;
-    kf[u] = ku[(2 * (t * NK + u / 2) + u % 2) * kWave];
+    piece[u % AHEAD] = ku[(2 * (t * NK + u / 2) + u % 2) * kWave];
   };
   auto score_step = [&](auto half, int u) __attribute__((always_inline)) {
     constexpr int t = decltype(half)::value;
@@ -468,7 +542,7 @@ __global__ __launch_bounds__((TileForm<DT, DC>::W) * kWave, 1) void k_chunk_tile
     for (int k = NP - 1; k >= 0; --k)
 #pragma unroll
       for (int x = 0; x < CT; ++x)
-        sc[t][x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[u], qf[x][k][u], u == 0 && k == NP - 1 ? v16f{} : sc[t][x], 0, 0, 0);
+        sc[t][x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(piece[u % AHEAD], qf[x][k][u], u == 0 && k == NP - 1 ? v16f{} : sc[t][x], 0, 0, 0);
   };
   // scales and presence of the block in turn and the next
   float ak_at[2] = {}, av_now = 0.f;
@@ -488,13 +562,15 @@ __global__ __launch_bounds__((TileForm<DT, DC>::W) * kWave, 1) void k_chunk_tile
     fetch_values(1);
     __syncthreads();
 #pragma unroll
-    for (int u = 0; u < STEPS; ++u) read_key(kl + lane, std::integral_constant<int, 0>{}, u);
+    for (int u = 0; u < AHEAD; ++u) read_key(kl + lane, std::integral_constant<int, 0>{}, u);
 #pragma unroll
-    for (int u = 0; u < STEPS; ++u) score_step(std::integral_constant<int, 0>{}, u);
-#pragma unroll
-    for (int u = 0; u < STEPS; ++u) read_key(kl + lane, std::integral_constant<int, 1>{}, u);
-    __syncthreads();
+    for (int u = 0; u < STEPS; ++u) {
+      score_step(std::integral_constant<int, 0>{}, u);
+      if (u + AHEAD < STEPS) read_key(kl + lane, std::integral_constant<int, 0>{}, u + AHEAD);
+      else read_key(kl + lane, std::integral_constant<int, 1>{}, u + AHEAD - STEPS);
+    }
   }
+  unsigned now = 0, next = 1, after = 2;       // places of the keys of blocks i, i + 1, i + 2
   constexpr bool FOLD = Form::kFold;
   const u4 one = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
   const bf8 ones = __builtin_bit_cast(bf8, one);
@@ -515,8 +591,11 @@ __global__ __launch_bounds__((TileForm<DT, DC>::W) * kWave, 1) void k_chunk_tile
     const float lift = nothing ? 0.f : __builtin_amdgcn_logf(fv), inverse_now = nothing ? 1.f : __fdiv_rn(1.f, fv);
     const bool masks = !there || (pg + 1) * kKvBlock > least;
     const bf8* vu = vl + (size_t)odd * KU * kWave + lane;
-    auto half = [&](auto which, const bf8* ku) __attribute__((always_inline)) {
+    // half t's exponentials and values, beside them the other half's scores, of this block (t = 0) or the next; keys_then: those
+    // of the scores after
+    auto half = [&](auto which, const bf8* keys_now, const bf8* keys_then) __attribute__((always_inline)) {
       constexpr int t = decltype(which)::value;
+      auto read_value = [&](int u) __attribute__((always_inline)) { piece[u % AHEAD] = vu[(4 * (u % ND) + 2 * t + u / ND) * kWave]; };
       if (masks) {
 #pragma unroll
         for (int x = 0; x < CT; ++x) {
@@ -575,7 +654,8 @@ __global__ __launch_bounds__((TileForm<DT, DC>::W) * kWave, 1) void k_chunk_tile
 #pragma unroll
       for (int u = 0; u < STEPS; ++u) {
         score_step(std::integral_constant<int, 1 - t>{}, u);
-        vf[u] = vu[(4 * (u % ND) + 2 * t + u / ND) * kWave];         // (in the registers of the key's piece)
+        if (u + AHEAD < STEPS) read_key(keys_now, std::integral_constant<int, 1 - t>{}, u + AHEAD);
+        else read_value(u + AHEAD - STEPS);
         exponentials(u * EARLY / STEPS, (u + 1) * EARLY / STEPS);
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -585,8 +665,9 @@ __global__ __launch_bounds__((TileForm<DT, DC>::W) * kWave, 1) void k_chunk_tile
 #pragma unroll
         for (int k = NP - 1; k >= 0; --k)
 #pragma unroll
-          for (int x = 0; x < CT; ++x) acc[x][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[u], pr[x][k][j], acc[x][c], 0, 0, 0);
-        read_key(ku, std::integral_constant<int, t>{}, u);
+          for (int x = 0; x < CT; ++x) acc[x][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(piece[u % AHEAD], pr[x][k][j], acc[x][c], 0, 0, 0);
+        if (u + AHEAD < STEPS) read_value(u + AHEAD);
+        else read_key(keys_then, std::integral_constant<int, t>{}, u + AHEAD - STEPS);
         if (FOLD && c == ND - 1) {
 #pragma unroll
           for (int k = NP - 1; k >= 0; --k)
@@ -598,25 +679,29 @@ __global__ __launch_bounds__((TileForm<DT, DC>::W) * kWave, 1) void k_chunk_tile
         if constexpr (t == 0) {
 #pragma unroll
           for (int n = 0; n < 2 * KP; ++n)
-            if (n * STEPS / (2 * KP) == u) put_key(odd, n / 2, n % 2);
+            if (n * STEPS / (2 * KP) == u) put_key(after, n / 2, n % 2);
         } else {
 #pragma unroll
-          for (int n = 0; n < 4 * VP; ++n)
-            if (n * STEPS / (4 * VP) == u) put_value(1 - odd, n / 4, n % 4);
+          for (int n = 0; n < 2 * VP; ++n)
+            if (n * STEPS / (2 * VP) == u) put_value(1 - odd, n / 2, n % 2);
         }
         __builtin_amdgcn_sched_barrier(0);
       }
     };
-    const bf8* ku = kl + (size_t)(1 - odd) * KU * kWave + lane;       // (what is read ahead is the next block's: half t beside half t's values)
-    half(std::integral_constant<int, 0>{}, ku);
+    const bf8 *keys_now = kl + now * KU * kWave + lane, *keys_next = kl + next * KU * kWave + lane;
+    half(std::integral_constant<int, 0>{}, keys_now, keys_next);
     ak_at[0] = ak_at[1];
     th_at[0] = th_at[1];
     ak_at[1] = ak;
     th_at[1] = there_k;
     fetch_keys(i + 3);
-    half(std::integral_constant<int, 1>{}, ku);
+    half(std::integral_constant<int, 1>{}, keys_next, keys_next);
     av_now = av;
     fetch_values(i + 2);
+    const unsigned free = now;
+    now = next;
+    next = after;
+    after = free;
     __syncthreads();
   }
 
@@ -625,7 +710,7 @@ __global__ __launch_bounds__((TileForm<DT, DC>::W) * kWave, 1) void k_chunk_tile
   for (int x = 0; x < CT; ++x) {
     const float l = FOLD ? fmaf(sum[x][0], inverse, total[x]) : across32_f(total[x], fadd2);
     if (!stored[x]) continue;
-    if (p.splits == 1) {
+    if (whole_tile) {
       const bool whole = vec & 2;
       T* to = static_cast<T*>(p.out) + (size_t)at[x].x * p.ldo + (size_t)at[x].y * d;
 #pragma unroll
@@ -646,7 +731,7 @@ __global__ __launch_bounds__((TileForm<DT, DC>::W) * kWave, 1) void k_chunk_tile
           }
         }
     } else {
-      float* to = p.part + (((size_t)at[x].x * p.heads + at[x].y) * p.splits + split) * (dv + 4);
+      float* to = p.part + (((size_t)me * 2 + (segment > 0 ? 1 : 0)) * Form::kRowsOfWg + (wave * CT + x) * 32 + col) * (dv + 4);
 #pragma unroll
       for (int t = 0; t < ND; ++t)
 #pragma unroll
@@ -660,11 +745,12 @@ __global__ __launch_bounds__((TileForm<DT, DC>::W) * kWave, 1) void k_chunk_tile
       }
     }
   }
+  }
 }
 
 // The parts of split sequences: a wave per (token, head).
 template <int DT>
-__global__ __launch_bounds__(256) void k_chunk_join(const ChunkParams p, unsigned tile_rows) {
+__global__ __launch_bounds__(256) void k_chunk_join(const ChunkParams p) {
   using T = typename Elem<DT>::T;
   const unsigned lane = threadIdx.x % kWave, dv = kv_dv(p.d), pitch = dv + 4, per = p.heads / p.kv_heads;
   const unsigned rows = (unsigned)(blockIdx.x * (256 / kWave) + threadIdx.x / kWave), t = rows / p.heads, h = rows % p.heads;
@@ -677,7 +763,7 @@ __global__ __launch_bounds__(256) void k_chunk_join(const ChunkParams p, unsigne
   Tile tile{b, f, e - f, 0, 0, 0};
   const int len = p.lens[b];
   tile.len = len < 0 ? 0u : min((unsigned)len, p.max_len);
-  const unsigned row = (t - f) * per + h % per, last = min(row / tile_rows * tile_rows + tile_rows, tile.n * per) - 1;
+  const unsigned row = (t - f) * per + h % per, last = min(row / kRows * kRows + kRows, tile.n * per) - 1;
   const unsigned tokens = p.run * kKvBlock, runs = max(1u, (seen_by(p, tile, last / per) + tokens - 1) / tokens);
   const float* part = p.part + ((size_t)t * p.heads + h) * p.splits * pitch;
   float m = -INFINITY;
@@ -697,67 +783,105 @@ __global__ __launch_bounds__(256) void k_chunk_join(const ChunkParams p, unsigne
       static_cast<T*>(p.out)[(size_t)t * p.ldo + (size_t)h * p.d + lane + 64 * j] = (T)(l == 0.f ? 0.f : __fdiv_rn(x[j], l));
 }
 
+// The same of the form for many rows: a workgroup for 32 rows of a tile and a kv head, eight threads a row.
+template <int DT, unsigned ROWS>
+__global__ __launch_bounds__(256) void k_chunk_join_tiles(const ChunkParams p, unsigned groups) {
+  using T = typename Elem<DT>::T;
+  const unsigned chunk = blockIdx.x % (ROWS / 32), kvh = blockIdx.x / (ROWS / 32) % p.kv_heads, slot = blockIdx.x / (ROWS / 32 * p.kv_heads);
+  const unsigned dv = kv_dv(p.d), pitch = dv + 4, per = p.heads / p.kv_heads;
+  const unsigned long long share = share_of(p, groups), base = (unsigned long long)p.plan[p.slots] * kvh;
+  const unsigned long long from = base + p.plan[slot], to = base + p.plan[slot + 1];
+  if (from == to) return;                                  // (no such tile)
+  const unsigned g0 = (unsigned)(from / share), g1 = (unsigned)((to - 1) / share);
+  if (g0 == g1) return;                                    // (one workgroup had all of it)
+  const Tile tile = find_tile<ROWS>(p, slot, per);
+  const unsigned r = chunk * 32 + threadIdx.x / 8, j0 = threadIdx.x % 8;
+  if (tile.b < 0 || r >= tile.rows) return;
+  // a workgroup's first part; of the first workgroup its last, if it had other tiles before
+  auto run = [&](unsigned g) { return p.part + (((size_t)g * 2 + (g == g0 && from % share != 0 ? 1 : 0)) * ROWS + r) * pitch; };
+  float m = -INFINITY, l = 0.f;
+  for (unsigned g = g0; g <= g1; ++g) m = fmaxf(m, run(g)[dv]);
+  const float top = finite_or_0(m);
+  v4f x[8] = {};
+  for (unsigned g = g0; g <= g1; ++g) {
+    const float* at = run(g);
+    const float w = __builtin_amdgcn_exp2f(at[dv] - top);
+    l = fmaf(w, at[dv + 1], l);
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (4 * (j0 + 8 * j) < dv) x[j] += w * *reinterpret_cast<const v4f*>(at + 4 * (j0 + 8 * j));
+  }
+  const unsigned i = tile.row0 + r;
+  T* dst = static_cast<T*>(p.out) + (size_t)(tile.first + i / per) * p.ldo + (size_t)(kvh * per + i % per) * p.d;
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (4 * (j0 + 8 * j) + k < p.d) dst[4 * (j0 + 8 * j) + k] = (T)(l == 0.f ? 0.f : __fdiv_rn(x[j][k], l));
+}
+
 struct Split {
-  unsigned run, splits, waves, tile_rows;
+  unsigned run, splits, waves, tile_rows, groups;          // groups: workgroups of the form for many rows
   bool tiles;
   size_t slots;
 };
-// rows of a workgroup of the form for many rows
-unsigned tile_rows(int dtype, size_t d) { return (dtype == MQ_BF16 && d <= 128) || (dtype == MQ_F16 && d <= 64) ? 256 : 128; }
 constexpr size_t kManyRows = 96;      // rows of a sequence on average from which on they share blocks through LDS
 Split split_of(int dtype, size_t B, size_t T, size_t max_len, int heads, int kv_heads, size_t d) {
   const size_t per = (size_t)(heads / kv_heads), blocks = (max_len + kKvBlock - 1) / kKvBlock;
   Split s{};
   // binary32 queries of wide heads do not fit beside the sums
   s.tiles = T * per / B >= kManyRows && !(dtype == MQ_F32 && d > 128);
-  s.tile_rows = s.tiles ? tile_rows(dtype, d) : kRows;
-  s.slots = T * per / s.tile_rows + B;
-  const size_t wgs = s.slots * (size_t)kv_heads;
   if (s.tiles) {
-    const size_t want = (1024 + wgs - 1) / wgs;
-    size_t run = (blocks + want - 1) / want;
-    if (run < 32) run = 32;
-    s.run = (unsigned)run;
-    s.splits = (unsigned)((blocks + run - 1) / run);
-    s.waves = kWaves;
+    const bool wide = (dtype == MQ_BF16 && d <= 128) || (d <= 64 && dtype == MQ_F16);
+    s.tile_rows = wide ? 256 : 128;
+    s.groups = wide ? 256 : 512;      // one workgroup of eight waves to a compute unit, or two of four
+    s.slots = T * per / s.tile_rows + B;
     return s;
   }
-  const size_t want = (512 + wgs - 1) / wgs;
-  if (blocks <= 2 * kWaves) {
-    s.run = (unsigned)blocks;
-    s.splits = 1;
-    s.waves = (unsigned)(blocks < kWaves ? blocks : kWaves);
-    return s;
-  }
-  size_t run = (blocks + want - 1) / want;
-  if (run < (size_t)kWaves) run = kWaves;
+  s.tile_rows = kRows;
+  s.slots = T * per / s.tile_rows + B;
+  const size_t wgs = s.slots * (size_t)kv_heads, want = (512 + wgs - 1) / wgs;
+  size_t run = blocks <= 2 * kWaves ? blocks : (blocks + want - 1) / want;
+  if (blocks > 2 * kWaves && run < (size_t)kWaves) run = kWaves;
   s.run = (unsigned)run;
   s.splits = (unsigned)((blocks + run - 1) / run);
-  s.waves = kWaves;
+  s.waves = (unsigned)(blocks < kWaves ? blocks : kWaves);
   return s;
+}
+// Floats of the parts, in front of the plan.
+size_t part_floats(const Split& s, size_t T, int heads, size_t d) {
+  const size_t pitch = kv_dv((unsigned)d) + 4;
+  if (s.tiles) return (size_t)s.groups * 2 * s.tile_rows * pitch;
+  return s.splits == 1 ? 4 : T * (size_t)heads * s.splits * pitch;
 }
 
 }  // namespace
 
 size_t chunk_attention_ws_bytes(size_t B, size_t T, size_t max_len, int heads, int kv_heads, size_t d) {
-  unsigned splits = 1;                // (whatever the type)
+  size_t most = 0;                    // (whatever the type)
   for (int dtype : {MQ_F32, MQ_F16, MQ_BF16}) {
-    const unsigned n = split_of(dtype, B, T, max_len, heads, kv_heads, d).splits;
-    splits = n > splits ? n : splits;
+    const Split s = split_of(dtype, B, T, max_len, heads, kv_heads, d);
+    const size_t n = part_floats(s, T, heads, d) + (s.tiles ? s.slots + 1 : 0);
+    most = n > most ? n : most;
   }
-  return splits == 1 ? 16 : T * (size_t)heads * splits * (kv_dv((unsigned)d) + 4) * sizeof(float);
+  return most * sizeof(float);
 }
 
 int launch_chunk_attention(const mq_kv_cache& cache, const int32_t* table, size_t table_width, const int32_t* first,
                            const int32_t* lens, size_t B, size_t T, size_t max_len, int causal, const void* q, size_t ldq,
                            int heads, int dtype, float scale, void* out, size_t ldo, void* ws, hipStream_t s) {
   const Split split = split_of(dtype, B, T, max_len, heads, cache.kv_heads, cache.head_dim);
-  const size_t wgs = split.slots * (size_t)cache.kv_heads * split.splits;
+  const size_t wgs = split.slots * (size_t)cache.kv_heads * (split.tiles ? 1 : split.splits);
   const size_t joins = (T * (size_t)heads + 3) / 4;
-  if (!launchable(wgs, 2 * kWaves * kWave) || (split.splits > 1 && !launchable(joins, 256))) return MQ_ERR_SHAPE;
-  const ChunkParams p{cache.keys, cache.values, cache.amax, table, first, lens, q, out, static_cast<float*>(ws), ldq, ldo,
+  // (blocks of all tiles are counted in 32 bits)
+  if (!launchable(wgs, 2 * kWaves * kWave) || (split.splits > 1 && !launchable(joins, 256)) ||
+      (split.tiles && !launchable(wgs * (split.tile_rows / 32), 256)) || (split.tiles && split.slots > (((size_t)1 << 32) - 1) / ((max_len + kKvBlock - 1) / kKvBlock)))
+    return MQ_ERR_SHAPE;
+  float* part = static_cast<float*>(ws);
+  const ChunkParams p{cache.keys, cache.values, cache.amax, table, first, lens, q, out, part, ldq, ldo,
                       table_width, cache.blocks, (unsigned)B, (unsigned)T, (unsigned)max_len, (unsigned)cache.kv_heads,
-                      (unsigned)heads, (unsigned)cache.head_dim, split.splits, split.run, scale * 1.44269504088896340736f, causal};
+                      (unsigned)heads, (unsigned)cache.head_dim, split.splits, split.run, scale * 1.44269504088896340736f, causal,
+                      reinterpret_cast<unsigned*>(part + part_floats(split, T, heads, cache.head_dim)), (unsigned)split.slots};
   const size_t piece = 16 / elem_bytes(dtype);
   // whole 16-byte pieces of queries, four neighbouring results at once
   const int vec = (cache.head_dim % piece == 0 && ldq % piece == 0 && reinterpret_cast<uintptr_t>(q) % 16 == 0 ? 1 : 0) |
@@ -770,15 +894,19 @@ int launch_chunk_attention(const mq_kv_cache& cache, const int32_t* table, size_
       if (split.tiles) {
         if constexpr (!(DT == MQ_F32 && DC > 2)) {
           using Form = TileForm<DT, DC>;
+          constexpr unsigned ROWS = Form::kRowsOfWg;
           auto kern = k_chunk_tiles<DT, DC>;
           if (Form::kLds > 65536)
             rc = check_hip(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)Form::kLds));
           if (rc != MQ_OK) return;
-          hipLaunchKernelGGL(kern, dim3((unsigned)wgs), dim3(Form::W * kWave), Form::kLds, s, p, vec);
+          hipLaunchKernelGGL(k_chunk_plan<ROWS>, dim3(1), dim3(kPlan), 0, s, p);
+          hipLaunchKernelGGL(kern, dim3(split.groups), dim3(Form::W * kWave), Form::kLds, s, p, vec);
+          hipLaunchKernelGGL((k_chunk_join_tiles<DT, ROWS>), dim3((unsigned)(wgs * (ROWS / 32))), dim3(256), 0, s, p, split.groups);
         }
       } else {
         const size_t ql = kParts<DT> * DC * 4 * kWave * 16, sums = kRows * (DC * 64 + 1) * sizeof(float);
         hipLaunchKernelGGL((k_chunk_attention<DT, DC>), dim3((unsigned)wgs), dim3(split.waves * kWave), ql > sums ? ql : sums, s, p);
+        if (split.splits > 1) hipLaunchKernelGGL(k_chunk_join<DT>, dim3((unsigned)joins), dim3(256), 0, s, p);
       }
       rc = check_hip(hipGetLastError());
     };
@@ -788,9 +916,7 @@ int launch_chunk_attention(const mq_kv_cache& cache, const int32_t* table, size_
       case 3: sized(std::integral_constant<int, 3>{}); break;
       default: sized(std::integral_constant<int, 4>{}); break;
     }
-    if (rc != MQ_OK || split.splits == 1) return rc;
-    hipLaunchKernelGGL(k_chunk_join<DT>, dim3((unsigned)joins), dim3(256), 0, s, p, split.tile_rows);
-    return check_hip(hipGetLastError());
+    return rc;
   });
 }
 
