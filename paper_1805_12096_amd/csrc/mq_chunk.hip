@@ -78,8 +78,9 @@ __device__ __forceinline__ unsigned seen_by(const ChunkParams& p, const Tile& t,
   return s < 0 ? 0u : (unsigned)s;
 }
 
+// (two waves a SIMD where 256 registers do: the compiler then leaves accumulation registers alone, and copies to and from them)
 template <int DT, int DC>             // DC: 64-column pieces of a key
-__global__ __launch_bounds__(kWaves * kWave) void k_chunk_attention(const ChunkParams p) {
+__global__ __launch_bounds__(kWaves * kWave, DC == 4 ? 1 : 2) void k_chunk_attention(const ChunkParams p) {
   using T = typename Elem<DT>::T;
   constexpr int NP = kParts<DT>;
   constexpr int NK = 2 * DC, ND = 2 * DC;      // 32-column pieces of a key, 32-column pieces of a value at most
@@ -288,12 +289,21 @@ __global__ __launch_bounds__(kWaves * kWave) void k_chunk_attention(const ChunkP
 // Lengths are known on the device only, so a first small launch sums up the blocks that each tile of rows sees.  The workgroups,
 // as many as run at once, share the blocks of all tiles and kv heads in one line equally: each has some tiles whole, and parts of
 // the tiles at its two ends, which go to the workspace and are joined.
-// The scale of a block's values goes into the exponent (for binary32, whose 24 bits the logarithm would cost some, into a
-// product), and the probabilities are summed by a product with ones, so that what is divided by is the sum of what is multiplied.
+// The scale of a block's values goes into the exponent (for binary32, whose 24 bits the logarithm would cost some, into a product).
 
 // Sums of matrix instructions times a factor, from accumulation registers and back.  (The compiler would otherwise take the
 // copies that the vector unit needs out of the branch, into every step.)
+// sum + a + b, as rounded: what is divided by then is the sum of what is multiplied.
+__device__ __forceinline__ float add2(__bf16 a, __bf16 b, float sum) {
+  typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+  return __builtin_amdgcn_fdot2_f32_bf16(b2{a, b}, b2{(__bf16)1.f, (__bf16)1.f}, sum, false);
+}
+template <bool VECTOR>
 __device__ __forceinline__ void scale_sums(v16f& o, float factor) {
+  if constexpr (VECTOR) {
+    o *= factor;
+    return;
+  }
   asm volatile("" : "+a"(o));
   o *= factor;
   asm volatile("" : "+a"(o));
@@ -572,9 +582,7 @@ __global__ __launch_bounds__((TileForm<DT, DC>::W) * kWave, 1) void k_chunk_tile
   }
   unsigned now = 0, next = 1, after = 2;       // places of the keys of blocks i, i + 1, i + 2
   constexpr bool FOLD = Form::kFold;
-  const u4 one = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
-  const bf8 ones = __builtin_bit_cast(bf8, one);
-  v16f sum[CT] = {};                           // of a half block's probabilities times the values' scale, in every register
+  float sum[CT] = {};                          // of a half block's probabilities times the values' scale, of this lane's tokens
   float inverse = 0.f;                         // of that scale
   for (unsigned i = 0; i < count; ++i) {
     const unsigned pg = start + i, odd = i % 2;
@@ -608,7 +616,10 @@ __global__ __launch_bounds__((TileForm<DT, DC>::W) * kWave, 1) void k_chunk_tile
       }
       if constexpr (FOLD) {
 #pragma unroll
-        for (int x = 0; x < CT; ++x) total[x] = fmaf(sum[x][0], inverse, total[x]);
+        for (int x = 0; x < CT; ++x) {
+          total[x] = fmaf(sum[x], inverse, total[x]);
+          sum[x] = 0.f;
+        }
         inverse = inverse_now;
       }
       float base[CT], mt[CT];
@@ -630,7 +641,7 @@ __global__ __launch_bounds__((TileForm<DT, DC>::W) * kWave, 1) void k_chunk_tile
           ref[x] = top;
           total[x] *= keep;
 #pragma unroll
-          for (int c = 0; c < ND; ++c) scale_sums(acc[x][c], keep);
+          for (int c = 0; c < ND; ++c) scale_sums<Form::W == 8>(acc[x][c], keep);
         }
       }
 #pragma unroll
@@ -647,7 +658,10 @@ __global__ __launch_bounds__((TileForm<DT, DC>::W) * kWave, 1) void k_chunk_tile
             __bf16 b[NP];
             split_bf16<NP>(FOLD ? e : e * fv, b);
 #pragma unroll
-            for (int k = 0; k < NP; ++k) pr[x][k][n / 8][n % 8] = b[k];
+            for (int k = 0; k < NP; ++k) {
+              pr[x][k][n / 8][n % 8] = b[k];
+              if (FOLD && n % 2 == 1) sum[x] = add2(pr[x][k][n / 8][n % 8 - 1], b[k], sum[x]);
+            }
           }
       };
       constexpr int EARLY = 12;                // (the others beside the first half of the sums of values)
@@ -668,13 +682,6 @@ __global__ __launch_bounds__((TileForm<DT, DC>::W) * kWave, 1) void k_chunk_tile
           for (int x = 0; x < CT; ++x) acc[x][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(piece[u % AHEAD], pr[x][k][j], acc[x][c], 0, 0, 0);
         if (u + AHEAD < STEPS) read_value(u + AHEAD);
         else read_key(keys_then, std::integral_constant<int, t>{}, u + AHEAD - STEPS);
-        if (FOLD && c == ND - 1) {
-#pragma unroll
-          for (int k = NP - 1; k >= 0; --k)
-#pragma unroll
-            for (int x = 0; x < CT; ++x)
-              sum[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ones, pr[x][k][j], j == 0 && k == NP - 1 ? v16f{} : sum[x], 0, 0, 0);
-        }
         if (j == 0) exponentials(EARLY + c * (16 - EARLY) / ND, EARLY + (c + 1) * (16 - EARLY) / ND);
         if constexpr (t == 0) {
 #pragma unroll
@@ -708,7 +715,7 @@ __global__ __launch_bounds__((TileForm<DT, DC>::W) * kWave, 1) void k_chunk_tile
   // every lane has four neighbouring columns of its row at a time
 #pragma unroll
   for (int x = 0; x < CT; ++x) {
-    const float l = FOLD ? fmaf(sum[x][0], inverse, total[x]) : across32_f(total[x], fadd2);
+    const float l = across32_f(FOLD ? fmaf(sum[x], inverse, total[x]) : total[x], fadd2);
     if (!stored[x]) continue;
     if (whole_tile) {
       const bool whole = vec & 2;
