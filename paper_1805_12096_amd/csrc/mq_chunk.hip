@@ -17,8 +17,8 @@ namespace mq {
 
 namespace {
 
-constexpr int kRows = 32;             // query rows of a tile
-constexpr int kWaves = 4;             // of a workgroup, at most
+constexpr unsigned kRows = 32;        // query rows of a tile where there are few
+constexpr unsigned kWaves = 4;        // of a workgroup of that form, at most
 // How far (as a power of two) a row's scores may rise over the reference that its sums are relative to before they are
 // rescaled: exponentials up to 2^8 lose nothing in a binary format, and a maximum that rises a little does not cost anything.
 constexpr float kSlack = 8.f;
@@ -29,13 +29,13 @@ struct ChunkParams {
   const int32_t *table, *first, *lens;
   const void* q;
   void* out;
-  float* part;                        // [T][heads][splits][dv + 4]: sums, reference, total; splits runs of `run` blocks
+  float* part;                        // [workgroups][2][rows of a tile][dv + 4]: sums, reference, total
   size_t ldq, ldo, table_width, blocks;
-  unsigned B, T, max_len, kv_heads, heads, d, splits, run;
+  unsigned B, T, max_len, kv_heads, heads, d;
   float scale2;                       // scale log2(e)
   int causal;
-  unsigned* plan;                     // many rows: [slots + 1] blocks of the tiles in front of each tile
-  unsigned slots;
+  unsigned* plan;                     // [slots + 1] blocks of the tiles in front of each tile
+  unsigned slots;                     // tiles at most
 };
 
 // Exponent of the power of two taken off a row whose largest magnitude is m.
@@ -50,6 +50,12 @@ __device__ __forceinline__ unsigned again(unsigned x) {
 __device__ __forceinline__ float finite_or_0(float m) { return m == -INFINITY ? 0.f : m; }
 __device__ __forceinline__ float fmax2(float a, float b) { return fmaxf(a, b); }
 __device__ __forceinline__ float fadd2(float a, float b) { return a + b; }
+
+// sum + a + b, as rounded: what is divided by then is the sum of what is multiplied.
+__device__ __forceinline__ float add2(__bf16 a, __bf16 b, float sum) {
+  typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+  return __builtin_amdgcn_fdot2_f32_bf16(b2{a, b}, b2{(__bf16)1.f, (__bf16)1.f}, sum, false);
+}
 
 // A tile of query rows: row i of its sequence's n x per is token i / per, head i % per of the group.
 struct Tile {
@@ -78,245 +84,12 @@ __device__ __forceinline__ unsigned seen_by(const ChunkParams& p, const Tile& t,
   return s < 0 ? 0u : (unsigned)s;
 }
 
-// (two waves a SIMD where 256 registers do: the compiler then leaves accumulation registers alone, and copies to and from them)
-template <int DT, int DC>             // DC: 64-column pieces of a key
-__global__ __launch_bounds__(kWaves * kWave, DC == 4 ? 1 : 2) void k_chunk_attention(const ChunkParams p) {
-  using T = typename Elem<DT>::T;
-  constexpr int NP = kParts<DT>;
-  constexpr int NK = 2 * DC, ND = 2 * DC;      // 32-column pieces of a key, 32-column pieces of a value at most
-  extern __shared__ __attribute__((aligned(16))) char smem[];
-  bf8* const ql = reinterpret_cast<bf8*>(smem);                                  // [NP][NK][2][64 lanes]
-  float* const sums = reinterpret_cast<float*>(smem);                            // [32][ND 32 + 1], afterwards
-  __shared__ float fac[kRows], stat[2][kWaves][kRows];
-  const unsigned lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), waves = blockDim.x / kWave;
-  const unsigned col = lane % 32, grp = lane / 32;
-  const unsigned split = blockIdx.x % p.splits, kvh = blockIdx.x / p.splits % p.kv_heads, slot = blockIdx.x / (p.splits * p.kv_heads);
-  const unsigned per = p.heads / p.kv_heads, d = p.d, dk = kv_dk(d), dv = kv_dv(d);
-  const Tile tile = find_tile<kRows>(p, slot, per);
-  if (tile.b < 0) return;
-  auto row_at = [&](unsigned r) {              // element offset of row r's queries in q, without the row pitch: token, head
-    const unsigned i = tile.row0 + r;
-    return make_uint2(tile.first + i / per, kvh * per + i % per);
-  };
-  const unsigned last = tile.row0 + tile.rows - 1;
-  const unsigned most = seen_by(p, tile, last / per), least = seen_by(p, tile, tile.row0 / per);
-  const unsigned mine_sees = seen_by(p, tile, min(tile.row0 + col, last) / per);
-  const unsigned nblocks = (most + kKvBlock - 1) / kKvBlock;
-  const unsigned start = split * p.run, end = min(start + p.run, nblocks);
-  if (split > 0 && start >= nblocks) return;   // (the first run answers for rows that see nothing)
-
-  // queries: a power of two off each row, so that its largest element is 1 .. 2, then parts in operand order
-  {
-    const unsigned j0 = threadIdx.x % 8, step = blockDim.x / 8;
-    for (unsigned rr = threadIdx.x / 8; rr < kRows; rr += step) {
-      float m = 0.f;
-      if (rr < tile.rows) {
-        const uint2 at = row_at(rr);
-        const T* src = static_cast<const T*>(p.q) + (size_t)at.x * p.ldq + (size_t)at.y * d;
-        for (unsigned j = j0; j < d; j += 8) {
-          const float x = fabsf((float)src[j]);
-          m = x <= 3.402823466e38f ? fmaxf(m, x) : INFINITY;
-          if (m == INFINITY) break;
-        }
-      }
-#pragma unroll
-      for (int off = 4; off >= 1; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, 8));
-      if (j0 == 0) fac[rr] = m;
-    }
-    __syncthreads();
-    for (unsigned u = threadIdx.x; u < NK * 2 * kWave; u += blockDim.x) {
-      const unsigned l = u % kWave, c = u / (2 * kWave), s = u / kWave % 2, rr = l % 32, k = 32 * c + 16 * (l / 32) + 8 * s;
-      const float m = fac[rr];
-      const int e = row_exponent(m);
-      const float mul = __uint_as_float((unsigned)(127 - e) << 23);          // 2^-e
-      bf8 part[NP];
-      const uint2 at = row_at(rr < tile.rows ? rr : 0);
-      const T* src = static_cast<const T*>(p.q) + (size_t)at.x * p.ldq + (size_t)at.y * d;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        float x = rr < tile.rows && k + j < d ? (float)src[k + j] : 0.f;
-        x = m == INFINITY ? NAN : x * mul;                                    // a row with a NaN or an infinity gives NaN
-        __bf16 v[NP];
-        split_bf16<NP>(x, v);
-#pragma unroll
-        for (int i = 0; i < NP; ++i) part[i][j] = v[i];
-      }
-#pragma unroll
-      for (int i = 0; i < NP; ++i) ql[(i * NK * 2 + c * 2 + s) * kWave + l] = part[i];
-    }
-    __syncthreads();
-  }
-  float qscale;
-  {
-    qscale = ldexpf(p.scale2, row_exponent(fac[col]));
-  }
-
-  float acc_top = -INFINITY, total = 0.f;      // of row l % 32; the total of this lane's tokens
-  v16f acc[ND] = {};
-  const int32_t* table = p.table + (size_t)tile.b * p.table_width;
-  for (unsigned pg = start + wave; pg < end; pg += waves) {
-    const int id = pg < p.table_width ? table[pg] : -1;
-    const int block = __builtin_amdgcn_readfirstlane(id);
-    const bool there = block >= 0 && (size_t)block < p.blocks;
-    if (!there) continue;
-    const size_t at = (size_t)block * p.kv_heads + kvh;
-    const float2 am = reinterpret_cast<const float2*>(p.amax)[at];
-    const int8_t* kp = p.keys + at * kKvBlock * dk + (size_t)col * dk + grp * 16;
-    const int8_t* vp = p.values + at * dv * kKvBlock + grp * 16;
-    u4 kf[2][NK], vf[ND][2];
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int c = 0; c < NK; ++c) kf[t][c] = *reinterpret_cast<const u4*>(kp + (size_t)t * 32 * dk + c * 32);
-#pragma unroll
-    for (int t = 0; t < ND; ++t)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) vf[t][h] = *reinterpret_cast<const u4*>(vp + (size_t)min(32 * t + col, dv - 1) * kKvBlock + 32 * h);
-    v16f sc[2] = {};
-#pragma unroll
-    for (int c = 0; c < NK; ++c)
-#pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        bf8 a[2];
-#pragma unroll
-        for (int t = 0; t < 2; ++t) a[t] = bf16_of_bytes(kf[t][c][2 * s], kf[t][c][2 * s + 1]);
-#pragma unroll
-        for (int i = NP - 1; i >= 0; --i) {
-          const bf8 b = ql[(i * NK * 2 + c * 2 + s) * kWave + lane];
-#pragma unroll
-          for (int t = 0; t < 2; ++t) sc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[t], b, sc[t], 0, 0, 0);
-        }
-      }
-    const float f = qscale * (am.x * (1.f / 127.f));
-    float mt = -INFINITY;
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) sc[t][r] *= f;
-    if ((pg + 1) * kKvBlock > least)
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (pg * kKvBlock + 32 * t + 8 * (r / 4) + 4 * grp + r % 4 >= mine_sees) sc[t][r] = -INFINITY;
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int r = 0; r < 16; r += 2) mt = max3(mt, sc[t][r], sc[t][r + 1]);
-    mt = across32_f(mt, fmax2);
-    if (__any(mt > acc_top + kSlack)) {
-      // (only for the rows concerned: no other row's result depends on theirs)
-      const float now = mt > acc_top + kSlack ? mt : acc_top, keep = now == acc_top ? 1.f : __builtin_amdgcn_exp2f(acc_top - now);
-      acc_top = now;
-      total *= keep;
-#pragma unroll
-      for (int t = 0; t < ND; ++t)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) acc[t][r] *= keep;
-    }
-    const float base = finite_or_0(acc_top);
-    const float fv = am.y * (1.f / 127.f);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      bf8 pr[NP];
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const float e = __builtin_amdgcn_exp2f(sc[j / 2][8 * (j % 2) + k] - base);
-        total += e;
-        __bf16 v[NP];
-        split_bf16<NP>(e * fv, v);
-#pragma unroll
-        for (int i = 0; i < NP; ++i) pr[i][k] = v[i];
-      }
-#pragma unroll
-      for (int t = 0; t < ND; ++t) {
-        const bf8 a = bf16_of_bytes(vf[t][0][j], vf[t][1][j]);
-#pragma unroll
-        for (int i = NP - 1; i >= 0; --i) acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, pr[i], acc[t], 0, 0, 0);
-      }
-    }
-  }
-  total = across32_f(total, fadd2);
-
-  // the waves, one after the other
-  if (grp == 0) {
-    stat[0][wave][col] = acc_top;
-    stat[1][wave][col] = total;
-  }
-  __syncthreads();                             // (and nobody reads queries any more)
-  float m = -INFINITY;
-  for (unsigned w = 0; w < waves; ++w) m = fmaxf(m, stat[0][w][col]);
-  const float weight = __builtin_amdgcn_exp2f(acc_top - finite_or_0(m));
-  const unsigned pitch = ND * 32 + 1;
-  for (unsigned w = 0; w < waves; ++w) {
-    if (w == wave)
-#pragma unroll
-      for (int t = 0; t < ND; ++t)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          float& to = sums[col * pitch + 32 * t + 8 * (r / 4) + 4 * grp + r % 4];
-          const float x = acc[t][r] * weight;
-          to = w == 0 ? x : to + x;
-        }
-    __syncthreads();
-  }
-  for (unsigned i = threadIdx.x; i < tile.rows * dv; i += blockDim.x) {
-    const unsigned r = i / dv, c = i % dv;
-    float mm = -INFINITY, l = 0.f;
-    for (unsigned w = 0; w < waves; ++w) mm = fmaxf(mm, stat[0][w][r]);
-    for (unsigned w = 0; w < waves; ++w) l = fmaf(__builtin_amdgcn_exp2f(stat[0][w][r] - finite_or_0(mm)), stat[1][w][r], l);
-    const float x = sums[r * pitch + c];
-    const uint2 at = row_at(r);
-    if (p.splits == 1) {
-      if (c < d) static_cast<T*>(p.out)[(size_t)at.x * p.ldo + (size_t)at.y * d + c] = (T)(l == 0.f ? 0.f : __fdiv_rn(x, l));
-    } else {
-      float* to = p.part + (((size_t)at.x * p.heads + at.y) * p.splits + split) * (dv + 4);
-      to[c] = x;
-      if (c == 0) {
-        to[dv] = mm;
-        to[dv + 1] = l;
-      }
-    }
-  }
-}
-
-// ---- many rows ----------------------------------------------------------------------------------------------------------
+// ---- equal shares ---------------------------------------------------------------------------------------------------------
 //
-// A workgroup's four waves have 32 CT rows each and go through the same blocks, which they bring into LDS together, converted to
-// bfloat16 once, in operand order.  Scores are 32 tokens ahead: their products stand beside the exponentials of the 32 tokens
-// before, and the conversions of blocks to come beside the products of the values.  One barrier a block; three places in
-// LDS for keys, since this block's and the next one's are read while those of the one after come, two for values.
 // Lengths are known on the device only, so a first small launch sums up the blocks that each tile of rows sees.  The workgroups,
 // as many as run at once, share the blocks of all tiles and kv heads in one line equally: each has some tiles whole, and parts of
-// the tiles at its two ends, which go to the workspace and are joined.
-// The scale of a block's values goes into the exponent (for binary32, whose 24 bits the logarithm would cost some, into a product).
-
-// Sums of matrix instructions times a factor, from accumulation registers and back.  (The compiler would otherwise take the
-// copies that the vector unit needs out of the branch, into every step.)
-// sum + a + b, as rounded: what is divided by then is the sum of what is multiplied.
-__device__ __forceinline__ float add2(__bf16 a, __bf16 b, float sum) {
-  typedef __bf16 b2 __attribute__((ext_vector_type(2)));
-  return __builtin_amdgcn_fdot2_f32_bf16(b2{a, b}, b2{(__bf16)1.f, (__bf16)1.f}, sum, false);
-}
-template <bool VECTOR>
-__device__ __forceinline__ void scale_sums(v16f& o, float factor) {
-  if constexpr (VECTOR) {
-    o *= factor;
-    return;
-  }
-  asm volatile("" : "+a"(o));
-  o *= factor;
-  asm volatile("" : "+a"(o));
-}
-
-template <int DT, int DC>
-struct TileForm {
-  // two waves a SIMD where their registers fit
-  static constexpr int NP = kParts<DT>, CT = 1, W = NP * DC <= 2 ? 8 : 4, kRowsOfWg = W * 32 * CT;
-  static constexpr int kUnits = 8 * DC;                    // 1 KB pieces of a block's keys, and of its values
-  static constexpr size_t kLds = 5 * (size_t)kUnits * 1024;       // three blocks of keys, two of values
-  static constexpr bool kFold = NP < 3;
-};
+// the tiles at its two ends, which go to the workspace and are joined.  (Runs of equal length, a workgroup each, cost two thirds
+// more where lengths differ: the longest sequence decides how many there are of every one, and most workgroups find nothing.)
 
 constexpr int kPlan = 1024;           // threads of the workgroup that plans
 constexpr unsigned kLeast = 8;        // blocks that a workgroup takes at least
@@ -368,35 +141,343 @@ __device__ __forceinline__ unsigned long long share_of(const ChunkParams& p, uns
   return max((unsigned long long)kLeast, (all + groups - 1) / groups);
 }
 
+// A workgroup's next part of the line: blocks [start, end) of a tile and a kv head; whole: all that the tile has.
+struct LinePart {
+  unsigned kvh, slot, start, end;
+  bool whole;
+};
+__device__ __forceinline__ LinePart part_at(const ChunkParams& p, unsigned long long at, unsigned long long to) {
+  const unsigned line = p.plan[p.slots];
+  const unsigned kvh = __builtin_amdgcn_readfirstlane((unsigned)(at / line)), place = (unsigned)(at - (unsigned long long)kvh * line);
+  const unsigned slot = (unsigned)__builtin_amdgcn_readfirstlane(wave_search(p.slots, place, [&](unsigned i) { return p.plan[i]; }));
+  const unsigned first = p.plan[slot], blocks = p.plan[slot + 1] - first, start = place - first;
+  const unsigned end = (unsigned)min((unsigned long long)blocks, start + (to - at));
+  return {kvh, slot, start, end, start == 0 && end == blocks};
+}
+// Calls f(part, where a part that is not whole goes) for all parts of this workgroup.  An eighth of the line to each XCD, whose
+// workgroups then read the same heads' blocks.
+template <typename F>
+__device__ __forceinline__ void each_part(const ChunkParams& p, F f) {
+  const unsigned me = blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8;
+  const unsigned long long share = share_of(p, gridDim.x), all = (unsigned long long)p.plan[p.slots] * p.kv_heads;
+  const unsigned long long to = min((me + 1) * share, all);
+  for (unsigned long long at = me * share, n = 0; at < to; ++n) {
+    const LinePart part = part_at(p, at, to);
+    at += part.end - part.start;
+    f(part, me * 2 + (n > 0 ? 1 : 0));
+  }
+}
+
+// ---- few rows -------------------------------------------------------------------------------------------------------------
+//
+// A workgroup has 32 rows; its waves take the blocks in turn, each straight from memory, and join in LDS.
+
+template <int DT, int DC>             // DC: 64-column pieces of a key
+__device__ __forceinline__ void few_rows(const ChunkParams& p, int vec, const LinePart& part, unsigned to_part) {
+  using T = typename Elem<DT>::T;
+  constexpr int NP = kParts<DT>;
+  constexpr int NK = 2 * DC, ND = 2 * DC;      // 32-column pieces of a key, 32-column pieces of a value at most
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  bf8* const ql = reinterpret_cast<bf8*>(smem);                                  // [NP][NK][2][64 lanes]
+  float* const sums = reinterpret_cast<float*>(smem);                            // [32][ND 32 + 1], afterwards
+  __shared__ unsigned fac[kRows];               // largest magnitudes, as bits
+  __shared__ float stat[2][kWaves][kRows];
+  // (unknown to the compiler to be the same each time: it would keep dozens of places and masks from one part to the next)
+  unsigned lane = threadIdx.x % kWave, d = p.d;
+  asm volatile("" : "+v"(lane), "+s"(d));
+  const unsigned wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), waves = blockDim.x / kWave, col = lane % 32, grp = lane / 32;
+  const unsigned per = p.heads / p.kv_heads, dk = kv_dk(d), dv = kv_dv(d), kvh = part.kvh;
+  const Tile tile = find_tile<kRows>(p, part.slot, per);
+  if (tile.b < 0) return;
+  auto row_at = [&](unsigned r) {              // element offset of row r's queries in q, without the row pitch: token, head
+    const unsigned i = tile.row0 + r;
+    return make_uint2(tile.first + i / per, kvh * per + i % per);
+  };
+  const unsigned last = tile.row0 + tile.rows - 1;
+  const unsigned most = seen_by(p, tile, last / per), least = seen_by(p, tile, tile.row0 / per);
+  const unsigned mine_sees = seen_by(p, tile, min(tile.row0 + col, last) / per);
+  const unsigned start = part.start, end = min(part.end, (most + kKvBlock - 1) / kKvBlock);
+
+  // this wave's blocks, every waves-th of the run: which ones is looked up 64 at a time, keys and values are asked for as soon as
+  // the registers of those of the block before are free
+  const int32_t* table = p.table + (size_t)tile.b * p.table_width;
+  const unsigned mine = end > start + wave ? __builtin_amdgcn_readfirstlane((end - start - wave + waves - 1) / waves) : 0u;
+  auto look = [&](unsigned i) {
+    const size_t pg = start + wave + (size_t)(i + lane) * waves;
+    return table[pg < p.table_width ? pg : p.table_width - 1];
+  };
+  int ids = look(0);
+  bool there = true, there_next = true;
+  size_t at_next = 0;
+  float2 am_next;
+  u4 kf[2][NK], vf[ND][2];
+  auto find = [&](unsigned i) {
+    if (i % kWave == 0 && i > 0) ids = look(i);
+    const int block = __builtin_amdgcn_readlane(ids, i % kWave);
+    there_next = block >= 0 && (size_t)block < p.blocks;
+    at_next = (size_t)(there_next ? block : 0) * p.kv_heads + kvh;
+  };
+  auto bring_keys = [&] {
+    const int8_t* kp = p.keys + at_next * kKvBlock * dk + (size_t)col * dk + grp * 16;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int c = 0; c < NK; ++c) kf[t][c] = *reinterpret_cast<const u4*>(kp + (size_t)t * 32 * dk + c * 32);
+    am_next = reinterpret_cast<const float2*>(p.amax)[at_next];
+  };
+  auto bring_values = [&] {
+    const int8_t* vp = p.values + at_next * dv * kKvBlock + grp * 16;
+#pragma unroll
+    for (int t = 0; t < ND; ++t)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) vf[t][h] = *reinterpret_cast<const u4*>(vp + (size_t)min(32 * t + col, dv - 1) * kKvBlock + 32 * h);
+  };
+
+  // queries: a power of two off each row, so that its largest element is 1 .. 2, then parts in operand order.  A thread has U units
+  // of 8 elements: unit u of lane l is elements 32 (u / 2) + 16 (l / 32) + 8 (u % 2) .. of row l % 32
+  constexpr int U = NK * 2;
+  {
+    const unsigned rr = min(col, tile.rows - 1);
+    const uint2 at = row_at(rr);
+    const T* src = static_cast<const T*>(p.q) + (size_t)at.x * p.ldq + (size_t)at.y * d;
+    if (threadIdx.x < kRows) fac[threadIdx.x] = 0;
+    __syncthreads();
+    auto unit = [&](unsigned u, float (&x)[8]) {
+      const unsigned k = 32 * (u / 2) + 16 * grp + 8 * (u % 2);
+      if (vec & 1) {
+        constexpr int W = 16 / sizeof(T);
+        typedef T tw __attribute__((ext_vector_type(W)));
+#pragma unroll
+        for (int j = 0; j < 8; j += W) {
+          tw w = {};
+          if (k + j < d) w = *reinterpret_cast<const tw*>(src + k + j);
+#pragma unroll
+          for (int i = 0; i < W; ++i) x[j + i] = (float)w[i];
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = k + j < d ? (float)src[k + j] : 0.f;
+      }
+    };
+    float m = 0.f;
+    for (unsigned u = wave; u < U; u += waves) {
+      float x[8];
+      unit(u, x);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) m = fabsf(x[j]) <= 3.402823466e38f ? fmaxf(m, fabsf(x[j])) : INFINITY;
+    }
+    // (magnitudes are in the order of their bits; a maximum does not depend on the order)
+    atomicMax(&fac[col], __float_as_uint(across32_f(m, fmax2)));
+    __syncthreads();
+    const float most_of_row = __uint_as_float(fac[col]);
+    const float mul = __uint_as_float((unsigned)(127 - row_exponent(most_of_row)) << 23) * (p.scale2 < 0.f ? -1.f : 1.f);
+    for (unsigned u = wave; u < U; u += waves) {
+      float x[8];
+      unit(u, x);
+      bf8 part[NP];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        __bf16 b[NP];
+        split_bf16<NP>(most_of_row == INFINITY ? NAN : x[j] * mul, b);        // a row with a NaN or an infinity gives NaN
+#pragma unroll
+        for (int i = 0; i < NP; ++i) part[i][j] = b[i];
+      }
+#pragma unroll
+      for (int i = 0; i < NP; ++i) ql[(i * U + u) * kWave + lane] = part[i];
+    }
+  }
+  if (mine > 0) {
+    find(0);
+    bring_keys();
+    bring_values();
+  }
+  __syncthreads();
+  const float qscale = ldexpf(fabsf(p.scale2), row_exponent(__uint_as_float(fac[col]))) * (1.f / 127.f);
+
+  float acc_top = -INFINITY, total = 0.f;      // of row l % 32; the total of this lane's tokens
+  v16f acc[ND] = {};
+  constexpr bool FOLD = NP < 3;
+  for (unsigned i = 0; i < mine; ++i) {
+    const unsigned pg = start + wave + i * waves;
+    const float2 am = am_next;
+    there = there_next;
+    if (i + 1 < mine) find(i + 1);
+    v16f sc[2] = {};
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      bf8 a[2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) a[t] = bf16_of_bytes(kf[t][u / 2][2 * (u % 2)], kf[t][u / 2][2 * (u % 2) + 1]);
+#pragma unroll
+      for (int k = NP - 1; k >= 0; --k) {
+        const bf8 b = ql[(k * U + u) * kWave + lane];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) sc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[t], b, sc[t], 0, 0, 0);
+      }
+    }
+    if (i + 1 < mine) bring_keys();
+    if (!there || (pg + 1) * kKvBlock > least) {
+      const long long room = (long long)mine_sees - (long long)pg * kKvBlock - 4 * (int)grp;
+      const int limit = !there || room < 0 ? 0 : room > kKvBlock ? kKvBlock : (int)room;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (limit <= 32 * t + 8 * (r / 4) + r % 4) sc[t][r] = -INFINITY;
+    }
+    float f = there ? qscale * am.x : 0.f, mt = -INFINITY;
+    f = f == 0.f ? 1e-30f : f;                 // (0 times a masked score would be NaN; others are below 2^24)
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; r += 2) mt = max3(mt, sc[t][r], sc[t][r + 1]);
+    mt = across32_f(mt, fmax2) * f;
+    if (__any(mt > acc_top + kSlack)) {
+      // (only for the rows concerned: no other row's result depends on theirs)
+      const float now = mt > acc_top + kSlack ? mt : acc_top, keep = now == acc_top ? 1.f : __builtin_amdgcn_exp2f(acc_top - now);
+      acc_top = now;
+      total *= keep;
+#pragma unroll
+      for (int t = 0; t < ND; ++t) acc[t] *= keep;
+    }
+    // (where there is no block, block 0 was read, whose maxima may be anything)
+    const float fv = there ? am.y * (1.f / 127.f) : 0.f;
+    const bool nothing = !there || (FOLD && fv < 1.2e-38f);      // values that are all zero (or below any normal number)
+    const float lift = nothing || !FOLD ? 0.f : __builtin_amdgcn_logf(fv), base = lift - finite_or_0(acc_top);
+    if (FOLD && nothing) {
+#pragma unroll
+      for (int t = 0; t < ND; ++t) vf[t][0] = vf[t][1] = u4{};
+    }
+    float sum = 0.f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      bf8 pr[NP];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float e = __builtin_amdgcn_exp2f(fmaf(sc[j / 2][8 * (j % 2) + k], f, base));
+        if (!FOLD) sum += e;
+        __bf16 v[NP];
+        split_bf16<NP>(FOLD ? e : e * fv, v);
+#pragma unroll
+        for (int n = 0; n < NP; ++n) {
+          pr[n][k] = v[n];
+          if (FOLD && k % 2 == 1) sum = add2(pr[n][k - 1], v[n], sum);
+        }
+      }
+#pragma unroll
+      for (int t = 0; t < ND; ++t) {
+        const bf8 a = bf16_of_bytes(vf[t][0][j], vf[t][1][j]);
+#pragma unroll
+        for (int k = NP - 1; k >= 0; --k) acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, pr[k], acc[t], 0, 0, 0);
+      }
+    }
+    total = FOLD ? fmaf(sum, nothing ? 1.f : __fdiv_rn(1.f, fv), total) : total + sum;
+    if (i + 1 < mine) bring_values();
+  }
+  total = across32_f(total, fadd2);
+
+  // the waves, one after the other
+  if (grp == 0) {
+    stat[0][wave][col] = acc_top;
+    stat[1][wave][col] = total;
+  }
+  __syncthreads();                             // (and nobody reads queries any more)
+  float m = -INFINITY;
+  for (unsigned w = 0; w < waves; ++w) m = fmaxf(m, stat[0][w][col]);
+  const float weight = __builtin_amdgcn_exp2f(acc_top - finite_or_0(m));
+  const unsigned pitch = ND * 32 + 1;
+  for (unsigned w = 0; w < waves; ++w) {
+    if (w == wave)
+#pragma unroll
+      for (int t = 0; t < ND; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          float& to = sums[col * pitch + 32 * t + 8 * (r / 4) + 4 * grp + r % 4];
+          const float x = acc[t][r] * weight;
+          to = w == 0 ? x : to + x;
+        }
+    __syncthreads();
+  }
+  for (unsigned i = threadIdx.x; i < tile.rows * dv; i += blockDim.x) {
+    const unsigned r = i / dv, c = i % dv;
+    float mm = -INFINITY, l = 0.f;
+    for (unsigned w = 0; w < waves; ++w) mm = fmaxf(mm, stat[0][w][r]);
+    for (unsigned w = 0; w < waves; ++w) l = fmaf(__builtin_amdgcn_exp2f(stat[0][w][r] - finite_or_0(mm)), stat[1][w][r], l);
+    const float x = sums[r * pitch + c];
+    const uint2 at = row_at(r);
+    if (part.whole) {
+      if (c < d) static_cast<T*>(p.out)[(size_t)at.x * p.ldo + (size_t)at.y * d + c] = (T)(l == 0.f ? 0.f : __fdiv_rn(x, l));
+    } else {
+      float* to = p.part + ((size_t)to_part * kRows + r) * (dv + 4);
+      to[c] = x;
+      if (c == 0) {
+        to[dv] = mm;
+        to[dv + 1] = l;
+      }
+    }
+  }
+}
+
+// One workgroup for each tile and kv head, or equal shares (SHARES).  (Two waves a SIMD where 256 registers do: the compiler then
+// leaves accumulation registers alone, and copies to and from them.)
+template <int DT, int DC, bool SHARES>
+__global__ __launch_bounds__(kWaves * kWave, DC > 2 ? 1 : 2) void k_chunk_few(const ChunkParams p, int vec) {
+  if constexpr (SHARES) {
+    each_part(p, [&](const LinePart& part, unsigned to) {
+      few_rows<DT, DC>(p, vec, part, to);
+      __syncthreads();
+    });
+  } else {
+    // (heads next to each other: on a chip whose workgroups go to its eight XCDs by turns, eight heads have one each)
+    few_rows<DT, DC>(p, vec, LinePart{blockIdx.x % p.kv_heads, blockIdx.x / p.kv_heads, 0, 0xffffffffu, true}, 0);
+  }
+}
+
+// ---- many rows ----------------------------------------------------------------------------------------------------------
+//
+// A workgroup's four waves have 32 CT rows each and go through the same blocks, which they bring into LDS together, converted to
+// bfloat16 once, in operand order.  Scores are 32 tokens ahead: their products stand beside the exponentials of the 32 tokens
+// before, and the conversions of blocks to come beside the products of the values.  One barrier a block; three places in
+// LDS for keys, since this block's and the next one's are read while those of the one after come, two for values.
+// The scale of a block's values goes into the exponent (for binary32, whose 24 bits the logarithm would cost some, into a product).
+
+// Sums of matrix instructions times a factor, from accumulation registers and back.  (The compiler would otherwise take the
+// copies that the vector unit needs out of the branch, into every step.)
+template <bool VECTOR>
+__device__ __forceinline__ void scale_sums(v16f& o, float factor) {
+  if constexpr (VECTOR) {
+    o *= factor;
+    return;
+  }
+  asm volatile("" : "+a"(o));
+  o *= factor;
+  asm volatile("" : "+a"(o));
+}
+
 template <int DT, int DC>
-__global__ __launch_bounds__((TileForm<DT, DC>::W) * kWave, 1) void k_chunk_tiles(const ChunkParams p, int vec) {
+struct TileForm {
+  // two waves a SIMD where their registers fit
+  static constexpr int NP = kParts<DT>, CT = 1, W = NP * DC <= 2 ? 8 : 4, kRowsOfWg = W * 32 * CT;
+  static constexpr int kUnits = 8 * DC;                    // 1 KB pieces of a block's keys, and of its values
+  static constexpr size_t kLds = 5 * (size_t)kUnits * 1024;       // three blocks of keys, two of values
+  static constexpr bool kFold = NP < 3;
+};
+
+template <int DT, int DC>
+__device__ __forceinline__ void many_rows(const ChunkParams& p, int vec, const LinePart& part, unsigned to_part) {
   using T = typename Elem<DT>::T;
   using Form = TileForm<DT, DC>;
   constexpr int NP = Form::NP, CT = Form::CT, W = Form::W, NK = 2 * DC, ND = 2 * DC, KU = Form::kUnits;
   extern __shared__ __attribute__((aligned(16))) bf8 tile_lds[];                 // keys [3][KU][64], values [2][KU][64]
   bf8 *const kl = tile_lds, *const vl = tile_lds + 3 * KU * kWave;
-  const unsigned per = p.heads / p.kv_heads;
-  // this workgroup's part of the line: an eighth of it for each XCD, whose workgroups then read the same heads' blocks
-  const unsigned me = blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8, line = p.plan[p.slots];
-  const unsigned long long share = share_of(p, gridDim.x), line_end = (unsigned long long)line * p.kv_heads;
-  const unsigned long long from = me * share, to_end = min(from + share, line_end);
-  unsigned segment = 0;
-  for (unsigned long long at_block = from; at_block < to_end; ++segment) {
   // (unknown to the compiler to be the same each time: it would keep dozens of places and masks from one part to the next)
   unsigned lane = threadIdx.x % kWave, d = p.d;
   asm volatile("" : "+v"(lane), "+s"(d));
   const unsigned wave = __builtin_amdgcn_readfirstlane((threadIdx.x - threadIdx.x % kWave + lane) / kWave), col = lane % 32, grp = lane / 32;
-  const unsigned dk = kv_dk(d), dv = kv_dv(d);
-  const unsigned kvh = __builtin_amdgcn_readfirstlane((unsigned)(at_block / line)), place = (unsigned)(at_block - (unsigned long long)kvh * line);
-  const unsigned slot = (unsigned)__builtin_amdgcn_readfirstlane(wave_search(p.slots, place, [&](unsigned i) { return p.plan[i]; }));
-  const unsigned tile_start = p.plan[slot], tile_end = p.plan[slot + 1], start = place - tile_start;
-  const unsigned long long left = to_end - at_block;
-  const unsigned end = (unsigned)min((unsigned long long)(tile_end - tile_start), start + left);
-  const bool whole_tile = start == 0 && end == tile_end - tile_start;
-  at_block += end - start;
-  const Tile tile = find_tile<Form::kRowsOfWg>(p, slot, per);
+  const unsigned per = p.heads / p.kv_heads, dk = kv_dk(d), dv = kv_dv(d), kvh = part.kvh, start = part.start;
+  const Tile tile = find_tile<Form::kRowsOfWg>(p, part.slot, per);
   const unsigned nblocks = (seen_by(p, tile, (tile.row0 + tile.rows - 1) / per) + kKvBlock - 1) / kKvBlock;
-  const unsigned count = min(end, nblocks) > start ? min(end, nblocks) - start : 0;
+  const unsigned count = min(part.end, nblocks) > start ? min(part.end, nblocks) - start : 0;
   // this wave's rows; past the tile's end they repeat its last and are not stored
   unsigned mine_sees[CT], least = 0xffffffffu;
   uint2 at[CT];
@@ -717,7 +798,7 @@ __global__ __launch_bounds__((TileForm<DT, DC>::W) * kWave, 1) void k_chunk_tile
   for (int x = 0; x < CT; ++x) {
     const float l = across32_f(FOLD ? fmaf(sum[x], inverse, total[x]) : total[x], fadd2);
     if (!stored[x]) continue;
-    if (whole_tile) {
+    if (part.whole) {
       const bool whole = vec & 2;
       T* to = static_cast<T*>(p.out) + (size_t)at[x].x * p.ldo + (size_t)at[x].y * d;
 #pragma unroll
@@ -738,7 +819,7 @@ __global__ __launch_bounds__((TileForm<DT, DC>::W) * kWave, 1) void k_chunk_tile
           }
         }
     } else {
-      float* to = p.part + (((size_t)me * 2 + (segment > 0 ? 1 : 0)) * Form::kRowsOfWg + (wave * CT + x) * 32 + col) * (dv + 4);
+      float* to = p.part + ((size_t)to_part * Form::kRowsOfWg + (wave * CT + x) * 32 + col) * (dv + 4);
 #pragma unroll
       for (int t = 0; t < ND; ++t)
 #pragma unroll
@@ -752,47 +833,16 @@ __global__ __launch_bounds__((TileForm<DT, DC>::W) * kWave, 1) void k_chunk_tile
       }
     }
   }
-  }
 }
 
-// The parts of split sequences: a wave per (token, head).
-template <int DT>
-__global__ __launch_bounds__(256) void k_chunk_join(const ChunkParams p) {
-  using T = typename Elem<DT>::T;
-  const unsigned lane = threadIdx.x % kWave, dv = kv_dv(p.d), pitch = dv + 4, per = p.heads / p.kv_heads;
-  const unsigned rows = (unsigned)(blockIdx.x * (256 / kWave) + threadIdx.x / kWave), t = rows / p.heads, h = rows % p.heads;
-  if (t >= p.T) return;
-  const int b = __builtin_amdgcn_readfirstlane(wave_search(p.B, t, [&](unsigned i) { return first_at(p.first, i, p.T); }));
-  if (b < 0) return;
-  const unsigned f = first_at(p.first, b, p.T), e = first_at(p.first, b + 1, p.T);
-  if (t >= e) return;
-  // runs of the tile that the row is in
-  Tile tile{b, f, e - f, 0, 0, 0};
-  const int len = p.lens[b];
-  tile.len = len < 0 ? 0u : min((unsigned)len, p.max_len);
-  const unsigned row = (t - f) * per + h % per, last = min(row / kRows * kRows + kRows, tile.n * per) - 1;
-  const unsigned tokens = p.run * kKvBlock, runs = max(1u, (seen_by(p, tile, last / per) + tokens - 1) / tokens);
-  const float* part = p.part + ((size_t)t * p.heads + h) * p.splits * pitch;
-  float m = -INFINITY;
-  for (unsigned s = 0; s < runs; ++s) m = fmaxf(m, part[s * pitch + dv]);
-  const float base = finite_or_0(m);
-  float l = 0.f, x[4] = {};
-  for (unsigned s = 0; s < runs; ++s) {
-    const float w = __builtin_amdgcn_exp2f(part[s * pitch + dv] - base);
-    l = fmaf(w, part[s * pitch + dv + 1], l);
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (lane + 64 * j < p.d) x[j] = fmaf(w, part[s * pitch + lane + 64 * j], x[j]);
-  }
-#pragma unroll
-  for (int j = 0; j < 4; ++j)
-    if (lane + 64 * j < p.d)
-      static_cast<T*>(p.out)[(size_t)t * p.ldo + (size_t)h * p.d + lane + 64 * j] = (T)(l == 0.f ? 0.f : __fdiv_rn(x[j], l));
+template <int DT, int DC>
+__global__ __launch_bounds__((TileForm<DT, DC>::W) * kWave, 1) void k_chunk_tiles(const ChunkParams p, int vec) {
+  each_part(p, [&](const LinePart& part, unsigned to) { many_rows<DT, DC>(p, vec, part, to); });
 }
 
-// The same of the form for many rows: a workgroup for 32 rows of a tile and a kv head, eight threads a row.
+// The parts of tiles that more than one workgroup had: a workgroup for 32 rows of a tile and a kv head, eight threads a row.
 template <int DT, unsigned ROWS>
-__global__ __launch_bounds__(256) void k_chunk_join_tiles(const ChunkParams p, unsigned groups) {
+__global__ __launch_bounds__(256) void k_chunk_join(const ChunkParams p, unsigned groups) {
   using T = typename Elem<DT>::T;
   const unsigned chunk = blockIdx.x % (ROWS / 32), kvh = blockIdx.x / (ROWS / 32) % p.kv_heads, slot = blockIdx.x / (ROWS / 32 * p.kv_heads);
   const unsigned dv = kv_dv(p.d), pitch = dv + 4, per = p.heads / p.kv_heads;
@@ -827,48 +877,39 @@ __global__ __launch_bounds__(256) void k_chunk_join_tiles(const ChunkParams p, u
       if (4 * (j0 + 8 * j) + k < p.d) dst[4 * (j0 + 8 * j) + k] = (T)(l == 0.f ? 0.f : __fdiv_rn(x[j][k], l));
 }
 
-struct Split {
-  unsigned run, splits, waves, tile_rows, groups;          // groups: workgroups of the form for many rows
-  bool tiles;
+struct Form {
+  bool many, shares;
+  unsigned tile_rows, groups;         // rows of a tile; workgroups that share the line
   size_t slots;
 };
 constexpr size_t kManyRows = 96;      // rows of a sequence on average from which on they share blocks through LDS
-Split split_of(int dtype, size_t B, size_t T, size_t max_len, int heads, int kv_heads, size_t d) {
+constexpr size_t kShort = 8;          // blocks of the longest sequence up to which a workgroup takes all of a tile's
+Form form_of(int dtype, size_t B, size_t T, size_t max_len, int heads, int kv_heads, size_t d) {
   const size_t per = (size_t)(heads / kv_heads), blocks = (max_len + kKvBlock - 1) / kKvBlock;
-  Split s{};
-  // binary32 queries of wide heads do not fit beside the sums
-  s.tiles = T * per / B >= kManyRows && !(dtype == MQ_F32 && d > 128);
-  if (s.tiles) {
+  Form f{};
+  // (binary32 queries of wide heads do not fit beside the sums)
+  f.many = T * per / B >= kManyRows && !(dtype == MQ_F32 && d > 128);
+  f.shares = f.many || blocks > kShort;
+  f.tile_rows = kRows;
+  f.groups = d <= 64 ? 768 : d <= 128 ? 512 : 256;
+  if (f.many) {
     const bool wide = (dtype == MQ_BF16 && d <= 128) || (d <= 64 && dtype == MQ_F16);
-    s.tile_rows = wide ? 256 : 128;
-    s.groups = wide ? 256 : 512;      // one workgroup of eight waves to a compute unit, or two of four
-    s.slots = T * per / s.tile_rows + B;
-    return s;
+    f.tile_rows = wide ? 256 : 128;
+    f.groups = wide ? 256 : 512;      // one workgroup of eight waves to a compute unit, or two of four
   }
-  s.tile_rows = kRows;
-  s.slots = T * per / s.tile_rows + B;
-  const size_t wgs = s.slots * (size_t)kv_heads, want = (512 + wgs - 1) / wgs;
-  size_t run = blocks <= 2 * kWaves ? blocks : (blocks + want - 1) / want;
-  if (blocks > 2 * kWaves && run < (size_t)kWaves) run = kWaves;
-  s.run = (unsigned)run;
-  s.splits = (unsigned)((blocks + run - 1) / run);
-  s.waves = (unsigned)(blocks < kWaves ? blocks : kWaves);
-  return s;
+  f.slots = T * per / f.tile_rows + B;
+  return f;
 }
 // Floats of the parts, in front of the plan.
-size_t part_floats(const Split& s, size_t T, int heads, size_t d) {
-  const size_t pitch = kv_dv((unsigned)d) + 4;
-  if (s.tiles) return (size_t)s.groups * 2 * s.tile_rows * pitch;
-  return s.splits == 1 ? 4 : T * (size_t)heads * s.splits * pitch;
-}
+size_t part_floats(const Form& f, size_t d) { return f.shares ? (size_t)f.groups * 2 * f.tile_rows * (kv_dv((unsigned)d) + 4) : 4; }
 
 }  // namespace
 
 size_t chunk_attention_ws_bytes(size_t B, size_t T, size_t max_len, int heads, int kv_heads, size_t d) {
   size_t most = 0;                    // (whatever the type)
   for (int dtype : {MQ_F32, MQ_F16, MQ_BF16}) {
-    const Split s = split_of(dtype, B, T, max_len, heads, kv_heads, d);
-    const size_t n = part_floats(s, T, heads, d) + (s.tiles ? s.slots + 1 : 0);
+    const Form f = form_of(dtype, B, T, max_len, heads, kv_heads, d);
+    const size_t n = part_floats(f, d) + (f.shares ? f.slots + 1 : 0);
     most = n > most ? n : most;
   }
   return most * sizeof(float);
@@ -877,53 +918,56 @@ size_t chunk_attention_ws_bytes(size_t B, size_t T, size_t max_len, int heads, i
 int launch_chunk_attention(const mq_kv_cache& cache, const int32_t* table, size_t table_width, const int32_t* first,
                            const int32_t* lens, size_t B, size_t T, size_t max_len, int causal, const void* q, size_t ldq,
                            int heads, int dtype, float scale, void* out, size_t ldo, void* ws, hipStream_t s) {
-  const Split split = split_of(dtype, B, T, max_len, heads, cache.kv_heads, cache.head_dim);
-  const size_t wgs = split.slots * (size_t)cache.kv_heads * (split.tiles ? 1 : split.splits);
-  const size_t joins = (T * (size_t)heads + 3) / 4;
+  const Form form = form_of(dtype, B, T, max_len, heads, cache.kv_heads, cache.head_dim);
+  const size_t tiles = form.slots * (size_t)cache.kv_heads, joins = tiles * (form.tile_rows / 32);
+  const size_t blocks = (max_len + kKvBlock - 1) / kKvBlock;
   // (blocks of all tiles are counted in 32 bits)
-  if (!launchable(wgs, 2 * kWaves * kWave) || (split.splits > 1 && !launchable(joins, 256)) ||
-      (split.tiles && !launchable(wgs * (split.tile_rows / 32), 256)) || (split.tiles && split.slots > (((size_t)1 << 32) - 1) / ((max_len + kKvBlock - 1) / kKvBlock)))
-    return MQ_ERR_SHAPE;
+  if (!launchable(joins, kWaves * kWave) || form.slots > (((size_t)1 << 32) - 1) / blocks) return MQ_ERR_SHAPE;
   float* part = static_cast<float*>(ws);
   const ChunkParams p{cache.keys, cache.values, cache.amax, table, first, lens, q, out, part, ldq, ldo,
                       table_width, cache.blocks, (unsigned)B, (unsigned)T, (unsigned)max_len, (unsigned)cache.kv_heads,
-                      (unsigned)heads, (unsigned)cache.head_dim, split.splits, split.run, scale * 1.44269504088896340736f, causal,
-                      reinterpret_cast<unsigned*>(part + part_floats(split, T, heads, cache.head_dim)), (unsigned)split.slots};
+                      (unsigned)heads, (unsigned)cache.head_dim, scale * 1.44269504088896340736f, causal,
+                      reinterpret_cast<unsigned*>(part + part_floats(form, cache.head_dim)), (unsigned)form.slots};
   const size_t piece = 16 / elem_bytes(dtype);
   // whole 16-byte pieces of queries, four neighbouring results at once
   const int vec = (cache.head_dim % piece == 0 && ldq % piece == 0 && reinterpret_cast<uintptr_t>(q) % 16 == 0 ? 1 : 0) |
                   (cache.head_dim % 4 == 0 && ldo % 4 == 0 && reinterpret_cast<uintptr_t>(out) % (4 * elem_bytes(dtype)) == 0 ? 2 : 0);
   return with_dtype(dtype, [&](auto dt) {
     constexpr int DT = decltype(dt)::value;
-    int rc = MQ_OK;
     auto sized = [&](auto dc) {
       constexpr int DC = decltype(dc)::value;
-      if (split.tiles) {
+      if (form.many) {
         if constexpr (!(DT == MQ_F32 && DC > 2)) {
-          using Form = TileForm<DT, DC>;
-          constexpr unsigned ROWS = Form::kRowsOfWg;
+          using Tiles = TileForm<DT, DC>;
+          constexpr unsigned ROWS = Tiles::kRowsOfWg;
           auto kern = k_chunk_tiles<DT, DC>;
-          if (Form::kLds > 65536)
-            rc = check_hip(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)Form::kLds));
-          if (rc != MQ_OK) return;
+          if (Tiles::kLds > 65536) {
+            const int rc = check_hip(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)Tiles::kLds));
+            if (rc != MQ_OK) return rc;
+          }
           hipLaunchKernelGGL(k_chunk_plan<ROWS>, dim3(1), dim3(kPlan), 0, s, p);
-          hipLaunchKernelGGL(kern, dim3(split.groups), dim3(Form::W * kWave), Form::kLds, s, p, vec);
-          hipLaunchKernelGGL((k_chunk_join_tiles<DT, ROWS>), dim3((unsigned)(wgs * (ROWS / 32))), dim3(256), 0, s, p, split.groups);
+          hipLaunchKernelGGL(kern, dim3(form.groups), dim3(Tiles::W * kWave), Tiles::kLds, s, p, vec);
+          hipLaunchKernelGGL((k_chunk_join<DT, ROWS>), dim3((unsigned)joins), dim3(256), 0, s, p, form.groups);
         }
-      } else {
-        const size_t ql = kParts<DT> * DC * 4 * kWave * 16, sums = kRows * (DC * 64 + 1) * sizeof(float);
-        hipLaunchKernelGGL((k_chunk_attention<DT, DC>), dim3((unsigned)wgs), dim3(split.waves * kWave), ql > sums ? ql : sums, s, p);
-        if (split.splits > 1) hipLaunchKernelGGL(k_chunk_join<DT>, dim3((unsigned)joins), dim3(256), 0, s, p);
+        return check_hip(hipGetLastError());
       }
-      rc = check_hip(hipGetLastError());
+      constexpr size_t ql = kParts<DT> * DC * 4 * kWave * 16, sums = kRows * (DC * 64 + 1) * sizeof(float), lds = ql > sums ? ql : sums;
+      if (!form.shares) {
+        const unsigned waves = (unsigned)(blocks < kWaves ? blocks : kWaves);
+        hipLaunchKernelGGL((k_chunk_few<DT, DC, false>), dim3((unsigned)tiles), dim3(waves * kWave), lds, s, p, vec);
+        return check_hip(hipGetLastError());
+      }
+      hipLaunchKernelGGL(k_chunk_plan<kRows>, dim3(1), dim3(kPlan), 0, s, p);
+      hipLaunchKernelGGL((k_chunk_few<DT, DC, true>), dim3(form.groups), dim3(kWaves * kWave), lds, s, p, vec);
+      hipLaunchKernelGGL((k_chunk_join<DT, kRows>), dim3((unsigned)joins), dim3(256), 0, s, p, form.groups);
+      return check_hip(hipGetLastError());
     };
     switch (kv_dk(p.d) / 64) {
-      case 1: sized(std::integral_constant<int, 1>{}); break;
-      case 2: sized(std::integral_constant<int, 2>{}); break;
-      case 3: sized(std::integral_constant<int, 3>{}); break;
-      default: sized(std::integral_constant<int, 4>{}); break;
+      case 1: return sized(std::integral_constant<int, 1>{});
+      case 2: return sized(std::integral_constant<int, 2>{});
+      case 3: return sized(std::integral_constant<int, 3>{});
+      default: return sized(std::integral_constant<int, 4>{});
     }
-    return rc;
   });
 }
 
