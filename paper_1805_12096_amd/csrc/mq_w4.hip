@@ -1,7 +1,8 @@
 // Parameters in 4 bits and products of a few rows with them (include/mq_serve.h): y = x w^T, w = (c - z) s.
 //
 // Packed: fragments of 16 rows x 128 elements, 1 KB, lane l of a wave 16 bytes: word w has the codes of row l % 16, elements
-// 32 w + 8 (l / 16) .., what lane l feeds to v_mfma_f32_16x16x32_bf16 as operand a.  Code 2 p lies in nibble p of the word's
+// 32 w + 8 (l / 16) .., what lane l feeds to v_mfma_f32_16x16x32_bf16 as operand b (x is a, so
+// that a lane has results of one row of the parameter, and needs one scale).  Code 2 p lies in nibble p of the word's
 // lower half, code 2 p + 1 in nibble p of the upper, so a pair shifted and masked once is two bfloat16 mantissas: 16 + c, exactly.
 // y = sum_g s (sum_k (16 + c) x - (16 + z) sum_k x): a product with ones gives sum_k x where the other product leaves its results.
 // Scales follow the fragments: a word for each (16 rows, group, row), 20 bits of mantissa of the scale and the zero below them.
@@ -130,117 +131,394 @@ struct XElem<MQ_ROWS8> { using T = int8_t; };
 template <int XT>
 constexpr int kXParts = XT == MQ_ROWS8 ? 1 : kParts<XT == MQ_ROWS8 ? MQ_BF16 : XT>;
 
-// 16 + c of eight codes
-__device__ __forceinline__ bf8 codes16(unsigned w) {
-  constexpr unsigned mask = 0x00780078u, top = 0x41804180u;
-  const u4 v = {(w << 3 & mask) | top, (w >> 1 & mask) | top, (w >> 5 & mask) | top, (w >> 9 & mask) | top};
-  return __builtin_bit_cast(bf8, v);
+// What a product takes of x and of codes.  8-bit rows: signed bytes and the codes as bytes, sums whole numbers (below 2^24, so
+// exact in binary32).  Others: bfloat16 parts and 16 + c, sums binary32.
+template <int XT>
+struct Operand {
+  static constexpr bool kBytes = XT == MQ_ROWS8;
+  static constexpr int NP = kXParts<XT>, kOffset = kBytes ? 0 : 16;
+  using Piece = typename std::conditional<kBytes, long, bf8>::type;
+  using Acc = typename std::conditional<kBytes, v4i, v4f>::type;
+  static __device__ __forceinline__ Acc mfma(Piece a, Piece b, Acc c) {
+    if constexpr (kBytes) return __builtin_amdgcn_mfma_i32_16x16x32_i8(a, b, c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ Piece codes(unsigned w) {
+    if constexpr (kBytes) {             // codes 0 4 1 5 2 6 3 7
+      return __builtin_bit_cast(long, make_uint2(w & 0x0f0f0f0fu, w >> 4 & 0x0f0f0f0fu));
+    } else {
+      constexpr unsigned mask = 0x00780078u, top = 0x41804180u;
+      const u4 v = {(w << 3 & mask) | top, (w >> 1 & mask) | top, (w >> 5 & mask) | top, (w >> 9 & mask) | top};
+      return __builtin_bit_cast(bf8, v);
+    }
+  }
+  static __device__ __forceinline__ Piece ones() {
+    if constexpr (kBytes) return 0x0101010101010101l;
+    else return __builtin_bit_cast(bf8, u4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u});
+  }
+};
+
+__device__ __forceinline__ float scale_of(unsigned w) { return __uint_as_float(w & kTopScale); }
+template <int XT>
+__device__ __forceinline__ float offset_of(unsigned w) {
+  return (float)(Operand<XT>::kOffset + (w & 15u));
 }
 
-// elements k .. k + 7 of a row as parts; left: how many there are
-template <int XT, int NP>
-__device__ __forceinline__ void x_parts(const typename XElem<XT>::T* src, int left, bool vec, bf8 (&part)[NP]) {
-  using T = typename XElem<XT>::T;
-  if constexpr (XT == MQ_ROWS8) {
-    uint2 b = make_uint2(0, 0);
-    if (vec) {
-      if (left >= 8) b = *reinterpret_cast<const uint2*>(src);
-    } else {
+// Elements k .. k + 7 of a row of x as they lie, zeros from K on.
+template <int XT>
+struct Raw {
+  typename XElem<XT>::T v[8];
+};
+template <int XT>
+__device__ __forceinline__ Raw<XT> raw8(const typename XElem<XT>::T* row, int k, int K) {
+  Raw<XT> r;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const unsigned v = j < left ? (unsigned)(uint8_t)src[j] : 0u;
-        if (j < 4) b.x |= v << 8 * j;
-        else b.y |= v << 8 * (j - 4);
-      }
-    }
-    part[0] = bf16_of_bytes(b.x, b.y);
+  for (int j = 0; j < 8; ++j) r.v[j] = k + j < K ? row[k + j] : (typename XElem<XT>::T)0;
+  return r;
+}
+// The same as operand parts.
+template <int XT>
+__device__ __forceinline__ void x_parts(const Raw<XT>& r, typename Operand<XT>::Piece (&part)[Operand<XT>::NP]) {
+  constexpr int NP = Operand<XT>::NP;
+  if constexpr (XT == MQ_ROWS8) {       // in the order of the codes
+    const uint2 b = __builtin_bit_cast(uint2, r);
+    part[0] = __builtin_bit_cast(long, make_uint2(__builtin_amdgcn_perm(b.y, b.x, 0x05010400u), __builtin_amdgcn_perm(b.y, b.x, 0x07030602u)));
+  } else if constexpr (NP == 1) {
+    part[0] = __builtin_bit_cast(bf8, r);
   } else {
-    T v[8];
-    if (vec) {                          // (rows are whole pieces then)
-      constexpr int W = 16 / sizeof(T);
-      typedef T tw __attribute__((ext_vector_type(W)));
-#pragma unroll
-      for (int j = 0; j < 8; j += W) {
-        tw w = {};
-        if (j < left) w = *reinterpret_cast<const tw*>(src + j);
-#pragma unroll
-        for (int i = 0; i < W; ++i) v[j + i] = w[i];
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = j < left ? src[j] : (T)0.f;
-    }
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       __bf16 p[NP];
-      if constexpr (NP == 1) p[0] = v[j];
-      else split_bf16<NP>((float)v[j], p);
+      split_bf16<NP>((float)r.v[j], p);
 #pragma unroll
       for (int i = 0; i < NP; ++i) part[i][j] = p[i];
     }
   }
 }
 
-// A workgroup has a row tile of the parameter and 16 MT rows of x; its waves take the fragments in turn and join in LDS.
-template <int XT, int GROUP, int MT>
-__global__ __launch_bounds__(512) void k_w4_product(const W4Params p) {
+// Few rows, of whole 16-byte pieces.  A workgroup has 16 NT rows of the parameter and 16 MT rows of x; its waves take the
+// fragments in turn, the next ones' loads ahead of this one's products, and join in LDS.  A lane of an operand has a row of x of its
+// own; loaded like that, every lane would be an access to the nearest cache of its own (64 a load instead of 8 .. 16, which bound
+// this form).  So x comes in lines, and each wave turns its lines in a part of LDS.
+template <int XT, int GROUP, int MT, int NT>
+__global__ __launch_bounds__(512) void k_w4_few(const W4Params p) {
   using T = typename XElem<XT>::T;
   constexpr int NP = kXParts<XT>, GF = kKT / GROUP, SG = GROUP / 32;      // groups of a fragment, steps of a group
-  extern __shared__ float lds[];                 // [waves][MT 16][17]
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  float* const lds = reinterpret_cast<float*>(smem);       // [waves][MT 16][NT 16 + 1], afterwards
   const unsigned lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), waves = blockDim.x / kWave;
-  const unsigned tile = blockIdx.x, m0 = blockIdx.y * 16 * MT, col = lane % 16, grp = lane / 16;
+  const unsigned tile = blockIdx.x * NT, m0 = blockIdx.y * 16 * MT, col = lane % 16, grp = lane / 16;
   const W4Dims d(p.N, p.K, GROUP);
-  const uint8_t* frag = p.packed + (size_t)tile * d.frags * 1024 + lane * 16;
-  const uint32_t* scales = reinterpret_cast<const uint32_t*>(p.packed + d.scales_at()) + (size_t)tile * d.groups * kNT + 4 * grp;
-  const T* row[MT];
+  const uint8_t* frag[NT];
+  const uint32_t* scales[NT];
 #pragma unroll
-  for (int t = 0; t < MT; ++t) row[t] = static_cast<const T*>(p.x) + (size_t)min(m0 + 16 * t + col, p.M - 1) * p.ldx;
-  const u4 one = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
-  const bf8 ones = __builtin_bit_cast(bf8, one);
-  float y[MT][4] = {};
-  for (unsigned f = wave; f < p.frags; f += waves) {
-    const u4 w = *reinterpret_cast<const u4*>(frag + (size_t)f * 1024);
-    u4 sc[GF];
+  for (int n = 0; n < NT; ++n) {                 // (a tile that is not there repeats the last)
+    const size_t t = min(tile + n, (unsigned)d.tiles - 1);
+    frag[n] = p.packed + t * d.frags * 1024 + lane * 16;
+    scales[n] = reinterpret_cast<const uint32_t*>(p.packed + d.scales_at()) + t * d.groups * kNT + col;
+  }
+  // a row's elements of a fragment are SLOTS pieces of 16 bytes; LINES rows to a load; piece j of row r lies at place j ^ (r & 7)
+  constexpr unsigned SLOTS = 8 * sizeof(T), LINES = kWave / SLOTS, XI = 16 / LINES, PER = 16 / sizeof(T);
+  u4* const turn = reinterpret_cast<u4*>(smem) + (size_t)wave * MT * 16 * SLOTS;
+  using Op = Operand<XT>;
+  using Piece = typename Op::Piece;
+  const Piece ones = Op::ones();
+  float y[NT][MT][4] = {};
+  // codes and scales of AHEAD fragments are on their way: enough that memory is busy; x, out of the nearest cache, of the next
+  constexpr int AHEAD = 4;
+  u4 w[AHEAD][NT];
+  unsigned sc[AHEAD][NT][GF];
+  u4 x[MT][XI];
+  auto load = [&](int at, unsigned f) __attribute__((always_inline)) {
+    f = min(f, p.frags - 1);
 #pragma unroll
-    for (int g = 0; g < GF; ++g) sc[g] = *reinterpret_cast<const u4*>(scales + ((size_t)f * GF + g) * kNT);
+    for (int n = 0; n < NT; ++n) {
+      w[at][n] = *reinterpret_cast<const u4*>(frag[n] + (size_t)f * 1024);
+#pragma unroll
+      for (int g = 0; g < GF; ++g) sc[at][n][g] = scales[n][((size_t)f * GF + g) * kNT];
+    }
+  };
+  auto load_x = [&](unsigned f) __attribute__((always_inline)) {
+    f = min(f, p.frags - 1);
+    const unsigned e = f * kKT + lane % SLOTS * PER;
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+#pragma unroll
+      for (unsigned i = 0; i < XI; ++i) {
+        const size_t m = min(m0 + 16 * t + i * LINES + lane / SLOTS, p.M - 1);
+        x[t][i] = *reinterpret_cast<const u4*>(static_cast<const T*>(p.x) + m * p.ldx + min(e, p.K - PER));
+        if (e >= p.K) x[t][i] = u4{};
+      }
+  };
+  auto turn_x = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+#pragma unroll
+      for (unsigned i = 0; i < XI; ++i) {
+        const unsigned r = i * LINES + lane / SLOTS;
+        turn[(16 * t + r) * SLOTS + ((lane % SLOTS) ^ (r & 7))] = x[t][i];
+      }
+  };
+  // elements 32 step + 8 grp .. of row 16 t + col
+  auto read_x = [&](int t, int step) __attribute__((always_inline)) {
+    const u4* const at = turn + (16 * t + col) * SLOTS;
+    if constexpr (sizeof(T) == 1) {
+      const uint2* const piece = reinterpret_cast<const uint2*>(at + ((2 * step + grp / 2) ^ (col & 7)));
+      return __builtin_bit_cast(Raw<XT>, piece[grp % 2]);
+    } else if constexpr (sizeof(T) == 2) {
+      return __builtin_bit_cast(Raw<XT>, at[(4 * step + grp) ^ (col & 7)]);
+    } else {
+      struct Two { u4 a, b; };
+      return __builtin_bit_cast(Raw<XT>, Two{at[(8 * step + 2 * grp) ^ (col & 7)], at[(8 * step + 2 * grp + 1) ^ (col & 7)]});
+    }
+  };
+  auto multiply = [&](int at) __attribute__((always_inline)) {
 #pragma unroll
     for (int g = 0; g < GF; ++g) {
-      v4f acc[MT] = {}, sum[MT] = {};
+      typename Op::Acc acc[NT][MT] = {}, sum[MT] = {};
 #pragma unroll
       for (int i = 0; i < SG; ++i) {
-        const int step = g * SG + i, k = (int)(f * kKT + step * 32 + 8 * grp), left = (int)p.K - k;
-        const bf8 a = codes16(w[step]);
+        const int step = g * SG + i;
+        Piece c[NT];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) c[n] = Op::codes(w[at][n][step]);
 #pragma unroll
         for (int t = 0; t < MT; ++t) {
-          bf8 x[NP];
-          x_parts<XT, NP>(row[t] + k, left, p.vec, x);
+          Piece xp[NP];
+          x_parts<XT>(read_x(t, step), xp);
 #pragma unroll
           for (int j = NP - 1; j >= 0; --j) {
-            acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, x[j], acc[t], 0, 0, 0);
-            sum[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, x[j], sum[t], 0, 0, 0);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) acc[n][t] = Op::mfma(xp[j], c[n], acc[n][t]);
+            sum[t] = Op::mfma(xp[j], ones, sum[t]);
           }
         }
       }
+      float total[MT][4];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const float s = __uint_as_float(sc[g][r] & kTopScale), z = (float)(16u + (sc[g][r] & 15u));
+      for (int t = 0; t < MT; ++t)
 #pragma unroll
-        for (int t = 0; t < MT; ++t) y[t][r] = fmaf(s, fmaf(-z, sum[t][r], acc[t][r]), y[t][r]);
+        for (int r = 0; r < 4; ++r) total[t][r] = (float)sum[t][r];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        const float s = scale_of(sc[at][n][g]), z = offset_of<XT>(sc[at][n][g]);
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) y[n][t][r] = fmaf(s, fmaf(-z, total[t][r], (float)acc[n][t][r]), y[n][t][r]);
       }
     }
-  }
+  };
 #pragma unroll
-  for (int t = 0; t < MT; ++t)
+  for (int i = 0; i < AHEAD; ++i) load(i, wave + i * waves);
+  load_x(wave);
+  for (unsigned f = wave; f < p.frags; f += AHEAD * waves)
 #pragma unroll
-    for (int r = 0; r < 4; ++r) lds[(wave * MT * 16 + t * 16 + col) * 17 + 4 * grp + r] = y[t][r];
+    for (int i = 0; i < AHEAD; ++i) {
+      const unsigned now = f + i * waves;
+      if (now >= p.frags) break;
+      turn_x();                                  // (a wave's accesses to LDS are in order)
+      load_x(now + waves);
+      multiply(i);
+      load(i, now + AHEAD * waves);
+    }
   __syncthreads();
-  for (unsigned i = threadIdx.x; i < MT * 256; i += blockDim.x) {
-    const unsigned m = m0 + i / 16, n = tile * kNT + i % 16;
+  constexpr int PITCH = NT * 16 + 1;
+#pragma unroll
+  for (int n = 0; n < NT; ++n)
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) lds[(wave * MT * 16 + t * 16 + 4 * grp + r) * PITCH + n * 16 + col] = y[n][t][r];
+  __syncthreads();
+  for (unsigned i = threadIdx.x; i < MT * 16 * NT * 16; i += blockDim.x) {
+    const unsigned mm = i / (NT * 16), nn = i % (NT * 16), m = m0 + mm, n = tile * kNT + nn;
     float v = 0.f;
-    for (unsigned w = 0; w < waves; ++w) v += lds[(w * MT * 16 + i / 16) * 17 + i % 16];
+    for (unsigned w = 0; w < waves; ++w) v += lds[(w * MT * 16 + mm) * PITCH + nn];
     if (m >= p.M || n >= p.N) continue;
     if (XT == MQ_ROWS8) v = __fdiv_rn(v, p.row_scale[m]);
     store_as(p.y, p.ytype, (size_t)m * p.ldy + n, p.bias != nullptr ? v + p.bias[n] : v);
+  }
+}
+
+// Many rows.  x comes as operand parts and sums of groups from a launch of its own (each is used by every row tile of the
+// parameter); a workgroup has 16 NT x 16 MT results and a run of fragments, its waves take the run's fragments in turn and join in
+// LDS, runs through the workspace.
+// (of three parts of x only half as many rows fit the registers beside those of the next step)
+constexpr int many_mt(int parts) { return parts == 3 ? 2 : 4; }
+constexpr int kManyNT = 4, kManyWaves = 4;
+
+// operand parts [row tile][fragment][step][part][lane], 16 bytes each (8 of 8-bit rows), then sums [row tile][32 elements][16 rows]
+struct XDims {
+  size_t tiles, frags;
+  int parts;
+  __host__ __device__ XDims(size_t M, size_t K, int np) : tiles((M + 15) / 16), frags((K + kKT - 1) / kKT), parts(np) {}
+  __host__ __device__ size_t sums_at() const { return tiles * frags * 4 * parts * 1024; }
+  __host__ __device__ size_t bytes() const { return sums_at() + tiles * frags * 4 * 16 * sizeof(float); }
+};
+
+template <int XT>
+__global__ __launch_bounds__(256) void k_w4_x(const W4Params p, uint8_t* to) {
+  constexpr int NP = kXParts<XT>;
+  const XDims x(p.M, p.K, NP);
+  const unsigned lane = threadIdx.x % kWave, col = lane % 16, grp = lane / 16;
+  const size_t steps = x.tiles * x.frags * 4;
+  for (size_t s = (size_t)blockIdx.x * 4 + threadIdx.x / kWave; s < steps; s += (size_t)gridDim.x * 4) {
+    const size_t tile = s / (x.frags * 4);
+    const int k = (int)(s % (x.frags * 4) * 32 + 8 * grp);
+    const size_t m = tile * 16 + col;
+    const typename XElem<XT>::T* row = static_cast<const typename XElem<XT>::T*>(p.x) + (m < p.M ? m : p.M - 1) * p.ldx;
+    Raw<XT> r{};
+    if (p.vec) {                        // (rows are whole 16-byte pieces)
+      using T = typename XElem<XT>::T;
+      typedef T t8 __attribute__((ext_vector_type(8)));
+      typedef t8 unaligned __attribute__((aligned(sizeof(T) == 1 ? 8 : 16)));
+      if (k + 8 <= (int)p.K) r = __builtin_bit_cast(Raw<XT>, *reinterpret_cast<const unaligned*>(row + k));
+      else if (k < (int)p.K) r = raw8<XT>(row, k, (int)p.K);
+    } else {
+      r = raw8<XT>(row, k, (int)p.K);
+    }
+    using Piece = typename Operand<XT>::Piece;
+    Piece part[NP];
+    x_parts<XT>(r, part);
+    Piece* dst = reinterpret_cast<Piece*>(to) + s * NP * kWave + lane;
+#pragma unroll
+    for (int i = 0; i < NP; ++i) dst[i * kWave] = part[i];
+    float sum = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sum += (float)r.v[j];
+    sum = across16_f(across32_f(sum, [](float a, float b) { return a + b; }), [](float a, float b) { return a + b; });
+    if (grp == 0) reinterpret_cast<float*>(to + x.sums_at())[s * 16 + col] = sum;
+  }
+}
+
+template <int XT, int GROUP>
+__global__ __launch_bounds__(kManyWaves * kWave, 2) void k_w4_many(const W4Params p, const uint8_t* xs, unsigned runs, unsigned run) {
+  constexpr int NP = kXParts<XT>, GF = kKT / GROUP, SG = GROUP / 32, MT = many_mt(NP), NT = kManyNT;
+  __shared__ float lds[MT * 16][NT * 16 + 1];
+  const unsigned lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), col = lane % 16, grp = lane / 16;
+  // neighbouring workgroups share rows of x: those of one XCD its parts
+  const unsigned ntiles = gridDim.x / runs, nt = blockIdx.x % ntiles, k0 = blockIdx.x / ntiles * run, k1 = min(k0 + run, p.frags);
+  const unsigned m0 = blockIdx.y * MT;
+  const W4Dims d(p.N, p.K, GROUP);
+  const XDims xd(p.M, p.K, NP);
+  const uint8_t* frag[NT];
+  const uint32_t* scales[NT];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    const size_t t = min(nt * NT + n, (unsigned)d.tiles - 1);
+    frag[n] = p.packed + t * d.frags * 1024 + lane * 16;
+    scales[n] = reinterpret_cast<const uint32_t*>(p.packed + d.scales_at()) + t * d.groups * kNT + col;
+  }
+  using Op = Operand<XT>;
+  using Piece = typename Op::Piece;
+  const Piece* xp[MT];
+  const float* xsum[MT];
+#pragma unroll
+  for (int t = 0; t < MT; ++t) {
+    const size_t tile = min(m0 + t, (unsigned)xd.tiles - 1);
+    xp[t] = reinterpret_cast<const Piece*>(xs) + tile * xd.frags * 4 * NP * kWave + lane;
+    xsum[t] = reinterpret_cast<const float*>(xs + xd.sums_at()) + tile * xd.frags * 4 * 16 + 4 * grp;
+  }
+  float y[NT][MT][4] = {};
+  // codes of the next fragment and x of the next step are on their way
+  u4 w[2][NT];
+  Piece x[2][MT][NP];
+  auto load = [&](int at, unsigned f) __attribute__((always_inline)) {
+#pragma unroll
+    for (int n = 0; n < NT; ++n) w[at][n] = *reinterpret_cast<const u4*>(frag[n] + (size_t)f * 1024);
+  };
+  auto load_x = [&](int at, unsigned f, int step) __attribute__((always_inline)) {
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+#pragma unroll
+      for (int j = 0; j < NP; ++j) x[at][t][j] = xp[t][(((size_t)f * 4 + step) * NP + j) * kWave];
+  };
+  auto multiply = [&](int at, unsigned f, unsigned next) __attribute__((always_inline)) {
+    typename Op::Acc acc[NT][MT];
+    v4f sum[MT];
+#pragma unroll
+    for (int step = 0; step < 4; ++step) {
+      const int g = step / SG;
+      load_x((step + 1) % 2, step < 3 ? f : next, (step + 1) % 4);
+#pragma unroll
+      for (int t = 0; t < MT; ++t) {
+        const v4f part = *reinterpret_cast<const v4f*>(xsum[t] + ((size_t)f * 4 + step) * 16);
+        sum[t] = step % SG == 0 ? part : sum[t] + part;
+      }
+      Piece c[NT];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) c[n] = Op::codes(w[at][n][step]);
+#pragma unroll
+      for (int t = 0; t < MT; ++t)
+#pragma unroll
+        for (int j = NP - 1; j >= 0; --j)
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+            acc[n][t] = Op::mfma(x[step % 2][t][j], c[n], step % SG == 0 && j == NP - 1 ? typename Op::Acc{} : acc[n][t]);
+      if (step % SG != SG - 1) continue;
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        const unsigned sc = scales[n][((size_t)f * GF + g) * kNT];
+        const float s = scale_of(sc), z = offset_of<XT>(sc);
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) y[n][t][r] = fmaf(s, fmaf(-z, sum[t][r], (float)acc[n][t][r]), y[n][t][r]);
+      }
+    }
+  };
+  unsigned f = k0 + wave;
+  if (f < k1) {
+    load(0, f);
+    load_x(0, f, 0);
+  }
+  while (f < k1) {
+    unsigned next = min(f + kManyWaves, k1 - 1);
+    load(1, next);
+    multiply(0, f, next);
+    f += kManyWaves;
+    if (f >= k1) break;
+    next = min(f + kManyWaves, k1 - 1);
+    load(0, next);
+    multiply(1, f, next);
+    f += kManyWaves;
+  }
+  for (unsigned v = 0; v < kManyWaves; ++v) {    // one wave after the other
+    if (v == wave)
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            float& to = lds[t * 16 + 4 * grp + r][n * 16 + col];
+            to = v == 0 ? y[n][t][r] : to + y[n][t][r];
+          }
+    __syncthreads();
+  }
+  for (unsigned i = threadIdx.x; i < MT * 16 * NT * 16; i += kManyWaves * kWave) {
+    const unsigned mm = i / (NT * 16), nn = i % (NT * 16), m = m0 * 16 + mm, n = nt * NT * 16 + nn;
+    if (m >= p.M || n >= p.N) continue;
+    float v = lds[mm][nn];
+    if (runs > 1) {
+      p.part[((size_t)(k0 / run) * p.M + m) * p.N + n] = v;
+      continue;
+    }
+    if (XT == MQ_ROWS8) v = __fdiv_rn(v, p.row_scale[m]);
+    store_as(p.y, p.ytype, (size_t)m * p.ldy + n, p.bias != nullptr ? v + p.bias[n] : v);
+  }
+}
+
+// The runs of a contraction, in order.
+__global__ __launch_bounds__(256) void k_w4_join(const W4Params p, unsigned runs) {
+  const size_t all = (size_t)p.M * p.N;
+  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (size_t)gridDim.x * 256) {
+    const size_t m = i / p.N, n = i % p.N;
+    float v = 0.f;
+    for (unsigned s = 0; s < runs; ++s) v += p.part[s * all + i];
+    if (p.row_scale != nullptr) v = __fdiv_rn(v, p.row_scale[m]);
+    store_as(p.y, p.ytype, m * p.ldy + n, p.bias != nullptr ? v + p.bias[n] : v);
   }
 }
 
@@ -269,28 +547,68 @@ int launch_w4_unpack(const void* packed, size_t N, size_t K, int group, float* w
   return check_hip(hipGetLastError());
 }
 
-size_t w4_product_ws_bytes(size_t, size_t, size_t) { return 16; }
+namespace {
+
+constexpr size_t kFewRows = 32;       // rows of x up to which the form for few rows is taken, if they are whole pieces
+struct ManyForm {
+  unsigned ntiles, chunks, runs, run;
+};
+ManyForm many_form(size_t M, size_t N, size_t K, int parts) {
+  const size_t rows = 16 * (size_t)many_mt(parts), nt = (N + 16 * kManyNT - 1) / (16 * kManyNT), mt = (M + rows - 1) / rows, frags = (K + kKT - 1) / kKT;
+  size_t want = (512 + nt * mt - 1) / (nt * mt);
+  const size_t most = (frags + kManyWaves - 1) / kManyWaves;
+  if (want > most) want = most;
+  if (want > 16) want = 16;
+  const size_t run = (frags + want - 1) / want;
+  return {(unsigned)nt, (unsigned)mt, (unsigned)((frags + run - 1) / run), (unsigned)run};
+}
+
+}  // namespace
+
+size_t w4_product_ws_bytes(size_t M, size_t N, size_t K) {
+  unsigned runs = 1;                   // (whatever the type)
+  for (int parts = 1; parts <= 3; ++parts) {
+    const unsigned n = many_form(M, N, K, parts).runs;
+    runs = n > runs ? n : runs;
+  }
+  return round_up(XDims(M, K, 3).bytes(), 256) + (runs > 1 ? (size_t)runs * M * N * sizeof(float) : 0);
+}
 
 int launch_w4_product(const void* x, size_t ldx, int xtype, const float* row_scale, const void* packed, size_t M, size_t N,
-                      size_t K, int group, const float* bias, void* y, size_t ldy, int ytype, void*, hipStream_t s) {
+                      size_t K, int group, const float* bias, void* y, size_t ldy, int ytype, void* ws, hipStream_t s) {
   const W4Dims d(N, K, group);
-  const size_t es = xtype == MQ_ROWS8 ? 1 : elem_bytes(xtype), piece = es == 1 ? 8 : 16 / es;
-  const W4Params p{x, row_scale, bias, static_cast<const uint8_t*>(packed), y, nullptr, ldx, ldy, (unsigned)M, (unsigned)N,
-                   (unsigned)K, (unsigned)d.frags, ytype,
+  const size_t es = xtype == MQ_ROWS8 ? 1 : elem_bytes(xtype), piece = 16 / es;
+  uint8_t* xs = static_cast<uint8_t*>(ws);
+  const W4Params p{x, row_scale, bias, static_cast<const uint8_t*>(packed), y,
+                   reinterpret_cast<float*>(xs + round_up(XDims(M, K, 3).bytes(), 256)), ldx, ldy, (unsigned)M,
+                   (unsigned)N, (unsigned)K, (unsigned)d.frags, ytype,
                    K % piece == 0 && ldx % piece == 0 && reinterpret_cast<uintptr_t>(x) % (piece * es) == 0};
-  const unsigned waves = d.frags < 8 ? (unsigned)d.frags : 8u;
   auto go = [&](auto xt, auto gr) {
-    auto sized = [&](auto mt) {
-      constexpr int MT = decltype(mt)::value;
-      const size_t chunks = (M + 16 * MT - 1) / (16 * MT);
-      if (!launchable(d.tiles * chunks, waves * kWave) || chunks > 65535) return (int)MQ_ERR_SHAPE;
-      hipLaunchKernelGGL((k_w4_product<decltype(xt)::value, decltype(gr)::value, MT>), dim3((unsigned)d.tiles, (unsigned)chunks),
-                         dim3(waves * kWave), waves * MT * 16 * 17 * sizeof(float), s, p);
-      return check_hip(hipGetLastError());
-    };
-    if (M <= 16) return sized(std::integral_constant<int, 1>{});
-    if (M <= 32) return sized(std::integral_constant<int, 2>{});
-    return sized(std::integral_constant<int, 4>{});
+    constexpr int XT = decltype(xt)::value, GROUP = decltype(gr)::value;
+    if (M <= kFewRows && p.vec) {
+      auto sized = [&](auto mt, auto nt) {
+        constexpr int MT = decltype(mt)::value, NT = decltype(nt)::value;
+        const size_t wgs = (d.tiles + NT - 1) / NT;
+        size_t waves = 4;
+        if (waves > d.frags) waves = d.frags;
+        if (!launchable(wgs, waves * kWave)) return (int)MQ_ERR_SHAPE;
+        hipLaunchKernelGGL((k_w4_few<XT, GROUP, MT, NT>), dim3((unsigned)wgs), dim3((unsigned)(waves * kWave)),
+                           waves * MT * 16 * (kKT * es > (NT * 16 + 1) * 4 ? kKT * es : (NT * 16 + 1) * 4), s, p);
+        return check_hip(hipGetLastError());
+      };
+      constexpr std::integral_constant<int, 1> one{};
+      constexpr std::integral_constant<int, 2> two{};
+      if (M <= 16) return d.tiles >= 512 ? sized(one, two) : sized(one, one);
+      return d.tiles >= 512 ? sized(two, two) : sized(two, one);
+    }
+    const ManyForm f = many_form(M, N, K, kXParts<XT>);
+    const size_t wgs = (size_t)f.ntiles * f.runs;
+    if (!launchable(wgs * f.chunks, kManyWaves * kWave) || f.chunks > 65535) return (int)MQ_ERR_SHAPE;
+    const size_t steps = XDims(M, K, 1).tiles * d.frags * 4;
+    hipLaunchKernelGGL(k_w4_x<XT>, dim3((unsigned)(steps < 16384 ? (steps + 3) / 4 : 4096)), dim3(256), 0, s, p, xs);
+    hipLaunchKernelGGL((k_w4_many<XT, GROUP>), dim3((unsigned)wgs, f.chunks), dim3(kManyWaves * kWave), 0, s, p, xs, f.runs, f.run);
+    if (f.runs > 1) hipLaunchKernelGGL(k_w4_join, dim3((unsigned)(M * N < 1048576 ? (M * N + 255) / 256 : 4096)), dim3(256), 0, s, p, f.runs);
+    return check_hip(hipGetLastError());
   };
   auto grouped = [&](auto xt) {
     if (group == 32) return go(xt, std::integral_constant<int, 32>{});
