@@ -176,13 +176,16 @@ __device__ __forceinline__ Raw<XT> raw8(const typename XElem<XT>::T* row, int k,
   for (int j = 0; j < 8; ++j) r.v[j] = k + j < K ? row[k + j] : (typename XElem<XT>::T)0;
   return r;
 }
+// Eight signed bytes in the order in which eight codes come out of a word.
+__device__ __forceinline__ long in_code_order(uint2 b) {
+  return __builtin_bit_cast(long, make_uint2(__builtin_amdgcn_perm(b.y, b.x, 0x05010400u), __builtin_amdgcn_perm(b.y, b.x, 0x07030602u)));
+}
 // The same as operand parts.
 template <int XT>
 __device__ __forceinline__ void x_parts(const Raw<XT>& r, typename Operand<XT>::Piece (&part)[Operand<XT>::NP]) {
   constexpr int NP = Operand<XT>::NP;
-  if constexpr (XT == MQ_ROWS8) {       // in the order of the codes
-    const uint2 b = __builtin_bit_cast(uint2, r);
-    part[0] = __builtin_bit_cast(long, make_uint2(__builtin_amdgcn_perm(b.y, b.x, 0x05010400u), __builtin_amdgcn_perm(b.y, b.x, 0x07030602u)));
+  if constexpr (XT == MQ_ROWS8) {
+    part[0] = in_code_order(__builtin_bit_cast(uint2, r));
   } else if constexpr (NP == 1) {
     part[0] = __builtin_bit_cast(bf8, r);
   } else {
@@ -199,7 +202,8 @@ __device__ __forceinline__ void x_parts(const Raw<XT>& r, typename Operand<XT>::
 // Few rows, of whole 16-byte pieces.  A workgroup has 16 NT rows of the parameter and 16 MT rows of x; its waves take the
 // fragments in turn, the next ones' loads ahead of this one's products, and join in LDS.  A lane of an operand has a row of x of its
 // own; loaded like that, every lane would be an access to the nearest cache of its own (64 a load instead of 8 .. 16, which bound
-// this form).  So x comes in lines, and each wave turns its lines in a part of LDS.
+// this form).  So x comes in lines, and each wave turns its lines, as operand parts, in a part of LDS; of rows that are not there
+// nothing is turned.
 template <int XT, int GROUP, int MT, int NT>
 __global__ __launch_bounds__(512) void k_w4_few(const W4Params p) {
   using T = typename XElem<XT>::T;
@@ -214,12 +218,14 @@ __global__ __launch_bounds__(512) void k_w4_few(const W4Params p) {
 #pragma unroll
   for (int n = 0; n < NT; ++n) {                 // (a tile that is not there repeats the last)
     const size_t t = min(tile + n, (unsigned)d.tiles - 1);
-    frag[n] = p.packed + t * d.frags * 1024 + lane * 16;
-    scales[n] = reinterpret_cast<const uint32_t*>(p.packed + d.scales_at()) + t * d.groups * kNT + col;
+    frag[n] = p.packed + t * d.frags * 1024;
+    scales[n] = reinterpret_cast<const uint32_t*>(p.packed + d.scales_at()) + t * d.groups * kNT;
   }
-  // a row's elements of a fragment are SLOTS pieces of 16 bytes; LINES rows to a load; piece j of row r lies at place j ^ (r & 7)
+  // a row's elements of a fragment are SLOTS pieces of 16 bytes, LINES rows to a load; of its parts PSLOTS pieces each, piece j of
+  // row r at place j ^ (r & 7)
   constexpr unsigned SLOTS = 8 * sizeof(T), LINES = kWave / SLOTS, XI = 16 / LINES, PER = 16 / sizeof(T);
-  u4* const turn = reinterpret_cast<u4*>(smem) + (size_t)wave * MT * 16 * SLOTS;
+  constexpr unsigned PSLOTS = XT == MQ_ROWS8 ? 8 : 16;
+  u4* const turn = reinterpret_cast<u4*>(smem) + (size_t)wave * MT * NP * 16 * PSLOTS;
   using Op = Operand<XT>;
   using Piece = typename Op::Piece;
   const Piece ones = Op::ones();
@@ -233,9 +239,9 @@ __global__ __launch_bounds__(512) void k_w4_few(const W4Params p) {
     f = min(f, p.frags - 1);
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      w[at][n] = *reinterpret_cast<const u4*>(frag[n] + (size_t)f * 1024);
+      w[at][n] = *reinterpret_cast<const u4*>(frag[n] + (size_t)f * 1024 + lane * 16);
 #pragma unroll
-      for (int g = 0; g < GF; ++g) sc[at][n][g] = scales[n][((size_t)f * GF + g) * kNT];
+      for (int g = 0; g < GF; ++g) sc[at][n][g] = (scales[n] + ((size_t)f * GF + g) * kNT)[col];
     }
   };
   auto load_x = [&](unsigned f) __attribute__((always_inline)) {
@@ -255,21 +261,38 @@ __global__ __launch_bounds__(512) void k_w4_few(const W4Params p) {
     for (int t = 0; t < MT; ++t)
 #pragma unroll
       for (unsigned i = 0; i < XI; ++i) {
-        const unsigned r = i * LINES + lane / SLOTS;
-        turn[(16 * t + r) * SLOTS + ((lane % SLOTS) ^ (r & 7))] = x[t][i];
+        if (m0 + 16 * t + i * LINES >= p.M) continue;
+        const unsigned r = i * LINES + lane / SLOTS, j = lane % SLOTS;
+        if constexpr (NP == 1) {
+          turn[(16 * t + r) * PSLOTS + (j ^ (r & 7))] = x[t][i];
+        } else {
+          typedef T tw __attribute__((ext_vector_type(PER)));
+          typedef __bf16 bw __attribute__((ext_vector_type(PER)));
+          const tw v = __builtin_bit_cast(tw, x[t][i]);
+          bw part[NP];
+#pragma unroll
+          for (unsigned e = 0; e < PER; ++e) {
+            __bf16 b[NP];
+            split_bf16<NP>((float)v[e], b);
+#pragma unroll
+            for (int k = 0; k < NP; ++k) part[k][e] = b[k];
+          }
+#pragma unroll
+          for (int k = 0; k < NP; ++k) {           // (binary32: half a place)
+            u4* const to = turn + ((t * NP + k) * 16 + r) * PSLOTS + ((j * PER / 8) ^ (r & 7));
+            reinterpret_cast<bw*>(to)[PER == 8 ? 0 : j % 2] = part[k];
+          }
+        }
       }
   };
-  // elements 32 step + 8 grp .. of row 16 t + col
-  auto read_x = [&](int t, int step) __attribute__((always_inline)) {
-    const u4* const at = turn + (16 * t + col) * SLOTS;
-    if constexpr (sizeof(T) == 1) {
-      const uint2* const piece = reinterpret_cast<const uint2*>(at + ((2 * step + grp / 2) ^ (col & 7)));
-      return __builtin_bit_cast(Raw<XT>, piece[grp % 2]);
-    } else if constexpr (sizeof(T) == 2) {
-      return __builtin_bit_cast(Raw<XT>, at[(4 * step + grp) ^ (col & 7)]);
+  // part k of elements 32 step + 8 grp .. of row 16 t + col
+  auto read_x = [&](int t, int k, int step) __attribute__((always_inline)) {
+    const u4* const at = turn + ((t * NP + k) * 16 + col) * PSLOTS;
+    if constexpr (XT == MQ_ROWS8) {
+      const uint2 b = reinterpret_cast<const uint2*>(at + ((2 * step + grp / 2) ^ (col & 7)))[grp % 2];
+      return in_code_order(b);
     } else {
-      struct Two { u4 a, b; };
-      return __builtin_bit_cast(Raw<XT>, Two{at[(8 * step + 2 * grp) ^ (col & 7)], at[(8 * step + 2 * grp + 1) ^ (col & 7)]});
+      return __builtin_bit_cast(bf8, at[(4 * step + grp) ^ (col & 7)]);
     }
   };
   auto multiply = [&](int at) __attribute__((always_inline)) {
@@ -284,13 +307,12 @@ __global__ __launch_bounds__(512) void k_w4_few(const W4Params p) {
         for (int n = 0; n < NT; ++n) c[n] = Op::codes(w[at][n][step]);
 #pragma unroll
         for (int t = 0; t < MT; ++t) {
-          Piece xp[NP];
-          x_parts<XT>(read_x(t, step), xp);
 #pragma unroll
           for (int j = NP - 1; j >= 0; --j) {
+            const Piece xp = read_x(t, j, step);
 #pragma unroll
-            for (int n = 0; n < NT; ++n) acc[n][t] = Op::mfma(xp[j], c[n], acc[n][t]);
-            sum[t] = Op::mfma(xp[j], ones, sum[t]);
+            for (int n = 0; n < NT; ++n) acc[n][t] = Op::mfma(xp, c[n], acc[n][t]);
+            sum[t] = Op::mfma(xp, ones, sum[t]);
           }
         }
       }
@@ -344,11 +366,11 @@ __global__ __launch_bounds__(512) void k_w4_few(const W4Params p) {
 // Many rows.  x comes as operand parts and sums of groups from a launch of its own (each is used by every row tile of the
 // parameter); a workgroup has 16 NT x 16 MT results and a run of fragments, its waves take the run's fragments in turn and join in
 // LDS, runs through the workspace.
-// (of three parts of x only half as many rows fit the registers beside those of the next step)
-constexpr int many_mt(int parts) { return parts == 3 ? 2 : 4; }
+// (of several parts of x only half as many rows fit the registers beside those of the next step)
+constexpr int many_mt(int parts) { return parts == 1 ? 4 : 2; }
 constexpr int kManyNT = 4, kManyWaves = 4;
 
-// operand parts [row tile][fragment][step][part][lane], 16 bytes each (8 of 8-bit rows), then sums [row tile][32 elements][16 rows]
+// operand parts [row tile][fragment][step][part][lane], 16 bytes each (8 of 8-bit rows), then sums [row tile][group][16 rows]
 struct XDims {
   size_t tiles, frags;
   int parts;
@@ -357,45 +379,52 @@ struct XDims {
   __host__ __device__ size_t bytes() const { return sums_at() + tiles * frags * 4 * 16 * sizeof(float); }
 };
 
-template <int XT>
+// a wave for each row tile and fragment
+template <int XT, int GROUP>
 __global__ __launch_bounds__(256) void k_w4_x(const W4Params p, uint8_t* to) {
-  constexpr int NP = kXParts<XT>;
+  using T = typename XElem<XT>::T;
+  using Piece = typename Operand<XT>::Piece;
+  constexpr int NP = kXParts<XT>, SG = GROUP / 32;
   const XDims x(p.M, p.K, NP);
   const unsigned lane = threadIdx.x % kWave, col = lane % 16, grp = lane / 16;
-  const size_t steps = x.tiles * x.frags * 4;
-  for (size_t s = (size_t)blockIdx.x * 4 + threadIdx.x / kWave; s < steps; s += (size_t)gridDim.x * 4) {
-    const size_t tile = s / (x.frags * 4);
-    const int k = (int)(s % (x.frags * 4) * 32 + 8 * grp);
-    const size_t m = tile * 16 + col;
-    const typename XElem<XT>::T* row = static_cast<const typename XElem<XT>::T*>(p.x) + (m < p.M ? m : p.M - 1) * p.ldx;
-    Raw<XT> r{};
-    if (p.vec) {                        // (rows are whole 16-byte pieces)
-      using T = typename XElem<XT>::T;
-      typedef T t8 __attribute__((ext_vector_type(8)));
-      typedef t8 unaligned __attribute__((aligned(sizeof(T) == 1 ? 8 : 16)));
-      if (k + 8 <= (int)p.K) r = __builtin_bit_cast(Raw<XT>, *reinterpret_cast<const unaligned*>(row + k));
-      else if (k < (int)p.K) r = raw8<XT>(row, k, (int)p.K);
-    } else {
-      r = raw8<XT>(row, k, (int)p.K);
-    }
-    using Piece = typename Operand<XT>::Piece;
-    Piece part[NP];
-    x_parts<XT>(r, part);
-    Piece* dst = reinterpret_cast<Piece*>(to) + s * NP * kWave + lane;
+  const size_t all = x.tiles * x.frags;
+  for (size_t s = (size_t)blockIdx.x * 4 + threadIdx.x / kWave; s < all; s += (size_t)gridDim.x * 4) {
+    const size_t m = s / x.frags * 16 + col;
+    const T* row = static_cast<const T*>(p.x) + (m < p.M ? m : p.M - 1) * p.ldx;
+    Raw<XT> r[4] = {};
 #pragma unroll
-    for (int i = 0; i < NP; ++i) dst[i * kWave] = part[i];
+    for (int i = 0; i < 4; ++i) {
+      const int k = (int)(s % x.frags * kKT + 32 * i + 8 * grp);
+      if (p.vec && k + 8 <= (int)p.K) {              // (rows are whole 16-byte pieces)
+        typedef T t8 __attribute__((ext_vector_type(8), aligned(sizeof(T) == 1 ? 8 : 16)));
+        r[i] = __builtin_bit_cast(Raw<XT>, *reinterpret_cast<const t8*>(row + k));
+      } else {
+        r[i] = raw8<XT>(row, k, (int)p.K);
+      }
+    }
     float sum = 0.f;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) sum += (float)r.v[j];
-    sum = across16_f(across32_f(sum, [](float a, float b) { return a + b; }), [](float a, float b) { return a + b; });
-    if (grp == 0) reinterpret_cast<float*>(to + x.sums_at())[s * 16 + col] = sum;
+    for (int i = 0; i < 4; ++i) {
+      Piece part[NP];
+      x_parts<XT>(r[i], part);
+      Piece* dst = reinterpret_cast<Piece*>(to) + (s * 4 + i) * NP * kWave + lane;
+#pragma unroll
+      for (int k = 0; k < NP; ++k) dst[k * kWave] = part[k];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sum += (float)r[i].v[j];
+      if (i % SG != SG - 1) continue;
+      auto add = [](float a, float b) { return a + b; };
+      sum = across16_f(across32_f(sum, add), add);
+      if (grp == 0) reinterpret_cast<float*>(to + x.sums_at())[(s * (4 / SG) + i / SG) * 16 + col] = sum;
+      sum = 0.f;
+    }
   }
 }
 
 template <int XT, int GROUP>
 __global__ __launch_bounds__(kManyWaves * kWave, 2) void k_w4_many(const W4Params p, const uint8_t* xs, unsigned runs, unsigned run) {
   constexpr int NP = kXParts<XT>, GF = kKT / GROUP, SG = GROUP / 32, MT = many_mt(NP), NT = kManyNT;
-  __shared__ float lds[MT * 16][NT * 16 + 1];
+  extern __shared__ float lds[];                 // [waves][MT 16][NT 16 + 1]
   const unsigned lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), col = lane % 16, grp = lane / 16;
   // neighbouring workgroups share rows of x: those of one XCD its parts
   const unsigned ntiles = gridDim.x / runs, nt = blockIdx.x % ntiles, k0 = blockIdx.x / ntiles * run, k1 = min(k0 + run, p.frags);
@@ -407,8 +436,8 @@ __global__ __launch_bounds__(kManyWaves * kWave, 2) void k_w4_many(const W4Param
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
     const size_t t = min(nt * NT + n, (unsigned)d.tiles - 1);
-    frag[n] = p.packed + t * d.frags * 1024 + lane * 16;
-    scales[n] = reinterpret_cast<const uint32_t*>(p.packed + d.scales_at()) + t * d.groups * kNT + col;
+    frag[n] = p.packed + t * d.frags * 1024;
+    scales[n] = reinterpret_cast<const uint32_t*>(p.packed + d.scales_at()) + t * d.groups * kNT;
   }
   using Op = Operand<XT>;
   using Piece = typename Op::Piece;
@@ -417,22 +446,27 @@ __global__ __launch_bounds__(kManyWaves * kWave, 2) void k_w4_many(const W4Param
 #pragma unroll
   for (int t = 0; t < MT; ++t) {
     const size_t tile = min(m0 + t, (unsigned)xd.tiles - 1);
-    xp[t] = reinterpret_cast<const Piece*>(xs) + tile * xd.frags * 4 * NP * kWave + lane;
-    xsum[t] = reinterpret_cast<const float*>(xs + xd.sums_at()) + tile * xd.frags * 4 * 16 + 4 * grp;
+    xp[t] = reinterpret_cast<const Piece*>(xs) + tile * xd.frags * 4 * NP * kWave;
+    xsum[t] = reinterpret_cast<const float*>(xs + xd.sums_at()) + tile * xd.frags * GF * 16;
   }
   float y[NT][MT][4] = {};
-  // codes of the next fragment and x of the next step are on their way
+  // codes and scales of the next fragment and x of the next step are on their way
   u4 w[2][NT];
+  unsigned sc[2][NT][GF];
   Piece x[2][MT][NP];
   auto load = [&](int at, unsigned f) __attribute__((always_inline)) {
 #pragma unroll
-    for (int n = 0; n < NT; ++n) w[at][n] = *reinterpret_cast<const u4*>(frag[n] + (size_t)f * 1024);
+    for (int n = 0; n < NT; ++n) {
+      w[at][n] = *reinterpret_cast<const u4*>(frag[n] + (size_t)f * 1024 + lane * 16);
+#pragma unroll
+      for (int g = 0; g < GF; ++g) sc[at][n][g] = (scales[n] + ((size_t)f * GF + g) * kNT)[col];
+    }
   };
   auto load_x = [&](int at, unsigned f, int step) __attribute__((always_inline)) {
 #pragma unroll
     for (int t = 0; t < MT; ++t)
 #pragma unroll
-      for (int j = 0; j < NP; ++j) x[at][t][j] = xp[t][(((size_t)f * 4 + step) * NP + j) * kWave];
+      for (int j = 0; j < NP; ++j) x[at][t][j] = (xp[t] + (((size_t)f * 4 + step) * NP + j) * kWave)[lane];
   };
   auto multiply = [&](int at, unsigned f, unsigned next) __attribute__((always_inline)) {
     typename Op::Acc acc[NT][MT];
@@ -441,11 +475,9 @@ __global__ __launch_bounds__(kManyWaves * kWave, 2) void k_w4_many(const W4Param
     for (int step = 0; step < 4; ++step) {
       const int g = step / SG;
       load_x((step + 1) % 2, step < 3 ? f : next, (step + 1) % 4);
+      if (step % SG == 0)
 #pragma unroll
-      for (int t = 0; t < MT; ++t) {
-        const v4f part = *reinterpret_cast<const v4f*>(xsum[t] + ((size_t)f * 4 + step) * 16);
-        sum[t] = step % SG == 0 ? part : sum[t] + part;
-      }
+        for (int t = 0; t < MT; ++t) sum[t] = reinterpret_cast<const v4f*>(xsum[t] + ((size_t)f * GF + g) * 16)[grp];
       Piece c[NT];
 #pragma unroll
       for (int n = 0; n < NT; ++n) c[n] = Op::codes(w[at][n][step]);
@@ -459,8 +491,7 @@ __global__ __launch_bounds__(kManyWaves * kWave, 2) void k_w4_many(const W4Param
       if (step % SG != SG - 1) continue;
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        const unsigned sc = scales[n][((size_t)f * GF + g) * kNT];
-        const float s = scale_of(sc), z = offset_of<XT>(sc);
+        const float s = scale_of(sc[at][n][g]), z = offset_of<XT>(sc[at][n][g]);
 #pragma unroll
         for (int t = 0; t < MT; ++t)
 #pragma unroll
@@ -474,7 +505,7 @@ __global__ __launch_bounds__(kManyWaves * kWave, 2) void k_w4_many(const W4Param
     load_x(0, f, 0);
   }
   while (f < k1) {
-    unsigned next = min(f + kManyWaves, k1 - 1);
+    unsigned next = min(f + kManyWaves, k1 - 1);      // (past the run's end: something that is there)
     load(1, next);
     multiply(0, f, next);
     f += kManyWaves;
@@ -484,23 +515,19 @@ __global__ __launch_bounds__(kManyWaves * kWave, 2) void k_w4_many(const W4Param
     multiply(1, f, next);
     f += kManyWaves;
   }
-  for (unsigned v = 0; v < kManyWaves; ++v) {    // one wave after the other
-    if (v == wave)
+  constexpr int PITCH = NT * 16 + 1;
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
+  for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int t = 0; t < MT; ++t)
+    for (int t = 0; t < MT; ++t)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            float& to = lds[t * 16 + 4 * grp + r][n * 16 + col];
-            to = v == 0 ? y[n][t][r] : to + y[n][t][r];
-          }
-    __syncthreads();
-  }
+      for (int r = 0; r < 4; ++r) lds[((wave * MT + t) * 16 + 4 * grp + r) * PITCH + n * 16 + col] = y[n][t][r];
+  __syncthreads();
   for (unsigned i = threadIdx.x; i < MT * 16 * NT * 16; i += kManyWaves * kWave) {
     const unsigned mm = i / (NT * 16), nn = i % (NT * 16), m = m0 * 16 + mm, n = nt * NT * 16 + nn;
     if (m >= p.M || n >= p.N) continue;
-    float v = lds[mm][nn];
+    float v = 0.f;
+    for (unsigned u = 0; u < kManyWaves; ++u) v += lds[(u * MT * 16 + mm) * PITCH + nn];
     if (runs > 1) {
       p.part[((size_t)(k0 / run) * p.M + m) * p.N + n] = v;
       continue;
@@ -549,13 +576,14 @@ int launch_w4_unpack(const void* packed, size_t N, size_t K, int group, float* w
 
 namespace {
 
-constexpr size_t kFewRows = 32;       // rows of x up to which the form for few rows is taken, if they are whole pieces
+// rows of x up to which the form for few rows is taken, if they are whole pieces (more parts fill LDS)
+constexpr size_t few_rows(int parts) { return parts == 1 ? 32 : 16; }
 struct ManyForm {
   unsigned ntiles, chunks, runs, run;
 };
 ManyForm many_form(size_t M, size_t N, size_t K, int parts) {
   const size_t rows = 16 * (size_t)many_mt(parts), nt = (N + 16 * kManyNT - 1) / (16 * kManyNT), mt = (M + rows - 1) / rows, frags = (K + kKT - 1) / kKT;
-  size_t want = (512 + nt * mt - 1) / (nt * mt);
+  size_t want = nt * mt < 512 ? 512 / (nt * mt) : 1;      // two workgroups to a compute unit
   const size_t most = (frags + kManyWaves - 1) / kManyWaves;
   if (want > most) want = most;
   if (want > 16) want = 16;
@@ -585,28 +613,37 @@ int launch_w4_product(const void* x, size_t ldx, int xtype, const float* row_sca
                    K % piece == 0 && ldx % piece == 0 && reinterpret_cast<uintptr_t>(x) % (piece * es) == 0};
   auto go = [&](auto xt, auto gr) {
     constexpr int XT = decltype(xt)::value, GROUP = decltype(gr)::value;
-    if (M <= kFewRows && p.vec) {
+    if (M <= few_rows(kXParts<XT>) && p.vec) {
       auto sized = [&](auto mt, auto nt) {
         constexpr int MT = decltype(mt)::value, NT = decltype(nt)::value;
         const size_t wgs = (d.tiles + NT - 1) / NT;
         size_t waves = 4;
+        constexpr size_t turned = XT == MQ_ROWS8 ? kKT : 2 * kKT * kXParts<XT>;         // bytes of a row in LDS
         if (waves > d.frags) waves = d.frags;
         if (!launchable(wgs, waves * kWave)) return (int)MQ_ERR_SHAPE;
         hipLaunchKernelGGL((k_w4_few<XT, GROUP, MT, NT>), dim3((unsigned)wgs), dim3((unsigned)(waves * kWave)),
-                           waves * MT * 16 * (kKT * es > (NT * 16 + 1) * 4 ? kKT * es : (NT * 16 + 1) * 4), s, p);
+                           waves * MT * 16 * (turned > (NT * 16 + 1) * 4 ? turned : (NT * 16 + 1) * 4), s, p);
         return check_hip(hipGetLastError());
       };
       constexpr std::integral_constant<int, 1> one{};
       constexpr std::integral_constant<int, 2> two{};
-      if (M <= 16) return d.tiles >= 512 ? sized(one, two) : sized(one, one);
-      return d.tiles >= 512 ? sized(two, two) : sized(two, one);
+      if constexpr (kXParts<XT> == 1) {
+        if (M > 16) return sized(two, one);
+      }
+      return sized(one, one);
     }
     const ManyForm f = many_form(M, N, K, kXParts<XT>);
     const size_t wgs = (size_t)f.ntiles * f.runs;
     if (!launchable(wgs * f.chunks, kManyWaves * kWave) || f.chunks > 65535) return (int)MQ_ERR_SHAPE;
-    const size_t steps = XDims(M, K, 1).tiles * d.frags * 4;
-    hipLaunchKernelGGL(k_w4_x<XT>, dim3((unsigned)(steps < 16384 ? (steps + 3) / 4 : 4096)), dim3(256), 0, s, p, xs);
-    hipLaunchKernelGGL((k_w4_many<XT, GROUP>), dim3((unsigned)wgs, f.chunks), dim3(kManyWaves * kWave), 0, s, p, xs, f.runs, f.run);
+    const size_t waves = XDims(M, K, 1).tiles * d.frags;
+    hipLaunchKernelGGL((k_w4_x<XT, GROUP>), dim3((unsigned)(waves < 16384 ? (waves + 3) / 4 : 4096)), dim3(256), 0, s, p, xs);
+    constexpr size_t lds = kManyWaves * many_mt(kXParts<XT>) * 16 * (kManyNT * 16 + 1) * sizeof(float);
+    auto kern = k_w4_many<XT, GROUP>;
+    if (lds > 65536) {
+      const int rc = check_hip(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+      if (rc != MQ_OK) return rc;
+    }
+    hipLaunchKernelGGL(kern, dim3((unsigned)wgs, f.chunks), dim3(kManyWaves * kWave), lds, s, p, xs, f.runs, f.run);
     if (f.runs > 1) hipLaunchKernelGGL(k_w4_join, dim3((unsigned)(M * N < 1048576 ? (M * N + 255) / 256 : 4096)), dim3(256), 0, s, p, f.runs);
     return check_hip(hipGetLastError());
   };
