@@ -172,13 +172,24 @@ __device__ __forceinline__ void each_part(const ChunkParams& p, F f) {
 //
 // A workgroup has 32 rows; its waves take the blocks in turn, each straight from memory, and join in LDS.
 
+// LDS of a wave's block of keys and values, loads of 1 KB of either, and waves of a workgroup at most: 160 KB hold its blocks and
+// the queries.
+template <int DC>
+constexpr unsigned kWaveBytes = 2 * kKvBlock * 64 * DC;
+template <int DC>
+constexpr int kLoads = 4 * DC;
+constexpr unsigned few_waves(int parts, int dc) { return dc == 4 && parts > 1 ? 3 : kWaves; }
+// s_waitcnt's operand for at most n loads on their way, nothing else waited for but LDS
+constexpr int waitcnt_loads(int n) { return (n & 15) | (n >> 4) << 14 | 0x0070; }
+
 template <int DT, int DC>             // DC: 64-column pieces of a key
 __device__ __forceinline__ void few_rows(const ChunkParams& p, int vec, const LinePart& part, unsigned to_part) {
   using T = typename Elem<DT>::T;
   constexpr int NP = kParts<DT>;
   constexpr int NK = 2 * DC, ND = 2 * DC;      // 32-column pieces of a key, 32-column pieces of a value at most
-  extern __shared__ __attribute__((aligned(16))) char smem[];
-  bf8* const ql = reinterpret_cast<bf8*>(smem);                                  // [NP][NK][2][64 lanes]
+  constexpr int U = NK * 2;                    // units of 8 elements of a query
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  bf8* const ql = reinterpret_cast<bf8*>(smem);                                  // [NP][U][64 lanes], then each wave's blocks
   float* const sums = reinterpret_cast<float*>(smem);                            // [32][ND 32 + 1], afterwards
   __shared__ unsigned fac[kRows];               // largest magnitudes, as bits
   __shared__ float stat[2][kWaves][kRows];
@@ -210,32 +221,55 @@ __device__ __forceinline__ void few_rows(const ChunkParams& p, int vec, const Li
   bool there = true, there_next = true;
   size_t at_next = 0;
   float2 am_next;
-  u4 kf[2][NK], vf[ND][2];
+  // this wave's part of LDS: keys as they lie, rows of dk bytes, then values, rows of 64; piece j of 16 bytes of row r lies at place
+  // j ^ turned(r), so that eight rows' pieces are on different banks
+  char* const mine_lds = smem + NP * U * 1024 + wave * kWaveBytes<DC>;
+  auto turned = [](unsigned r) { return DC % 2 == 0 ? r & 7 : r >> 1 & 3; };
   auto find = [&](unsigned i) {
     if (i % kWave == 0 && i > 0) ids = look(i);
     const int block = __builtin_amdgcn_readlane(ids, i % kWave);
     there_next = block >= 0 && (size_t)block < p.blocks;
     at_next = (size_t)(there_next ? block : 0) * p.kv_heads + kvh;
   };
+  auto bring = [&](const int8_t* from, unsigned to) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
+                                     (__attribute__((address_space(3))) void*)(mine_lds + to), 16, 0, 0);
+  };
+  // kLoads loads each, whatever the width
   auto bring_keys = [&] {
-    const int8_t* kp = p.keys + at_next * kKvBlock * dk + (size_t)col * dk + grp * 16;
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int c = 0; c < NK; ++c) kf[t][c] = *reinterpret_cast<const u4*>(kp + (size_t)t * 32 * dk + c * 32);
+    const int8_t* kp = p.keys + at_next * kKvBlock * dk;
     am_next = reinterpret_cast<const float2*>(p.amax)[at_next];
+#pragma unroll
+    for (int i = 0; i < kLoads<DC>; ++i) {
+      const unsigned piece = i * kWave + lane, r = piece / (4 * DC), j = piece % (4 * DC);
+      bring(kp + (size_t)r * dk + (j ^ turned(r)) * 16, i * 1024);
+    }
   };
   auto bring_values = [&] {
-    const int8_t* vp = p.values + at_next * dv * kKvBlock + grp * 16;
+    const int8_t* vp = p.values + at_next * dv * kKvBlock;
 #pragma unroll
-    for (int t = 0; t < ND; ++t)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) vf[t][h] = *reinterpret_cast<const u4*>(vp + (size_t)min(32 * t + col, dv - 1) * kKvBlock + 32 * h);
+    for (int i = 0; i < kLoads<DC>; ++i) {                 // (16 rows each; those that are not there repeat the last)
+      const unsigned at = min((unsigned)i, dv / 16 - 1), r = at * 16 + lane / 4;
+      bring(vp + r * kKvBlock + ((lane % 4) ^ (r >> 1 & 3)) * 16, kKvBlock * 64 * DC + at * 1024);
+    }
+  };
+  auto key_piece = [&](int t, int c) {                     // row 32 t + col, bytes 32 c + 16 grp ..
+    const unsigned r = 32 * t + col;
+    return *reinterpret_cast<const u4*>(mine_lds + r * (64 * DC) + ((2 * c + grp) ^ turned(r)) * 16);
+  };
+  auto value_piece = [&](int t, int h) {                   // row 32 t + col, bytes 16 grp + 32 h ..
+    const unsigned r = 32 * t + col;
+    return *reinterpret_cast<const u4*>(mine_lds + kKvBlock * 64 * DC + r * kKvBlock + ((grp + 2 * h) ^ (r >> 1 & 3)) * 16);
+  };
+  // until at most N of this wave's loads are on their way, and all that it read from LDS is there
+  auto arrived = [&](auto n) {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(waitcnt_loads(decltype(n)::value));
+    asm volatile("" ::: "memory");
   };
 
-  // queries: a power of two off each row, so that its largest element is 1 .. 2, then parts in operand order.  A thread has U units
-  // of 8 elements: unit u of lane l is elements 32 (u / 2) + 16 (l / 32) + 8 (u % 2) .. of row l % 32
-  constexpr int U = NK * 2;
+  // queries: a power of two off each row, so that its largest element is 1 .. 2, then parts in operand order.  Unit u of lane l is
+  // elements 32 (u / 2) + 16 (l / 32) + 8 (u % 2) .. of row l % 32
   {
     const unsigned rr = min(col, tile.rows - 1);
     const uint2 at = row_at(rr);
@@ -302,12 +336,17 @@ __device__ __forceinline__ void few_rows(const ChunkParams& p, int vec, const Li
     const float2 am = am_next;
     there = there_next;
     if (i + 1 < mine) find(i + 1);
+    arrived(std::integral_constant<int, kLoads<DC>>{});    // (all but this block's values)
     v16f sc[2] = {};
+    u4 kf[2];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       bf8 a[2];
 #pragma unroll
-      for (int t = 0; t < 2; ++t) a[t] = bf16_of_bytes(kf[t][u / 2][2 * (u % 2)], kf[t][u / 2][2 * (u % 2) + 1]);
+      for (int t = 0; t < 2; ++t) {
+        if (u % 2 == 0) kf[t] = key_piece(t, u / 2);
+        a[t] = bf16_of_bytes(kf[t][2 * (u % 2)], kf[t][2 * (u % 2) + 1]);
+      }
 #pragma unroll
       for (int k = NP - 1; k >= 0; --k) {
         const bf8 b = ql[(k * U + u) * kWave + lane];
@@ -315,6 +354,7 @@ __device__ __forceinline__ void few_rows(const ChunkParams& p, int vec, const Li
         for (int t = 0; t < 2; ++t) sc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[t], b, sc[t], 0, 0, 0);
       }
     }
+    arrived(std::integral_constant<int, kLoads<DC>>{});    // (nothing is read from the keys' place any more)
     if (i + 1 < mine) bring_keys();
     if (!there || (pg + 1) * kKvBlock > least) {
       const long long room = (long long)mine_sees - (long long)pg * kKvBlock - 4 * (int)grp;
@@ -344,11 +384,11 @@ __device__ __forceinline__ void few_rows(const ChunkParams& p, int vec, const Li
     const float fv = there ? am.y * (1.f / 127.f) : 0.f;
     const bool nothing = !there || (FOLD && fv < 1.2e-38f);      // values that are all zero (or below any normal number)
     const float lift = nothing || !FOLD ? 0.f : __builtin_amdgcn_logf(fv), base = lift - finite_or_0(acc_top);
-    if (FOLD && nothing) {
-#pragma unroll
-      for (int t = 0; t < ND; ++t) vf[t][0] = vf[t][1] = u4{};
-    }
+    const unsigned any = FOLD && nothing ? 0u : ~0u;
     float sum = 0.f;
+    u4 vf[ND][2];
+    if (i + 1 < mine) arrived(std::integral_constant<int, kLoads<DC>>{});      // (all but the next block's keys)
+    else arrived(std::integral_constant<int, 0>{});
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       bf8 pr[NP];
@@ -366,13 +406,20 @@ __device__ __forceinline__ void few_rows(const ChunkParams& p, int vec, const Li
       }
 #pragma unroll
       for (int t = 0; t < ND; ++t) {
-        const bf8 a = bf16_of_bytes(vf[t][0][j], vf[t][1][j]);
+        if (j == 0) {
+          vf[t][0] = value_piece(t, 0);
+          vf[t][1] = value_piece(t, 1);
+        }
+        const bf8 a = bf16_of_bytes(vf[t][0][j] & any, vf[t][1][j] & any);
 #pragma unroll
         for (int k = NP - 1; k >= 0; --k) acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, pr[k], acc[t], 0, 0, 0);
       }
     }
     total = FOLD ? fmaf(sum, nothing ? 1.f : __fdiv_rn(1.f, fv), total) : total + sum;
-    if (i + 1 < mine) bring_values();
+    if (i + 1 < mine) {
+      arrived(std::integral_constant<int, kLoads<DC>>{});
+      bring_values();
+    }
   }
   total = across32_f(total, fadd2);
 
@@ -951,14 +998,23 @@ int launch_chunk_attention(const mq_kv_cache& cache, const int32_t* table, size_
         }
         return check_hip(hipGetLastError());
       }
-      constexpr size_t ql = kParts<DT> * DC * 4 * kWave * 16, sums = kRows * (DC * 64 + 1) * sizeof(float), lds = ql > sums ? ql : sums;
-      if (!form.shares) {
-        const unsigned waves = (unsigned)(blocks < kWaves ? blocks : kWaves);
-        hipLaunchKernelGGL((k_chunk_few<DT, DC, false>), dim3((unsigned)tiles), dim3(waves * kWave), lds, s, p, vec);
+      constexpr unsigned most_waves = few_waves(kParts<DT>, DC);
+      // (the sums' place afterwards is smaller)
+      auto lds_of = [](unsigned waves) { return (size_t)kParts<DT> * DC * 4096 + waves * kWaveBytes<DC>; };
+      auto go = [&](auto kern, unsigned grid, unsigned waves) {
+        const size_t lds = lds_of(waves);
+        if (lds > 65536) {
+          const int rc = check_hip(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+          if (rc != MQ_OK) return rc;
+        }
+        hipLaunchKernelGGL(kern, dim3(grid), dim3(waves * kWave), lds, s, p, vec);
         return check_hip(hipGetLastError());
+      };
+      if (!form.shares) {
+        return go(k_chunk_few<DT, DC, false>, (unsigned)tiles, (unsigned)(blocks < most_waves ? blocks : most_waves));
       }
       hipLaunchKernelGGL(k_chunk_plan<kRows>, dim3(1), dim3(kPlan), 0, s, p);
-      hipLaunchKernelGGL((k_chunk_few<DT, DC, true>), dim3(form.groups), dim3(kWaves * kWave), lds, s, p, vec);
+      if (const int rc = go(k_chunk_few<DT, DC, true>, form.groups, most_waves); rc != MQ_OK) return rc;
       hipLaunchKernelGGL((k_chunk_join<DT, kRows>), dim3((unsigned)joins), dim3(256), 0, s, p, form.groups);
       return check_hip(hipGetLastError());
     };

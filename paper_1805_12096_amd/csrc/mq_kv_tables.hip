@@ -4,6 +4,9 @@
 // takes the minimum of what its users want of it, 0 for reading (or keeping), b + 1 for row b that will write to it.  Minima of
 // integers do not depend on their order.  A row keeps a block that it writes to iff the word is its own; blocks whose word was
 // never touched are free.
+// Two forms: where tables and cache are small, one workgroup does all but the copies with the words in LDS; else the words lie in
+// the workspace and clearing, counting, handing out and writing are launches of their own.  Bound by launches and by chains of
+// dependent loads (parent, length, entry) where little is copied, by the copies' bytes where much is.
 #include "mq_serve_common.h"
 
 namespace mq {
@@ -50,9 +53,15 @@ __global__ __launch_bounds__(kT) void k_tables_count(const Tables p) {
   const size_t b = (size_t)blockIdx.x * (kT / kWave) + threadIdx.x / kWave;
   if (b >= p.B_new) return;
   const RowOf r = row_of(p, b);
-  for (unsigned j = threadIdx.x % kWave; j < r.held; j += kWave) {
-    const int e = r.entries[j], want = r.open && j + 1 == r.held ? (int)b + 1 : 0;
-    if (is_block(p, e) && __hip_atomic_load(p.state + e, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) > want) atomicMin(p.state + e, want);
+  for (unsigned j = threadIdx.x % kWave; j < r.held; j += 4 * kWave) {
+    int e[4];                                              // (four loads at a time)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) e[i] = r.entries[min(j + i * kWave, r.held - 1)];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const unsigned at = j + i * kWave;
+      if (at < r.held && is_block(p, e[i])) atomicMin(p.state + e[i], r.open && at + 1 == r.held ? (int)b + 1 : 0);      // (nobody waits)
+    }
   }
 }
 
@@ -199,16 +208,171 @@ __global__ __launch_bounds__(kT) void k_compact_apply(const Tables p, const mq_k
   for (unsigned i = wg / groups; i < moves; i += movers) copy_block(c, from[i], to[i], wg % groups, groups);
 }
 
+// ---- small tables ---------------------------------------------------------------------------------------------------------
+
+constexpr size_t kSmallBlocks = 8192, kSmallRows = 4096, kSmallEntries = 16384;
+// words and a list of the blocks, then the rows
+constexpr size_t small_lds(size_t blocks, size_t rows) { return 2 * round_up(blocks, 2) * sizeof(int32_t) + rows * sizeof(int4); }
+
+// A row in LDS: its parent (-1: none), tokens, end of its blocks (below 0: its last one held will be written to), first new block.
+__device__ __forceinline__ unsigned held_of(const int4& r) { return ((unsigned)r.y + kKvBlock - 1) / kKvBlock; }
+__device__ __forceinline__ unsigned end_of(const int4& r) { return (unsigned)r.z & 0x7fffffffu; }
+
+// The rows and the words of the blocks, in LDS.  A thread for each row, then for each entry: loads that depend on each other are
+// few, and all rows' at once.
+__device__ __forceinline__ void count_small(const Tables& p, int32_t* state, int4* rows) {
+  for (unsigned b = threadIdx.x; b < p.B_new; b += kScan) {
+    const RowOf r = row_of(p, b);
+    rows[b] = make_int4((int)((r.entries - p.table) / p.width), (int)r.len, (int)(r.end | (r.open ? 0x80000000u : 0u)), 0);
+  }
+  for (unsigned i = threadIdx.x; i < p.blocks; i += kScan) state[i] = p.keep != nullptr && p.keep[i] != 0 ? 0 : kFree;
+  __syncthreads();
+  const unsigned width = (unsigned)p.width, entries = p.B_new * width;
+  for (unsigned i = threadIdx.x; i < entries; i += kScan) {
+    const unsigned b = i / width, j = i % width, held = held_of(rows[b]);
+    if (j >= held) continue;
+    const int e = p.table[(size_t)rows[b].x * width + j];
+    if (is_block(p, e)) atomicMin(state + e, rows[b].z < 0 && j + 1 == held ? (int)b + 1 : 0);
+  }
+  __syncthreads();
+}
+
+// Everything of a fork but the copies, which row b's pair (from, to) at p.list + 2 b says; to < 0: none.
+__global__ __launch_bounds__(kScan) void k_fork_small(const Tables p) {
+  extern __shared__ __attribute__((aligned(16))) int32_t words[];
+  __shared__ unsigned box[kScan / kWave];
+  const unsigned half = (p.blocks + 1) / 2 * 2;
+  int32_t *state = words, *list = words + half;
+  int4* rows = reinterpret_cast<int4*>(words + 2 * half);
+  count_small(p, state, rows);
+  unsigned found = 0;
+  for (unsigned at = 0; at < p.blocks; at += kScan) {
+    const unsigned i = at + threadIdx.x;
+    const bool free = i < p.blocks && state[i] == kFree;
+    unsigned all;
+    const unsigned before = scan(free, box, all);
+    if (free) list[found + before] = (int)i;
+    found += all;
+  }
+  __syncthreads();
+  const unsigned width = (unsigned)p.width;
+  unsigned needs = 0;
+  for (unsigned at = 0; at < p.B_new; at += kScan) {
+    const unsigned b = at + threadIdx.x;
+    unsigned mine = 0, all;
+    int from = -1;
+    int4 r{};
+    if (b < p.B_new) {
+      r = rows[b];
+      const unsigned held = held_of(r);
+      if (r.z < 0) {
+        const int e = p.table[(size_t)r.x * width + held - 1];
+        if (is_block(p, e) && state[e] != (int)b + 1) from = e;
+      }
+      mine = end_of(r) - held + (from >= 0 ? 1 : 0);
+    }
+    const unsigned first = needs + scan(mine, box, all);
+    needs += all;
+    if (b < p.B_new) {
+      const int to = from >= 0 && first < found ? list[first] : -1;
+      reinterpret_cast<int2*>(p.list)[b] = make_int2(from, to);
+      p.lens_new[b] = r.y;
+      // (what the last pass needs: whether the last block held is a copy, and which)
+      rows[b].w = (int)(first + (from >= 0 ? 1 : 0));
+      rows[b].z = (int)(end_of(r) | (from >= 0 ? 0x80000000u : 0u));
+    }
+  }
+  __syncthreads();
+  for (unsigned i = threadIdx.x; i < p.B_new * width; i += kScan) {
+    const unsigned b = i / width, j = i % width;
+    const int4 r = rows[b];
+    const unsigned held = held_of(r);
+    int e = -1;
+    if (j < held && !(r.z < 0 && j + 1 == held)) {
+      e = p.table[(size_t)r.x * width + j];
+      if (!is_block(p, e)) e = -1;
+    } else if (j < end_of(r)) {
+      const unsigned at = (unsigned)r.w + j - held;        // (a copy: one in front of the first)
+      e = at < found ? list[at] : -1;
+    }
+    p.table_new[i] = e;
+  }
+  if (threadIdx.x == 0) *p.missing = needs > found ? (int)(needs - found) : 0;
+}
+
+__global__ __launch_bounds__(kT) void k_fork_copy(const int32_t* pairs, const mq_kv_cache c, unsigned groups) {
+  const int2 pair = reinterpret_cast<const int2*>(pairs)[blockIdx.x / groups];
+  if (pair.y >= 0) copy_block(c, pair.x, pair.y, blockIdx.x % groups, groups);
+}
+
+// Everything of a compaction but the copies: pairs (from, to) at p.list, their number at p.offset.
+__global__ __launch_bounds__(kScan) void k_compact_small(const Tables p) {
+  extern __shared__ __attribute__((aligned(16))) int32_t words[];
+  __shared__ unsigned box[kScan / kWave];
+  const unsigned half = (p.blocks + 1) / 2 * 2;
+  int32_t *state = words, *holes = words + half;           // a block's word becomes where it is afterwards
+  int4* rows = reinterpret_cast<int4*>(words + 2 * half);
+  count_small(p, state, rows);
+  unsigned mine = 0, used;
+  for (unsigned i = threadIdx.x; i < p.blocks; i += kScan) mine += state[i] != kFree;
+  scan(mine, box, used);
+  unsigned n_holes = 0, moves = 0;
+  for (unsigned at = 0; at < p.blocks; at += kScan) {
+    const unsigned i = at + threadIdx.x;
+    const bool is = i < p.blocks && state[i] != kFree, hole = i < used && !is, move = i >= used && is;
+    unsigned all;
+    const unsigned before = scan((hole ? 1u : 0u) | (move ? 1u << 16 : 0u), box, all);
+    // holes lie below `used`, so that all are listed before the first block that moves is met -- but for those of the same round
+    if (hole) holes[n_holes + (before & 0xffffu)] = (int)i;
+    __syncthreads();
+    int to = is ? (int)i : -1;
+    if (move) {
+      to = holes[moves + (before >> 16)];
+      reinterpret_cast<int2*>(p.list)[moves + (before >> 16)] = make_int2((int)i, to);
+    }
+    if (i < p.blocks) {
+      p.moved[i] = to;
+      state[i] = to;
+    }
+    n_holes += all & 0xffffu;
+    moves += all >> 16;
+  }
+  __syncthreads();
+  const unsigned width = (unsigned)p.width;
+  for (unsigned i = threadIdx.x; i < p.B * width; i += kScan) {
+    const int e = i % width < held_of(rows[i / width]) ? p.table[i] : -1;
+    p.table_new[i] = is_block(p, e) ? state[e] : -1;
+  }
+  if (threadIdx.x == 0) {
+    *p.used = (int)used;
+    p.offset[0] = (int)moves;
+  }
+}
+
+__global__ __launch_bounds__(kT) void k_compact_copy(const int32_t* pairs, const int32_t* moves, const mq_kv_cache c, unsigned groups) {
+  const unsigned movers = gridDim.x / groups, n = (unsigned)moves[0];
+  for (unsigned i = blockIdx.x / groups; i < n; i += movers) {
+    const int2 pair = reinterpret_cast<const int2*>(pairs)[i];
+    copy_block(c, pair.x, pair.y, blockIdx.x % groups, groups);
+  }
+}
+
 // workgroups that share a copy: 16 KB each
 unsigned copy_groups(const mq_kv_cache& c) {
   const size_t bytes = (size_t)c.kv_heads * kKvBlock * (kv_dk((unsigned)c.head_dim) + kv_dv((unsigned)c.head_dim));
   return (unsigned)((bytes + 16383) / 16384);
 }
+int allow_lds(const void* kernel, size_t bytes) {
+  return bytes <= 65536 ? (int)MQ_OK : check_hip(hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+}
 unsigned clear_wgs(size_t blocks) { return (unsigned)((blocks + kT - 1) / kT < 1024 ? (blocks + kT - 1) / kT : 1024); }
 
 }  // namespace
 
-size_t kv_fork_ws_bytes(size_t blocks, size_t B_new, size_t) { return (2 * blocks + B_new + 1) * sizeof(int32_t); }
+size_t kv_fork_ws_bytes(size_t blocks, size_t B_new, size_t) {
+  const size_t words = 2 * blocks > 2 * B_new ? 2 * blocks : 2 * B_new;        // words and list, or pairs
+  return (words + B_new + 1) * sizeof(int32_t);
+}
 size_t kv_compact_ws_bytes(size_t blocks) { return (2 * blocks + 4) * sizeof(int32_t); }
 
 int launch_kv_fork(const mq_kv_cache& cache, const int32_t* keep, const int32_t* table, size_t table_width, const int32_t* lens,
@@ -217,6 +381,15 @@ int launch_kv_fork(const mq_kv_cache& cache, const int32_t* keep, const int32_t*
   const unsigned groups = copy_groups(cache);
   if (!launchable(B_new * groups, kT)) return MQ_ERR_SHAPE;
   int32_t* w = static_cast<int32_t*>(ws);
+  if (cache.blocks <= kSmallBlocks && B_new <= kSmallRows && B_new <= kSmallEntries / table_width) {
+    const size_t lds = small_lds(cache.blocks, B_new);
+    if (const int rc = allow_lds(reinterpret_cast<const void*>(k_fork_small), lds); rc != MQ_OK) return rc;
+    const Tables p{keep, table, lens, parent, grow, table_new, lens_new, missing, nullptr, nullptr, nullptr, w, w + 2 * B_new,
+                   table_width, (unsigned)B, (unsigned)B_new, (unsigned)cache.blocks};
+    hipLaunchKernelGGL(k_fork_small, dim3(1), dim3(kScan), lds, s, p);
+    hipLaunchKernelGGL(k_fork_copy, dim3((unsigned)(B_new * groups)), dim3(kT), 0, s, w, cache, groups);
+    return check_hip(hipGetLastError());
+  }
   const Tables p{keep, table, lens, parent, grow, table_new, lens_new, missing, nullptr, nullptr, w, w + cache.blocks,
                  w + 2 * cache.blocks, table_width, (unsigned)B, (unsigned)B_new, (unsigned)cache.blocks};
   hipLaunchKernelGGL(k_tables_clear, dim3(clear_wgs(cache.blocks)), dim3(kT), 0, s, p);
@@ -231,14 +404,23 @@ int launch_kv_compact(const mq_kv_cache& cache, const int32_t* keep, const int32
   if (!launchable((B + 3) / 4, kT)) return MQ_ERR_SHAPE;
   const unsigned groups = copy_groups(cache);
   int32_t* w = static_cast<int32_t*>(ws);
+  const size_t most = cache.blocks / 2 + 1;
+  const unsigned movers = (unsigned)(most < 512 ? most : 512);
+  if (cache.blocks <= kSmallBlocks && B <= kSmallRows && B <= kSmallEntries / table_width) {
+    const size_t lds = small_lds(cache.blocks, B);
+    if (const int rc = allow_lds(reinterpret_cast<const void*>(k_compact_small), lds); rc != MQ_OK) return rc;
+    const Tables p{keep, table, lens, nullptr, nullptr, table_new, nullptr, nullptr, moved, used, nullptr, w, w + 2 * cache.blocks + 2,
+                   table_width, (unsigned)B, (unsigned)B, (unsigned)cache.blocks};
+    hipLaunchKernelGGL(k_compact_small, dim3(1), dim3(kScan), lds, s, p);
+    hipLaunchKernelGGL(k_compact_copy, dim3(movers * groups), dim3(kT), 0, s, w, w + 2 * cache.blocks + 2, cache, groups);
+    return check_hip(hipGetLastError());
+  }
   const Tables p{keep, table, lens, nullptr, nullptr, table_new, nullptr, nullptr, moved, used, w, w + cache.blocks,
                  w + 2 * cache.blocks + 2, table_width, (unsigned)B, (unsigned)B, (unsigned)cache.blocks};
   hipLaunchKernelGGL(k_tables_clear, dim3(clear_wgs(cache.blocks)), dim3(kT), 0, s, p);
   hipLaunchKernelGGL(k_tables_count, dim3((unsigned)((B + 3) / 4)), dim3(kT), 0, s, p);
   hipLaunchKernelGGL(k_compact_plan, dim3(1), dim3(kScan), 0, s, p);
   const unsigned table_wgs = (unsigned)(B < 1024 ? B : 1024);
-  const size_t most = cache.blocks / 2 + 1;
-  const unsigned movers = (unsigned)(most < 512 ? most : 512);
   hipLaunchKernelGGL(k_compact_apply, dim3(table_wgs + movers * groups), dim3(kT), 0, s, p, cache, table_wgs, groups);
   return check_hip(hipGetLastError());
 }

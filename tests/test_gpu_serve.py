@@ -332,23 +332,28 @@ def moved_contents(before, copies):
 
 
 @pytest.mark.parametrize("seed", range(12))
-@pytest.mark.parametrize("room", ["plenty", "scarce"])
+@pytest.mark.parametrize("room", ["plenty", "scarce", "large"])
 def test_fork(seed, room):
+    """large: more blocks, or larger tables, than one workgroup does alone."""
     g = gen(100 + seed)
     rnd = np.random.RandomState(seed)
     B, width = rnd.randint(1, 40), rnd.randint(1, 9)
     n = rnd.randint(1, 90)
+    if room == "large" and seed % 2:
+        width, n = width + 200, n + 80
     lens = rnd.randint(-3, width * BLOCK + 10, B)
     lens[rnd.rand(B) < 0.3] //= BLOCK
     lens[rnd.rand(B) < 0.3] *= BLOCK
     lens = np.clip(lens, -5, 2 ** 20)
     blocks = rnd.randint(1, 5) if room == "scarce" and seed % 3 == 0 else B * width + (3 * n if room == "plenty" else n // 3)
+    if room == "large":
+        blocks = B * width + n + (0 if seed % 2 else 17000)
     # tables with shared, repeated and absent blocks
     table = rnd.randint(-2, blocks + 2, (B, width)) if seed % 2 else rnd.permutation(max(blocks, B * width))[:B * width].reshape(B, width)
     parent = rnd.randint(-2, B + 2, n)
     grow = rnd.randint(-1, 130, n) * (rnd.rand(n) < 0.8)
     keep = (rnd.rand(blocks) < 0.2).astype(np.int32) * 5 if seed % 4 else None
-    heads, dim = [(1, 64), (2, 33), (3, 128), (1, 256)][seed % 4]
+    heads, dim = [(1, 64), (2, 33), (3, 128), (1, 256)][seed % 4] if room != "large" else (1, 20)
     cache = random_cache(g, blocks, heads, dim)
     before = contents(cache)
     got = fork_call(cache, None if keep is None else i32(keep), i32(table), i32(lens), i32(parent), i32(grow))
@@ -399,16 +404,19 @@ def compact_expected(keep, table, lens, blocks):
     return out, moved, count, list(zip(late, holes))
 
 
-@pytest.mark.parametrize("seed", range(12))
+@pytest.mark.parametrize("seed", range(16))
 def test_compact(seed):
+    """The last four with more blocks, or a larger table, than one workgroup does alone."""
     g = gen(200 + seed)
     rnd = np.random.RandomState(50 + seed)
     B, width = rnd.randint(1, 60), rnd.randint(1, 9)
     blocks = [1, 7, 1023, 1024, 1025, 5000][seed % 6]
+    if seed >= 12:
+        B, width, blocks = [(40, 5, 20000), (130, 130, 3000), (1, 1, 16385), (700, 30, 700)][seed - 12]
     lens = rnd.randint(-3, width * BLOCK + 10, B)
     table = rnd.randint(-2, blocks + 2, (B, width))
     keep = (rnd.rand(blocks) < [0.05, 0.5, 0.0][seed % 3]).astype(np.int32) if seed % 4 else None
-    heads, dim = [(1, 64), (2, 33), (3, 128), (1, 256)][seed % 4]
+    heads, dim = [(1, 64), (2, 33), (3, 128), (1, 256)][seed % 4] if seed < 12 else (2, 20)
     cache = random_cache(g, blocks, heads, dim)
     before = contents(cache)
     t = i32(table)
