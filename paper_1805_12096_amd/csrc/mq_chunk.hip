@@ -34,7 +34,7 @@ struct ChunkParams {
   unsigned B, T, max_len, kv_heads, heads, d;
   float scale2;                       // scale log2(e)
   int causal;
-  unsigned* plan;                     // [slots + 1] blocks of the tiles in front of each tile
+  unsigned* plan;                     // [slots + 1] blocks of the tiles in front of each tile, then at 16 bytes [slots] tiles
   unsigned slots;                     // tiles at most
 };
 
@@ -58,7 +58,7 @@ __device__ __forceinline__ float add2(__bf16 a, __bf16 b, float sum) {
 }
 
 // A tile of query rows: row i of its sequence's n x per is token i / per, head i % per of the group.
-struct Tile {
+struct alignas(8) Tile {
   int b;                              // sequence, -1: no such tile
   unsigned first, n, row0, rows, len; // its first token row and new tokens, the tile's first row and rows, tokens in the cache
 };
@@ -99,6 +99,10 @@ __device__ __forceinline__ unsigned tile_blocks(const ChunkParams& p, const Tile
   return t.b < 0 ? 0u : max(1u, (seen_by(p, t, (t.row0 + t.rows - 1) / per) + kKvBlock - 1) / kKvBlock);
 }
 
+__device__ __forceinline__ Tile* planned(const ChunkParams& p) {
+  return reinterpret_cast<Tile*>(p.plan + (p.slots + 4) / 4 * 4);
+}
+
 template <unsigned ROWS>
 __global__ __launch_bounds__(kPlan) void k_chunk_plan(const ChunkParams p) {
   __shared__ unsigned box[kPlan / kWave];
@@ -114,7 +118,11 @@ __global__ __launch_bounds__(kPlan) void k_chunk_plan(const ChunkParams p) {
       else hi = mid;
     }
     unsigned n = 0;
-    if (slot < p.slots) n = tile_blocks(p, tile_of<ROWS>(p, (int)lo, slot, per), per);
+    if (slot < p.slots) {
+      const Tile t = tile_of<ROWS>(p, (int)lo, slot, per);
+      n = tile_blocks(p, t, per);
+      planned(p)[slot] = t;
+    }
     unsigned x = n;
 #pragma unroll
     for (int off = 1; off < kWave; off <<= 1) {
@@ -143,26 +151,35 @@ __device__ __forceinline__ unsigned long long share_of(const ChunkParams& p, uns
 
 // A workgroup's next part of the line: blocks [start, end) of a tile and a kv head; whole: all that the tile has.
 struct LinePart {
-  unsigned kvh, slot, start, end;
+  unsigned kvh, start, end;
   bool whole;
+  Tile tile;
 };
-__device__ __forceinline__ LinePart part_at(const ChunkParams& p, unsigned long long at, unsigned long long to) {
-  const unsigned line = p.plan[p.slots];
-  const unsigned kvh = __builtin_amdgcn_readfirstlane((unsigned)(at / line)), place = (unsigned)(at - (unsigned long long)kvh * line);
-  const unsigned slot = (unsigned)__builtin_amdgcn_readfirstlane(wave_search(p.slots, place, [&](unsigned i) { return p.plan[i]; }));
-  const unsigned first = p.plan[slot], blocks = p.plan[slot + 1] - first, start = place - first;
+__device__ __forceinline__ LinePart part_at(const ChunkParams& p, unsigned line, unsigned long long at, unsigned long long to) {
+  unsigned kvh = 0;                   // (no division: there are few heads, and a workgroup has one or two)
+  unsigned long long place = at;
+  while (place >= line) {
+    place -= line;
+    ++kvh;
+  }
+  const unsigned slot = (unsigned)__builtin_amdgcn_readfirstlane(wave_search(p.slots, (unsigned)place, [&](unsigned i) { return p.plan[i]; }));
+  const Tile t = planned(p)[slot];
+  const unsigned first = p.plan[slot], blocks = p.plan[slot + 1] - first, start = (unsigned)place - first;
   const unsigned end = (unsigned)min((unsigned long long)blocks, start + (to - at));
-  return {kvh, slot, start, end, start == 0 && end == blocks};
+  auto uniform = [](unsigned x) { return (unsigned)__builtin_amdgcn_readfirstlane((int)x); };
+  return {kvh, uniform(start), uniform(end), start == 0 && end == blocks,
+          Tile{(int)uniform((unsigned)t.b), uniform(t.first), uniform(t.n), uniform(t.row0), uniform(t.rows), uniform(t.len)}};
 }
 // Calls f(part, where a part that is not whole goes) for all parts of this workgroup.  An eighth of the line to each XCD, whose
 // workgroups then read the same heads' blocks.
 template <typename F>
 __device__ __forceinline__ void each_part(const ChunkParams& p, F f) {
   const unsigned me = blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8;
-  const unsigned long long share = share_of(p, gridDim.x), all = (unsigned long long)p.plan[p.slots] * p.kv_heads;
+  const unsigned line = p.plan[p.slots];
+  const unsigned long long share = share_of(p, gridDim.x), all = (unsigned long long)line * p.kv_heads;
   const unsigned long long to = min((me + 1) * share, all);
   for (unsigned long long at = me * share, n = 0; at < to; ++n) {
-    const LinePart part = part_at(p, at, to);
+    const LinePart part = part_at(p, line, at, to);
     at += part.end - part.start;
     f(part, me * 2 + (n > 0 ? 1 : 0));
   }
@@ -198,8 +215,7 @@ __device__ __forceinline__ void few_rows(const ChunkParams& p, int vec, const Li
   asm volatile("" : "+v"(lane), "+s"(d));
   const unsigned wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), waves = blockDim.x / kWave, col = lane % 32, grp = lane / 32;
   const unsigned per = p.heads / p.kv_heads, dk = kv_dk(d), dv = kv_dv(d), kvh = part.kvh;
-  const Tile tile = find_tile<kRows>(p, part.slot, per);
-  if (tile.b < 0) return;
+  const Tile tile = part.tile;
   auto row_at = [&](unsigned r) {              // element offset of row r's queries in q, without the row pitch: token, head
     const unsigned i = tile.row0 + r;
     return make_uint2(tile.first + i / per, kvh * per + i % per);
@@ -268,6 +284,11 @@ __device__ __forceinline__ void few_rows(const ChunkParams& p, int vec, const Li
     asm volatile("" ::: "memory");
   };
 
+  if (mine > 0) {
+    find(0);
+    bring_keys();
+    bring_values();
+  }
   // queries: a power of two off each row, so that its largest element is 1 .. 2, then parts in operand order.  Unit u of lane l is
   // elements 32 (u / 2) + 16 (l / 32) + 8 (u % 2) .. of row l % 32
   {
@@ -319,11 +340,6 @@ __device__ __forceinline__ void few_rows(const ChunkParams& p, int vec, const Li
 #pragma unroll
       for (int i = 0; i < NP; ++i) ql[(i * U + u) * kWave + lane] = part[i];
     }
-  }
-  if (mine > 0) {
-    find(0);
-    bring_keys();
-    bring_values();
   }
   __syncthreads();
   const float qscale = ldexpf(fabsf(p.scale2), row_exponent(__uint_as_float(fac[col]))) * (1.f / 127.f);
@@ -476,7 +492,8 @@ __global__ __launch_bounds__(kWaves * kWave, DC > 2 ? 1 : 2) void k_chunk_few(co
     });
   } else {
     // (heads next to each other: on a chip whose workgroups go to its eight XCDs by turns, eight heads have one each)
-    few_rows<DT, DC>(p, vec, LinePart{blockIdx.x % p.kv_heads, blockIdx.x / p.kv_heads, 0, 0xffffffffu, true}, 0);
+    const Tile tile = find_tile<kRows>(p, blockIdx.x / p.kv_heads, p.heads / p.kv_heads);
+    if (tile.b >= 0) few_rows<DT, DC>(p, vec, LinePart{blockIdx.x % p.kv_heads, 0, 0xffffffffu, true, tile}, 0);
   }
 }
 
@@ -522,7 +539,7 @@ __device__ __forceinline__ void many_rows(const ChunkParams& p, int vec, const L
   asm volatile("" : "+v"(lane), "+s"(d));
   const unsigned wave = __builtin_amdgcn_readfirstlane((threadIdx.x - threadIdx.x % kWave + lane) / kWave), col = lane % 32, grp = lane / 32;
   const unsigned per = p.heads / p.kv_heads, dk = kv_dk(d), dv = kv_dv(d), kvh = part.kvh, start = part.start;
-  const Tile tile = find_tile<Form::kRowsOfWg>(p, part.slot, per);
+  const Tile tile = part.tile;
   const unsigned nblocks = (seen_by(p, tile, (tile.row0 + tile.rows - 1) / per) + kKvBlock - 1) / kKvBlock;
   const unsigned count = min(part.end, nblocks) > start ? min(part.end, nblocks) - start : 0;
   // this wave's rows; past the tile's end they repeat its last and are not stored
@@ -898,22 +915,34 @@ __global__ __launch_bounds__(256) void k_chunk_join(const ChunkParams p, unsigne
   if (from == to) return;                                  // (no such tile)
   const unsigned g0 = (unsigned)(from / share), g1 = (unsigned)((to - 1) / share);
   if (g0 == g1) return;                                    // (one workgroup had all of it)
-  const Tile tile = find_tile<ROWS>(p, slot, per);
+  const Tile tile = planned(p)[slot];
   const unsigned r = chunk * 32 + threadIdx.x / 8, j0 = threadIdx.x % 8;
   if (tile.b < 0 || r >= tile.rows) return;
   // a workgroup's first part; of the first workgroup its last, if it had other tiles before
   auto run = [&](unsigned g) { return p.part + (((size_t)g * 2 + (g == g0 && from % share != 0 ? 1 : 0)) * ROWS + r) * pitch; };
+  // references and totals of eight parts at a time, one for each thread of the row
   float m = -INFINITY, l = 0.f;
-  for (unsigned g = g0; g <= g1; ++g) m = fmaxf(m, run(g)[dv]);
+  for (unsigned g = g0 + j0; g <= g1; g += 8) m = fmaxf(m, run(g)[dv]);
+#pragma unroll
+  for (int off = 4; off >= 1; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, 8));
   const float top = finite_or_0(m);
   v4f x[8] = {};
-  for (unsigned g = g0; g <= g1; ++g) {
-    const float* at = run(g);
-    const float w = __builtin_amdgcn_exp2f(at[dv] - top);
-    l = fmaf(w, at[dv + 1], l);
+  for (unsigned at = g0; at <= g1; at += 8) {
+    const unsigned mine = min(at + j0, g1), n = min(g1 - at + 1, 8u);
+    const float2 stat = *reinterpret_cast<const float2*>(run(mine) + dv);
+    const float w = at + j0 <= g1 ? __builtin_amdgcn_exp2f(stat.x - top) : 0.f;
+    float part_l = at + j0 <= g1 ? w * stat.y : 0.f;       // (a row of NaNs has a weight of 0 and a total of NaN)
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (4 * (j0 + 8 * j) < dv) x[j] += w * *reinterpret_cast<const v4f*>(at + 4 * (j0 + 8 * j));
+    for (int off = 4; off >= 1; off >>= 1) part_l += __shfl_xor(part_l, off, 8);
+    l += part_l;
+#pragma unroll 2
+    for (unsigned k = 0; k < n; ++k) {
+      const float* from_run = run(at + k);
+      const float wk = __shfl(w, (int)k, 8);
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (4 * (j0 + 8 * j) < dv) x[j] += wk * *reinterpret_cast<const v4f*>(from_run + 4 * (j0 + 8 * j));
+    }
   }
   const unsigned i = tile.row0 + r;
   T* dst = static_cast<T*>(p.out) + (size_t)(tile.first + i / per) * p.ldo + (size_t)(kvh * per + i % per) * p.d;
@@ -956,7 +985,7 @@ size_t chunk_attention_ws_bytes(size_t B, size_t T, size_t max_len, int heads, i
   size_t most = 0;                    // (whatever the type)
   for (int dtype : {MQ_F32, MQ_F16, MQ_BF16}) {
     const Form f = form_of(dtype, B, T, max_len, heads, kv_heads, d);
-    const size_t n = part_floats(f, d) + (f.shares ? f.slots + 1 : 0);
+    const size_t n = part_floats(f, d) + (f.shares ? (f.slots + 4) / 4 * 4 + f.slots * sizeof(Tile) / sizeof(float) : 0);
     most = n > most ? n : most;
   }
   return most * sizeof(float);
