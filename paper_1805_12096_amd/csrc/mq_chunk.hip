@@ -207,13 +207,13 @@ __device__ __forceinline__ void few_rows(const ChunkParams& p, int vec, const Li
   constexpr int U = NK * 2;                    // units of 8 elements of a query
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   bf8* const ql = reinterpret_cast<bf8*>(smem);                                  // [NP][U][64 lanes], then each wave's blocks
-  float* const sums = reinterpret_cast<float*>(smem);                            // [32][ND 32 + 1], afterwards
   __shared__ unsigned fac[kRows];               // largest magnitudes, as bits
   __shared__ float stat[2][kWaves][kRows];
   // (unknown to the compiler to be the same each time: it would keep dozens of places and masks from one part to the next)
   unsigned lane = threadIdx.x % kWave, d = p.d;
   asm volatile("" : "+v"(lane), "+s"(d));
-  const unsigned wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), waves = blockDim.x / kWave, col = lane % 32, grp = lane / 32;
+  constexpr unsigned W = few_waves(NP, DC);
+  const unsigned wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), col = lane % 32, grp = lane / 32;
   const unsigned per = p.heads / p.kv_heads, dk = kv_dk(d), dv = kv_dv(d), kvh = part.kvh;
   const Tile tile = part.tile;
   auto row_at = [&](unsigned r) {              // element offset of row r's queries in q, without the row pitch: token, head
@@ -225,12 +225,12 @@ __device__ __forceinline__ void few_rows(const ChunkParams& p, int vec, const Li
   const unsigned mine_sees = seen_by(p, tile, min(tile.row0 + col, last) / per);
   const unsigned start = part.start, end = min(part.end, (most + kKvBlock - 1) / kKvBlock);
 
-  // this wave's blocks, every waves-th of the run: which ones is looked up 64 at a time, keys and values are asked for as soon as
+  // this wave's blocks, every W-th of the part: which ones is looked up 64 at a time, keys and values are asked for as soon as
   // the registers of those of the block before are free
   const int32_t* table = p.table + (size_t)tile.b * p.table_width;
-  const unsigned mine = end > start + wave ? __builtin_amdgcn_readfirstlane((end - start - wave + waves - 1) / waves) : 0u;
+  const unsigned mine = end > start + wave ? __builtin_amdgcn_readfirstlane((end - start - wave + W - 1) / W) : 0u;
   auto look = [&](unsigned i) {
-    const size_t pg = start + wave + (size_t)(i + lane) * waves;
+    const size_t pg = start + wave + (size_t)(i + lane) * W;
     return table[pg < p.table_width ? pg : p.table_width - 1];
   };
   int ids = look(0);
@@ -296,49 +296,49 @@ __device__ __forceinline__ void few_rows(const ChunkParams& p, int vec, const Li
     const uint2 at = row_at(rr);
     const T* src = static_cast<const T*>(p.q) + (size_t)at.x * p.ldq + (size_t)at.y * d;
     if (threadIdx.x < kRows) fac[threadIdx.x] = 0;
-    __syncthreads();
-    auto unit = [&](unsigned u, float (&x)[8]) {
-      const unsigned k = 32 * (u / 2) + 16 * grp + 8 * (u % 2);
+    constexpr unsigned EACH = (U + W - 1) / W;             // units of a wave
+    float x[EACH][8], m = 0.f;
+#pragma unroll
+    for (unsigned n = 0; n < EACH; ++n) {
+      const unsigned u = wave + W * n, k = 32 * (u / 2) + 16 * grp + 8 * (u % 2);
       if (vec & 1) {
-        constexpr int W = 16 / sizeof(T);
-        typedef T tw __attribute__((ext_vector_type(W)));
+        constexpr int E = 16 / sizeof(T);
+        typedef T tw __attribute__((ext_vector_type(E)));
 #pragma unroll
-        for (int j = 0; j < 8; j += W) {
-          tw w = {};
-          if (k + j < d) w = *reinterpret_cast<const tw*>(src + k + j);
+        for (int j = 0; j < 8; j += E) {
+          const tw w = *reinterpret_cast<const tw*>(src + min(k + j, d - E));
 #pragma unroll
-          for (int i = 0; i < W; ++i) x[j + i] = (float)w[i];
+          for (int i = 0; i < E; ++i) x[n][j + i] = k + j < d ? (float)w[i] : 0.f;
         }
       } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = k + j < d ? (float)src[k + j] : 0.f;
+        for (int j = 0; j < 8; ++j) x[n][j] = k + j < d ? (float)src[k + j] : 0.f;
       }
-    };
-    float m = 0.f;
-    for (unsigned u = wave; u < U; u += waves) {
-      float x[8];
-      unit(u, x);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) m = fabsf(x[j]) <= 3.402823466e38f ? fmaxf(m, fabsf(x[j])) : INFINITY;
     }
+#pragma unroll
+    for (unsigned n = 0; n < EACH; ++n)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) m = fmaxf(m, fabsf(x[n][j]) <= 3.402823466e38f ? fabsf(x[n][j]) : INFINITY);
+    __syncthreads();
     // (magnitudes are in the order of their bits; a maximum does not depend on the order)
     atomicMax(&fac[col], __float_as_uint(across32_f(m, fmax2)));
     __syncthreads();
     const float most_of_row = __uint_as_float(fac[col]);
     const float mul = __uint_as_float((unsigned)(127 - row_exponent(most_of_row)) << 23) * (p.scale2 < 0.f ? -1.f : 1.f);
-    for (unsigned u = wave; u < U; u += waves) {
-      float x[8];
-      unit(u, x);
+#pragma unroll
+    for (unsigned n = 0; n < EACH; ++n) {
+      const unsigned u = wave + W * n;
       bf8 part[NP];
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         __bf16 b[NP];
-        split_bf16<NP>(most_of_row == INFINITY ? NAN : x[j] * mul, b);        // a row with a NaN or an infinity gives NaN
+        split_bf16<NP>(most_of_row == INFINITY ? NAN : x[n][j] * mul, b);     // a row with a NaN or an infinity gives NaN
 #pragma unroll
         for (int i = 0; i < NP; ++i) part[i][j] = b[i];
       }
+      if (u < U)
 #pragma unroll
-      for (int i = 0; i < NP; ++i) ql[(i * U + u) * kWave + lane] = part[i];
+        for (int i = 0; i < NP; ++i) ql[(i * U + u) * kWave + lane] = part[i];
     }
   }
   __syncthreads();
@@ -348,7 +348,7 @@ __device__ __forceinline__ void few_rows(const ChunkParams& p, int vec, const Li
   v16f acc[ND] = {};
   constexpr bool FOLD = NP < 3;
   for (unsigned i = 0; i < mine; ++i) {
-    const unsigned pg = start + wave + i * waves;
+    const unsigned pg = start + wave + i * W;
     const float2 am = am_next;
     there = there_next;
     if (i + 1 < mine) find(i + 1);
@@ -439,45 +439,58 @@ __device__ __forceinline__ void few_rows(const ChunkParams& p, int vec, const Li
   }
   total = across32_f(total, fadd2);
 
-  // the waves, one after the other
+  // every wave leaves its sums where its blocks were, rows of 64 DC numbers, four at place j ^ (row & 7); eight threads join a row
   if (grp == 0) {
     stat[0][wave][col] = acc_top;
     stat[1][wave][col] = total;
   }
-  __syncthreads();                             // (and nobody reads queries any more)
-  float m = -INFINITY;
-  for (unsigned w = 0; w < waves; ++w) m = fmaxf(m, stat[0][w][col]);
-  const float weight = __builtin_amdgcn_exp2f(acc_top - finite_or_0(m));
-  const unsigned pitch = ND * 32 + 1;
-  for (unsigned w = 0; w < waves; ++w) {
-    if (w == wave)
+  {
+    v4f* const mine_sums = reinterpret_cast<v4f*>(mine_lds) + col * (16 * DC);
 #pragma unroll
-      for (int t = 0; t < ND; ++t)
+    for (int t = 0; t < ND; ++t)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          float& to = sums[col * pitch + 32 * t + 8 * (r / 4) + 4 * grp + r % 4];
-          const float x = acc[t][r] * weight;
-          to = w == 0 ? x : to + x;
-        }
-    __syncthreads();
+      for (int r = 0; r < 16; r += 4)
+        mine_sums[(8 * t + r / 2 + grp) ^ (col & 7)] = v4f{acc[t][r], acc[t][r + 1], acc[t][r + 2], acc[t][r + 3]};
   }
-  for (unsigned i = threadIdx.x; i < tile.rows * dv; i += blockDim.x) {
-    const unsigned r = i / dv, c = i % dv;
-    float mm = -INFINITY, l = 0.f;
-    for (unsigned w = 0; w < waves; ++w) mm = fmaxf(mm, stat[0][w][r]);
-    for (unsigned w = 0; w < waves; ++w) l = fmaf(__builtin_amdgcn_exp2f(stat[0][w][r] - finite_or_0(mm)), stat[1][w][r], l);
-    const float x = sums[r * pitch + c];
+  __syncthreads();
+  for (unsigned r = threadIdx.x / 8; r < tile.rows; r += W * kWave / 8) {
+    const unsigned j0 = threadIdx.x % 8;
+    float m = -INFINITY, l = 0.f, weight[W];
+#pragma unroll
+    for (unsigned w = 0; w < W; ++w) m = fmaxf(m, stat[0][w][r]);
+#pragma unroll
+    for (unsigned w = 0; w < W; ++w) {
+      weight[w] = __builtin_amdgcn_exp2f(stat[0][w][r] - finite_or_0(m));
+      l = fmaf(weight[w], stat[1][w][r], l);
+    }
     const uint2 at = row_at(r);
-    if (part.whole) {
-      if (c < d) static_cast<T*>(p.out)[(size_t)at.x * p.ldo + (size_t)at.y * d + c] = (T)(l == 0.f ? 0.f : __fdiv_rn(x, l));
-    } else {
-      float* to = p.part + ((size_t)to_part * kRows + r) * (dv + 4);
-      to[c] = x;
-      if (c == 0) {
-        to[dv] = mm;
-        to[dv + 1] = l;
+    T* const out = static_cast<T*>(p.out) + (size_t)at.x * p.ldo + (size_t)at.y * d;
+    float* const parts = p.part + ((size_t)to_part * kRows + r) * (dv + 4);
+    const char* const first = smem + NP * U * 1024 + r * (256 * DC);
+#pragma unroll
+    for (int j = 0; j < 2 * DC; ++j) {
+      const unsigned c4 = j0 + 8 * j, c = 4 * c4;
+      if (c >= dv) continue;
+      v4f x = {};
+#pragma unroll
+      for (unsigned w = 0; w < W; ++w) x += weight[w] * *reinterpret_cast<const v4f*>(first + w * kWaveBytes<DC> + (c4 ^ (r & 7)) * 16);
+      if (!part.whole) {
+        *reinterpret_cast<v4f*>(parts + c) = x;
+        continue;
+      }
+      typedef T t4 __attribute__((ext_vector_type(4)));
+      t4 v;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] = (T)(l == 0.f ? 0.f : __fdiv_rn(x[k], l));
+      if ((vec & 2) && c < d) {
+        *reinterpret_cast<t4*>(out + c) = v;
+      } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (c + k < d) out[c + k] = v[k];
       }
     }
+    if (!part.whole && j0 == 0) *reinterpret_cast<float2*>(parts + dv) = make_float2(m, l);
   }
 }
 
@@ -655,7 +668,7 @@ __device__ __forceinline__ void many_rows(const ChunkParams& p, int vec, const L
       float v[8];
       piece(u, v);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) m = fabsf(v[j]) <= 3.402823466e38f ? fmaxf(m, fabsf(v[j])) : INFINITY;
+      for (int j = 0; j < 8; ++j) m = fmaxf(m, fabsf(v[j]) <= 3.402823466e38f ? fabsf(v[j]) : INFINITY);
     }
     m = across32_f(m, fmax2);
     const int e = row_exponent(m);
@@ -904,53 +917,63 @@ __global__ __launch_bounds__((TileForm<DT, DC>::W) * kWave, 1) void k_chunk_tile
   each_part(p, [&](const LinePart& part, unsigned to) { many_rows<DT, DC>(p, vec, part, to); });
 }
 
-// The parts of tiles that more than one workgroup had: a workgroup for 32 rows of a tile and a kv head, eight threads a row.
+// The parts of tiles that more than one workgroup had.  A workgroup for eight rows of a tile and a kv head, 32 threads a row, where
+// rows are few and parts may be many; for 32 rows, eight threads a row, where there are many rows of few parts.
+constexpr unsigned join_rows(unsigned tile_rows) { return tile_rows > kRows ? 32 : 8; }
 template <int DT, unsigned ROWS>
 __global__ __launch_bounds__(256) void k_chunk_join(const ChunkParams p, unsigned groups) {
   using T = typename Elem<DT>::T;
-  const unsigned chunk = blockIdx.x % (ROWS / 32), kvh = blockIdx.x / (ROWS / 32) % p.kv_heads, slot = blockIdx.x / (ROWS / 32 * p.kv_heads);
+  constexpr unsigned JR = join_rows(ROWS), TH = 256 / JR, NX = 64 / TH, AHEAD = TH / 4;      // threads of a row, fours of columns each
+  const unsigned chunk = blockIdx.x % (ROWS / JR), kvh = blockIdx.x / (ROWS / JR) % p.kv_heads, slot = blockIdx.x / (ROWS / JR * p.kv_heads);
   const unsigned dv = kv_dv(p.d), pitch = dv + 4, per = p.heads / p.kv_heads;
-  const unsigned long long share = share_of(p, groups), base = (unsigned long long)p.plan[p.slots] * kvh;
-  const unsigned long long from = base + p.plan[slot], to = base + p.plan[slot + 1];
-  if (from == to) return;                                  // (no such tile)
-  const unsigned g0 = (unsigned)(from / share), g1 = (unsigned)((to - 1) / share);
-  if (g0 == g1) return;                                    // (one workgroup had all of it)
   const Tile tile = planned(p)[slot];
-  const unsigned r = chunk * 32 + threadIdx.x / 8, j0 = threadIdx.x % 8;
+  const unsigned first = p.plan[slot], last = p.plan[slot + 1];
+  const unsigned long long share = share_of(p, groups), base = (unsigned long long)p.plan[p.slots] * kvh;
+  const unsigned r = chunk * JR + threadIdx.x / TH, j0 = threadIdx.x % TH;
   if (tile.b < 0 || r >= tile.rows) return;
+  const unsigned g0 = (unsigned)((base + first) / share), g1 = (unsigned)((base + last - 1) / share), runs = g1 - g0 + 1;
+  if (runs == 1) return;                                   // (one workgroup had all of it)
+  const bool inside = base + first != g0 * share;
   // a workgroup's first part; of the first workgroup its last, if it had other tiles before
-  auto run = [&](unsigned g) { return p.part + (((size_t)g * 2 + (g == g0 && from % share != 0 ? 1 : 0)) * ROWS + r) * pitch; };
-  // references and totals of eight parts at a time, one for each thread of the row
+  auto run = [&](unsigned i) { return p.part + (((size_t)(g0 + i) * 2 + (i == 0 && inside ? 1 : 0)) * ROWS + r) * pitch; };
+  auto over = [](float v, auto op) {                       // the threads of a row
+#pragma unroll
+    for (int off = TH / 2; off >= 1; off >>= 1) v = op(v, __shfl_xor(v, off, TH));
+    return v;
+  };
+  // references of TH parts at a time, one for each thread
   float m = -INFINITY, l = 0.f;
-  for (unsigned g = g0 + j0; g <= g1; g += 8) m = fmaxf(m, run(g)[dv]);
+  for (unsigned i = j0; i < runs; i += TH) m = fmaxf(m, run(i)[dv]);
+  const float top = finite_or_0(over(m, fmax2));
+  v4f x[NX] = {};
+  for (unsigned at = 0; at < runs; at += TH) {
+    const float2 stat = *reinterpret_cast<const float2*>(run(min(at + j0, runs - 1)) + dv);
+    const bool mine = at + j0 < runs;
+    const float w = mine ? __builtin_amdgcn_exp2f(stat.x - top) : 0.f;
+    l += over(mine ? w * stat.y : 0.f, fadd2);             // (a row of NaNs has weights of 0 and totals of NaN)
+    for (unsigned k = 0; k < min(runs - at, TH); k += AHEAD) {
+      v4f v[AHEAD][NX];
 #pragma unroll
-  for (int off = 4; off >= 1; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, 8));
-  const float top = finite_or_0(m);
-  v4f x[8] = {};
-  for (unsigned at = g0; at <= g1; at += 8) {
-    const unsigned mine = min(at + j0, g1), n = min(g1 - at + 1, 8u);
-    const float2 stat = *reinterpret_cast<const float2*>(run(mine) + dv);
-    const float w = at + j0 <= g1 ? __builtin_amdgcn_exp2f(stat.x - top) : 0.f;
-    float part_l = at + j0 <= g1 ? w * stat.y : 0.f;       // (a row of NaNs has a weight of 0 and a total of NaN)
+      for (unsigned i = 0; i < AHEAD; ++i)
 #pragma unroll
-    for (int off = 4; off >= 1; off >>= 1) part_l += __shfl_xor(part_l, off, 8);
-    l += part_l;
-#pragma unroll 2
-    for (unsigned k = 0; k < n; ++k) {
-      const float* from_run = run(at + k);
-      const float wk = __shfl(w, (int)k, 8);
+        for (unsigned j = 0; j < NX; ++j)
+          v[i][j] = *reinterpret_cast<const v4f*>(run(min(at + k + i, runs - 1)) + min(4 * (j0 + TH * j), dv - 4));
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (4 * (j0 + 8 * j) < dv) x[j] += wk * *reinterpret_cast<const v4f*>(from_run + 4 * (j0 + 8 * j));
+      for (unsigned i = 0; i < AHEAD; ++i) {
+        const float wi = __shfl(w, (int)(k + i), TH);
+        if (at + k + i >= runs) continue;
+#pragma unroll
+        for (unsigned j = 0; j < NX; ++j) x[j] += wi * v[i][j];
+      }
     }
   }
   const unsigned i = tile.row0 + r;
   T* dst = static_cast<T*>(p.out) + (size_t)(tile.first + i / per) * p.ldo + (size_t)(kvh * per + i % per) * p.d;
 #pragma unroll
-  for (int j = 0; j < 8; ++j)
+  for (unsigned j = 0; j < NX; ++j)
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (4 * (j0 + 8 * j) + k < p.d) dst[4 * (j0 + 8 * j) + k] = (T)(l == 0.f ? 0.f : __fdiv_rn(x[j][k], l));
+    for (unsigned k = 0; k < 4; ++k)
+      if (4 * (j0 + TH * j) + k < p.d) dst[4 * (j0 + TH * j) + k] = (T)(l == 0.f ? 0.f : __fdiv_rn(x[j][k], l));
 }
 
 struct Form {
@@ -995,7 +1018,7 @@ int launch_chunk_attention(const mq_kv_cache& cache, const int32_t* table, size_
                            const int32_t* lens, size_t B, size_t T, size_t max_len, int causal, const void* q, size_t ldq,
                            int heads, int dtype, float scale, void* out, size_t ldo, void* ws, hipStream_t s) {
   const Form form = form_of(dtype, B, T, max_len, heads, cache.kv_heads, cache.head_dim);
-  const size_t tiles = form.slots * (size_t)cache.kv_heads, joins = tiles * (form.tile_rows / 32);
+  const size_t tiles = form.slots * (size_t)cache.kv_heads, joins = tiles * (form.tile_rows / join_rows(form.tile_rows));
   const size_t blocks = (max_len + kKvBlock - 1) / kKvBlock;
   // (blocks of all tiles are counted in 32 bits)
   if (!launchable(joins, kWaves * kWave) || form.slots > (((size_t)1 << 32) - 1) / blocks) return MQ_ERR_SHAPE;
@@ -1027,11 +1050,9 @@ int launch_chunk_attention(const mq_kv_cache& cache, const int32_t* table, size_
         }
         return check_hip(hipGetLastError());
       }
-      constexpr unsigned most_waves = few_waves(kParts<DT>, DC);
-      // (the sums' place afterwards is smaller)
-      auto lds_of = [](unsigned waves) { return (size_t)kParts<DT> * DC * 4096 + waves * kWaveBytes<DC>; };
-      auto go = [&](auto kern, unsigned grid, unsigned waves) {
-        const size_t lds = lds_of(waves);
+      constexpr unsigned waves = few_waves(kParts<DT>, DC);
+      constexpr size_t lds = (size_t)kParts<DT> * DC * 4096 + waves * kWaveBytes<DC>;
+      auto go = [&](auto kern, unsigned grid) {
         if (lds > 65536) {
           const int rc = check_hip(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
           if (rc != MQ_OK) return rc;
@@ -1040,10 +1061,10 @@ int launch_chunk_attention(const mq_kv_cache& cache, const int32_t* table, size_
         return check_hip(hipGetLastError());
       };
       if (!form.shares) {
-        return go(k_chunk_few<DT, DC, false>, (unsigned)tiles, (unsigned)(blocks < most_waves ? blocks : most_waves));
+        return go(k_chunk_few<DT, DC, false>, (unsigned)tiles);
       }
       hipLaunchKernelGGL(k_chunk_plan<kRows>, dim3(1), dim3(kPlan), 0, s, p);
-      if (const int rc = go(k_chunk_few<DT, DC, true>, form.groups, most_waves); rc != MQ_OK) return rc;
+      if (const int rc = go(k_chunk_few<DT, DC, true>, form.groups); rc != MQ_OK) return rc;
       hipLaunchKernelGGL((k_chunk_join<DT, kRows>), dim3((unsigned)joins), dim3(256), 0, s, p, form.groups);
       return check_hip(hipGetLastError());
     };
