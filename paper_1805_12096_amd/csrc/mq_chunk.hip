@@ -981,13 +981,18 @@ struct Form {
   unsigned tile_rows, groups;         // rows of a tile; workgroups that share the line
   size_t slots;
 };
-constexpr size_t kManyRows = 96;      // rows of a sequence on average from which on they share blocks through LDS
+// The form for many rows, us of a call, few rows / many: heads of 128, 32 over 8, 8 sequences on 4000 tokens, 128 rows of a kv
+// head 55 / 69 (bfloat16), 85 / 96 (binary16), 100 / 103 (binary32), 192 rows 73 / 67, 113 / 128, 134 / 139, 256 rows 85 / 73, 135 /
+// 130, 163 / 143; heads of 64, 8, 64 sequences on 400, binary32, 96 rows 38 / 46, 128 rows 91 / 52.  Its plan, its longer start and
+// its parts take 30 us of any call: heads of 64, 8 over 2, 64 sequences on 400, bfloat16, 256 rows 19 / 33, 512 rows 63 / 52.
+constexpr size_t many_rows(size_t d) { return d <= 64 ? 128 : 160; }       // rows of a sequence on average
+constexpr size_t kManyWork = (size_t)1 << 31;      // rows x longest sequence x width
 constexpr size_t kShort = 8;          // blocks of the longest sequence up to which a workgroup takes all of a tile's
 Form form_of(int dtype, size_t B, size_t T, size_t max_len, int heads, int kv_heads, size_t d) {
   const size_t per = (size_t)(heads / kv_heads), blocks = (max_len + kKvBlock - 1) / kKvBlock;
   Form f{};
   // (binary32 queries of wide heads do not fit beside the sums)
-  f.many = T * per / B >= kManyRows && !(dtype == MQ_F32 && d > 128);
+  f.many = T * per / B >= many_rows(d) && T * (size_t)heads * d >= kManyWork / max_len && !(dtype == MQ_F32 && d > 128);
   f.shares = f.many || blocks > kShort;
   f.tile_rows = kRows;
   f.groups = d <= 64 ? 768 : d <= 128 ? 512 : 256;

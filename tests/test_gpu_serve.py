@@ -142,12 +142,15 @@ CHUNKS = [
     ([40, 1], [41, 190], 5, 5, 160),
     ([130, 257, 1], [700, 257, 3], 12, 3, 96),
     ([1, 1, 1], [4500, 33, 0], 7, 1, 64),
-    # many rows: whole tiles and ragged ends, several runs of blocks
+    # many rows (and tables so wide that there may be much to do): whole tiles and ragged ends, parts of tiles
     ([300, 0, 77], [300, 10, 2500], 4, 2, 64),
     ([513, 70], [5000, 90], 4, 1, 128),
     ([200], [4400], 3, 3, 192),
     ([129, 260], [131, 2300], 2, 1, 250),
     ([64], [64], 16, 2, 40),
+    # and few rows of a call that may be long
+    ([3, 1, 0, 20], [1200, 64, 7, 3000], 8, 2, 128),
+    ([2], [4097], 4, 4, 256),
 ]
 
 
@@ -160,11 +163,11 @@ def test_chunk(dtype, causal, case):
     T = sum(new)
     need = sum(-(-n // BLOCK) for n in lens) + 2
     cache = random_cache(g, need, kv_heads, dim)
-    width = max(1, max(-(-n // BLOCK) for n in lens)) + case % 2
+    width = max(1, max(-(-n // BLOCK) for n in lens)) + case % 2 + (2000 if case >= 10 else 0)
     table = tables(g, lens, width, need)
     first = np.concatenate([[0], np.cumsum(new)])
     q = normal(g, T, heads * dim).to(dtype).to(DEV)
-    max_len = max(1, max(lens))
+    max_len = max(1, max(lens)) if case < 10 else width * BLOCK
     out = chunk_call(cache, i32(table), i32(first), i32(lens), max_len, causal, q, heads, dim ** -0.5)
     check_chunk(out, *chunk_expected(cache, table, first, lens, max_len, causal, q, heads, dim ** -0.5, dtype))
 
