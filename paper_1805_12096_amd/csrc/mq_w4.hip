@@ -199,6 +199,12 @@ __device__ __forceinline__ void x_parts(const Raw<XT>& r, typename Operand<XT>::
   }
 }
 
+// Steps of 32 elements after which the zero is taken off a sum and the scale put to it: a group's, but for binary32 each, since
+// the difference of sum (16 + c) x and (16 + z) sum x loses more the longer they have grown (against 64 bits, groups of 128, 100 rows:
+// 1.2e-6 off with a group's sums, 6e-7 with 32 elements').
+template <int XT, int GROUP>
+constexpr int kEvery = XT == MQ_F32 ? 1 : GROUP / 32;
+
 // Few rows, of whole 16-byte pieces.  A workgroup has 16 NT rows of the parameter and 16 MT rows of x; its waves take the
 // fragments in turn, the next ones' loads ahead of this one's products, and join in LDS.  A lane of an operand has a row of x of its
 // own; loaded like that, every lane would be an access to the nearest cache of its own (64 a load instead of 8 .. 16, which bound
@@ -208,6 +214,7 @@ template <int XT, int GROUP, int MT, int NT>
 __global__ __launch_bounds__(512) void k_w4_few(const W4Params p) {
   using T = typename XElem<XT>::T;
   constexpr int NP = kXParts<XT>, GF = kKT / GROUP, SG = GROUP / 32;      // groups of a fragment, steps of a group
+  constexpr int EVERY = kEvery<XT, GROUP>;
   extern __shared__ __attribute__((aligned(16))) char smem[];
   float* const lds = reinterpret_cast<float*>(smem);       // [waves][MT 16][NT 16 + 1], afterwards
   const unsigned lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), waves = blockDim.x / kWave;
@@ -296,38 +303,31 @@ __global__ __launch_bounds__(512) void k_w4_few(const W4Params p) {
     }
   };
   auto multiply = [&](int at) __attribute__((always_inline)) {
+    typename Op::Acc acc[NT][MT], sum[MT];
 #pragma unroll
-    for (int g = 0; g < GF; ++g) {
-      typename Op::Acc acc[NT][MT] = {}, sum[MT] = {};
+    for (int step = 0; step < 4; ++step) {
+      Piece c[NT];
 #pragma unroll
-      for (int i = 0; i < SG; ++i) {
-        const int step = g * SG + i;
-        Piece c[NT];
+      for (int n = 0; n < NT; ++n) c[n] = Op::codes(w[at][n][step]);
 #pragma unroll
-        for (int n = 0; n < NT; ++n) c[n] = Op::codes(w[at][n][step]);
+      for (int t = 0; t < MT; ++t) {
 #pragma unroll
-        for (int t = 0; t < MT; ++t) {
+        for (int j = NP - 1; j >= 0; --j) {
+          const bool begins = step % EVERY == 0 && j == NP - 1;
+          const Piece xp = read_x(t, j, step);
 #pragma unroll
-          for (int j = NP - 1; j >= 0; --j) {
-            const Piece xp = read_x(t, j, step);
-#pragma unroll
-            for (int n = 0; n < NT; ++n) acc[n][t] = Op::mfma(xp, c[n], acc[n][t]);
-            sum[t] = Op::mfma(xp, ones, sum[t]);
-          }
+          for (int n = 0; n < NT; ++n) acc[n][t] = Op::mfma(xp, c[n], begins ? typename Op::Acc{} : acc[n][t]);
+          sum[t] = Op::mfma(xp, ones, begins ? typename Op::Acc{} : sum[t]);
         }
       }
-      float total[MT][4];
-#pragma unroll
-      for (int t = 0; t < MT; ++t)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) total[t][r] = (float)sum[t][r];
+      if (step % EVERY != EVERY - 1) continue;
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        const float s = scale_of(sc[at][n][g]), z = offset_of<XT>(sc[at][n][g]);
+        const float s = scale_of(sc[at][n][step / SG]), z = offset_of<XT>(sc[at][n][step / SG]);
 #pragma unroll
         for (int t = 0; t < MT; ++t)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) y[n][t][r] = fmaf(s, fmaf(-z, total[t][r], (float)acc[n][t][r]), y[n][t][r]);
+          for (int r = 0; r < 4; ++r) y[n][t][r] = fmaf(s, fmaf(-z, (float)sum[t][r], (float)acc[n][t][r]), y[n][t][r]);
       }
     }
   };
@@ -370,7 +370,7 @@ __global__ __launch_bounds__(512) void k_w4_few(const W4Params p) {
 constexpr int many_mt(int parts) { return parts == 1 ? 4 : 2; }
 constexpr int kManyNT = 4, kManyWaves = 4;
 
-// operand parts [row tile][fragment][step][part][lane], 16 bytes each (8 of 8-bit rows), then sums [row tile][group][16 rows]
+// operand parts [row tile][fragment][step][part][lane], 16 bytes each (8 of 8-bit rows), then sums of kEvery steps [row tile][..][16 rows]
 struct XDims {
   size_t tiles, frags;
   int parts;
@@ -384,7 +384,7 @@ template <int XT, int GROUP>
 __global__ __launch_bounds__(256) void k_w4_x(const W4Params p, uint8_t* to) {
   using T = typename XElem<XT>::T;
   using Piece = typename Operand<XT>::Piece;
-  constexpr int NP = kXParts<XT>, SG = GROUP / 32;
+  constexpr int NP = kXParts<XT>, EVERY = kEvery<XT, GROUP>;
   const XDims x(p.M, p.K, NP);
   const unsigned lane = threadIdx.x % kWave, col = lane % 16, grp = lane / 16;
   const size_t all = x.tiles * x.frags;
@@ -412,10 +412,10 @@ __global__ __launch_bounds__(256) void k_w4_x(const W4Params p, uint8_t* to) {
       for (int k = 0; k < NP; ++k) dst[k * kWave] = part[k];
 #pragma unroll
       for (int j = 0; j < 8; ++j) sum += (float)r[i].v[j];
-      if (i % SG != SG - 1) continue;
+      if (i % EVERY != EVERY - 1) continue;
       auto add = [](float a, float b) { return a + b; };
       sum = across16_f(across32_f(sum, add), add);
-      if (grp == 0) reinterpret_cast<float*>(to + x.sums_at())[(s * (4 / SG) + i / SG) * 16 + col] = sum;
+      if (grp == 0) reinterpret_cast<float*>(to + x.sums_at())[(s * (4 / EVERY) + i / EVERY) * 16 + col] = sum;
       sum = 0.f;
     }
   }
@@ -423,7 +423,7 @@ __global__ __launch_bounds__(256) void k_w4_x(const W4Params p, uint8_t* to) {
 
 template <int XT, int GROUP>
 __global__ __launch_bounds__(kManyWaves * kWave, 2) void k_w4_many(const W4Params p, const uint8_t* xs, unsigned runs, unsigned run) {
-  constexpr int NP = kXParts<XT>, GF = kKT / GROUP, SG = GROUP / 32, MT = many_mt(NP), NT = kManyNT;
+  constexpr int NP = kXParts<XT>, GF = kKT / GROUP, SG = GROUP / 32, MT = many_mt(NP), NT = kManyNT, EVERY = kEvery<XT, GROUP>;
   extern __shared__ float lds[];                 // [waves][MT 16][NT 16 + 1]
   const unsigned lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), col = lane % 16, grp = lane / 16;
   // neighbouring workgroups share rows of x: those of one XCD its parts
@@ -447,7 +447,7 @@ __global__ __launch_bounds__(kManyWaves * kWave, 2) void k_w4_many(const W4Param
   for (int t = 0; t < MT; ++t) {
     const size_t tile = min(m0 + t, (unsigned)xd.tiles - 1);
     xp[t] = reinterpret_cast<const Piece*>(xs) + tile * xd.frags * 4 * NP * kWave;
-    xsum[t] = reinterpret_cast<const float*>(xs + xd.sums_at()) + tile * xd.frags * GF * 16;
+    xsum[t] = reinterpret_cast<const float*>(xs + xd.sums_at()) + tile * xd.frags * (4 / EVERY) * 16;
   }
   float y[NT][MT][4] = {};
   // codes and scales of the next fragment and x of the next step are on their way
@@ -473,11 +473,10 @@ __global__ __launch_bounds__(kManyWaves * kWave, 2) void k_w4_many(const W4Param
     v4f sum[MT];
 #pragma unroll
     for (int step = 0; step < 4; ++step) {
-      const int g = step / SG;
       load_x((step + 1) % 2, step < 3 ? f : next, (step + 1) % 4);
-      if (step % SG == 0)
+      if (step % EVERY == 0)
 #pragma unroll
-        for (int t = 0; t < MT; ++t) sum[t] = reinterpret_cast<const v4f*>(xsum[t] + ((size_t)f * GF + g) * 16)[grp];
+        for (int t = 0; t < MT; ++t) sum[t] = reinterpret_cast<const v4f*>(xsum[t] + ((size_t)f * (4 / EVERY) + step / EVERY) * 16)[grp];
       Piece c[NT];
 #pragma unroll
       for (int n = 0; n < NT; ++n) c[n] = Op::codes(w[at][n][step]);
@@ -487,11 +486,11 @@ __global__ __launch_bounds__(kManyWaves * kWave, 2) void k_w4_many(const W4Param
         for (int j = NP - 1; j >= 0; --j)
 #pragma unroll
           for (int n = 0; n < NT; ++n)
-            acc[n][t] = Op::mfma(x[step % 2][t][j], c[n], step % SG == 0 && j == NP - 1 ? typename Op::Acc{} : acc[n][t]);
-      if (step % SG != SG - 1) continue;
+            acc[n][t] = Op::mfma(x[step % 2][t][j], c[n], step % EVERY == 0 && j == NP - 1 ? typename Op::Acc{} : acc[n][t]);
+      if (step % EVERY != EVERY - 1) continue;
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        const float s = scale_of(sc[at][n][g]), z = offset_of<XT>(sc[at][n][g]);
+        const float s = scale_of(sc[at][n][step / SG]), z = offset_of<XT>(sc[at][n][step / SG]);
 #pragma unroll
         for (int t = 0; t < MT; ++t)
 #pragma unroll
