@@ -35,7 +35,7 @@ struct ChunkParams {
   float scale2;                       // scale log2(e)
   int causal;
   unsigned* plan;                     // [slots + 1] blocks of the tiles in front of each tile, then at 16 bytes [slots] tiles
-  unsigned slots;                     // tiles at most
+  unsigned slots, least;              // tiles at most; blocks that a workgroup takes at least
 };
 
 // Exponent of the power of two taken off a row whose largest magnitude is m.
@@ -92,7 +92,6 @@ __device__ __forceinline__ unsigned seen_by(const ChunkParams& p, const Tile& t,
 // more where lengths differ: the longest sequence decides how many there are of every one, and most workgroups find nothing.)
 
 constexpr int kPlan = 1024;           // threads of the workgroup that plans
-constexpr unsigned kLeast = 8;        // blocks that a workgroup takes at least
 
 // Blocks that a tile's last row sees, one at least: every tile belongs to somebody.
 __device__ __forceinline__ unsigned tile_blocks(const ChunkParams& p, const Tile& t, unsigned per) {
@@ -146,7 +145,7 @@ __global__ __launch_bounds__(kPlan) void k_chunk_plan(const ChunkParams p) {
 // Blocks of the line that a workgroup has.
 __device__ __forceinline__ unsigned long long share_of(const ChunkParams& p, unsigned groups) {
   const unsigned long long all = (unsigned long long)p.plan[p.slots] * p.kv_heads;
-  return max((unsigned long long)kLeast, (all + groups - 1) / groups);
+  return max((unsigned long long)p.least, (all + groups - 1) / groups);
 }
 
 // A workgroup's next part of the line: blocks [start, end) of a tile and a kv head; whole: all that the tile has.
@@ -383,6 +382,7 @@ __device__ __forceinline__ void few_rows(const ChunkParams& p, int vec, const Li
     }
     float f = there ? qscale * am.x : 0.f, mt = -INFINITY;
     f = f == 0.f ? 1e-30f : f;                 // (0 times a masked score would be NaN; others are below 2^24)
+    settle(sc[0], sc[1]);
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -785,6 +785,7 @@ __device__ __forceinline__ void many_rows(const ChunkParams& p, int vec, const L
 #pragma unroll
       for (int x = 0; x < CT; ++x) {
         float m = -INFINITY;
+        settle(sc[t][x]);
 #pragma unroll
         for (int r = 0; r < 16; r += 2) m = max3(m, sc[t][x][r], sc[t][x][r + 1]);
         mt[x] = across32_f(m, fmax2) * f[x];
@@ -987,7 +988,7 @@ struct Form {
 // its parts take 30 us of any call: heads of 64, 8 over 2, 64 sequences on 400, bfloat16, 256 rows 19 / 33, 512 rows 63 / 52.
 constexpr size_t many_rows(size_t d) { return d <= 64 ? 128 : 160; }       // rows of a sequence on average
 constexpr size_t kManyWork = (size_t)1 << 31;      // rows x longest sequence x width
-constexpr size_t kShort = 8;          // blocks of the longest sequence up to which a workgroup takes all of a tile's
+constexpr size_t kShort = 32;         // blocks of the longest sequence up to which a workgroup takes all of a tile's
 Form form_of(int dtype, size_t B, size_t T, size_t max_len, int heads, int kv_heads, size_t d) {
   const size_t per = (size_t)(heads / kv_heads), blocks = (max_len + kKvBlock - 1) / kKvBlock;
   Form f{};
@@ -1031,7 +1032,7 @@ int launch_chunk_attention(const mq_kv_cache& cache, const int32_t* table, size_
   const ChunkParams p{cache.keys, cache.values, cache.amax, table, first, lens, q, out, part, ldq, ldo,
                       table_width, cache.blocks, (unsigned)B, (unsigned)T, (unsigned)max_len, (unsigned)cache.kv_heads,
                       (unsigned)heads, (unsigned)cache.head_dim, scale * 1.44269504088896340736f, causal,
-                      reinterpret_cast<unsigned*>(part + part_floats(form, cache.head_dim)), (unsigned)form.slots};
+                      reinterpret_cast<unsigned*>(part + part_floats(form, cache.head_dim)), (unsigned)form.slots, form.many ? 8u : 4u};
   const size_t piece = 16 / elem_bytes(dtype);
   // whole 16-byte pieces of queries, four neighbouring results at once
   const int vec = (cache.head_dim % piece == 0 && ldq % piece == 0 && reinterpret_cast<uintptr_t>(q) % 16 == 0 ? 1 : 0) |

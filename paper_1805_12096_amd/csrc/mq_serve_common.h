@@ -42,7 +42,12 @@ __device__ __forceinline__ bf8 bf16_of_bytes(unsigned lo, unsigned hi) {
                 upper(f32_of_byte<0>(hi), f32_of_byte<1>(hi)), upper(f32_of_byte<2>(hi), f32_of_byte<3>(hi))};
   return __builtin_bit_cast(bf8, w);
 }
-// The largest of three, NaNs left out (fmaxf would quiet each operand in an instruction of its own).
+// Sums of matrix instructions that inline assembly reads next: it keeps the wait states (12 of a 32 x 32 x 16 product) that the
+// compiler keeps only in front of instructions of its own.
+__device__ __forceinline__ void settle(v16f& a, v16f& b) { asm volatile("s_nop 15" : "+v"(a), "+v"(b)); }
+__device__ __forceinline__ void settle(v16f& a) { asm volatile("s_nop 15" : "+v"(a)); }
+// The largest of three, NaNs left out (fmaxf would quiet each operand in an instruction of its own).  settle() goes in front of
+// it where a matrix instruction wrote an operand.
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float y;
   asm("v_max3_f32 %0, %1, %2, %3" : "=v"(y) : "v"(a), "v"(b), "v"(c));
