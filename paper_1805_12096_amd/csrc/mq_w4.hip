@@ -576,7 +576,7 @@ int launch_w4_unpack(const void* packed, size_t N, size_t K, int group, float* w
 namespace {
 
 // rows of x up to which the form for few rows is taken, if they are whole pieces (more parts fill LDS)
-constexpr size_t few_rows(int parts) { return parts == 1 ? 32 : 16; }
+constexpr size_t few_rows(int parts) { return parts == 1 ? 32 : parts == 2 ? 16 : 8; }
 struct ManyForm {
   unsigned ntiles, chunks, runs, run;
 };
