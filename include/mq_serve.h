@@ -37,9 +37,12 @@ extern "C" {
  *     ldo = ldq); rows that belong to no sequence are left as they are.
  * Queries enter the products exactly: one, two or three bfloat16 parts (bfloat16, binary16, binary32; elements below 2^-100 of
  * their row's largest may be lost).  The cache's integers are bfloat16 values as they are.  Probabilities times the scale of the
- * values' block enter as as many parts, 8, 16 or 24 bits.  Sums and softmax statistics are binary32.
- * ws: device, 16-byte aligned, mq_chunk_attention_ws_bytes (0 for invalid arguments).  One launch, two where sequences are split
- * over workgroups. */
+ * values' block enter as as many parts, 8, 16 or 24 bits (16-bit types: values of a
+ * block whose largest is below 2^-119 count as zeros, and bits of values below 2^-100 may be lost).  Sums and softmax statistics
+ * are binary32.
+ * ws: device, 16-byte aligned, mq_chunk_attention_ws_bytes (0 for invalid arguments).  One launch where max_len <= 2048 and rows
+ * are few, else three: shares are planned from the lengths, computed, and joined.  Calls of which that plan cannot count the
+ * blocks in 32 bits (some 2^32 / (max_len / 64) tiles of 32 rows) are refused with MQ_ERR_SHAPE. */
 size_t mq_chunk_attention_ws_bytes(size_t B, size_t T, size_t max_len, int heads, int kv_heads, size_t head_dim);
 int mq_chunk_attention(const mq_kv_cache* cache, const int32_t* table, size_t table_width, const int32_t* first,
                        const int32_t* lens, size_t B, size_t T, size_t max_len, int causal, const void* q, size_t ldq, int heads,
@@ -101,8 +104,8 @@ int mq_add_rms_norm_pack8(const void* x, size_t ldx, const void* r, size_t ldr, 
 /* ---- parameters in 4 bits ------------------------------------------------------
  * Element k of row n of an [N x K] parameter is (c - z) s with a code c and, for every group of `group` (32, 64 or 128) neighbours
  * along k, a zero z, both in 0 .. 15, and a scale s.  The last group of a row may be shorter.  groups = ceil(K / group).
- * Scales are held with 20 bits of mantissa (rounded to nearest; all of a binary16 or bfloat16 value, except that scales below
- * 2^-126 become 0).  N, K <= 2^24.
+ * Scales are held with 20 bits of mantissa (rounded to nearest: all of a binary16 or bfloat16 value; scales below 2^-126 are
+ * rounded to multiples of 2^-145).  N, K <= 2^24.
  *   mq_w4_bytes: size of the packed parameter (0 for invalid arguments), opaque and position independent.
  *   mq_w4_pack: codes device uint8 [N x K] (the low four bits count), scales device float [N x groups], zeros device uint8
  *     [N x groups] or NULL (8 everywhere).
@@ -122,7 +125,8 @@ int mq_w4_unpack(const void* packed, size_t N, size_t K, int group, float* w, vo
  * x enters the products exactly (1, 1, 2, 3 bfloat16 parts for int8, bfloat16, binary16, binary32; of magnitudes below 2^-100 the
  * last bits of the latter may be lost), codes exactly, scales after the sums over a group; sums are binary32.  y must not
  * overlap x.  packed: 16-byte aligned.  ws: device, 16-byte aligned, mq_w4_product_ws_bytes(M, N, K) bytes (0 for invalid
- * arguments).  One launch, two where a contraction is split over workgroups. */
+ * arguments).  One launch for up to 32, 16 or 8 rows (8-bit and bfloat16, binary16, binary32) if they are whole 16-byte pieces,
+ * else two, or three where a contraction is split over workgroups. */
 #define MQ_ROWS8 3
 size_t mq_w4_product_ws_bytes(size_t M, size_t N, size_t K);
 int mq_w4_product(const void* x, size_t ldx, int xtype, const float* row_scale, const void* packed, size_t M, size_t N, size_t K,

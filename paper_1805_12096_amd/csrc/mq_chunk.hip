@@ -88,8 +88,8 @@ __device__ __forceinline__ unsigned seen_by(const ChunkParams& p, const Tile& t,
 //
 // Lengths are known on the device only, so a first small launch sums up the blocks that each tile of rows sees.  The workgroups,
 // as many as run at once, share the blocks of all tiles and kv heads in one line equally: each has some tiles whole, and parts of
-// the tiles at its two ends, which go to the workspace and are joined.  (Runs of equal length, a workgroup each, cost two thirds
-// more where lengths differ: the longest sequence decides how many there are of every one, and most workgroups find nothing.)
+// the tiles at its two ends, which go to the workspace and are joined.  (Instead of runs of equal length, a workgroup each, as many
+// of every tile as the longest needs: 64 sequences of 512 .. 4096 tokens with 256 new ones, 526 us; equal shares 453.)
 
 constexpr int kPlan = 1024;           // threads of the workgroup that plans
 
@@ -186,7 +186,12 @@ __device__ __forceinline__ void each_part(const ChunkParams& p, F f) {
 
 // ---- few rows -------------------------------------------------------------------------------------------------------------
 //
-// A workgroup has 32 rows; its waves take the blocks in turn, each straight from memory, and join in LDS.
+// A workgroup has 32 rows; its waves take the blocks in turn, each through its own part of LDS with no barrier, and join there.
+// Bound by the bytes of the cache where sequences are long: 32 sequences of 4 new tokens, 32 heads over 8 of 128, 16000 tokens
+// held, 1.05 GB in 216 us, 4.6 TB/s of 4.7 that a copy reaches; up to 4000 held, 243 MB in 76 us (3.2 TB/s), of which plan,
+// start and join take 20.  Few tokens are bound by the way of one block, some 1.5 us: 64 sequences of up to 512 8.4 us.
+// Blocks come by the loads that go to LDS directly, 1 KB each in whole lines (a lane that loads its own row is an access of its own
+// to the nearest cache, 64 a load: 117 us), keys of the next block as soon as this one's are in registers, values likewise.
 
 // LDS of a wave's block of keys and values, loads of 1 KB of either, and waves of a workgroup at most: 160 KB hold its blocks and
 // the queries.
@@ -512,11 +517,15 @@ __global__ __launch_bounds__(kWaves * kWave, DC > 2 ? 1 : 2) void k_chunk_few(co
 
 // ---- many rows ----------------------------------------------------------------------------------------------------------
 //
-// A workgroup's four waves have 32 CT rows each and go through the same blocks, which they bring into LDS together, converted to
+// A workgroup's waves have 32 rows each and go through the same blocks, which they bring into LDS together, converted to
 // bfloat16 once, in operand order.  Scores are 32 tokens ahead: their products stand beside the exponentials of the 32 tokens
 // before, and the conversions of blocks to come beside the products of the values.  One barrier a block; three places in
 // LDS for keys, since this block's and the next one's are read while those of the one after come, two for values.
 // The scale of a block's values goes into the exponent (for binary32, whose 24 bits the logarithm would cost some, into a product).
+// Bound by what a SIMD can issue: 32 heads of 128 over 8, four pieces of 300 .. 1100 tokens on 2000 .. 16000, bfloat16, 328 GFLOP
+// in 420 us (780 TFLOP/s of 1236 that a large library product reaches).  Of the 794 thousand clocks of a SIMD the matrix unit has
+// 338 and the vector unit 431, which hardly overlap: exponentials, conversions, masks and sums cost as much as the products.
+// One workgroup of eight waves shares each block where registers let two waves stay on a SIMD (with four of 64 rows each: 714 us).
 
 // Sums of matrix instructions times a factor, from accumulation registers and back.  (The compiler would otherwise take the
 // copies that the vector unit needs out of the branch, into every step.)
@@ -534,7 +543,7 @@ __device__ __forceinline__ void scale_sums(v16f& o, float factor) {
 template <int DT, int DC>
 struct TileForm {
   // two waves a SIMD where their registers fit
-  static constexpr int NP = kParts<DT>, CT = 1, W = NP * DC <= 2 ? 8 : 4, kRowsOfWg = W * 32 * CT;
+  static constexpr int NP = kParts<DT>, W = NP * DC <= 2 ? 8 : 4, kRowsOfWg = W * 32;
   static constexpr int kUnits = 8 * DC;                    // 1 KB pieces of a block's keys, and of its values
   static constexpr size_t kLds = 5 * (size_t)kUnits * 1024;       // three blocks of keys, two of values
   static constexpr bool kFold = NP < 3;
@@ -544,7 +553,7 @@ template <int DT, int DC>
 __device__ __forceinline__ void many_rows(const ChunkParams& p, int vec, const LinePart& part, unsigned to_part) {
   using T = typename Elem<DT>::T;
   using Form = TileForm<DT, DC>;
-  constexpr int NP = Form::NP, CT = Form::CT, W = Form::W, NK = 2 * DC, ND = 2 * DC, KU = Form::kUnits;
+  constexpr int NP = Form::NP, W = Form::W, NK = 2 * DC, ND = 2 * DC, KU = Form::kUnits;
   extern __shared__ __attribute__((aligned(16))) bf8 tile_lds[];                 // keys [3][KU][64], values [2][KU][64]
   bf8 *const kl = tile_lds, *const vl = tile_lds + 3 * KU * kWave;
   // (unknown to the compiler to be the same each time: it would keep dozens of places and masks from one part to the next)
@@ -556,17 +565,11 @@ __device__ __forceinline__ void many_rows(const ChunkParams& p, int vec, const L
   const unsigned nblocks = (seen_by(p, tile, (tile.row0 + tile.rows - 1) / per) + kKvBlock - 1) / kKvBlock;
   const unsigned count = min(part.end, nblocks) > start ? min(part.end, nblocks) - start : 0;
   // this wave's rows; past the tile's end they repeat its last and are not stored
-  unsigned mine_sees[CT], least = 0xffffffffu;
-  uint2 at[CT];
-  bool stored[CT];
-#pragma unroll
-  for (int x = 0; x < CT; ++x) {
-    const unsigned r = (wave * CT + x) * 32 + col, i = tile.row0 + min(r, tile.rows - 1);
-    stored[x] = r < tile.rows;
-    at[x] = make_uint2(tile.first + i / per, kvh * per + i % per);
-    mine_sees[x] = seen_by(p, tile, i / per);
-  }
-  least = __builtin_amdgcn_readfirstlane(mine_sees[0]);    // (ascends along the rows)
+  const unsigned row = wave * 32 + col, in_seq = tile.row0 + min(row, tile.rows - 1);
+  const bool stored = row < tile.rows;
+  const uint2 at = make_uint2(tile.first + in_seq / per, kvh * per + in_seq % per);
+  const unsigned mine_sees = seen_by(p, tile, in_seq / per);
+  const unsigned least = __builtin_amdgcn_readfirstlane(mine_sees);        // (ascends along the rows)
 
   // what a wave brings: keys piece n: units 2 i, 2 i + 1 with i = wave + W n = t NK + c: token 32 t + col, bytes 32 c + 16 grp ..
   // values piece n: units 2 i, 2 i + 1 with i = wave + W n = 2 tile + half: row 32 tile + col, 8 bytes of either 16 that hold lane
@@ -640,61 +643,52 @@ __device__ __forceinline__ void many_rows(const ChunkParams& p, int vec, const L
   fetch_keys(0);
 
   // queries in operand order, a power of two off each row
-  bf8 qf[CT][NP][NK * 2];
-  float qscale[CT];
+  bf8 qf[NP][NK * 2];
+  const T* src = static_cast<const T*>(p.q) + (size_t)at.x * p.ldq + (size_t)at.y * d;
+  float m = 0.f;
+  auto query = [&](int u, float (&v)[8]) {
+    const unsigned k = 32 * (u / 2) + 16 * grp + 8 * (u % 2), d = again(p.d);
+    if (vec & 1) {
+      constexpr int W = 16 / sizeof(T);
+      typedef T tw __attribute__((ext_vector_type(W)));
 #pragma unroll
-  for (int x = 0; x < CT; ++x) {
-    const T* src = static_cast<const T*>(p.q) + (size_t)at[x].x * p.ldq + (size_t)at[x].y * d;
-    float m = 0.f;
-    auto piece = [&](int u, float (&v)[8]) {
-      const unsigned k = 32 * (u / 2) + 16 * grp + 8 * (u % 2), d = again(p.d);
-      if (vec & 1) {
-        constexpr int W = 16 / sizeof(T);
-        typedef T tw __attribute__((ext_vector_type(W)));
+      for (int j = 0; j < 8; j += W) {
+        tw w = {};
+        if (k + j < d) w = *reinterpret_cast<const tw*>(src + k + j);
 #pragma unroll
-        for (int j = 0; j < 8; j += W) {
-          tw w = {};
-          if (k + j < d) w = *reinterpret_cast<const tw*>(src + k + j);
-#pragma unroll
-          for (int i = 0; i < W; ++i) v[j + i] = (float)w[i];
-        }
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = k + j < d ? (float)src[k + j] : 0.f;
+        for (int i = 0; i < W; ++i) v[j + i] = (float)w[i];
       }
-    };
+    } else {
 #pragma unroll
-    for (int u = 0; u < NK * 2; ++u) {
-      float v[8];
-      piece(u, v);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) m = fmaxf(m, fabsf(v[j]) <= 3.402823466e38f ? fabsf(v[j]) : INFINITY);
+      for (int j = 0; j < 8; ++j) v[j] = k + j < d ? (float)src[k + j] : 0.f;
     }
-    m = across32_f(m, fmax2);
-    const int e = row_exponent(m);
-    const float mul = __uint_as_float((unsigned)(127 - e) << 23) * (p.scale2 < 0.f ? -1.f : 1.f);
-    qscale[x] = ldexpf(fabsf(p.scale2), e) * (1.f / 127.f);
+  };
 #pragma unroll
-    for (int u = 0; u < NK * 2; ++u) {
-      float v[8];
-      piece(u, v);
+  for (int u = 0; u < NK * 2; ++u) {
+    float v[8];
+    query(u, v);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        __bf16 b[NP];
-        split_bf16<NP>(m == INFINITY ? NAN : v[j] * mul, b);
+    for (int j = 0; j < 8; ++j) m = fmaxf(m, fabsf(v[j]) <= 3.402823466e38f ? fabsf(v[j]) : INFINITY);
+  }
+  m = across32_f(m, fmax2);
+  const int e = row_exponent(m);
+  const float mul = __uint_as_float((unsigned)(127 - e) << 23) * (p.scale2 < 0.f ? -1.f : 1.f);
+  const float qscale = ldexpf(fabsf(p.scale2), e) * (1.f / 127.f);
 #pragma unroll
-        for (int i = 0; i < NP; ++i) qf[x][i][u][j] = b[i];
-      }
+  for (int u = 0; u < NK * 2; ++u) {
+    float v[8];
+    query(u, v);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      __bf16 b[NP];
+      split_bf16<NP>(m == INFINITY ? NAN : v[j] * mul, b);
+#pragma unroll
+      for (int i = 0; i < NP; ++i) qf[i][u][j] = b[i];
     }
   }
 
-  float ref[CT], total[CT];
-  v16f acc[CT][ND] = {}, sc[2][CT];            // sums; scores of a block's two halves
-#pragma unroll
-  for (int x = 0; x < CT; ++x) {
-    ref[x] = -INFINITY;
-    total[x] = 0.f;
-  }
+  float ref = -INFINITY, total = 0.f;
+  v16f acc[ND] = {}, sc[2];                    // sums; scores of a block's two halves
   // a half block's scores take STEPS products a row tile and part, its sums of values as many: their pieces are asked for from
   // LDS four products ahead
   constexpr int STEPS = NK * 2, AHEAD = 4;
@@ -708,9 +702,7 @@ __device__ __forceinline__ void many_rows(const ChunkParams& p, int vec, const L
     constexpr int t = decltype(half)::value;
 #pragma unroll
     for (int k = NP - 1; k >= 0; --k)
-#pragma unroll
-      for (int x = 0; x < CT; ++x)
-        sc[t][x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(piece[u % AHEAD], qf[x][k][u], u == 0 && k == NP - 1 ? v16f{} : sc[t][x], 0, 0, 0);
+      sc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(piece[u % AHEAD], qf[k][u], u == 0 && k == NP - 1 ? v16f{} : sc[t], 0, 0, 0);
   };
   // scales and presence of the block in turn and the next
   float ak_at[2] = {}, av_now = 0.f;
@@ -737,20 +729,17 @@ __device__ __forceinline__ void many_rows(const ChunkParams& p, int vec, const L
       if (u + AHEAD < STEPS) read_key(kl + lane, std::integral_constant<int, 0>{}, u + AHEAD);
       else read_key(kl + lane, std::integral_constant<int, 1>{}, u + AHEAD - STEPS);
     }
+    settle(sc[0]);                             // (later scores have half a block's sums of values behind them)
   }
   unsigned now = 0, next = 1, after = 2;       // places of the keys of blocks i, i + 1, i + 2
   constexpr bool FOLD = Form::kFold;
-  float sum[CT] = {};                          // of a half block's probabilities times the values' scale, of this lane's tokens
+  float sum = 0.f;                             // of a half block's probabilities times the values' scale, of this lane's tokens
   float inverse = 0.f;                         // of that scale
   for (unsigned i = 0; i < count; ++i) {
     const unsigned pg = start + i, odd = i % 2;
     const bool there = th_at[0];
-    float f[CT];
-#pragma unroll
-    for (int x = 0; x < CT; ++x) {
-      f[x] = there ? qscale[x] * ak_at[0] : 0.f;
-      f[x] = f[x] == 0.f ? 1e-30f : f[x];      // (0 times a masked score would be NaN; others are below 2^24)
-    }
+    float f = there ? qscale * ak_at[0] : 0.f;
+    f = f == 0.f ? 1e-30f : f;                 // (0 times a masked score would be NaN; others are below 2^24)
     // (where there is no block, block 0 was read, whose maxima may be anything)
     const float fv = there ? av_now * (1.f / 127.f) : 0.f;
     const bool nothing = !there || no_values(av_now);
@@ -763,65 +752,46 @@ __device__ __forceinline__ void many_rows(const ChunkParams& p, int vec, const L
       constexpr int t = decltype(which)::value;
       auto read_value = [&](int u) __attribute__((always_inline)) { piece[u % AHEAD] = vu[(4 * (u % ND) + 2 * t + u / ND) * kWave]; };
       if (masks) {
+        const long long room = (long long)mine_sees - (long long)pg * kKvBlock - 4 * (int)grp;
+        const int limit = !there || room < 0 ? 0 : room > kKvBlock ? kKvBlock : (int)room;
 #pragma unroll
-        for (int x = 0; x < CT; ++x) {
-          const long long room = (long long)mine_sees[x] - (long long)pg * kKvBlock - 4 * (int)grp;
-          const int limit = !there || room < 0 ? 0 : room > kKvBlock ? kKvBlock : (int)room;
-#pragma unroll
-          for (int r = 0; r < 16; ++r)
-            if (limit <= 32 * t + 8 * (r / 4) + r % 4) sc[t][x][r] = -INFINITY;
-        }
+        for (int r = 0; r < 16; ++r)
+          if (limit <= 32 * t + 8 * (r / 4) + r % 4) sc[t][r] = -INFINITY;
       }
       if constexpr (FOLD) {
-#pragma unroll
-        for (int x = 0; x < CT; ++x) {
-          total[x] = fmaf(sum[x], inverse, total[x]);
-          sum[x] = 0.f;
-        }
+        total = fmaf(sum, inverse, total);
+        sum = 0.f;
         inverse = inverse_now;
       }
-      float base[CT], mt[CT];
-      bool rises = false;
+      float m = -INFINITY;
 #pragma unroll
-      for (int x = 0; x < CT; ++x) {
-        float m = -INFINITY;
-        settle(sc[t][x]);
+      for (int r = 0; r < 16; r += 2) m = max3(m, sc[t][r], sc[t][r + 1]);
+      const float mt = across32_f(m, fmax2) * f;
+      if (__builtin_expect(__any(mt > ref + kSlack), 0)) {
+        // (only for the rows concerned: no other row's result depends on theirs)
+        const float top = mt > ref + kSlack ? mt : ref;
+        const float keep = top == ref ? 1.f : __builtin_amdgcn_exp2f(ref - top);
+        ref = top;
+        total *= keep;
 #pragma unroll
-        for (int r = 0; r < 16; r += 2) m = max3(m, sc[t][x][r], sc[t][x][r + 1]);
-        mt[x] = across32_f(m, fmax2) * f[x];
-        rises |= mt[x] > ref[x] + kSlack;
+        for (int c = 0; c < ND; ++c) scale_sums<Form::W == 8>(acc[c], keep);
       }
-      if (__builtin_expect(__any(rises), 0)) {
-#pragma unroll
-        for (int x = 0; x < CT; ++x) {
-          // (only for the rows concerned: no other row's result depends on theirs)
-          const float top = mt[x] > ref[x] + kSlack ? mt[x] : ref[x];
-          const float keep = top == ref[x] ? 1.f : __builtin_amdgcn_exp2f(ref[x] - top);
-          ref[x] = top;
-          total[x] *= keep;
-#pragma unroll
-          for (int c = 0; c < ND; ++c) scale_sums<Form::W == 8>(acc[x][c], keep);
-        }
-      }
-#pragma unroll
-      for (int x = 0; x < CT; ++x) base[x] = FOLD ? lift - finite_or_0(ref[x]) : -finite_or_0(ref[x]);
-      bf8 pr[CT][NP][2];
+      const float base = FOLD ? lift - finite_or_0(ref) : -finite_or_0(ref);
+      bf8 pr[NP][2];
       // exponentials [from, end) of the 16 that a lane has of each row
       auto exponentials = [&](int from, int end) __attribute__((always_inline)) {
 #pragma unroll
-        for (int x = 0; x < CT; ++x)
+        for (int n = from; n < end; ++n) {
+          const float e = __builtin_amdgcn_exp2f(fmaf(sc[t][n], f, base));
+          if (!FOLD) total += e;
+          __bf16 b[NP];
+          split_bf16<NP>(FOLD ? e : e * fv, b);
 #pragma unroll
-          for (int n = from; n < end; ++n) {
-            const float e = __builtin_amdgcn_exp2f(fmaf(sc[t][x][n], f[x], base[x]));
-            if (!FOLD) total[x] += e;
-            __bf16 b[NP];
-            split_bf16<NP>(FOLD ? e : e * fv, b);
-#pragma unroll
-            for (int k = 0; k < NP; ++k) {
-              pr[x][k][n / 8][n % 8] = b[k];
-              if (FOLD && n % 2 == 1) sum[x] = add2(pr[x][k][n / 8][n % 8 - 1], b[k], sum[x]);
-            }
+          for (int k = 0; k < NP; ++k) {
+            pr[k][n / 8][n % 8] = b[k];
+            if (FOLD && n % 2 == 1) sum = add2(pr[k][n / 8][n % 8 - 1], b[k], sum);
           }
+        }
       };
       constexpr int EARLY = 12;                // (the others beside the first half of the sums of values)
 #pragma unroll
@@ -837,8 +807,7 @@ __device__ __forceinline__ void many_rows(const ChunkParams& p, int vec, const L
         const int j = u / ND, c = u % ND;
 #pragma unroll
         for (int k = NP - 1; k >= 0; --k)
-#pragma unroll
-          for (int x = 0; x < CT; ++x) acc[x][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(piece[u % AHEAD], pr[x][k][j], acc[x][c], 0, 0, 0);
+          acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(piece[u % AHEAD], pr[k][j], acc[c], 0, 0, 0);
         if (u + AHEAD < STEPS) read_value(u + AHEAD);
         else read_key(keys_then, std::integral_constant<int, t>{}, u + AHEAD - STEPS);
         if (j == 0) exponentials(EARLY + c * (16 - EARLY) / ND, EARLY + (c + 1) * (16 - EARLY) / ND);
@@ -872,43 +841,40 @@ __device__ __forceinline__ void many_rows(const ChunkParams& p, int vec, const L
   }
 
   // every lane has four neighbouring columns of its row at a time
+  const float l = across32_f(FOLD ? fmaf(sum, inverse, total) : total, fadd2);
+  if (!stored) return;
+  if (part.whole) {
+    const bool whole = vec & 2;
+    T* to = static_cast<T*>(p.out) + (size_t)at.x * p.ldo + (size_t)at.y * d;
 #pragma unroll
-  for (int x = 0; x < CT; ++x) {
-    const float l = across32_f(FOLD ? fmaf(sum[x], inverse, total[x]) : total[x], fadd2);
-    if (!stored[x]) continue;
-    if (part.whole) {
-      const bool whole = vec & 2;
-      T* to = static_cast<T*>(p.out) + (size_t)at[x].x * p.ldo + (size_t)at[x].y * d;
+    for (int t = 0; t < ND; ++t)
 #pragma unroll
-      for (int t = 0; t < ND; ++t)
+      for (int r = 0; r < 16; r += 4) {
+        const unsigned c = 32 * t + 2 * r + 4 * grp, end = again(p.d);
+        T v[4];
 #pragma unroll
-        for (int r = 0; r < 16; r += 4) {
-          const unsigned c = 32 * t + 2 * r + 4 * grp, end = again(p.d);
-          T v[4];
+        for (int j = 0; j < 4; ++j) v[j] = (T)(l == 0.f ? 0.f : __fdiv_rn(acc[t][r + j], l));
+        if (whole && c < end) {
+          typedef T t4 __attribute__((ext_vector_type(4)));
+          *reinterpret_cast<t4*>(to + c) = t4{v[0], v[1], v[2], v[3]};
+        } else {
 #pragma unroll
-          for (int j = 0; j < 4; ++j) v[j] = (T)(l == 0.f ? 0.f : __fdiv_rn(acc[x][t][r + j], l));
-          if (whole && c < end) {
-            typedef T t4 __attribute__((ext_vector_type(4)));
-            *reinterpret_cast<t4*>(to + c) = t4{v[0], v[1], v[2], v[3]};
-          } else {
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-              if (c + j < end) to[c + j] = v[j];
-          }
+          for (int j = 0; j < 4; ++j)
+            if (c + j < end) to[c + j] = v[j];
         }
-    } else {
-      float* to = p.part + ((size_t)to_part * Form::kRowsOfWg + (wave * CT + x) * 32 + col) * (dv + 4);
-#pragma unroll
-      for (int t = 0; t < ND; ++t)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const unsigned c = 32 * t + 8 * r + 4 * grp;
-          if (c < dv) *reinterpret_cast<v4f*>(to + c) = v4f{acc[x][t][4 * r], acc[x][t][4 * r + 1], acc[x][t][4 * r + 2], acc[x][t][4 * r + 3]};
-        }
-      if (grp == 0) {
-        to[dv] = ref[x];
-        to[dv + 1] = l;
       }
+  } else {
+    float* to = p.part + ((size_t)to_part * Form::kRowsOfWg + wave * 32 + col) * (dv + 4);
+#pragma unroll
+    for (int t = 0; t < ND; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const unsigned c = 32 * t + 8 * r + 4 * grp;
+        if (c < dv) *reinterpret_cast<v4f*>(to + c) = v4f{acc[t][4 * r], acc[t][4 * r + 1], acc[t][4 * r + 2], acc[t][4 * r + 3]};
+      }
+    if (grp == 0) {
+      to[dv] = ref;
+      to[dv + 1] = l;
     }
   }
 }

@@ -156,18 +156,19 @@ CHUNKS = [
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("causal", [True, False])
-@pytest.mark.parametrize("case", range(len(CHUNKS)))
-def test_chunk(dtype, causal, case):
+@pytest.mark.parametrize("case,room", [(c, 0 if c < 10 else 2000) for c in range(len(CHUNKS))] + [(c, 60) for c in range(10)])
+def test_chunk(dtype, causal, case, room):
+    """room: columns that the table has more than it needs, for calls that say only that sequences may be as long as it is."""
     new, lens, heads, kv_heads, dim = CHUNKS[case]
     g = gen(case)
     T = sum(new)
     need = sum(-(-n // BLOCK) for n in lens) + 2
     cache = random_cache(g, need, kv_heads, dim)
-    width = max(1, max(-(-n // BLOCK) for n in lens)) + case % 2 + (2000 if case >= 10 else 0)
+    width = max(1, max(-(-n // BLOCK) for n in lens)) + case % 2 + room
     table = tables(g, lens, width, need)
     first = np.concatenate([[0], np.cumsum(new)])
     q = normal(g, T, heads * dim).to(dtype).to(DEV)
-    max_len = max(1, max(lens)) if case < 10 else width * BLOCK
+    max_len = width * BLOCK if room else max(1, max(lens))
     out = chunk_call(cache, i32(table), i32(first), i32(lens), max_len, causal, q, heads, dim ** -0.5)
     check_chunk(out, *chunk_expected(cache, table, first, lens, max_len, causal, q, heads, dim ** -0.5, dtype))
 
@@ -198,28 +199,30 @@ def test_chunk_lists_tables_and_rows_that_are_odd(dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-def test_chunk_bad_queries_stay_with_themselves(dtype):
+@pytest.mark.parametrize("max_len", [1200, 4096])
+def test_chunk_bad_queries_stay_with_themselves(dtype, max_len):
     g = gen(6)
     heads, kv_heads, dim = 4, 2, 64
     new, lens = [20, 30], [100, 1200]
     cache = random_cache(g, 24, kv_heads, dim)
-    table, first = tables(g, lens, 19, 24), np.array([0, 20, 50])
+    table, first = tables(g, lens, 64, 24), np.array([0, 20, 50])
     q = normal(g, 50, heads * dim).to(dtype)
     good = q.clone()
     q[3, 5], q[25, 64 + 63], q[49, 200], q[30, :64] = math.nan, math.inf, -math.inf, math.inf
-    args = cache, i32(table), i32(first), i32(lens), 1200, True
+    args = cache, i32(table), i32(first), i32(lens), max_len, True
     out, clean = (chunk_call(*args, x.to(DEV), heads, 0.125) for x in (q, good))
     bad = torch.isnan(q) | torch.isinf(q)
     bad = bad.view(50, heads, dim).any(-1)
     assert torch.isnan(out.view(50, heads, dim)[bad.to(DEV)]).all()
     assert torch.equal(out.view(50, heads, dim)[~bad.to(DEV)], clean.view(50, heads, dim)[~bad.to(DEV)])
     # queries with nothing to see give zeros, whatever they hold
-    out = chunk_call(cache, i32(table), i32(first), i32([2, 0]), 1200, True, q.to(DEV), heads, 0.125)
+    out = chunk_call(cache, i32(table), i32(first), i32([2, 0]), max_len, True, q.to(DEV), heads, 0.125)
     assert (out[:18] == 0).all() and (out[20:] == 0).all() and not torch.isnan(out[18:20]).any()
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
-def test_chunk_large_and_small_magnitudes(dtype):
+@pytest.mark.parametrize("max_len", [400, 4096])
+def test_chunk_large_and_small_magnitudes(dtype, max_len):
     """Scales of blocks that differ by 2^80, queries of any magnitude: references move, nothing overflows on the way."""
     g = gen(7)
     heads, kv_heads, dim = 2, 1, 64
@@ -227,12 +230,12 @@ def test_chunk_large_and_small_magnitudes(dtype):
     cache = random_cache(g, 8, kv_heads, dim)
     cache.amax[:, 0, 1] = torch.tensor([2.0 ** (20 * (i % 5) - 40) for i in range(8)], device=DEV)
     cache.amax[3, 0, 1] = 0
-    table, first = tables(g, lens, 7, 8), np.array([0, 10])
+    table, first = tables(g, lens, 64, 8), np.array([0, 10])
     for power in (-100, -20, 0, 60):
         q = (normal(g, 10, heads * dim) * 2.0 ** power).to(dtype).to(DEV)
         scale = 2.0 ** -(power + 3)
-        out = chunk_call(cache, i32(table), i32(first), i32(lens), 400, True, q, heads, scale)
-        check_chunk(out, *chunk_expected(cache, table, first, lens, 400, True, q, heads, scale, dtype))
+        out = chunk_call(cache, i32(table), i32(first), i32(lens), max_len, True, q, heads, scale)
+        check_chunk(out, *chunk_expected(cache, table, first, lens, max_len, True, q, heads, scale, dtype))
 
 
 def test_chunk_of_one_token_is_cached_attention():
