@@ -67,7 +67,8 @@ int mq_chunk_attention(const mq_kv_cache* cache, const int32_t* table, size_t ta
  *     block among them is lost to its row: where missing is not 0, continue fewer rows from the old table; no block that the old
  *     table's rows hold and that some row continues has been written to).
  * The old table's other rows are not valid any more: their free blocks may have been handed out.
- * ws: device, 16-byte aligned, mq_kv_fork_ws_bytes (0 for invalid arguments).  blocks < 2^30. */
+ * ws: device, 16-byte aligned, mq_kv_fork_ws_bytes (0 for invalid arguments).  blocks < 2^30, B_new table_width < 2^32.  Two
+ * launches for small tables (up to 8192 blocks, 4096 rows, 16384 entries), else four. */
 size_t mq_kv_fork_ws_bytes(size_t blocks, size_t B_new, size_t table_width);
 int mq_kv_fork(const mq_kv_cache* cache, const int32_t* keep, const int32_t* table, size_t table_width, const int32_t* lens,
                size_t B, const int32_t* parent, const int32_t* grow, size_t B_new, int32_t* table_new, int32_t* lens_new,
@@ -79,7 +80,8 @@ int mq_kv_fork(const mq_kv_cache* cache, const int32_t* keep, const int32_t* tab
  *     and entries that are no block are -1.
  *   moved: device int32 [blocks], required: where each block is now, -1 for unused ones (for holders of kept blocks).
  *   used: device int32 [1], U.
- * keep as above (and to be renumbered by the caller, from moved).  ws: mq_kv_compact_ws_bytes.  blocks < 2^30. */
+ * keep as above (and to be renumbered by the caller, from moved).  ws: mq_kv_compact_ws_bytes.  blocks < 2^30.  Two launches for
+ * small tables, as above, else four. */
 size_t mq_kv_compact_ws_bytes(size_t blocks);
 int mq_kv_compact(const mq_kv_cache* cache, const int32_t* keep, const int32_t* table, size_t table_width, const int32_t* lens,
                   size_t B, int32_t* table_new, int32_t* moved, int32_t* used, void* ws, size_t ws_bytes, void* stream);
@@ -87,8 +89,8 @@ int mq_kv_compact(const mq_kv_cache* cache, const int32_t* keep, const int32_t* 
 /* ---- residual addition and root-mean-square norm -----------------------------------
  * For M rows of d <= 16384 elements of a type:
  *   h = x + r, rounded to the type (h = x where r is NULL);   y = h / sqrt(mean(h^2) + eps) gamma
- * in binary32 (h^2 is summed in binary32: below 2^60 nothing overflows).  gamma: device float [d].  h: rows that receive h, or
- * NULL; h may be x or r itself (with its ld), and y may be x, r or none of them, but h and y must not overlap.  One launch each.
+ * in binary32 (h^2 is summed in binary32: below 2^56 nothing overflows).  gamma: device float [d].  h: rows that receive h, or
+ * NULL; h may be x or r itself, and y may be, with its ld, but h and y must not overlap.  One launch each.
  *   mq_add_rms_norm:        y rounded to the type, rows ldy apart.
  *   mq_add_rms_norm_rows8:  q[m][i] = clamp(rne(y s), +-127) as int8 rows ldq apart, with a multiplier for each row,
  *     s = scale[m] = 127 / max |y| (1 for a row of zeros; NaN, and zeros in q, for a row that holds a NaN or an infinity).
@@ -123,8 +125,9 @@ int mq_w4_unpack(const void* packed, size_t N, size_t K, int group, float* w, vo
  *     float [M] (an element q stands for q / row_scale[m], as mq_add_rms_norm_rows8 leaves them); row_scale is NULL for the others.
  *   y: M rows of N elements, ldy apart, of type ytype (an mq_dtype).  bias: device float [N] or NULL.
  * x enters the products exactly (1, 1, 2, 3 bfloat16 parts for int8, bfloat16, binary16, binary32; of magnitudes below 2^-100 the
- * last bits of the latter may be lost), codes exactly, scales after the sums over a group; sums are binary32.  y must not
- * overlap x.  packed: 16-byte aligned.  ws: device, 16-byte aligned, mq_w4_product_ws_bytes(M, N, K) bytes (0 for invalid
+ * last bits of the latter may be lost), codes exactly, scales after the sums over a group (binary32: over 32 elements); sums are
+ * binary32, and up to 31 sum |x| over a group must be one of its numbers.  A row of x with a NaN or an infinity gives no finite
+ * number.  y must not overlap x.  packed: 16-byte aligned.  ws: device, 16-byte aligned, mq_w4_product_ws_bytes(M, N, K) bytes (0 for invalid
  * arguments).  One launch for up to 32, 16 or 8 rows (8-bit and bfloat16, binary16, binary32) if they are whole 16-byte pieces,
  * else two, or three where a contraction is split over workgroups. */
 #define MQ_ROWS8 3

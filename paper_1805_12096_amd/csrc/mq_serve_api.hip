@@ -74,7 +74,7 @@ int mq_kv_fork(const mq_kv_cache* cache, const int32_t* keep, const int32_t* tab
       ws == nullptr)
     return MQ_ERR_NULL;
   if (!count_ok(B) || !count_ok(B_new) || cache->blocks >= kMaxTableBlocks || table_width > kMaxTableBlocks / 64 ||
-      B > kMaxElems / table_width || B_new > kMaxElems / table_width)
+      B > kMaxElems / table_width || B_new > 0xffffffffu / table_width)        // (new entries are counted in 32 bits)
     return MQ_ERR_SHAPE;
   if (!aligned(keep, 4) || !aligned(lens, 4) || !aligned(parent, 4) || !aligned(grow, 4) || !aligned(table_new, 4) ||
       !aligned(lens_new, 4) || !aligned(missing, 4) || !aligned(ws, 16))

@@ -107,7 +107,7 @@ REFUSALS = {
         (dict(B=1 << 23), SHAPE), (dict(T=1 << 28, ldq=256, ldo=256), SHAPE)],
     "mq_kv_fork": TABLE_REFUSALS + [
         (dict(parent=None), NULL), (dict(grow=None), NULL), (dict(lens_new=None), NULL), (dict(missing=None), NULL),
-        (dict(B_new=0), SHAPE), (dict(B_new=(1 << 30) + 1), SHAPE), (dict(B_new=1 << 29), SHAPE), (dict(parent=G + 2), ALIGN),
+        (dict(B_new=0), SHAPE), (dict(B_new=(1 << 30) + 1), SHAPE), (dict(B_new=1 << 29), SHAPE), (dict(B_new=1 << 10, table_width=1 << 22), SHAPE), (dict(parent=G + 2), ALIGN),
         (dict(grow=G + 1), ALIGN), (dict(lens_new=G + 2), ALIGN), (dict(missing=G + 2), ALIGN)],
     "mq_kv_compact": TABLE_REFUSALS + [
         (dict(moved=None), NULL), (dict(used=None), NULL), (dict(moved=G + 2), ALIGN), (dict(used=G + 2), ALIGN),

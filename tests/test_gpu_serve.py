@@ -279,6 +279,34 @@ def test_chunk_in_place_and_captured():
         assert torch.equal(out, want), i
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+def test_chunk_of_many_rows_captured_beside_another_stream(dtype):
+    """The form for many rows from a graph, replayed while the same call runs on another stream with a workspace of its own."""
+    g = gen(19)
+    heads, kv_heads, dim, new, lens = 8, 2, 128, [300, 170], [4000, 900]
+    T, width = sum(new), 100
+    cache = random_cache(g, 90, kv_heads, dim)
+    table, first, n = i32(tables(g, lens, width, 90)), i32(np.concatenate([[0], np.cumsum(new)])), i32(lens)
+    q = normal(g, T, heads * dim).to(dtype).to(DEV)
+    args = cache, table, first, n, width * BLOCK, True, q, heads, 0.09
+    chunk_call(*args)
+    out = torch.zeros_like(q)
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.graph(graph):
+        chunk_call(*args, out=out)
+    for i in range(3):
+        q.copy_(normal(g, T, heads * dim).to(dtype))
+        out.zero_()
+        beside = torch.zeros_like(q)
+        want = chunk_call(*args)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            chunk_call(*args, out=beside)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.equal(beside, want), i
+
+
 # ---- fork and compact -----------------------------------------------------------------------------------------------------
 
 def fork_expected(keep, table, lens, parent, grow, blocks):
@@ -667,6 +695,31 @@ def test_w4_product_keeps_bad_rows_apart():
         bad = product(x)
         rest = [m for m in range(M) if m not in (3, 17)]
         assert torch.isnan(bad[3]).all() and not torch.isfinite(bad[17]).any() and torch.equal(bad[rest], good[rest])
+
+
+@pytest.mark.parametrize("xtype", TYPES)
+@pytest.mark.parametrize("M", [3, 40])
+def test_w4_product_captured(xtype, M):
+    g = gen(20)
+    N, K, group = 200, 1024, 64
+    codes, s, z, _ = w4_inputs(g, N, K, group)
+    packed = mq.w4_pack(codes, s, z, group)
+    ws = torch.full((2, mq.mq_w4_product_ws_bytes(M, N, K)), 255, dtype=torch.uint8, device=DEV)
+    code, x = mq.dtype_code(xtype), torch.zeros((M, K), dtype=xtype, device=DEV)
+
+    def product(y, ws):
+        mq.mq_w4_product(x, K, code, None, packed, M, N, K, group, None, y, N, mq.MQ_F32, ws, ws.numel())
+        return y
+    out = product(torch.zeros((M, N), device=DEV), ws[0])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        product(out, ws[0])
+    for i in range(3):
+        x.copy_(normal(g, M, K).to(xtype))
+        want = product(torch.zeros((M, N), device=DEV), ws[1])
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and bool(out.any()), i
 
 
 # ---- together -----------------------------------------------------------------------------------------------------------------
