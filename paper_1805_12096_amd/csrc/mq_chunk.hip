@@ -36,6 +36,7 @@ struct ChunkParams {
   int causal;
   unsigned* plan;                     // [slots + 1] blocks of the tiles in front of each tile, then at 16 bytes [slots] tiles
   unsigned slots, least;              // tiles at most; blocks that a workgroup takes at least
+  int here;                           // whether the workgroups plan for themselves
 };
 
 // Exponent of the power of two taken off a row whose largest magnitude is m.
@@ -64,13 +65,16 @@ struct alignas(8) Tile {
 };
 // Tiles of sequence b lie from tile number first[b] per / ROWS + b on: enough for each, whatever the lengths.
 template <unsigned ROWS>
-__device__ __forceinline__ Tile tile_of(const ChunkParams& p, int b, unsigned slot, unsigned per) {
-  if (b < 0) return {-1, 0, 0, 0, 0, 0};
-  const unsigned f = first_at(p.first, b, p.T), e = first_at(p.first, b + 1, p.T), n = e > f ? e - f : 0;
-  const unsigned row0 = (slot - (f * per / ROWS + b)) * ROWS;
+__device__ __forceinline__ Tile tile_of(const ChunkParams& p, int b, unsigned f, unsigned e, unsigned slot, unsigned per) {
+  const unsigned n = e > f ? e - f : 0, row0 = (slot - (f * per / ROWS + b)) * ROWS;
   if (row0 >= n * per) return {-1, 0, 0, 0, 0, 0};
   const int len = p.lens[b];
   return {b, f, n, row0, min(n * per - row0, ROWS), len < 0 ? 0u : min((unsigned)len, p.max_len)};
+}
+template <unsigned ROWS>
+__device__ __forceinline__ Tile tile_of(const ChunkParams& p, int b, unsigned slot, unsigned per) {
+  if (b < 0) return {-1, 0, 0, 0, 0, 0};
+  return tile_of<ROWS>(p, b, first_at(p.first, b, p.T), first_at(p.first, b + 1, p.T), slot, per);
 }
 template <unsigned ROWS>
 __device__ __forceinline__ Tile find_tile(const ChunkParams& p, unsigned slot, unsigned per) {
@@ -102,49 +106,99 @@ __device__ __forceinline__ Tile* planned(const ChunkParams& p) {
   return reinterpret_cast<Tile*>(p.plan + (p.slots + 4) / 4 * 4);
 }
 
+// sum over the threads in front of this one of the workgroup, and over all
+template <int WAVES>
+__device__ __forceinline__ unsigned sum_ahead(unsigned n, unsigned* box, unsigned& all) {
+  const unsigned lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  unsigned x = n;
+#pragma unroll
+  for (int off = 1; off < kWave; off <<= 1) {
+    const unsigned y = __shfl_up(x, off, kWave);
+    if (lane >= (unsigned)off) x += y;
+  }
+  __syncthreads();
+  if (lane == kWave - 1) box[wave] = x;
+  __syncthreads();
+  unsigned before = x - n;
+  all = 0;
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) {
+    if (w < (int)wave) before += box[w];
+    all += box[w];
+  }
+  return before;
+}
+// The sequence in [0, B) whose tiles a slot is among: those of sequence b start at first(b) per / ROWS + b.
+template <unsigned ROWS, typename F>
+__device__ __forceinline__ unsigned sequence_of(unsigned B, unsigned slot, unsigned per, F first) {
+  unsigned lo = 0, hi = B;
+  while (hi - lo > 1) {
+    const unsigned mid = (lo + hi) / 2;
+    if (first(mid) * per / ROWS + mid <= slot) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+
 template <unsigned ROWS>
 __global__ __launch_bounds__(kPlan) void k_chunk_plan(const ChunkParams p) {
   __shared__ unsigned box[kPlan / kWave];
-  const unsigned lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, per = p.heads / p.kv_heads;
+  const unsigned per = p.heads / p.kv_heads;
   unsigned ahead = 0;
   for (unsigned at = 0; at < p.slots; at += kPlan) {
     const unsigned slot = at + threadIdx.x;
-    // a thread's own search: tiles of sequence b start at first[b] per / ROWS + b
-    unsigned lo = 0, hi = p.B;
-    while (hi - lo > 1) {
-      const unsigned mid = (lo + hi) / 2;
-      if (first_at(p.first, mid, p.T) * per / ROWS + mid <= slot) lo = mid;
-      else hi = mid;
-    }
-    unsigned n = 0;
+    const unsigned b = sequence_of<ROWS>(p.B, slot, per, [&](unsigned i) { return first_at(p.first, i, p.T); });
+    unsigned n = 0, all;
     if (slot < p.slots) {
-      const Tile t = tile_of<ROWS>(p, (int)lo, slot, per);
+      const Tile t = tile_of<ROWS>(p, (int)b, slot, per);
       n = tile_blocks(p, t, per);
       planned(p)[slot] = t;
     }
-    unsigned x = n;
-#pragma unroll
-    for (int off = 1; off < kWave; off <<= 1) {
-      const unsigned y = __shfl_up(x, off, kWave);
-      if (lane >= (unsigned)off) x += y;
-    }
-    __syncthreads();
-    if (lane == kWave - 1) box[wave] = x;
-    __syncthreads();
-    unsigned before = ahead + x - n;
-#pragma unroll
-    for (int w = 0; w < kPlan / kWave; ++w) {
-      if (w < (int)wave) before += box[w];
-      ahead += box[w];
-    }
-    if (slot < p.slots) p.plan[slot] = before;
+    const unsigned before = sum_ahead<kPlan / kWave>(n, box, all);
+    if (slot < p.slots) p.plan[slot] = ahead + before;
+    ahead += all;
   }
   if (threadIdx.x == 0) p.plan[p.slots] = ahead;
 }
 
-// Blocks of the line that a workgroup has.
-__device__ __forceinline__ unsigned long long share_of(const ChunkParams& p, unsigned groups) {
-  const unsigned long long all = (unsigned long long)p.plan[p.slots] * p.kv_heads;
+// The same by every workgroup of few rows for itself, in LDS: a launch less, for the way of three loads.  The first one leaves the plan
+// for the join.  (Two workgroups of 78 KB to a compute unit have room for as many tiles.)
+constexpr unsigned kHere = 192;
+struct PlanHere {
+  unsigned starts[kHere + 1], box[kWaves];
+  Tile tiles[kHere];
+};
+template <unsigned WAVES>
+__device__ __forceinline__ void plan_here(const ChunkParams& p, PlanHere& to) {
+  static_assert(WAVES * kWave >= kHere, "a thread for each tile");
+  const unsigned slot = threadIdx.x, per = p.heads / p.kv_heads;
+  for (unsigned b = threadIdx.x; b <= p.B; b += WAVES * kWave) to.starts[b] = first_at(p.first, b, p.T);      // (B <= slots)
+  __syncthreads();
+  Tile t{-1, 0, 0, 0, 0, 0};
+  if (slot < p.slots) {
+    const unsigned b = sequence_of<kRows>(p.B, slot, per, [&](unsigned i) { return to.starts[i]; });
+    t = tile_of<kRows>(p, (int)b, to.starts[b], to.starts[b + 1], slot, per);
+  }
+  unsigned all;
+  const unsigned before = sum_ahead<WAVES>(tile_blocks(p, t, per), to.box, all);       // (nobody reads what starts held any more)
+  if (slot < p.slots) {
+    to.starts[slot] = before;
+    to.tiles[slot] = t;
+  }
+  if (slot == 0) to.starts[p.slots] = all;
+  if (blockIdx.x == 0) {
+    if (slot < p.slots) {
+      p.plan[slot] = before;
+      planned(p)[slot] = t;
+    }
+    if (slot == 0) p.plan[p.slots] = all;
+  }
+  __syncthreads();
+}
+
+// Blocks of the line that a workgroup has, of `line` to a kv head.
+__device__ __forceinline__ unsigned long long share_of(const ChunkParams& p, unsigned line, unsigned groups) {
+  const unsigned long long all = (unsigned long long)line * p.kv_heads;
   return max((unsigned long long)p.least, (all + groups - 1) / groups);
 }
 
@@ -154,16 +208,17 @@ struct LinePart {
   bool whole;
   Tile tile;
 };
-__device__ __forceinline__ LinePart part_at(const ChunkParams& p, unsigned line, unsigned long long at, unsigned long long to) {
+__device__ __forceinline__ LinePart part_at(const ChunkParams& p, const unsigned* starts, const Tile* tiles, unsigned line,
+                                            unsigned long long at, unsigned long long to) {
   unsigned kvh = 0;                   // (no division: there are few heads, and a workgroup has one or two)
   unsigned long long place = at;
   while (place >= line) {
     place -= line;
     ++kvh;
   }
-  const unsigned slot = (unsigned)__builtin_amdgcn_readfirstlane(wave_search(p.slots, (unsigned)place, [&](unsigned i) { return p.plan[i]; }));
-  const Tile t = planned(p)[slot];
-  const unsigned first = p.plan[slot], blocks = p.plan[slot + 1] - first, start = (unsigned)place - first;
+  const unsigned slot = (unsigned)__builtin_amdgcn_readfirstlane(wave_search(p.slots, (unsigned)place, [&](unsigned i) { return starts[i]; }));
+  const Tile t = tiles[slot];
+  const unsigned first = starts[slot], blocks = starts[slot + 1] - first, start = (unsigned)place - first;
   const unsigned end = (unsigned)min((unsigned long long)blocks, start + (to - at));
   auto uniform = [](unsigned x) { return (unsigned)__builtin_amdgcn_readfirstlane((int)x); };
   return {kvh, uniform(start), uniform(end), start == 0 && end == blocks,
@@ -172,13 +227,13 @@ __device__ __forceinline__ LinePart part_at(const ChunkParams& p, unsigned line,
 // Calls f(part, where a part that is not whole goes) for all parts of this workgroup.  An eighth of the line to each XCD, whose
 // workgroups then read the same heads' blocks.
 template <typename F>
-__device__ __forceinline__ void each_part(const ChunkParams& p, F f) {
+__device__ __forceinline__ void each_part(const ChunkParams& p, const unsigned* starts, const Tile* tiles, F f) {
   const unsigned me = blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8;
-  const unsigned line = p.plan[p.slots];
-  const unsigned long long share = share_of(p, gridDim.x), all = (unsigned long long)line * p.kv_heads;
+  const unsigned line = (unsigned)__builtin_amdgcn_readfirstlane((int)starts[p.slots]);
+  const unsigned long long share = share_of(p, line, gridDim.x), all = (unsigned long long)line * p.kv_heads;
   const unsigned long long to = min((me + 1) * share, all);
   for (unsigned long long at = me * share, n = 0; at < to; ++n) {
-    const LinePart part = part_at(p, line, at, to);
+    const LinePart part = part_at(p, starts, tiles, line, at, to);
     at += part.end - part.start;
     f(part, me * 2 + (n > 0 ? 1 : 0));
   }
@@ -504,7 +559,9 @@ __device__ __forceinline__ void few_rows(const ChunkParams& p, int vec, const Li
 template <int DT, int DC, bool SHARES>
 __global__ __launch_bounds__(kWaves * kWave, DC > 2 ? 1 : 2) void k_chunk_few(const ChunkParams p, int vec) {
   if constexpr (SHARES) {
-    each_part(p, [&](const LinePart& part, unsigned to) {
+    __shared__ PlanHere mine;
+    if (p.here) plan_here<few_waves(kParts<DT>, DC)>(p, mine);
+    each_part(p, p.here ? mine.starts : p.plan, p.here ? mine.tiles : planned(p), [&](const LinePart& part, unsigned to) {
       few_rows<DT, DC>(p, vec, part, to);
       __syncthreads();
     });
@@ -881,7 +938,7 @@ __device__ __forceinline__ void many_rows(const ChunkParams& p, int vec, const L
 
 template <int DT, int DC>
 __global__ __launch_bounds__((TileForm<DT, DC>::W) * kWave, 1) void k_chunk_tiles(const ChunkParams p, int vec) {
-  each_part(p, [&](const LinePart& part, unsigned to) { many_rows<DT, DC>(p, vec, part, to); });
+  each_part(p, p.plan, planned(p), [&](const LinePart& part, unsigned to) { many_rows<DT, DC>(p, vec, part, to); });
 }
 
 // The parts of tiles that more than one workgroup had.  A workgroup for eight rows of a tile and a kv head, 32 threads a row, where
@@ -895,7 +952,8 @@ __global__ __launch_bounds__(256) void k_chunk_join(const ChunkParams p, unsigne
   const unsigned dv = kv_dv(p.d), pitch = dv + 4, per = p.heads / p.kv_heads;
   const Tile tile = planned(p)[slot];
   const unsigned first = p.plan[slot], last = p.plan[slot + 1];
-  const unsigned long long share = share_of(p, groups), base = (unsigned long long)p.plan[p.slots] * kvh;
+  const unsigned line = p.plan[p.slots];
+  const unsigned long long share = share_of(p, line, groups), base = (unsigned long long)line * kvh;
   const unsigned r = chunk * JR + threadIdx.x / TH, j0 = threadIdx.x % TH;
   if (tile.b < 0 || r >= tile.rows) return;
   const unsigned g0 = (unsigned)((base + first) / share), g1 = (unsigned)((base + last - 1) / share), runs = g1 - g0 + 1;
@@ -998,7 +1056,8 @@ int launch_chunk_attention(const mq_kv_cache& cache, const int32_t* table, size_
   const ChunkParams p{cache.keys, cache.values, cache.amax, table, first, lens, q, out, part, ldq, ldo,
                       table_width, cache.blocks, (unsigned)B, (unsigned)T, (unsigned)max_len, (unsigned)cache.kv_heads,
                       (unsigned)heads, (unsigned)cache.head_dim, scale * 1.44269504088896340736f, causal,
-                      reinterpret_cast<unsigned*>(part + part_floats(form, cache.head_dim)), (unsigned)form.slots, form.many ? 8u : 4u};
+                      reinterpret_cast<unsigned*>(part + part_floats(form, cache.head_dim)), (unsigned)form.slots, form.many ? 8u : 4u,
+                      !form.many && form.slots <= kHere};
   const size_t piece = 16 / elem_bytes(dtype);
   // whole 16-byte pieces of queries, four neighbouring results at once
   const int vec = (cache.head_dim % piece == 0 && ldq % piece == 0 && reinterpret_cast<uintptr_t>(q) % 16 == 0 ? 1 : 0) |
@@ -1035,7 +1094,7 @@ int launch_chunk_attention(const mq_kv_cache& cache, const int32_t* table, size_
       if (!form.shares) {
         return go(k_chunk_few<DT, DC, false>, (unsigned)tiles);
       }
-      hipLaunchKernelGGL(k_chunk_plan<kRows>, dim3(1), dim3(kPlan), 0, s, p);
+      if (!p.here) hipLaunchKernelGGL(k_chunk_plan<kRows>, dim3(1), dim3(kPlan), 0, s, p);
       if (const int rc = go(k_chunk_few<DT, DC, true>, form.groups); rc != MQ_OK) return rc;
       hipLaunchKernelGGL((k_chunk_join<DT, kRows>), dim3((unsigned)joins), dim3(256), 0, s, p, form.groups);
       return check_hip(hipGetLastError());
