@@ -65,16 +65,15 @@ struct alignas(8) Tile {
 };
 // Tiles of sequence b lie from tile number first[b] per / ROWS + b on: enough for each, whatever the lengths.
 template <unsigned ROWS>
-__device__ __forceinline__ Tile tile_of(const ChunkParams& p, int b, unsigned f, unsigned e, unsigned slot, unsigned per) {
+__device__ __forceinline__ Tile tile_of(const ChunkParams& p, int b, unsigned f, unsigned e, int len, unsigned slot, unsigned per) {
   const unsigned n = e > f ? e - f : 0, row0 = (slot - (f * per / ROWS + b)) * ROWS;
   if (row0 >= n * per) return {-1, 0, 0, 0, 0, 0};
-  const int len = p.lens[b];
   return {b, f, n, row0, min(n * per - row0, ROWS), len < 0 ? 0u : min((unsigned)len, p.max_len)};
 }
 template <unsigned ROWS>
 __device__ __forceinline__ Tile tile_of(const ChunkParams& p, int b, unsigned slot, unsigned per) {
   if (b < 0) return {-1, 0, 0, 0, 0, 0};
-  return tile_of<ROWS>(p, b, first_at(p.first, b, p.T), first_at(p.first, b + 1, p.T), slot, per);
+  return tile_of<ROWS>(p, b, first_at(p.first, b, p.T), first_at(p.first, b + 1, p.T), p.lens[b], slot, per);
 }
 template <unsigned ROWS>
 __device__ __forceinline__ Tile find_tile(const ChunkParams& p, unsigned slot, unsigned per) {
@@ -161,7 +160,7 @@ __global__ __launch_bounds__(kPlan) void k_chunk_plan(const ChunkParams p) {
   if (threadIdx.x == 0) p.plan[p.slots] = ahead;
 }
 
-// The same by every workgroup of few rows for itself, in LDS: a launch less, for the way of three loads.  The first one leaves the plan
+// The same by every workgroup of few rows for itself, in LDS: a launch less, for the way of two loads.  The first one leaves the plan
 // for the join.  (Two workgroups of 78 KB to a compute unit have room for as many tiles.)
 constexpr unsigned kHere = 192;
 struct PlanHere {
@@ -172,15 +171,18 @@ template <unsigned WAVES>
 __device__ __forceinline__ void plan_here(const ChunkParams& p, PlanHere& to) {
   static_assert(WAVES * kWave >= kHere, "a thread for each tile");
   const unsigned slot = threadIdx.x, per = p.heads / p.kv_heads;
-  for (unsigned b = threadIdx.x; b <= p.B; b += WAVES * kWave) to.starts[b] = first_at(p.first, b, p.T);      // (B <= slots)
+  for (unsigned b = threadIdx.x; b <= p.B; b += WAVES * kWave) {                      // (B <= slots)
+    to.starts[b] = first_at(p.first, b, p.T);
+    if (b < p.B) to.tiles[b].len = (unsigned)p.lens[b];
+  }
   __syncthreads();
   Tile t{-1, 0, 0, 0, 0, 0};
   if (slot < p.slots) {
     const unsigned b = sequence_of<kRows>(p.B, slot, per, [&](unsigned i) { return to.starts[i]; });
-    t = tile_of<kRows>(p, (int)b, to.starts[b], to.starts[b + 1], slot, per);
+    t = tile_of<kRows>(p, (int)b, to.starts[b], to.starts[b + 1], (int)to.tiles[b].len, slot, per);
   }
   unsigned all;
-  const unsigned before = sum_ahead<WAVES>(tile_blocks(p, t, per), to.box, all);       // (nobody reads what starts held any more)
+  const unsigned before = sum_ahead<WAVES>(tile_blocks(p, t, per), to.box, all);       // (nobody reads what they held any more)
   if (slot < p.slots) {
     to.starts[slot] = before;
     to.tiles[slot] = t;
@@ -196,10 +198,18 @@ __device__ __forceinline__ void plan_here(const ChunkParams& p, PlanHere& to) {
   __syncthreads();
 }
 
-// Blocks of the line that a workgroup has, of `line` to a kv head.
-__device__ __forceinline__ unsigned long long share_of(const ChunkParams& p, unsigned line, unsigned groups) {
-  const unsigned long long all = (unsigned long long)line * p.kv_heads;
-  return max((unsigned long long)p.least, (all + groups - 1) / groups);
+// Blocks of the line that a workgroup has, of `line` to a kv head, and where the next kv head's begin: at another workgroup, if there
+// are enough of them (one that had the ends of two would take its way to memory twice).
+struct Share {
+  unsigned long long blocks, pitch;
+};
+__device__ __forceinline__ Share share_of(const ChunkParams& p, unsigned line, unsigned groups) {
+  const unsigned each = groups / p.kv_heads;
+  if (each >= 4) {
+    const unsigned blocks = max(p.least, (line + each - 1) / each);
+    return {blocks, (unsigned long long)((line + blocks - 1) / blocks) * blocks};
+  }
+  return {max((unsigned long long)p.least, ((unsigned long long)line * p.kv_heads + groups - 1) / groups), line};
 }
 
 // A workgroup's next part of the line: blocks [start, end) of a tile and a kv head; whole: all that the tile has.
@@ -208,18 +218,12 @@ struct LinePart {
   bool whole;
   Tile tile;
 };
-__device__ __forceinline__ LinePart part_at(const ChunkParams& p, const unsigned* starts, const Tile* tiles, unsigned line,
-                                            unsigned long long at, unsigned long long to) {
-  unsigned kvh = 0;                   // (no division: there are few heads, and a workgroup has one or two)
-  unsigned long long place = at;
-  while (place >= line) {
-    place -= line;
-    ++kvh;
-  }
-  const unsigned slot = (unsigned)__builtin_amdgcn_readfirstlane(wave_search(p.slots, (unsigned)place, [&](unsigned i) { return starts[i]; }));
+__device__ __forceinline__ LinePart part_at(const ChunkParams& p, const unsigned* starts, const Tile* tiles, unsigned kvh,
+                                            unsigned place, unsigned long long most) {
+  const unsigned slot = (unsigned)__builtin_amdgcn_readfirstlane(wave_search(p.slots, place, [&](unsigned i) { return starts[i]; }));
   const Tile t = tiles[slot];
-  const unsigned first = starts[slot], blocks = starts[slot + 1] - first, start = (unsigned)place - first;
-  const unsigned end = (unsigned)min((unsigned long long)blocks, start + (to - at));
+  const unsigned first = starts[slot], blocks = starts[slot + 1] - first, start = place - first;
+  const unsigned end = (unsigned)min((unsigned long long)blocks, start + most);
   auto uniform = [](unsigned x) { return (unsigned)__builtin_amdgcn_readfirstlane((int)x); };
   return {kvh, uniform(start), uniform(end), start == 0 && end == blocks,
           Tile{(int)uniform((unsigned)t.b), uniform(t.first), uniform(t.n), uniform(t.row0), uniform(t.rows), uniform(t.len)}};
@@ -230,11 +234,19 @@ template <typename F>
 __device__ __forceinline__ void each_part(const ChunkParams& p, const unsigned* starts, const Tile* tiles, F f) {
   const unsigned me = blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8;
   const unsigned line = (unsigned)__builtin_amdgcn_readfirstlane((int)starts[p.slots]);
-  const unsigned long long share = share_of(p, line, gridDim.x), all = (unsigned long long)line * p.kv_heads;
-  const unsigned long long to = min((me + 1) * share, all);
-  for (unsigned long long at = me * share, n = 0; at < to; ++n) {
-    const LinePart part = part_at(p, starts, tiles, line, at, to);
+  const Share share = share_of(p, line, gridDim.x);
+  const unsigned long long to = min((me + 1) * share.blocks, share.pitch * p.kv_heads);
+  unsigned kvh = 0;                   // (no division: there are few heads, and a workgroup has one or two)
+  unsigned long long at = me * share.blocks, place = at;
+  for (unsigned n = 0; at < to; ++n) {
+    while (place >= share.pitch) {
+      place -= share.pitch;
+      ++kvh;
+    }
+    if (place >= line) break;         // (a kv head's last share may be shorter)
+    const LinePart part = part_at(p, starts, tiles, kvh, (unsigned)place, to - at);
     at += part.end - part.start;
+    place += part.end - part.start;
     f(part, me * 2 + (n > 0 ? 1 : 0));
   }
 }
@@ -953,7 +965,8 @@ __global__ __launch_bounds__(256) void k_chunk_join(const ChunkParams p, unsigne
   const Tile tile = planned(p)[slot];
   const unsigned first = p.plan[slot], last = p.plan[slot + 1];
   const unsigned line = p.plan[p.slots];
-  const unsigned long long share = share_of(p, line, groups), base = (unsigned long long)line * kvh;
+  const Share split = share_of(p, line, groups);
+  const unsigned long long share = split.blocks, base = split.pitch * kvh;
   const unsigned r = chunk * JR + threadIdx.x / TH, j0 = threadIdx.x % TH;
   if (tile.b < 0 || r >= tile.rows) return;
   const unsigned g0 = (unsigned)((base + first) / share), g1 = (unsigned)((base + last - 1) / share), runs = g1 - g0 + 1;
@@ -1003,7 +1016,7 @@ __global__ __launch_bounds__(256) void k_chunk_join(const ChunkParams p, unsigne
 
 struct Form {
   bool many, shares;
-  unsigned tile_rows, groups;         // rows of a tile; workgroups that share the line
+  unsigned tile_rows, groups, least;  // rows of a tile; workgroups that share the line, blocks that one takes at least
   size_t slots;
 };
 // The form for many rows, us of a call, few rows / many: heads of 128, 32 over 8, 8 sequences on 4000 tokens, 128 rows of a kv
@@ -1020,6 +1033,7 @@ Form form_of(int dtype, size_t B, size_t T, size_t max_len, int heads, int kv_he
   f.many = T * per / B >= many_rows(d) && T * (size_t)heads * d >= kManyWork / max_len && !(dtype == MQ_F32 && d > 128);
   f.shares = f.many || blocks > kShort;
   f.tile_rows = kRows;
+  f.least = f.many ? 8 : 4;
   f.groups = d <= 64 ? 768 : d <= 128 ? 512 : 256;
   if (f.many) {
     const bool wide = (dtype == MQ_BF16 && d <= 128) || (d <= 64 && dtype == MQ_F16);
@@ -1027,6 +1041,10 @@ Form form_of(int dtype, size_t B, size_t T, size_t max_len, int heads, int kv_he
     f.groups = wide ? 256 : 512;      // one workgroup of eight waves to a compute unit, or two of four
   }
   f.slots = T * per / f.tile_rows + B;
+  // no more workgroups than there may be shares of the least length
+  const size_t least = f.least, line = blocks < ((size_t)1 << 40) / f.slots ? f.slots * blocks * kv_heads : (size_t)1 << 40;
+  const size_t most = (line + 8 * least - 1) / (8 * least) * 8;
+  if (f.groups > most) f.groups = (unsigned)most;
   return f;
 }
 // Floats of the parts, in front of the plan.
@@ -1050,13 +1068,13 @@ int launch_chunk_attention(const mq_kv_cache& cache, const int32_t* table, size_
   const Form form = form_of(dtype, B, T, max_len, heads, cache.kv_heads, cache.head_dim);
   const size_t tiles = form.slots * (size_t)cache.kv_heads, joins = tiles * (form.tile_rows / join_rows(form.tile_rows));
   const size_t blocks = (max_len + kKvBlock - 1) / kKvBlock;
-  // (blocks of all tiles are counted in 32 bits)
-  if (!launchable(joins, kWaves * kWave) || form.slots > (((size_t)1 << 32) - 1) / blocks) return MQ_ERR_SHAPE;
+  // (blocks of all tiles are counted in 32 bits, with room for sums)
+  if (!launchable(joins, kWaves * kWave) || form.slots > (((size_t)1 << 31) - 1) / blocks) return MQ_ERR_SHAPE;
   float* part = static_cast<float*>(ws);
   const ChunkParams p{cache.keys, cache.values, cache.amax, table, first, lens, q, out, part, ldq, ldo,
                       table_width, cache.blocks, (unsigned)B, (unsigned)T, (unsigned)max_len, (unsigned)cache.kv_heads,
                       (unsigned)heads, (unsigned)cache.head_dim, scale * 1.44269504088896340736f, causal,
-                      reinterpret_cast<unsigned*>(part + part_floats(form, cache.head_dim)), (unsigned)form.slots, form.many ? 8u : 4u,
+                      reinterpret_cast<unsigned*>(part + part_floats(form, cache.head_dim)), (unsigned)form.slots, form.least,
                       !form.many && form.slots <= kHere};
   const size_t piece = 16 / elem_bytes(dtype);
   // whole 16-byte pieces of queries, four neighbouring results at once
