@@ -40,9 +40,10 @@ extern "C" {
  * values' block enter as as many parts, 8, 16 or 24 bits (16-bit types: values of a
  * block whose largest is below 2^-119 count as zeros, and bits of values below 2^-100 may be lost).  Sums and softmax statistics
  * are binary32.
- * ws: device, 16-byte aligned, mq_chunk_attention_ws_bytes (0 for invalid arguments).  One launch where max_len <= 2048 and rows
- * are few, else three: shares are planned from the lengths, computed, and joined.  Calls of which that plan cannot count the
- * blocks in 31 bits (some 2^31 / (max_len / 64) tiles of 32 rows) are refused with MQ_ERR_SHAPE. */
+ * ws: device, 16-byte aligned, mq_chunk_attention_ws_bytes (0 for invalid arguments).  One launch where max_len <= 1152 (up to
+ * 2048 if there is work for all of the chip) and rows are few, else two or three: shares are planned from the lengths, computed, and
+ * joined.  Calls of which that plan cannot count the blocks in 31 bits (some 2^31 / (max_len / 64) tiles of 32 rows) are refused with
+ * MQ_ERR_SHAPE. */
 size_t mq_chunk_attention_ws_bytes(size_t B, size_t T, size_t max_len, int heads, int kv_heads, size_t head_dim);
 int mq_chunk_attention(const mq_kv_cache* cache, const int32_t* table, size_t table_width, const int32_t* first,
                        const int32_t* lens, size_t B, size_t T, size_t max_len, int causal, const void* q, size_t ldq, int heads,

@@ -34,7 +34,7 @@ struct ChunkParams {
   unsigned B, T, max_len, kv_heads, heads, d;
   float scale2;                       // scale log2(e)
   int causal;
-  unsigned* plan;                     // [slots + 1] blocks of the tiles in front of each tile, then at 16 bytes [slots] tiles
+  unsigned* plan;                     // [slots + 1] blocks of the tiles in front of each tile, the share, then at 16 bytes [slots] tiles
   unsigned slots, least;              // tiles at most; blocks that a workgroup takes at least
   int here;                           // whether the workgroups plan for themselves
 };
@@ -102,7 +102,21 @@ __device__ __forceinline__ unsigned tile_blocks(const ChunkParams& p, const Tile
 }
 
 __device__ __forceinline__ Tile* planned(const ChunkParams& p) {
-  return reinterpret_cast<Tile*>(p.plan + (p.slots + 4) / 4 * 4);
+  return reinterpret_cast<Tile*>(p.plan + (p.slots + 5) / 4 * 4);
+}
+
+// Blocks that a workgroup has, where there are `each` >= 4 workgroups to a kv head and `line` blocks.
+__device__ __forceinline__ unsigned share_of_head(const ChunkParams& p, unsigned line, unsigned each) {
+  return max(p.least, (line + each - 1) / each);
+}
+// Blocks of the line that a workgroup has, and where the next kv head's begin: at another workgroup, if there are enough of them (one
+// that had the ends of two would take its way to memory twice).
+struct Share {
+  unsigned long long blocks, pitch;
+};
+__device__ __forceinline__ Share share_of(const ChunkParams& p, unsigned line, unsigned planned, unsigned groups) {
+  if (groups / p.kv_heads >= 4) return {planned, (unsigned long long)((line + planned - 1) / planned) * planned};
+  return {max((unsigned long long)p.least, ((unsigned long long)line * p.kv_heads + groups - 1) / groups), line};
 }
 
 // sum over the threads in front of this one of the workgroup, and over all
@@ -140,7 +154,7 @@ __device__ __forceinline__ unsigned sequence_of(unsigned B, unsigned slot, unsig
 }
 
 template <unsigned ROWS>
-__global__ __launch_bounds__(kPlan) void k_chunk_plan(const ChunkParams p) {
+__global__ __launch_bounds__(kPlan) void k_chunk_plan(const ChunkParams p, unsigned groups) {
   __shared__ unsigned box[kPlan / kWave];
   const unsigned per = p.heads / p.kv_heads;
   unsigned ahead = 0;
@@ -157,14 +171,20 @@ __global__ __launch_bounds__(kPlan) void k_chunk_plan(const ChunkParams p) {
     if (slot < p.slots) p.plan[slot] = ahead + before;
     ahead += all;
   }
-  if (threadIdx.x == 0) p.plan[p.slots] = ahead;
+  if (threadIdx.x == 0) {
+    p.plan[p.slots] = ahead;
+    p.plan[p.slots + 1] = share_of_head(p, ahead, max(groups / p.kv_heads, 1u));
+  }
 }
 
 // The same by every workgroup of few rows for itself, in LDS: a launch less, for the way of two loads.  The first one leaves the plan
 // for the join.  (Two workgroups of 78 KB to a compute unit have room for as many tiles.)
-constexpr unsigned kHere = 192;
+// Where there are at least four workgroups to a tile and shares are short each has blocks of one only, for the same reason: tiles begin
+// at a share of their own, whose last may have less (8 sequences of 4 new tokens on 4000, 32 heads over 8 of 128: 33.5 -> 26.9 us;
+// 16 on 12000, shares of 63: 85 -> 94, so not there).
+constexpr unsigned kHere = 192, kAlone = 16;
 struct PlanHere {
-  unsigned starts[kHere + 1], box[kWaves];
+  unsigned starts[kHere + 2], box[kWaves];
   Tile tiles[kHere];
 };
 template <unsigned WAVES>
@@ -181,40 +201,43 @@ __device__ __forceinline__ void plan_here(const ChunkParams& p, PlanHere& to) {
     const unsigned b = sequence_of<kRows>(p.B, slot, per, [&](unsigned i) { return to.starts[i]; });
     t = tile_of<kRows>(p, (int)b, to.starts[b], to.starts[b + 1], (int)to.tiles[b].len, slot, per);
   }
-  unsigned all;
-  const unsigned before = sum_ahead<WAVES>(tile_blocks(p, t, per), to.box, all);       // (nobody reads what they held any more)
+  const unsigned n = tile_blocks(p, t, per), each = max(gridDim.x / p.kv_heads, 1u);
+  unsigned all, tiles;
+  sum_ahead<WAVES>(n > 0 ? 1u : 0u, to.box, tiles);         // (nobody reads what they held any more)
+  unsigned before = sum_ahead<WAVES>(n, to.box, all), share = share_of_head(p, all, each);
+  const unsigned line = all;
+  auto alone = [&](unsigned blocks) {                       // (whole turns of the waves)
+    share = (blocks + kWaves - 1) / kWaves * kWaves;
+    before = sum_ahead<WAVES>((n + share - 1) / share * share, to.box, all);
+  };
+  if (tiles <= each / 4 && share <= kAlone) {
+    alone(share);
+    if (all > each * share) alone(share_of_head(p, line, each - tiles));       // (enough whatever the lengths)
+  }
   if (slot < p.slots) {
     to.starts[slot] = before;
     to.tiles[slot] = t;
   }
-  if (slot == 0) to.starts[p.slots] = all;
+  if (slot == 0) {
+    to.starts[p.slots] = all;
+    to.starts[p.slots + 1] = share;
+  }
   if (blockIdx.x == 0) {
     if (slot < p.slots) {
       p.plan[slot] = before;
       planned(p)[slot] = t;
     }
-    if (slot == 0) p.plan[p.slots] = all;
+    if (slot == 0) {
+      p.plan[p.slots] = all;
+      p.plan[p.slots + 1] = share;
+    }
   }
   __syncthreads();
 }
 
-// Blocks of the line that a workgroup has, of `line` to a kv head, and where the next kv head's begin: at another workgroup, if there
-// are enough of them (one that had the ends of two would take its way to memory twice).
-struct Share {
-  unsigned long long blocks, pitch;
-};
-__device__ __forceinline__ Share share_of(const ChunkParams& p, unsigned line, unsigned groups) {
-  const unsigned each = groups / p.kv_heads;
-  if (each >= 4) {
-    const unsigned blocks = max(p.least, (line + each - 1) / each);
-    return {blocks, (unsigned long long)((line + blocks - 1) / blocks) * blocks};
-  }
-  return {max((unsigned long long)p.least, ((unsigned long long)line * p.kv_heads + groups - 1) / groups), line};
-}
-
 // A workgroup's next part of the line: blocks [start, end) of a tile and a kv head; whole: all that the tile has.
 struct LinePart {
-  unsigned kvh, start, end;
+  unsigned kvh, start, end, next;     // next: where the next tile begins in the line
   bool whole;
   Tile tile;
 };
@@ -222,10 +245,10 @@ __device__ __forceinline__ LinePart part_at(const ChunkParams& p, const unsigned
                                             unsigned place, unsigned long long most) {
   const unsigned slot = (unsigned)__builtin_amdgcn_readfirstlane(wave_search(p.slots, place, [&](unsigned i) { return starts[i]; }));
   const Tile t = tiles[slot];
-  const unsigned first = starts[slot], blocks = starts[slot + 1] - first, start = place - first;
+  const unsigned blocks = tile_blocks(p, t, p.heads / p.kv_heads), start = place - starts[slot];
   const unsigned end = (unsigned)min((unsigned long long)blocks, start + most);
   auto uniform = [](unsigned x) { return (unsigned)__builtin_amdgcn_readfirstlane((int)x); };
-  return {kvh, uniform(start), uniform(end), start == 0 && end == blocks,
+  return {kvh, uniform(start), uniform(end), uniform(starts[slot + 1]), start == 0 && end == blocks,
           Tile{(int)uniform((unsigned)t.b), uniform(t.first), uniform(t.n), uniform(t.row0), uniform(t.rows), uniform(t.len)}};
 }
 // Calls f(part, where a part that is not whole goes) for all parts of this workgroup.  An eighth of the line to each XCD, whose
@@ -234,7 +257,7 @@ template <typename F>
 __device__ __forceinline__ void each_part(const ChunkParams& p, const unsigned* starts, const Tile* tiles, F f) {
   const unsigned me = blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8;
   const unsigned line = (unsigned)__builtin_amdgcn_readfirstlane((int)starts[p.slots]);
-  const Share share = share_of(p, line, gridDim.x);
+  const Share share = share_of(p, line, (unsigned)__builtin_amdgcn_readfirstlane((int)starts[p.slots + 1]), gridDim.x);
   const unsigned long long to = min((me + 1) * share.blocks, share.pitch * p.kv_heads);
   unsigned kvh = 0;                   // (no division: there are few heads, and a workgroup has one or two)
   unsigned long long at = me * share.blocks, place = at;
@@ -245,8 +268,9 @@ __device__ __forceinline__ void each_part(const ChunkParams& p, const unsigned* 
     }
     if (place >= line) break;         // (a kv head's last share may be shorter)
     const LinePart part = part_at(p, starts, tiles, kvh, (unsigned)place, to - at);
-    at += part.end - part.start;
-    place += part.end - part.start;
+    const unsigned next = part.next - (unsigned)place;
+    at += next;
+    place += next;
     f(part, me * 2 + (n > 0 ? 1 : 0));
   }
 }
@@ -580,7 +604,7 @@ __global__ __launch_bounds__(kWaves * kWave, DC > 2 ? 1 : 2) void k_chunk_few(co
   } else {
     // (heads next to each other: on a chip whose workgroups go to its eight XCDs by turns, eight heads have one each)
     const Tile tile = find_tile<kRows>(p, blockIdx.x / p.kv_heads, p.heads / p.kv_heads);
-    if (tile.b >= 0) few_rows<DT, DC>(p, vec, LinePart{blockIdx.x % p.kv_heads, 0, 0xffffffffu, true, tile}, 0);
+    if (tile.b >= 0) few_rows<DT, DC>(p, vec, LinePart{blockIdx.x % p.kv_heads, 0, 0xffffffffu, 0, true, tile}, 0);
   }
 }
 
@@ -965,7 +989,7 @@ __global__ __launch_bounds__(256) void k_chunk_join(const ChunkParams p, unsigne
   const Tile tile = planned(p)[slot];
   const unsigned first = p.plan[slot], last = p.plan[slot + 1];
   const unsigned line = p.plan[p.slots];
-  const Share split = share_of(p, line, groups);
+  const Share split = share_of(p, line, p.plan[p.slots + 1], groups);
   const unsigned long long share = split.blocks, base = split.pitch * kvh;
   const unsigned r = chunk * JR + threadIdx.x / TH, j0 = threadIdx.x % TH;
   if (tile.b < 0 || r >= tile.rows) return;
@@ -1025,13 +1049,17 @@ struct Form {
 // its parts take 30 us of any call: heads of 64, 8 over 2, 64 sequences on 400, bfloat16, 256 rows 19 / 33, 512 rows 63 / 52.
 constexpr size_t many_rows(size_t d) { return d <= 64 ? 128 : 160; }       // rows of a sequence on average
 constexpr size_t kManyWork = (size_t)1 << 31;      // rows x longest sequence x width
-constexpr size_t kShort = 32;         // blocks of the longest sequence up to which a workgroup takes all of a tile's
+// Blocks of the longest sequence up to which a workgroup takes all of a tile's: where equal shares would be one turn of the waves at
+// most (three blocks a workgroup), and else.  One workgroup / shares, us: bfloat16, 32 heads over 8 of 128, 4 new tokens, 1 sequence
+// on 1000 tokens 15.2 / 17.5, 1300 18.9 / 15.5, 2000 23.0 / 15.8, 4 on 2000 25.2 / 20.8, 8 on 1300 21.0 / 21.7, 16 on 1700 24.2 / 28.7,
+// on 2000 26.3 / 30.2, 32 on 2000 40 / 42; binary32, 8 heads of 64, 16 on 1300 20.1 / 30.7.
+constexpr size_t kShort = 18, kLong = 32;
 Form form_of(int dtype, size_t B, size_t T, size_t max_len, int heads, int kv_heads, size_t d) {
   const size_t per = (size_t)(heads / kv_heads), blocks = (max_len + kKvBlock - 1) / kKvBlock;
   Form f{};
   // (binary32 queries of wide heads do not fit beside the sums)
   f.many = T * per / B >= many_rows(d) && T * (size_t)heads * d >= kManyWork / max_len && !(dtype == MQ_F32 && d > 128);
-  f.shares = f.many || blocks > kShort;
+  f.shares = f.many || blocks > kLong;
   f.tile_rows = kRows;
   f.least = f.many ? 8 : 4;
   f.groups = d <= 64 ? 768 : d <= 128 ? 512 : 256;
@@ -1041,6 +1069,7 @@ Form form_of(int dtype, size_t B, size_t T, size_t max_len, int heads, int kv_he
     f.groups = wide ? 256 : 512;      // one workgroup of eight waves to a compute unit, or two of four
   }
   f.slots = T * per / f.tile_rows + B;
+  if (blocks > kShort && f.slots <= kHere && f.slots * blocks * kv_heads <= (size_t)3 * f.groups) f.shares = true;
   // no more workgroups than there may be shares of the least length
   const size_t least = f.least, line = blocks < ((size_t)1 << 40) / f.slots ? f.slots * blocks * kv_heads : (size_t)1 << 40;
   const size_t most = (line + 8 * least - 1) / (8 * least) * 8;
@@ -1056,7 +1085,7 @@ size_t chunk_attention_ws_bytes(size_t B, size_t T, size_t max_len, int heads, i
   size_t most = 0;                    // (whatever the type)
   for (int dtype : {MQ_F32, MQ_F16, MQ_BF16}) {
     const Form f = form_of(dtype, B, T, max_len, heads, kv_heads, d);
-    const size_t n = part_floats(f, d) + (f.shares ? (f.slots + 4) / 4 * 4 + f.slots * sizeof(Tile) / sizeof(float) : 0);
+    const size_t n = part_floats(f, d) + (f.shares ? (f.slots + 5) / 4 * 4 + f.slots * sizeof(Tile) / sizeof(float) : 0);
     most = n > most ? n : most;
   }
   return most * sizeof(float);
@@ -1093,7 +1122,7 @@ int launch_chunk_attention(const mq_kv_cache& cache, const int32_t* table, size_
             const int rc = check_hip(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)Tiles::kLds));
             if (rc != MQ_OK) return rc;
           }
-          hipLaunchKernelGGL(k_chunk_plan<ROWS>, dim3(1), dim3(kPlan), 0, s, p);
+          hipLaunchKernelGGL(k_chunk_plan<ROWS>, dim3(1), dim3(kPlan), 0, s, p, form.groups);
           hipLaunchKernelGGL(kern, dim3(form.groups), dim3(Tiles::W * kWave), Tiles::kLds, s, p, vec);
           hipLaunchKernelGGL((k_chunk_join<DT, ROWS>), dim3((unsigned)joins), dim3(256), 0, s, p, form.groups);
         }
@@ -1112,7 +1141,7 @@ int launch_chunk_attention(const mq_kv_cache& cache, const int32_t* table, size_
       if (!form.shares) {
         return go(k_chunk_few<DT, DC, false>, (unsigned)tiles);
       }
-      if (!p.here) hipLaunchKernelGGL(k_chunk_plan<kRows>, dim3(1), dim3(kPlan), 0, s, p);
+      if (!p.here) hipLaunchKernelGGL(k_chunk_plan<kRows>, dim3(1), dim3(kPlan), 0, s, p, form.groups);
       if (const int rc = go(k_chunk_few<DT, DC, true>, form.groups); rc != MQ_OK) return rc;
       hipLaunchKernelGGL((k_chunk_join<DT, kRows>), dim3((unsigned)joins), dim3(256), 0, s, p, form.groups);
       return check_hip(hipGetLastError());

@@ -151,12 +151,18 @@ CHUNKS = [
     # and few rows of a call that may be long
     ([3, 1, 0, 20], [1200, 64, 7, 3000], 8, 2, 128),
     ([2], [4097], 4, 4, 256),
+    # more tiles, and more heads, than workgroups plan for; tiles of one head that fit a share each, and that do not
+    ([1 + i % 3 for i in range(210)], [1 + i * 37 % 300 for i in range(210)], 2, 1, 64),
+    ([3, 1], [700, 70], 200, 200, 16),
+    ([3, 0, 2], [130, 5, 64], 1024, 1024, 8),
+    ([4, 4, 4], [1500, 900, 1501], 8, 2, 64),
+    ([2] * 24, [100 + 53 * i for i in range(24)], 4, 4, 64),
 ]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("causal", [True, False])
-@pytest.mark.parametrize("case,room", [(c, 0 if c < 10 else 2000) for c in range(len(CHUNKS))] + [(c, 60) for c in range(10)])
+@pytest.mark.parametrize("case,room", [(c, 0 if c < 10 else 2000 if c < 17 else 30) for c in range(len(CHUNKS))] + [(c, 60) for c in range(10)])
 def test_chunk(dtype, causal, case, room):
     """room: columns that the table has more than it needs, for calls that say only that sequences may be as long as it is."""
     new, lens, heads, kv_heads, dim = CHUNKS[case]
