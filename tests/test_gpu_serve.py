@@ -226,6 +226,37 @@ def test_chunk_bad_queries_stay_with_themselves(dtype, max_len):
     assert (out[:18] == 0).all() and (out[20:] == 0).all() and not torch.isnan(out[18:20]).any()
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("max_len,new", [(320, [3, 40]), (6400, [3, 40]), (64000, [300, 40])])
+def test_chunk_negative_and_zero_scales(dtype, max_len, new):
+    g = gen(15)
+    heads, kv_heads, dim, lens = 6, 2, 48, [300, 171]
+    cache = random_cache(g, 12, kv_heads, dim)
+    table, first = tables(g, lens, 1000, 12), np.concatenate([[0], np.cumsum(new)])
+    q = normal(g, sum(new), heads * dim).to(dtype).to(DEV)
+    for scale in (-0.1, 0.0):
+        out = chunk_call(cache, i32(table), i32(first), i32(lens), max_len, True, q, heads, scale)
+        expected, _ = chunk_expected(cache, table, first, lens, max_len, True, q, heads, scale, dtype)
+        _, tol = chunk_expected(cache, table, first, lens, max_len, True, q, heads, -scale, dtype)     # (depends on its magnitude)
+        # (the rounding of the result itself, which is another one for the other sign)
+        check_chunk(out, expected, tol + half_step(dtype, expected))
+
+
+@pytest.mark.parametrize("max_len", [320, 6400, 64000])
+def test_chunk_with_a_bad_list_stays_inside_its_rows(max_len):
+    g = gen(16)
+    heads, kv_heads, dim, T = 4, 2, 64, 700
+    cache = random_cache(g, 12, kv_heads, dim)
+    table, lens = tables(g, [300] * 2, 1000, 12), [300, 300, 1 << 30, -5, 17]
+    table = np.concatenate([table, table, table[:1]])
+    store = torch.full((T + 20, heads * dim), 7.0, device=DEV)
+    q = normal(g, T, heads * dim).to(DEV)
+    for first in ([5, 2, 600, 7, 1000, -3], [700, 0, 700, 0, 700, 0], [-9, 300, 299, 298, 2 ** 31 - 1, 5]):
+        chunk_call(cache, i32(table), i32(first), i32(lens), max_len, True, q, heads, 0.1, store[10:10 + T])
+        assert (store[:10] == 7.0).all() and (store[10 + T:] == 7.0).all()
+        assert not torch.isnan(store).any()
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("max_len", [400, 4096])
 def test_chunk_large_and_small_magnitudes(dtype, max_len):
