@@ -7,7 +7,7 @@
 // Two forms: where tables and cache are small, one workgroup does all but the copies with the words in LDS; else the words lie in
 // the workspace and clearing, counting, handing out and writing are launches of their own.  Bound by launches and by chains of
 // dependent loads (parent, length, entry) where little is copied, by the copies' bytes where much is: 300 rows of 5 columns 14 us
-// (in four launches 20), of which the tables are 5; 90 rows compacted 13 (19); 226 MB of moved blocks in 47 of 59 us, 4.8 TB/s.
+// (in four launches 20), of which the tables are 5; 90 rows compacted 13 (19); 226 MB of moved blocks in 47 of 58 us, 4.8 TB/s.
 #include "mq_serve_common.h"
 
 namespace mq {
@@ -229,11 +229,20 @@ __device__ __forceinline__ void count_small(const Tables& p, int32_t* state, int
   for (unsigned i = threadIdx.x; i < p.blocks; i += kScan) state[i] = p.keep != nullptr && p.keep[i] != 0 ? 0 : kFree;
   __syncthreads();
   const unsigned width = (unsigned)p.width, entries = p.B_new * width;
-  for (unsigned i = threadIdx.x; i < entries; i += kScan) {
-    const unsigned b = i / width, j = i % width, held = held_of(rows[b]);
-    if (j >= held) continue;
-    const int e = p.table[(size_t)rows[b].x * width + j];
-    if (is_block(p, e)) atomicMin(state + e, rows[b].z < 0 && j + 1 == held ? (int)b + 1 : 0);
+  for (unsigned at = threadIdx.x; at < entries; at += 4 * kScan) {
+    int e[4];                                              // (four loads at a time)
+#pragma unroll
+    for (unsigned k = 0; k < 4; ++k) {
+      const unsigned i = min(at + k * kScan, entries - 1);
+      e[k] = p.table[(size_t)rows[i / width].x * width + i % width];
+    }
+#pragma unroll
+    for (unsigned k = 0; k < 4; ++k) {
+      const unsigned i = at + k * kScan, b = i / width, j = i % width;
+      if (i >= entries) break;
+      const unsigned held = held_of(rows[b]);
+      if (j < held && is_block(p, e[k])) atomicMin(state + e[k], rows[b].z < 0 && j + 1 == held ? (int)b + 1 : 0);
+    }
   }
   __syncthreads();
 }
@@ -340,9 +349,16 @@ __global__ __launch_bounds__(kScan) void k_compact_small(const Tables p) {
   }
   __syncthreads();
   const unsigned width = (unsigned)p.width;
-  for (unsigned i = threadIdx.x; i < p.B * width; i += kScan) {
-    const int e = i % width < held_of(rows[i / width]) ? p.table[i] : -1;
-    p.table_new[i] = is_block(p, e) ? state[e] : -1;
+  const unsigned entries = p.B * width;
+  for (unsigned at = threadIdx.x; at < entries; at += 4 * kScan) {
+    int e[4];
+#pragma unroll
+    for (unsigned k = 0; k < 4; ++k) e[k] = p.table[min(at + k * kScan, entries - 1)];
+#pragma unroll
+    for (unsigned k = 0; k < 4; ++k) {
+      const unsigned i = at + k * kScan;
+      if (i < entries) p.table_new[i] = i % width < held_of(rows[i / width]) && is_block(p, e[k]) ? state[e[k]] : -1;
+    }
   }
   if (threadIdx.x == 0) {
     *p.used = (int)used;
