@@ -49,6 +49,30 @@ __device__ __forceinline__ unsigned again(unsigned x) {
   return x;
 }
 __device__ __forceinline__ float finite_or_0(float m) { return m == -INFINITY ? 0.f : m; }
+
+// A block's value is integer x unit x m.  m goes into the exponent of its tokens' weights, which the exponential flushes below
+// 2^-126: an m below 2^-60 would take weights with it that count in the denominator.  There m is 1 .. 2 and the power of two, unit,
+// is put to the integers (which stay bfloat16 values).  Values below any normal number are zeros.
+struct ValueScale {
+  float m, unit;
+};
+__device__ __forceinline__ ValueScale value_scale(float amax) {
+  const float s = amax * (1.f / 127.f);
+  const unsigned b = __float_as_uint(s);
+  if (s < 0x1p-126f) return {1.f, 0.f};
+  if (s < 0x1p-60f) return {__uint_as_float((b & 0x007fffffu) | 0x3f800000u), __uint_as_float(b & 0x7f800000u)};
+  return {s, 1.f};
+}
+__device__ __forceinline__ unsigned uniform_bits(float x) { return (unsigned)__builtin_amdgcn_readfirstlane((int)__float_as_uint(x)); }
+// Integers as bfloat16 values times a unit (its bits), the same for the wave; it is 1 but for very small values.
+__device__ __forceinline__ bf8 in_units(bf8 v, unsigned unit) {
+  if (unit != 0x3f800000u) {
+    const float f = __uint_as_float(unit);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = (__bf16)((float)v[i] * f);
+  }
+  return v;
+}
 __device__ __forceinline__ float fmax2(float a, float b) { return fmaxf(a, b); }
 __device__ __forceinline__ float fadd2(float a, float b) { return a + b; }
 
@@ -494,9 +518,9 @@ __device__ __forceinline__ void few_rows(const ChunkParams& p, int vec, const Li
     }
     // (where there is no block, block 0 was read, whose maxima may be anything)
     const float fv = there ? am.y * (1.f / 127.f) : 0.f;
-    const bool nothing = !there || (FOLD && fv < 1.2e-38f);      // values that are all zero (or below any normal number)
-    const float lift = nothing || !FOLD ? 0.f : __builtin_amdgcn_logf(fv), base = lift - finite_or_0(acc_top);
-    const unsigned any = FOLD && nothing ? 0u : ~0u;
+    const ValueScale vs = FOLD ? value_scale(there ? am.y : 0.f) : ValueScale{1.f, 1.f};
+    const unsigned unit = uniform_bits(vs.unit);
+    const float base = (FOLD ? __builtin_amdgcn_logf(vs.m) : 0.f) - finite_or_0(acc_top);
     float sum = 0.f;
     u4 vf[ND][2];
     if (i + 1 < mine) arrived(std::integral_constant<int, kLoads<DC>>{});      // (all but the next block's keys)
@@ -522,12 +546,12 @@ __device__ __forceinline__ void few_rows(const ChunkParams& p, int vec, const Li
           vf[t][0] = value_piece(t, 0);
           vf[t][1] = value_piece(t, 1);
         }
-        const bf8 a = bf16_of_bytes(vf[t][0][j] & any, vf[t][1][j] & any);
+        const bf8 a = in_units(bf16_of_bytes(vf[t][0][j], vf[t][1][j]), unit);
 #pragma unroll
         for (int k = NP - 1; k >= 0; --k) acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, pr[k], acc[t], 0, 0, 0);
       }
     }
-    total = FOLD ? fmaf(sum, nothing ? 1.f : __fdiv_rn(1.f, fv), total) : total + sum;
+    total = FOLD ? fmaf(sum, __fdiv_rn(1.f, vs.m), total) : total + sum;
     if (i + 1 < mine) {
       arrived(std::integral_constant<int, kLoads<DC>>{});
       bring_values();
@@ -709,17 +733,27 @@ __device__ __forceinline__ void many_rows(const ChunkParams& p, int vec, const L
       }
     av = p.amax[2 * b + 1];
   };
-  // values that are all zero (or below any normal number): their scale has no logarithm
-  auto no_values = [&](float a) { return Form::kFold && a * (1.f / 127.f) < 1.2e-38f; };
   auto put_key = [&](unsigned buf, int n, int s) {
     if (W * n + W <= 2 * NK || wave + W * n < 2 * NK)
       kl[(buf * KU + 2 * (wave + W * n) + s) * kWave + lane] = bf16_of_bytes(rk[n][2 * s], rk[n][2 * s + 1]);
   };
   auto put_value = [&](unsigned buf, int n, int j) {
-    const unsigned any = no_values(av) ? 0u : ~0u;
     if (W * n + W <= 2 * ND || wave + W * n < 2 * ND)
-      vl[(buf * KU + 2 * (wave + W * n) + j) * kWave + lane] =
-          bf16_of_bytes((j ? rv[n][0].y : rv[n][0].x) & any, (j ? rv[n][1].y : rv[n][1].x) & any);
+      vl[(buf * KU + 2 * (wave + W * n) + j) * kWave + lane] = bf16_of_bytes(j ? rv[n][0].y : rv[n][0].x, j ? rv[n][1].y : rv[n][1].x);
+  };
+  // (very small values are put in their unit afterwards, each wave its own: the steps that put them stay in one piece)
+  auto put_units = [&](unsigned buf) {
+    if (!Form::kFold) return;
+    const unsigned unit = uniform_bits(value_scale(av).unit);
+    if (unit == 0x3f800000u) return;
+#pragma unroll
+    for (int n = 0; n < VP; ++n)
+      if (W * n + W <= 2 * ND || wave + W * n < 2 * ND)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          bf8& v = vl[(buf * KU + 2 * (wave + W * n) + j) * kWave + lane];
+          v = in_units(v, unit);
+        }
   };
   auto put_keys = [&](unsigned buf) {
 #pragma unroll
@@ -732,6 +766,7 @@ __device__ __forceinline__ void many_rows(const ChunkParams& p, int vec, const L
     for (int n = 0; n < VP; ++n)
 #pragma unroll
       for (int j = 0; j < 2; ++j) put_value(buf, n, j);
+    put_units(buf);
   };
   fetch_keys(0);
 
@@ -835,8 +870,8 @@ __device__ __forceinline__ void many_rows(const ChunkParams& p, int vec, const L
     f = f == 0.f ? 1e-30f : f;                 // (0 times a masked score would be NaN; others are below 2^24)
     // (where there is no block, block 0 was read, whose maxima may be anything)
     const float fv = there ? av_now * (1.f / 127.f) : 0.f;
-    const bool nothing = !there || no_values(av_now);
-    const float lift = nothing ? 0.f : __builtin_amdgcn_logf(fv), inverse_now = nothing ? 1.f : __fdiv_rn(1.f, fv);
+    const ValueScale vs = FOLD ? value_scale(there ? av_now : 0.f) : ValueScale{1.f, 1.f};
+    const float lift = __builtin_amdgcn_logf(vs.m), inverse_now = __fdiv_rn(1.f, vs.m);
     const bool masks = !there || (pg + 1) * kKvBlock > least;
     const bf8* vu = vl + (size_t)odd * KU * kWave + lane;
     // half t's exponentials and values, beside them the other half's scores, of this block (t = 0) or the next; keys_then: those
@@ -924,6 +959,7 @@ __device__ __forceinline__ void many_rows(const ChunkParams& p, int vec, const L
     th_at[1] = there_k;
     fetch_keys(i + 3);
     half(std::integral_constant<int, 1>{}, keys_next, keys_next);
+    put_units(1 - odd);
     av_now = av;
     fetch_values(i + 2);
     const unsigned free = now;

@@ -1,0 +1,73 @@
+"""Corners of the serving operators' ranges (include/mq_serve.h) on the GPU, against the same formulas in 64 bits.
+
+Tolerances come from the number formats, before any run: a rounding to a type is off by at most half a step, and where operands or
+sums are whole multiples of a power of two that fit the 24 bits of binary32, products and sums are exact.
+"""
+
+import numpy as np
+import pytest
+import torch
+
+import paper_1805_12096_amd as mq
+from test_gpu_serve import BF16, BLOCK, DEV, F16, F32, TYPES, check_chunk, chunk_call, chunk_expected, gen, i32, normal, random_cache, tables
+
+pytestmark = pytest.mark.gpu
+
+
+# ---- attention of new tokens: scales of the values ----------------------------------------------------------------------------
+
+# new tokens, tokens in the cache with them, heads, kv heads, width, columns that the table has more: few rows, one workgroup a tile;
+# few rows in equal shares; many rows
+FORMS = {"few": ([3, 20], [320, 300], 4, 2, 64, 0), "shares": ([3, 20], [640, 1300], 4, 2, 64, 100), "many": ([300, 170], [700, 1300], 8, 2, 64, 2000),
+         "few wide": ([5], [384], 4, 2, 200, 0), "many wide": ([400], [1500], 4, 1, 128, 2000), "many widest": ([200], [900], 8, 2, 256, 2000)}
+
+
+def a_call(form, seed):
+    """(cache, table, first, lens, width of the table, queries in 64 bits, heads) of a form."""
+    new, lens, heads, kv_heads, dim, room = FORMS[form]
+    g = gen(seed)
+    need = sum(-(-n // BLOCK) for n in lens)
+    cache = random_cache(g, need, kv_heads, dim)
+    width = max(-(-n // BLOCK) for n in lens) + room
+    return cache, tables(g, lens, width, need), np.concatenate([[0], np.cumsum(new)]), lens, width, normal(g, sum(new), heads * dim), heads
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("power", [-130, -127, -120, -119, -118, -110, -100, -90, -70, -61, -53, -52, -30])
+def test_weights_of_small_values_count(form, dtype, power):
+    """Blocks whose values are very small beside ordinary ones: their tokens' weights stand in the denominator all the same.  (The
+    smallest powers are those of amax; a value is a whole number of 127th of it.)"""
+    cache, table, first, lens, width, q, heads = a_call(form, 30)
+    cache.amax[:, :, 1] *= 2.0 ** power
+    for b in range(len(lens)):                               # an ordinary block in four
+        for j in range(b, -(-lens[b] // BLOCK), 4):
+            cache.amax[table[b][j], :, 1] = 1.5
+    q, scale = q.to(dtype).to(DEV), 0.7 * cache.head_dim ** -0.5
+    args = cache, i32(table), i32(first), i32(lens), width * BLOCK
+    check_chunk(chunk_call(*args, True, q, heads, scale), *chunk_expected(cache, table, first, lens, width * BLOCK, True, q, heads, scale, dtype))
+
+
+@pytest.mark.parametrize("form", ["few", "shares", "many"])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_weights_of_values_of_every_size(form, dtype):
+    """Scales that change from block to block, from none to large, and scores over 20 binary orders."""
+    cache, table, first, lens, width, q, heads = a_call(form, 31)
+    powers = [0.0] + [2.0 ** p for p in (-140, -119, 3, -60, -118, 8 if dtype == F16 else 30, -90, -54, -53, -52, 5, -20)]
+    for e in range(cache.blocks):
+        cache.amax[e, :, 1] = powers[e % len(powers)] * 1.3
+    q, scale = q.to(dtype).to(DEV), 1.2 * cache.head_dim ** -0.5
+    args = cache, i32(table), i32(first), i32(lens), width * BLOCK
+    check_chunk(chunk_call(*args, True, q, heads, scale), *chunk_expected(cache, table, first, lens, width * BLOCK, True, q, heads, scale, dtype))
+
+
+@pytest.mark.parametrize("form", ["few", "shares", "many"])
+@pytest.mark.parametrize("power", [-100, -80, -55, -50])
+def test_values_that_are_small_throughout(form, power):
+    """Results are as exact in proportion where all values are small (bfloat16 and binary32 have them)."""
+    cache, table, first, lens, width, q, heads = a_call(form, 32)
+    cache.amax[:, :, 1] *= 2.0 ** power
+    for dtype in (BF16, F32):
+        x, scale = q.to(dtype).to(DEV), cache.head_dim ** -0.5
+        args = cache, i32(table), i32(first), i32(lens), width * BLOCK
+        check_chunk(chunk_call(*args, False, x, heads, scale), *chunk_expected(cache, table, first, lens, width * BLOCK, False, x, heads, scale, dtype))
