@@ -39,9 +39,10 @@ struct ChunkParams {
   int here;                           // whether the workgroups plan for themselves
 };
 
-// Exponent of the power of two taken off a row whose largest magnitude is m.
+// Exponent of the power of two taken off a row whose largest magnitude is m.  (126 at most: the multiplier 2^-127 is no normal number,
+// and its bits would be those of zero; a row of 2^127 and more keeps magnitudes of 2 .. 4.)
 __device__ __forceinline__ int row_exponent(float m) {
-  return m > 0.f && m < INFINITY ? max((int)(__float_as_uint(m) >> 23) - 127, -126) : 0;
+  return m > 0.f && m < INFINITY ? min(max((int)(__float_as_uint(m) >> 23) - 127, -126), 126) : 0;
 }
 // The same number, and nothing that the compiler keeps comparisons with: dozens of kept masks do not fit the scalar registers.
 __device__ __forceinline__ unsigned again(unsigned x) {
@@ -408,8 +409,8 @@ __device__ __forceinline__ void few_rows(const ChunkParams& p, int vec, const Li
     bring_keys();
     bring_values();
   }
-  // queries: a power of two off each row, so that its largest element is 1 .. 2, then parts in operand order.  Unit u of lane l is
-  // elements 32 (u / 2) + 16 (l / 32) + 8 (u % 2) .. of row l % 32
+  // queries: a power of two off each row, so that its largest element is 1 .. 2 (4 from 2^127 on), then parts in operand order.  Unit u
+  // of lane l is elements 32 (u / 2) + 16 (l / 32) + 8 (u % 2) .. of row l % 32
   {
     const unsigned rr = min(col, tile.rows - 1);
     const uint2 at = row_at(rr);

@@ -71,3 +71,19 @@ def test_values_that_are_small_throughout(form, power):
         x, scale = q.to(dtype).to(DEV), cache.head_dim ** -0.5
         args = cache, i32(table), i32(first), i32(lens), width * BLOCK
         check_chunk(chunk_call(*args, False, x, heads, scale), *chunk_expected(cache, table, first, lens, width * BLOCK, False, x, heads, scale, dtype))
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_queries_next_to_the_largest_number(form, dtype):
+    """Rows whose largest element lies between 2^127 and the type's largest number, beside keys and a scale that are small."""
+    cache, table, first, lens, width, q, heads = a_call(form, 33)
+    cache.amax[:, :, 0] *= 2.0 ** -8
+    d, T = cache.head_dim, len(q)
+    q = q.double().view(T, heads, d).clamp(-3, 3) * 2.0 ** 125
+    at = torch.arange(T * heads).view(T, heads)
+    q.scatter_(2, (at % d)[..., None], ((1 - 2 * (at % 2)) * (1 + at % 50 / 51) * 2.0 ** 127)[..., None].double())
+    q = q.to(dtype).view(T, heads * d).to(DEV)
+    assert torch.isfinite(q).all() and (q.view(T, heads, d).abs().amax(-1) >= 2.0 ** 127).all()
+    args, scale = (cache, i32(table), i32(first), i32(lens), width * BLOCK), 2.0 ** -119
+    check_chunk(chunk_call(*args, True, q, heads, scale), *chunk_expected(cache, table, first, lens, width * BLOCK, True, q, heads, scale, dtype))
