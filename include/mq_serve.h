@@ -37,9 +37,9 @@ extern "C" {
  *     ldo = ldq); rows that belong to no sequence are left as they are.
  * Queries enter the products exactly: one, two or three bfloat16 parts (bfloat16, binary16, binary32; elements below 2^-100 of
  * their row's largest may be lost).  The cache's integers are bfloat16 values as they are.  Probabilities times the scale of the
- * values' block enter as as many parts, 8, 16 or 24 bits (16-bit types: values of a
- * block whose largest is below 2^-119 count as zeros, and bits of values below 2^-100 may be lost; the weights of such tokens count
- * in the denominator all the same).  Sums and softmax statistics are binary32.
+ * values' block enter as two parts (16-bit types, 16 bits) or three (binary32, 24 bits).  16-bit types: values of a block whose
+ * largest is below 2^-119 count as zeros, and bits of values below 2^-100 may be lost; the weights of such tokens count in the
+ * denominator all the same.  Sums and softmax statistics are binary32.
  * ws: device, 16-byte aligned, mq_chunk_attention_ws_bytes (0 for invalid arguments).  One launch where max_len <= 1152 (up to
  * 2048 if there is work for all of the chip) and rows are few, else two or three: shares are planned from the lengths, computed, and
  * joined.  Calls of which that plan cannot count the blocks in 31 bits (some 2^31 / (max_len / 64) tiles of 32 rows) are refused with

@@ -5,8 +5,8 @@
 // tokens x the heads of the group, are rows of one product: S^T = K q^T on v_mfma_f32_32x32x16_bf16, 32 tokens of K as operand
 // a, 32 query rows as operand b.  Lane l then has, for row l % 32, the scores of tokens 8 (r / 4) + 4 (l / 32) + r % 4 of 32, and
 // the cache keeps the values of a block in an order (kv_place) in which these lanes' probabilities are operand b of out^T = V^T p^T
-// as they are.  The cache's integers are bfloat16 values exactly (8 bits); queries and probabilities enter as one, two or three
-// bfloat16 parts.  Scales: a block's for the keys goes into the scores' factor, a block's for the values into the probabilities,
+// as they are.  The cache's integers are bfloat16 values exactly (8 bits); queries enter as one, two or three bfloat16 parts,
+// probabilities as two or three.  Scales: a block's for the keys goes into the scores' factor, a block's for the values into the probabilities,
 // so sums stay in the accumulators from block to block.
 #include <type_traits>
 
@@ -49,6 +49,10 @@ __device__ __forceinline__ unsigned again(unsigned x) {
   asm volatile("" : "+s"(x));
   return x;
 }
+// How many bfloat16 parts hold a probability: 16 bits for 16-bit types.  (One part, 8 bits, is as coarse as a bfloat16 result: four
+// pieces of 300 .. 1100 tokens on 2000 .. 16000 in 412 us instead of 542, but off by 2.3e-3 from 64 bits instead of 1.7e-3.)
+template <int DT>
+constexpr int kWeightParts = DT == MQ_F32 ? 3 : 2;
 __device__ __forceinline__ float finite_or_0(float m) { return m == -INFINITY ? 0.f : m; }
 
 // A block's value is integer x unit x m.  m goes into the exponent of its tokens' weights, which the exponential flushes below
@@ -322,7 +326,7 @@ constexpr int waitcnt_loads(int n) { return (n & 15) | (n >> 4) << 14 | 0x0070; 
 template <int DT, int DC>             // DC: 64-column pieces of a key
 __device__ __forceinline__ void few_rows(const ChunkParams& p, int vec, const LinePart& part, unsigned to_part) {
   using T = typename Elem<DT>::T;
-  constexpr int NP = kParts<DT>;
+  constexpr int NP = kParts<DT>, PP = kWeightParts<DT>;
   constexpr int NK = 2 * DC, ND = 2 * DC;      // 32-column pieces of a key, 32-column pieces of a value at most
   constexpr int U = NK * 2;                    // units of 8 elements of a query
   extern __shared__ __attribute__((aligned(1024))) char smem[];
@@ -466,7 +470,7 @@ __device__ __forceinline__ void few_rows(const ChunkParams& p, int vec, const Li
 
   float acc_top = -INFINITY, total = 0.f;      // of row l % 32; the total of this lane's tokens
   v16f acc[ND] = {};
-  constexpr bool FOLD = NP < 3;
+  constexpr bool FOLD = PP < 3;
   for (unsigned i = 0; i < mine; ++i) {
     const unsigned pg = start + wave + i * W;
     const float2 am = am_next;
@@ -528,15 +532,15 @@ __device__ __forceinline__ void few_rows(const ChunkParams& p, int vec, const Li
     else arrived(std::integral_constant<int, 0>{});
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      bf8 pr[NP];
+      bf8 pr[PP];
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
         const float e = __builtin_amdgcn_exp2f(fmaf(sc[j / 2][8 * (j % 2) + k], f, base));
         if (!FOLD) sum += e;
-        __bf16 v[NP];
-        split_bf16<NP>(FOLD ? e : e * fv, v);
+        __bf16 v[PP];
+        split_bf16<PP>(FOLD ? e : e * fv, v);
 #pragma unroll
-        for (int n = 0; n < NP; ++n) {
+        for (int n = 0; n < PP; ++n) {
           pr[n][k] = v[n];
           if (FOLD && k % 2 == 1) sum = add2(pr[n][k - 1], v[n], sum);
         }
@@ -549,7 +553,7 @@ __device__ __forceinline__ void few_rows(const ChunkParams& p, int vec, const Li
         }
         const bf8 a = in_units(bf16_of_bytes(vf[t][0][j], vf[t][1][j]), unit);
 #pragma unroll
-        for (int k = NP - 1; k >= 0; --k) acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, pr[k], acc[t], 0, 0, 0);
+        for (int k = PP - 1; k >= 0; --k) acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, pr[k], acc[t], 0, 0, 0);
       }
     }
     total = FOLD ? fmaf(sum, __fdiv_rn(1.f, vs.m), total) : total + sum;
@@ -661,17 +665,17 @@ __device__ __forceinline__ void scale_sums(v16f& o, float factor) {
 template <int DT, int DC>
 struct TileForm {
   // two waves a SIMD where their registers fit
-  static constexpr int NP = kParts<DT>, W = NP * DC <= 2 ? 8 : 4, kRowsOfWg = W * 32;
+  static constexpr int NP = kParts<DT>, PP = kWeightParts<DT>, W = NP * DC <= 2 ? 8 : 4, kRowsOfWg = W * 32;
   static constexpr int kUnits = 8 * DC;                    // 1 KB pieces of a block's keys, and of its values
   static constexpr size_t kLds = 5 * (size_t)kUnits * 1024;       // three blocks of keys, two of values
-  static constexpr bool kFold = NP < 3;
+  static constexpr bool kFold = PP < 3;
 };
 
 template <int DT, int DC>
 __device__ __forceinline__ void many_rows(const ChunkParams& p, int vec, const LinePart& part, unsigned to_part) {
   using T = typename Elem<DT>::T;
   using Form = TileForm<DT, DC>;
-  constexpr int NP = Form::NP, W = Form::W, NK = 2 * DC, ND = 2 * DC, KU = Form::kUnits;
+  constexpr int NP = Form::NP, PP = Form::PP, W = Form::W, NK = 2 * DC, ND = 2 * DC, KU = Form::kUnits;
   extern __shared__ __attribute__((aligned(16))) bf8 tile_lds[];                 // keys [3][KU][64], values [2][KU][64]
   bf8 *const kl = tile_lds, *const vl = tile_lds + 3 * KU * kWave;
   // (unknown to the compiler to be the same each time: it would keep dozens of places and masks from one part to the next)
@@ -906,17 +910,17 @@ __device__ __forceinline__ void many_rows(const ChunkParams& p, int vec, const L
         for (int c = 0; c < ND; ++c) scale_sums<Form::W == 8>(acc[c], keep);
       }
       const float base = FOLD ? lift - finite_or_0(ref) : -finite_or_0(ref);
-      bf8 pr[NP][2];
+      bf8 pr[PP][2];
       // exponentials [from, end) of the 16 that a lane has of each row
       auto exponentials = [&](int from, int end) __attribute__((always_inline)) {
 #pragma unroll
         for (int n = from; n < end; ++n) {
           const float e = __builtin_amdgcn_exp2f(fmaf(sc[t][n], f, base));
           if (!FOLD) total += e;
-          __bf16 b[NP];
-          split_bf16<NP>(FOLD ? e : e * fv, b);
+          __bf16 b[PP];
+          split_bf16<PP>(FOLD ? e : e * fv, b);
 #pragma unroll
-          for (int k = 0; k < NP; ++k) {
+          for (int k = 0; k < PP; ++k) {
             pr[k][n / 8][n % 8] = b[k];
             if (FOLD && n % 2 == 1) sum = add2(pr[k][n / 8][n % 8 - 1], b[k], sum);
           }
@@ -935,7 +939,7 @@ __device__ __forceinline__ void many_rows(const ChunkParams& p, int vec, const L
       for (int u = 0; u < STEPS; ++u) {
         const int j = u / ND, c = u % ND;
 #pragma unroll
-        for (int k = NP - 1; k >= 0; --k)
+        for (int k = PP - 1; k >= 0; --k)
           acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(piece[u % AHEAD], pr[k][j], acc[c], 0, 0, 0);
         if (u + AHEAD < STEPS) read_value(u + AHEAD);
         else read_key(keys_then, std::integral_constant<int, t>{}, u + AHEAD - STEPS);

@@ -9,7 +9,8 @@ import pytest
 import torch
 
 import paper_1805_12096_amd as mq
-from test_gpu_serve import BF16, BLOCK, DEV, F16, F32, TYPES, check_chunk, chunk_call, chunk_expected, gen, i32, normal, random_cache, tables
+from test_gpu_serve import (BF16, BLOCK, DEV, F16, F32, TYPES, check_chunk, chunk_call, chunk_expected, gen, half_step, i32, normal,
+                            random_cache, tables)
 
 pytestmark = pytest.mark.gpu
 
@@ -87,3 +88,21 @@ def test_queries_next_to_the_largest_number(form, dtype):
     assert torch.isfinite(q).all() and (q.view(T, heads, d).abs().amax(-1) >= 2.0 ** 127).all()
     args, scale = (cache, i32(table), i32(first), i32(lens), width * BLOCK), 2.0 ** -119
     check_chunk(chunk_call(*args, True, q, heads, scale), *chunk_expected(cache, table, first, lens, width * BLOCK, True, q, heads, scale, dtype))
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("dtype", [F16, BF16])
+def test_probabilities_of_short_types_hold_sixteen_bits(form, dtype):
+    """Queries that see a few tokens, scores of about 1: results are off by their own rounding and 2^-15 of the largest value, as those
+    of a type whose probabilities enter in two parts."""
+    new, lens, heads, kv_heads, dim, room = FORMS[form]
+    g = gen(34)
+    lens = list(new) if len(new) * new[0] > 100 else [n + 4 for n in new]
+    cache = random_cache(g, 40, kv_heads, dim)
+    width = max(-(-n // BLOCK) for n in lens) + room
+    table, first = tables(g, lens, width, 40), np.concatenate([[0], np.cumsum(new)])
+    q, scale = normal(g, sum(new), heads * dim).to(dtype).to(DEV), 0.3 * dim ** -0.5
+    args = cache, i32(table), i32(first), i32(lens), width * BLOCK
+    want, tol = chunk_expected(cache, table, first, lens, width * BLOCK, True, q, heads, scale, F16)
+    tol = tol - half_step(F16, want) + half_step(dtype, want)
+    check_chunk(chunk_call(*args, True, q, heads, scale), want, tol)
