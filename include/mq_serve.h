@@ -90,11 +90,13 @@ int mq_kv_compact(const mq_kv_cache* cache, const int32_t* keep, const int32_t* 
 /* ---- residual addition and root-mean-square norm -----------------------------------
  * For M rows of d <= 16384 elements of a type:
  *   h = x + r, rounded to the type (h = x where r is NULL);   y = h / sqrt(mean(h^2) + eps) gamma
- * in binary32 (h^2 is summed in binary32: below 2^56 nothing overflows).  gamma: device float [d].  h: rows that receive h, or
- * NULL; h may be x or r itself, and y may be, with its ld, but h and y must not overlap.  One launch each.
+ * in binary32 (h^2 is summed in binary32: below 2^56 nothing overflows; squares of elements below 2^-63 lose bits, which shows where
+ * eps is smaller still).  gamma: device float [d].  h: rows that receive h, or NULL; h may be x or r itself, and y may be, with its
+ * ld, but h and y must not overlap.  One launch each.
  *   mq_add_rms_norm:        y rounded to the type, rows ldy apart.
  *   mq_add_rms_norm_rows8:  q[m][i] = clamp(rne(y s), +-127) as int8 rows ldq apart, with a multiplier for each row,
- *     s = scale[m] = 127 / max |y| (1 for a row of zeros; NaN, and zeros in q, for a row that holds a NaN or an infinity).
+ *     s = scale[m] = 127 / max |y|, the largest binary32 number at most (1 for a row of zeros; NaN, and zeros in q, for a row that
+ *     holds a NaN or an infinity).
  *   mq_add_rms_norm_pack8:  q = quant_int(y, s[0]), device float [1] given, as the packed 8-bit operand of mq.h's products
  *     (mq_packed_bytes(8, M, d) bytes, padding included, 16-byte aligned). */
 int mq_add_rms_norm(const void* x, size_t ldx, const void* r, size_t ldr, int dtype, const float* gamma, size_t M, size_t d,

@@ -119,7 +119,8 @@ __global__ __launch_bounds__(256) void k_rms_norm(const NormArgs p, unsigned wid
   if constexpr (FORM == kNormRows8) {
     most = row_reduce<WIDE_ROW>(most, box[1], [](float a, float b) { return fmaxf(a, b); });
     // a NaN or an infinity in h shows in the sum of squares, one that gamma makes in the maximum or not at all
-    s = !(sum <= 3.402823466e38f) || most == INFINITY ? NAN : most > 0.f ? __fdiv_rn(127.f, most) : 1.f;
+    // (an infinite multiplier, of a row below 127 / the largest number, would make 127 of all that is not zero)
+    s = !(sum <= 3.402823466e38f) || most == INFINITY ? NAN : most > 0.f ? fminf(__fdiv_rn(127.f, most), 3.402823466e38f) : 1.f;
     if (t == 0) p.scale[m] = s;
   } else {
     s = *p.s;

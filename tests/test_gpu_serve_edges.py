@@ -3,13 +3,14 @@
 Tolerances come from the number formats, before any run: a rounding to a type is off by at most half a step, and where operands or
 sums are whole multiples of a power of two that fit the 24 bits of binary32, products and sums are exact.
 """
+import math
 
 import numpy as np
 import pytest
 import torch
 
 import paper_1805_12096_amd as mq
-from test_gpu_serve import (BF16, BLOCK, DEV, F16, F32, TYPES, check_chunk, chunk_call, chunk_expected, gen, half_step, i32, normal,
+from test_gpu_serve import (BF16, BLOCK, DEV, EPS32, F16, F32, TYPES, check_chunk, chunk_call, chunk_expected, gen, half_step, i32, normal,
                             random_cache, tables)
 
 pytestmark = pytest.mark.gpu
@@ -106,3 +107,30 @@ def test_probabilities_of_short_types_hold_sixteen_bits(form, dtype):
     want, tol = chunk_expected(cache, table, first, lens, width * BLOCK, True, q, heads, scale, F16)
     tol = tol - half_step(F16, want) + half_step(dtype, want)
     check_chunk(chunk_call(*args, True, q, heads, scale), want, tol)
+
+
+# ---- norm -----------------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("d", [40, 512, 1000])
+@pytest.mark.parametrize("power", [-149, -130, -125, -121, -119, -110])
+def test_multipliers_of_very_small_rows_are_finite(dtype, d, power):
+    """127 / max |y| where that is a number, the largest number where it would be past it; a row that is all zeros has 1."""
+    g, M = gen(d), 5
+    x, gamma = normal(g, M, d).to(dtype).to(DEV), torch.full((d,), 2.0 ** power, device=DEV)
+    x[3] = 0
+    z = x.double()
+    y = z / torch.sqrt((z * z).mean(-1, keepdim=True) + 1e-5) * gamma.double()
+    q, scale = torch.empty((M, d), dtype=torch.int8, device=DEV), torch.empty(M, device=DEV)
+    mq.mq_add_rms_norm_rows8(x, d, None, d, mq.dtype_code(dtype), gamma, M, d, 1e-5, None, d, q, d, scale)
+    assert scale[3] == 1 and not q[3].any()
+    rows, most = [0, 1, 2, 4], torch.finfo(F32).max
+    assert torch.isfinite(scale).all()
+    # y is off by 43 eps32 in proportion (sums of squares) or by half of 2^-149, whichever is more, its largest element likewise
+    top = y[rows].abs().amax(-1)
+    off = 43 * EPS32 * top + 2.0 ** -150
+    low, high = 127 / (top + off) * (1 - EPS32), torch.where(top > off, 127 / (top - off) * (1 + EPS32), torch.full_like(top, math.inf))
+    s = scale[rows].double()
+    if power > -149:                                         # (there a row may be zeros altogether)
+        assert ((s >= low.clamp(max=most)) & (s <= high.clamp(max=most))).all()
+        assert ((q[rows].double() - y[rows] * s[:, None]).abs() <= 0.5 + (off * s)[:, None] + 127 * EPS32).all()
