@@ -128,11 +128,11 @@ int mq_w4_unpack(const void* packed, size_t N, size_t K, int group, float* w, vo
  *     float [M] (an element q stands for q / row_scale[m], as mq_add_rms_norm_rows8 leaves them); row_scale is NULL for the others.
  *   y: M rows of N elements, ldy apart, of type ytype (an mq_dtype).  bias: device float [N] or NULL.
  * x enters the products exactly (1, 1, 2, 3 bfloat16 parts for int8, bfloat16, binary16, binary32; of magnitudes below 2^-100 the
- * last bits of the latter may be lost), codes exactly, scales after the sums over a group (binary32: over 32 elements); sums are
- * binary32, and up to 31 sum |x| over a group must be one of its numbers.  A row of x with a NaN or an infinity gives no finite
- * number.  y must not overlap x.  packed: 16-byte aligned.  ws: device, 16-byte aligned, mq_w4_product_ws_bytes(M, N, K) bytes (0 for invalid
- * arguments).  One launch for up to 32, 16 or 8 rows (8-bit and bfloat16, binary16, binary32) if they are whole 16-byte pieces,
- * else two, or three where a contraction is split over workgroups. */
+ * last bits of the latter may be lost), codes and zeros exactly (of binary32 rows c - z, of the others c and z in sums of their own),
+ * scales after the sums over a group; sums are binary32, and up to 31 sum |x| over a group must be one of its numbers.  A row of x
+ * with a NaN or an infinity gives no finite number.  y must not overlap x.  packed: 16-byte aligned.  ws: device, 16-byte aligned,
+ * mq_w4_product_ws_bytes(M, N, K) bytes (0 for invalid arguments).  One launch for up to 32, 16 or 8 rows (8-bit and bfloat16,
+ * binary16, binary32) if they are whole 16-byte pieces, else two, or three where a contraction is split over workgroups. */
 #define MQ_ROWS8 3
 size_t mq_w4_product_ws_bytes(size_t M, size_t N, size_t K);
 int mq_w4_product(const void* x, size_t ldx, int xtype, const float* row_scale, const void* packed, size_t M, size_t N, size_t K,

@@ -5,6 +5,8 @@
 // that a lane has results of one row of the parameter, and needs one scale).  Code 2 p lies in nibble p of the word's
 // lower half, code 2 p + 1 in nibble p of the upper, so a pair shifted and masked once is two bfloat16 mantissas: 16 + c, exactly.
 // y = sum_g s (sum_k (16 + c) x - (16 + z) sum_k x): a product with ones gives sum_k x where the other product leaves its results.
+// That difference is off by roundings of up to 31 sum |x|.  Of binary32 rows they would show (one element, its zero next to its code: 16
+// times the rounding of the result), so there c - z is formed in bytes and y = sum_g s sum_k (c - z) x.
 // Scales follow the fragments: a word for each (16 rows, group, row), 20 bits of mantissa of the scale and the zero below them.
 #include <type_traits>
 
@@ -132,10 +134,10 @@ template <int XT>
 constexpr int kXParts = XT == MQ_ROWS8 ? 1 : kParts<XT == MQ_ROWS8 ? MQ_BF16 : XT>;
 
 // What a product takes of x and of codes.  8-bit rows: signed bytes and the codes as bytes, sums whole numbers (below 2^24, so
-// exact in binary32).  Others: bfloat16 parts and 16 + c, sums binary32.
+// exact in binary32).  Others: bfloat16 parts and 16 + c, of binary32 c - z, sums binary32.
 template <int XT>
 struct Operand {
-  static constexpr bool kBytes = XT == MQ_ROWS8;
+  static constexpr bool kBytes = XT == MQ_ROWS8, kNoZeros = XT == MQ_F32;       // (kNoZeros: nothing is left to take off)
   static constexpr int NP = kXParts<XT>, kOffset = kBytes ? 0 : 16;
   using Piece = typename std::conditional<kBytes, long, bf8>::type;
   using Acc = typename std::conditional<kBytes, v4i, v4f>::type;
@@ -143,9 +145,18 @@ struct Operand {
     if constexpr (kBytes) return __builtin_amdgcn_mfma_i32_16x16x32_i8(a, b, c, 0, 0, 0);
     else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
   }
-  static __device__ __forceinline__ Piece codes(unsigned w) {
+  // scale: the word that holds the group's zero
+  static __device__ __forceinline__ Piece codes(unsigned w, unsigned scale) {
     if constexpr (kBytes) {             // codes 0 4 1 5 2 6 3 7
       return __builtin_bit_cast(long, make_uint2(w & 0x0f0f0f0fu, w >> 4 & 0x0f0f0f0fu));
+    } else if constexpr (kNoZeros) {
+      const unsigned z = (scale & 15u) * 0x01010101u;
+      auto less = [&](unsigned c) { return (((c & 0x0f0f0f0fu) | 0x80808080u) - z) ^ 0x80808080u; };         // (no byte borrows)
+      const unsigned a = less(w), b = less(w >> 4);
+      auto pair = [](float x, float y) { return __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302u); };
+      const u4 v = {pair(f32_of_byte<0>(a), f32_of_byte<2>(a)), pair(f32_of_byte<0>(b), f32_of_byte<2>(b)),
+                    pair(f32_of_byte<1>(a), f32_of_byte<3>(a)), pair(f32_of_byte<1>(b), f32_of_byte<3>(b))};
+      return __builtin_bit_cast(bf8, v);
     } else {
       constexpr unsigned mask = 0x00780078u, top = 0x41804180u;
       const u4 v = {(w << 3 & mask) | top, (w >> 1 & mask) | top, (w >> 5 & mask) | top, (w >> 9 & mask) | top};
@@ -199,11 +210,9 @@ __device__ __forceinline__ void x_parts(const Raw<XT>& r, typename Operand<XT>::
   }
 }
 
-// Steps of 32 elements after which the zero is taken off a sum and the scale put to it: a group's, but for binary32 each, since
-// the difference of sum (16 + c) x and (16 + z) sum x loses more the longer they have grown (against 64 bits, groups of 128, 100 rows:
-// 1.2e-6 off with a group's sums, 6e-7 with 32 elements').
-template <int XT, int GROUP>
-constexpr int kEvery = XT == MQ_F32 ? 1 : GROUP / 32;
+// Steps of 32 elements of a group, after which its zero is taken off a sum and its scale put to it.
+template <int GROUP>
+constexpr int kEvery = GROUP / 32;
 
 constexpr unsigned kFewWaves = 4;      // of a workgroup, at most
 
@@ -218,7 +227,7 @@ template <int XT, int GROUP, int MT>
 __global__ __launch_bounds__(kFewWaves * kWave, 2) void k_w4_few(const W4Params p) {
   using T = typename XElem<XT>::T;
   constexpr int NP = kXParts<XT>, GF = kKT / GROUP, SG = GROUP / 32;      // groups of a fragment, steps of a group
-  constexpr int EVERY = kEvery<XT, GROUP>;
+  constexpr int EVERY = kEvery<GROUP>;
   extern __shared__ __attribute__((aligned(16))) char smem[];
   float* const lds = reinterpret_cast<float*>(smem);       // [waves][MT 16][17], afterwards
   const unsigned lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), waves = blockDim.x / kWave;
@@ -301,7 +310,7 @@ __global__ __launch_bounds__(kFewWaves * kWave, 2) void k_w4_few(const W4Params 
     typename Op::Acc acc[MT], sum[MT];
 #pragma unroll
     for (int step = 0; step < 4; ++step) {
-      const Piece c = Op::codes(w[at][step]);
+      const Piece c = Op::codes(w[at][step], sc[at][step / SG]);
 #pragma unroll
       for (int t = 0; t < MT; ++t) {
 #pragma unroll
@@ -309,7 +318,7 @@ __global__ __launch_bounds__(kFewWaves * kWave, 2) void k_w4_few(const W4Params 
           const bool begins = step % EVERY == 0 && j == NP - 1;
           const Piece xp = read_x(t, j, step);
           acc[t] = Op::mfma(xp, c, begins ? typename Op::Acc{} : acc[t]);
-          sum[t] = Op::mfma(xp, ones, begins ? typename Op::Acc{} : sum[t]);
+          if constexpr (!Op::kNoZeros) sum[t] = Op::mfma(xp, ones, begins ? typename Op::Acc{} : sum[t]);
         }
       }
       if (step % EVERY != EVERY - 1) continue;
@@ -317,7 +326,8 @@ __global__ __launch_bounds__(kFewWaves * kWave, 2) void k_w4_few(const W4Params 
 #pragma unroll
       for (int t = 0; t < MT; ++t)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) y[t][r] = fmaf(s, fmaf(-z, (float)sum[t][r], (float)acc[t][r]), y[t][r]);
+        for (int r = 0; r < 4; ++r)
+          y[t][r] = fmaf(s, Op::kNoZeros ? (float)acc[t][r] : fmaf(-z, (float)sum[t][r], (float)acc[t][r]), y[t][r]);
     }
   };
 #pragma unroll
@@ -372,7 +382,7 @@ template <int XT, int GROUP>
 __global__ __launch_bounds__(256) void k_w4_x(const W4Params p, uint8_t* to) {
   using T = typename XElem<XT>::T;
   using Piece = typename Operand<XT>::Piece;
-  constexpr int NP = kXParts<XT>, EVERY = kEvery<XT, GROUP>;
+  constexpr int NP = kXParts<XT>, EVERY = kEvery<GROUP>;
   const XDims x(p.M, p.K, NP);
   const unsigned lane = threadIdx.x % kWave, col = lane % 16, grp = lane / 16;
   const size_t all = x.tiles * x.frags;
@@ -398,6 +408,7 @@ __global__ __launch_bounds__(256) void k_w4_x(const W4Params p, uint8_t* to) {
       Piece* dst = reinterpret_cast<Piece*>(to) + (s * 4 + i) * NP * kWave + lane;
 #pragma unroll
       for (int k = 0; k < NP; ++k) dst[k * kWave] = part[k];
+      if (Operand<XT>::kNoZeros) continue;
 #pragma unroll
       for (int j = 0; j < 8; ++j) sum += (float)r[i].v[j];
       if (i % EVERY != EVERY - 1) continue;
@@ -411,7 +422,7 @@ __global__ __launch_bounds__(256) void k_w4_x(const W4Params p, uint8_t* to) {
 
 template <int XT, int GROUP>
 __global__ __launch_bounds__(kManyWaves * kWave, 2) void k_w4_many(const W4Params p, const uint8_t* xs, unsigned runs, unsigned run) {
-  constexpr int NP = kXParts<XT>, GF = kKT / GROUP, SG = GROUP / 32, MT = many_mt(NP), NT = kManyNT, EVERY = kEvery<XT, GROUP>;
+  constexpr int NP = kXParts<XT>, GF = kKT / GROUP, SG = GROUP / 32, MT = many_mt(NP), NT = kManyNT, EVERY = kEvery<GROUP>;
   extern __shared__ float lds[];                 // [waves][MT 16][NT 16 + 1]
   const unsigned lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), col = lane % 16, grp = lane / 16;
   // neighbouring workgroups share rows of x: those of one XCD its parts
@@ -462,12 +473,14 @@ __global__ __launch_bounds__(kManyWaves * kWave, 2) void k_w4_many(const W4Param
 #pragma unroll
     for (int step = 0; step < 4; ++step) {
       load_x((step + 1) % 2, step < 3 ? f : next, (step + 1) % 4);
-      if (step % EVERY == 0)
+      // (the compiler would ask for them where they are used: 11000 x 4096, groups of 128, 64 rows 48 us instead of 31)
+      if (Op::kNoZeros) __builtin_amdgcn_sched_barrier(0);
+      if (!Op::kNoZeros && step % EVERY == 0)
 #pragma unroll
         for (int t = 0; t < MT; ++t) sum[t] = reinterpret_cast<const v4f*>(xsum[t] + ((size_t)f * (4 / EVERY) + step / EVERY) * 16)[grp];
       Piece c[NT];
 #pragma unroll
-      for (int n = 0; n < NT; ++n) c[n] = Op::codes(w[at][n][step]);
+      for (int n = 0; n < NT; ++n) c[n] = Op::codes(w[at][n][step], sc[at][n][step / SG]);
 #pragma unroll
       for (int t = 0; t < MT; ++t)
 #pragma unroll
@@ -482,7 +495,8 @@ __global__ __launch_bounds__(kManyWaves * kWave, 2) void k_w4_many(const W4Param
 #pragma unroll
         for (int t = 0; t < MT; ++t)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) y[n][t][r] = fmaf(s, fmaf(-z, sum[t][r], (float)acc[n][t][r]), y[n][t][r]);
+          for (int r = 0; r < 4; ++r)
+            y[n][t][r] = fmaf(s, Op::kNoZeros ? (float)acc[n][t][r] : fmaf(-z, sum[t][r], (float)acc[n][t][r]), y[n][t][r]);
       }
     }
   };

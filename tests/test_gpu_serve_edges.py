@@ -134,3 +134,34 @@ def test_multipliers_of_very_small_rows_are_finite(dtype, d, power):
     if power > -149:                                         # (there a row may be zeros altogether)
         assert ((s >= low.clamp(max=most)) & (s <= high.clamp(max=most))).all()
         assert ((q[rows].double() - y[rows] * s[:, None]).abs() <= 0.5 + (off * s)[:, None] + 127 * EPS32).all()
+
+
+# ---- products with 4-bit parameters -------------------------------------------------------------------------------------------
+
+def product(x, packed, N, group, out, rs=None, bias=None, K=None):
+    """y of an x of which K columns count."""
+    M, K = len(x), K or x.shape[1]
+    y = torch.full((M, N), 7.0, dtype=out, device=DEV)
+    ws = torch.full((mq.mq_w4_product_ws_bytes(M, N, K),), 255, dtype=torch.uint8, device=DEV)
+    mq.mq_w4_product(x, x.stride(0), mq.MQ_ROWS8 if rs is not None else mq.dtype_code(x.dtype), rs, packed, M, N, K, group, bias, y, N,
+                     mq.dtype_code(out), ws, ws.numel())
+    return y
+
+
+@pytest.mark.parametrize("M", [1, 5, 8, 9, 70])
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("K", [32, 300, 1000])
+def test_zeros_next_to_codes_cost_no_bits(M, group, K):
+    """Binary32 rows with one element each, codes and zeros that differ by 1: the result is that element times the scale, rounded
+    (a power of two here: not even that), however large codes and zeros are."""
+    g, N = gen(M), 40
+    groups = -(-K // group)
+    zeros = torch.randint(0, 15, (N, groups), generator=g).to(torch.uint8)
+    codes = (zeros[:, torch.arange(K) // group] + 1).to(torch.uint8)
+    scales = 2.0 ** torch.randint(-3, 4, (N, groups), generator=g).float()
+    packed = mq.w4_pack(codes.to(DEV), scales.to(DEV), zeros.to(DEV), group)
+    x, at = torch.zeros(M, K), torch.randint(0, K, (M,), generator=g)
+    x[torch.arange(M), at] = normal(g, M)
+    want = x[torch.arange(M), at][:, None] * scales[:, at // group].T
+    y = product(x.to(DEV), packed, N, group, F32).cpu()
+    assert ((y.double() - want.double()).abs() <= EPS32 * want.abs()).all(), float(((y - want) / want).abs().max()) / EPS32
