@@ -10,8 +10,8 @@ import pytest
 import torch
 
 import paper_1805_12096_amd as mq
-from test_gpu_serve import (BF16, BLOCK, DEV, EPS32, F16, F32, TYPES, check_chunk, chunk_call, chunk_expected, gen, half_step, i32, normal,
-                            random_cache, tables)
+from test_gpu_serve import (BF16, BLOCK, DEV, EPS32, F16, F32, PARTS, TYPES, check_chunk, chunk_call, chunk_expected, gen, half_step, i32,
+                            normal, product_tolerance, random_cache, tables, w4_inputs)
 
 pytestmark = pytest.mark.gpu
 
@@ -165,3 +165,54 @@ def test_zeros_next_to_codes_cost_no_bits(M, group, K):
     want = x[torch.arange(M), at][:, None] * scales[:, at // group].T
     y = product(x.to(DEV), packed, N, group, F32).cpu()
     assert ((y.double() - want.double()).abs() <= EPS32 * want.abs()).all(), float(((y - want) / want).abs().max()) / EPS32
+
+
+@pytest.mark.parametrize("M", [1, 6, 9, 16, 40])
+@pytest.mark.parametrize("xtype", [F32, F16, BF16])
+def test_every_bit_of_x_counts(M, xtype):
+    """Rows with one element each and codes 15 off their zeros: 15 times the element, off by few roundings of 31 times it.  The last
+    of its parts is about 2^-18 (binary32), 2^-9 (binary16) of it."""
+    g, N, K, group = gen(M), 33, 512, 64
+    packed = mq.w4_pack(torch.full((N, K), 15, dtype=torch.uint8, device=DEV), torch.ones((N, K // group), device=DEV),
+                        torch.zeros((N, K // group), dtype=torch.uint8, device=DEV), group)
+    x, at = torch.zeros(M, K, dtype=xtype), torch.randint(0, K, (M,), generator=g)
+    # values whose parts are all there: bits at the top, in the middle and at the end
+    x[torch.arange(M), at] = (1 + 2.0 ** -9 * 1.3333334 * (1 + torch.arange(M) / 50)).to(xtype) * (2.0 ** torch.randint(-9, 9, (M,), generator=g)).to(xtype)
+    want = 15 * x[torch.arange(M), at].double()[:, None].expand(M, N)
+    y = product(x.to(DEV), packed, N, group, F32).double().cpu()
+    assert ((y - want).abs() <= 31 * 8 * EPS32 / 2 * want.abs() / 15).all(), float(((y - want) / want).abs().max())
+
+
+# rows, width; few rows of whole pieces: of one and two row tiles, fragments fewer and more than waves ahead, ragged ends
+FEW = [(17, 128), (24, 336), (31, 624), (32, 2192), (18, 4096), (32, 16), (29, 8208), (9, 384), (16, 2064), (12, 80), (3, 2304), (8, 5120), (1, 10000),
+       (5, 48), (7, 640)]
+
+
+@pytest.mark.parametrize("M,K", FEW)
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("xtype", ["rows8", F32, F16, BF16])
+def test_few_rows_of_whole_pieces(M, K, group, xtype):
+    """Every form for few rows (binary16 and binary32 take it up to 16 and 8 rows, so others here see the form for many)."""
+    g, N = gen(M * K + group), 16 * (M % 3 + 1) + M % 5
+    codes, s, z, w = w4_inputs(g, N, K, group, M % 2 == 0)
+    packed = mq.w4_pack(codes, s, z, group)
+    bias = normal(g, N).to(DEV) if M % 4 else None
+    ld, rs = K + 16 * (M % 2), None
+    if xtype == "rows8":
+        x = torch.full((M, ld), 55, dtype=torch.int8, device=DEV)
+        x[:, :K] = torch.randint(-127, 128, (M, K), generator=g).to(torch.int8)
+        rs, out = (5 + 10 * torch.rand(M, generator=g)).to(DEV), BF16 if group == 64 else F32
+        x64 = x[:, :K].double().cpu() / rs.double().cpu()[:, None]
+    else:
+        x, out = torch.full((M, ld), math.nan, dtype=xtype, device=DEV), xtype if group == 64 else F32
+        x[:, :K] = normal(g, M, K).to(xtype)
+        x64 = x[:, :K].double().cpu()
+    want = x64 @ w.T + (0 if bias is None else bias.double().cpu())
+    w31 = (62.0 * s.double().cpu())[:, torch.arange(K) // group]
+    tol = product_tolerance(x64, w31, K, group, 1 if xtype == "rows8" else PARTS[xtype], out, want)
+    off = (product(x, packed, N, group, out, rs, bias, K).double().cpu() - want).abs()
+    assert (off <= tol).all(), float((off / tol).max())
+    if xtype == "rows8" and out == F32 and bias is None:
+        # whole numbers: sums of a group are exact; its fused operation, the join of up to four waves and the quotient are off by
+        # half a step each of something that is at most sum |x| |w|
+        assert (off <= (-(-K // group) + 4 + 1) * EPS32 / 2 * (x64.abs() @ w.abs().T)).all()
