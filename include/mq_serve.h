@@ -123,7 +123,8 @@ int mq_w4_pack(const uint8_t* codes, const float* scales, const uint8_t* zeros, 
 int mq_w4_prepare(const float* w, size_t N, size_t K, int group, void* packed, void* stream);
 int mq_w4_unpack(const void* packed, size_t N, size_t K, int group, float* w, void* stream);
 
-/* y[m][n] = sum_k x[m][k] (c[n][k] - z) s + bias[n] for a few rows (about 1 to 200; any number is served).
+/* y[m][n] = sum_k x[m][k] (c[n][k] - z) s + bias[n] for a few rows (about 1 to 200; any number is served but for launches of 2^32
+ * threads: some rows / 32 x N / 64 >= 2^24).
  *   x: M rows of K elements, ldx apart, of type xtype: an mq_dtype, or MQ_ROWS8: int8 with the multipliers row_scale, device
  *     float [M] (an element q stands for q / row_scale[m], as mq_add_rms_norm_rows8 leaves them); row_scale is NULL for the others.
  *   y: M rows of N elements, ldy apart, of type ytype (an mq_dtype).  bias: device float [N] or NULL.

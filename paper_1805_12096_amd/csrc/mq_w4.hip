@@ -421,13 +421,14 @@ __global__ __launch_bounds__(256) void k_w4_x(const W4Params p, uint8_t* to) {
 }
 
 template <int XT, int GROUP>
-__global__ __launch_bounds__(kManyWaves * kWave, 2) void k_w4_many(const W4Params p, const uint8_t* xs, unsigned runs, unsigned run) {
+__global__ __launch_bounds__(kManyWaves * kWave, 2) void k_w4_many(const W4Params p, const uint8_t* xs, unsigned ntiles, unsigned runs, unsigned run) {
   constexpr int NP = kXParts<XT>, GF = kKT / GROUP, SG = GROUP / 32, MT = many_mt(NP), NT = kManyNT, EVERY = kEvery<GROUP>;
   extern __shared__ float lds[];                 // [waves][MT 16][NT 16 + 1]
   const unsigned lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), col = lane % 16, grp = lane / 16;
   // neighbouring workgroups share rows of x: those of one XCD its parts
-  const unsigned ntiles = gridDim.x / runs, nt = blockIdx.x % ntiles, k0 = blockIdx.x / ntiles * run, k1 = min(k0 + run, p.frags);
-  const unsigned m0 = blockIdx.y * MT;
+  // (all in one axis: the others have no more than 65535 workgroups)
+  const unsigned m0 = blockIdx.x / (ntiles * runs) * MT, at = blockIdx.x % (ntiles * runs);
+  const unsigned nt = at % ntiles, k0 = at / ntiles * run, k1 = min(k0 + run, p.frags);
   const W4Dims d(p.N, p.K, GROUP);
   const XDims xd(p.M, p.K, NP);
   const uint8_t* frag[NT];
@@ -630,8 +631,8 @@ int launch_w4_product(const void* x, size_t ldx, int xtype, const float* row_sca
       return sized(std::integral_constant<int, 1>{});
     }
     const ManyForm f = many_form(M, N, K, kXParts<XT>);
-    const size_t wgs = (size_t)f.ntiles * f.runs;
-    if (!launchable(wgs * f.chunks, kManyWaves * kWave) || f.chunks > 65535) return (int)MQ_ERR_SHAPE;
+    const size_t wgs = (size_t)f.ntiles * f.runs * f.chunks;
+    if (!launchable(wgs, kManyWaves * kWave)) return (int)MQ_ERR_SHAPE;
     const size_t waves = XDims(M, K, 1).tiles * d.frags;
     hipLaunchKernelGGL((k_w4_x<XT, GROUP>), dim3((unsigned)(waves < 16384 ? (waves + 3) / 4 : 4096)), dim3(256), 0, s, p, xs);
     constexpr size_t lds = kManyWaves * many_mt(kXParts<XT>) * 16 * (kManyNT * 16 + 1) * sizeof(float);
@@ -640,7 +641,7 @@ int launch_w4_product(const void* x, size_t ldx, int xtype, const float* row_sca
       const int rc = check_hip(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
       if (rc != MQ_OK) return rc;
     }
-    hipLaunchKernelGGL(kern, dim3((unsigned)wgs, f.chunks), dim3(kManyWaves * kWave), lds, s, p, xs, f.runs, f.run);
+    hipLaunchKernelGGL(kern, dim3((unsigned)wgs), dim3(kManyWaves * kWave), lds, s, p, xs, f.ntiles, f.runs, f.run);
     if (f.runs > 1) hipLaunchKernelGGL(k_w4_join, dim3((unsigned)(M * N < 1048576 ? (M * N + 255) / 256 : 4096)), dim3(256), 0, s, p, f.runs);
     return check_hip(hipGetLastError());
   };

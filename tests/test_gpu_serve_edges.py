@@ -216,3 +216,16 @@ def test_few_rows_of_whole_pieces(M, K, group, xtype):
         # whole numbers: sums of a group are exact; its fused operation, the join of up to four waves and the quotient are off by
         # half a step each of something that is at most sum |x| |w|
         assert (off <= (-(-K // group) + 4 + 1) * EPS32 / 2 * (x64.abs() @ w.abs().T)).all()
+
+
+@pytest.mark.parametrize("xtype,M", [(F32, 65535 * 32 + 33), (BF16, 65535 * 64 + 65)])
+def test_millions_of_rows(xtype, M):
+    """More rows than one axis of a launch has workgroups for; each row is the product of its own."""
+    g, N, K, group = gen(41), 3, 4, 32
+    codes, s, z, w = w4_inputs(g, N, K, group)
+    packed = mq.w4_pack(codes, s, z, group)
+    x = (torch.arange(M, device=DEV)[:, None] * torch.tensor([1, 3, 7, 11], device=DEV) % 251 - 125).to(xtype)
+    y = product(x, packed, N, group, F32)
+    # whole numbers below 2^7 by whole numbers below 2^4, times a scale: one rounding each for it, the zero's product and the sum
+    want = x.double() @ w.T.contiguous().to(DEV)
+    assert ((y.double() - want).abs() <= 4 * EPS32 * 4 * 125 * 62 * s.max()).all()
