@@ -42,8 +42,9 @@ extern "C" {
  * denominator all the same.  Sums and softmax statistics are binary32.
  * ws: device, 16-byte aligned, mq_chunk_attention_ws_bytes (0 for invalid arguments).  One launch where max_len <= 1152 (up to
  * 2048 if there is work for all of the chip) and rows are few, else two or three: shares are planned from the lengths, computed, and
- * joined.  Calls of which that plan cannot count the blocks in 31 bits (some 2^31 / (max_len / 64) tiles of 32 rows) are refused with
- * MQ_ERR_SHAPE. */
+ * joined.  Refused with MQ_ERR_SHAPE are calls that would take a launch of 2^32 threads (2^24 tiles of 32 rows x kv heads in one launch,
+ * 2^22 where parts are joined), and calls of which that plan cannot count the blocks in 31 bits (some 2^31 / (max_len / 64) tiles of 32
+ * rows). */
 size_t mq_chunk_attention_ws_bytes(size_t B, size_t T, size_t max_len, int heads, int kv_heads, size_t head_dim);
 int mq_chunk_attention(const mq_kv_cache* cache, const int32_t* table, size_t table_width, const int32_t* first,
                        const int32_t* lens, size_t B, size_t T, size_t max_len, int causal, const void* q, size_t ldq, int heads,

@@ -1138,8 +1138,8 @@ int launch_chunk_attention(const mq_kv_cache& cache, const int32_t* table, size_
   const Form form = form_of(dtype, B, T, max_len, heads, cache.kv_heads, cache.head_dim);
   const size_t tiles = form.slots * (size_t)cache.kv_heads, joins = tiles * (form.tile_rows / join_rows(form.tile_rows));
   const size_t blocks = (max_len + kKvBlock - 1) / kKvBlock;
-  // (blocks of all tiles are counted in 32 bits, with room for sums)
-  if (!launchable(joins, kWaves * kWave) || form.slots > (((size_t)1 << 31) - 1) / blocks) return MQ_ERR_SHAPE;
+  // (parts are joined where shares are equal only, and there blocks of all tiles are counted in 32 bits, with room for sums)
+  if (!launchable(form.shares ? joins : tiles, kWaves * kWave) || form.slots > (((size_t)1 << 31) - 1) / blocks) return MQ_ERR_SHAPE;
   float* part = static_cast<float*>(ws);
   const ChunkParams p{cache.keys, cache.values, cache.amax, table, first, lens, q, out, part, ldq, ldo,
                       table_width, cache.blocks, (unsigned)B, (unsigned)T, (unsigned)max_len, (unsigned)cache.kv_heads,

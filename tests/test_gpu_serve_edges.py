@@ -229,3 +229,21 @@ def test_millions_of_rows(xtype, M):
     # whole numbers below 2^7 by whole numbers below 2^4, times a scale: one rounding each for it, the zero's product and the sum
     want = x.double() @ w.T.contiguous().to(DEV)
     assert ((y.double() - want).abs() <= 4 * EPS32 * 4 * 125 * 62 * s.max()).all()
+
+
+def test_more_short_sequences_than_a_join_would_have_places():
+    """Single launches are bounded by their own workgroups: 131072 sequences of one new token, 32 heads.  Held against calls of a
+    quarter of them."""
+    g, B, heads, dim, blocks = gen(42), 131072 + 96, 32, 8, 600
+    cache = random_cache(g, blocks, heads, dim)
+    table = torch.randint(0, blocks, (B, 2), generator=g, dtype=torch.int32).to(DEV)
+    lens = torch.randint(0, 129, (B,), generator=g, dtype=torch.int32).to(DEV)
+    q = normal(g, B, heads * dim).to(BF16).to(DEV)
+
+    def call(at, n):
+        return chunk_call(cache, table[at:at + n], torch.arange(n + 1, dtype=torch.int32, device=DEV), lens[at:at + n], 128, True, q[at:at + n], heads, 0.3)
+    assert mq.mq_chunk_attention_ws_bytes(B, B, 128, heads, heads, dim) > 0
+    whole = call(0, B)
+    step = B // 4
+    for at in range(0, B, step):
+        assert torch.equal(whole[at:at + step], call(at, step))
