@@ -109,6 +109,34 @@ def test_probabilities_of_short_types_hold_sixteen_bits(form, dtype):
     check_chunk(chunk_call(*args, True, q, heads, scale), want, tol)
 
 
+@pytest.mark.parametrize("form", ["few", "shares", "many"])
+@pytest.mark.parametrize("dtype,bits", [(F32, 18), (F16, 10)])
+def test_every_bit_of_a_query_counts(form, dtype, bits):
+    """Two elements that differ in their last bit, against keys of 1 and -1: all sums are multiples of 2^-bits below 4, so scores are
+    exact but for their factor (of four roundings): the lowest bit decides between two tokens.  A query without its last part
+    would give both the same weight."""
+    new, lens, heads, kv_heads, dim, room = FORMS[form]
+    g = gen(35)
+    T, need = sum(new), sum(-(-n // BLOCK) for n in lens)
+    cache = random_cache(g, need, kv_heads, dim)
+    width = max(-(-n // BLOCK) for n in lens) + room
+    table, first = tables(g, lens, width, need), np.concatenate([[0], np.cumsum(new)])
+    cache.keys.zero_()
+    cache.keys[:, :, ::2, 0], cache.keys[:, :, ::2, dim - 1] = 1, -1
+    cache.amax[:, :, 0] = 127.0
+    q = torch.zeros(T, heads, dim)
+    q[..., 0], q[..., dim - 1] = 1 + 2.0 ** -9 + 2.0 ** -bits, 1 + 2.0 ** -9
+    if bits == 10:
+        q[..., 0], q[..., dim - 1] = 1 + 2.0 ** -10, 1
+    q = q.view(T, -1).to(dtype).to(DEV)
+    scale = 2.0 ** bits                                      # scores are 1 and 0 by turns
+    want, _ = chunk_expected(cache, table, first, lens, width * BLOCK, True, q, heads, scale, dtype)
+    out = chunk_call(cache, i32(table), i32(first), i32(lens), width * BLOCK, True, q, heads, scale)
+    # weights are off by 8 eps32 and their parts, sums of up to n of them by (n + 64) eps32; values are up to 2.5 and the result rounded
+    off = (8 * EPS32 + 2.0 ** (-15 if dtype == F16 else -23) + (max(lens) + 64) * EPS32) * 2.5
+    check_chunk(out, want, off + half_step(dtype, want))
+
+
 # ---- norm -----------------------------------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("dtype", TYPES)
