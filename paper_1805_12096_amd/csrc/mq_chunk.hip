@@ -1084,12 +1084,17 @@ struct Form {
   unsigned tile_rows, groups, least;  // rows of a tile; workgroups that share the line, blocks that one takes at least
   size_t slots;
 };
-// The form for many rows, us of a call, few rows / many: heads of 128, 32 over 8, 8 sequences on 4000 tokens, 128 rows of a kv
-// head 55 / 69 (bfloat16), 85 / 96 (binary16), 100 / 103 (binary32), 192 rows 73 / 67, 113 / 128, 134 / 139, 256 rows 85 / 73, 135 /
-// 130, 163 / 143; heads of 64, 8, 64 sequences on 400, binary32, 96 rows 38 / 46, 128 rows 91 / 52.  Its plan, its longer start and
-// its parts take 30 us of any call: heads of 64, 8 over 2, 64 sequences on 400, bfloat16, 256 rows 19 / 33, 512 rows 63 / 52.
-constexpr size_t many_rows(size_t d) { return d <= 64 ? 128 : 160; }       // rows of a sequence on average
-constexpr size_t kManyWork = (size_t)1 << 31;      // rows x longest sequence x width
+// The form for many rows is for calls whose rows of a sequence and kv head, on average, fill its tiles (256 or 128 rows; past their rows it
+// works for nothing), and that are long enough for its plan, its longer start and its parts, some 30 us.  Few rows / many, us of a call
+// (rows, then rows x longest sequence x width of all heads in 10^9):
+// heads of 128, 32 over 8, 8 sequences on 4000: bfloat16 (tiles of 256) 160 (5.3) 73 / 77, 192 (6.3) 82 / 79, 256 (8.5) 96 / 85, 288 (9.6) 127 /
+//   135, 384 (13) 144 / 128; binary16 (128) 128 (4.2) 89 / 97, 192 (6.3) 115 / 130, 256 (8.5) 139 / 132; binary32 (128) 192 134 / 138, 256 164 / 145;
+//   16 over 16, 16 on 2000, binary16, 128 (8.9) 171 / 129, 192 (13) 246 / 230; 8 over 8, 64 on 1000, 96 (6.9) 179 / 126;
+// of 64, 16 over 4, 16 on 8000: bfloat16 (256) 256 (8.5) 101 / 103, 384 (13) 148 / 166, 512 (17) 189 / 169; binary32 (128) 256 142 / 132, 384
+//   209 / 185; 8 over 8, 64 on 1000: bfloat16 256 (11) 112 / 122, 384 (17) 171 / 230, binary32 256 151 / 156;
+// of 256, 8 over 4, 4 on 4000: bfloat16 (128) 512 (8.9) 119 / 148, 768 (14) 180 / 173, 1024 (19) 221 / 201; of 192, 16 over 4, 768 (9.9) 139 / 136.
+constexpr size_t kManyWork[] = {(size_t)3 << 32, (size_t)3 << 31, (size_t)5 << 31};       // heads up to 64, 128, 256
+constexpr bool many_rows(size_t rows, size_t tile, size_t d) { return rows * 8 >= round_up(rows, tile) * (d <= 64 ? 7 : 6); }
 // Blocks of the longest sequence up to which a workgroup takes all of a tile's: where equal shares would be one turn of the waves at
 // most (three blocks a workgroup), and else.  One workgroup / shares, us: bfloat16, 32 heads over 8 of 128, 4 new tokens, 1 sequence
 // on 1000 tokens 15.2 / 17.5, 1300 18.9 / 15.5, 2000 23.0 / 15.8, 4 on 2000 25.2 / 20.8, 8 on 1300 21.0 / 21.7, 16 on 1700 24.2 / 28.7,
@@ -1098,16 +1103,18 @@ constexpr size_t kShort = 18, kLong = 32;
 Form form_of(int dtype, size_t B, size_t T, size_t max_len, int heads, int kv_heads, size_t d) {
   const size_t per = (size_t)(heads / kv_heads), blocks = (max_len + kKvBlock - 1) / kKvBlock;
   Form f{};
+  const bool wide = (dtype == MQ_BF16 && d <= 128) || (d <= 64 && dtype == MQ_F16);
+  const size_t rows = T * per / B, tile = wide ? 256 : 128;
   // (binary32 queries of wide heads do not fit beside the sums)
-  f.many = T * per / B >= many_rows(d) && T * (size_t)heads * d >= kManyWork / max_len && !(dtype == MQ_F32 && d > 128);
+  f.many = rows > 0 && many_rows(rows, tile, d) && T * (size_t)heads * d >= kManyWork[d <= 64 ? 0 : d <= 128 ? 1 : 2] / max_len &&
+           !(dtype == MQ_F32 && d > 128);
   f.shares = f.many || blocks > kLong;
   f.tile_rows = kRows;
   f.least = f.many ? 8 : 4;
   f.groups = d <= 64 ? 768 : d <= 128 ? 512 : 256;
   if (f.many) {
-    const bool wide = (dtype == MQ_BF16 && d <= 128) || (d <= 64 && dtype == MQ_F16);
-    f.tile_rows = wide ? 256 : 128;
-    f.groups = wide ? 256 : 512;      // one workgroup of eight waves to a compute unit, or two of four
+    f.tile_rows = (unsigned)tile;
+    f.groups = wide ? 256 : 512;
   }
   f.slots = T * per / f.tile_rows + B;
   if (blocks > kShort && f.slots <= kHere && f.slots * blocks * kv_heads <= (size_t)3 * f.groups) f.shares = true;

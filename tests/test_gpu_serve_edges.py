@@ -275,3 +275,91 @@ def test_more_short_sequences_than_a_join_would_have_places():
     step = B // 4
     for at in range(0, B, step):
         assert torch.equal(whole[at:at + step], call(at, step))
+
+
+# ---- the form for many rows: what the other forms are held to elsewhere --------------------------------------------------------
+
+MANY = [f for f in FORMS if f.startswith("many")]
+
+
+@pytest.mark.parametrize("form", MANY)
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("dim", [None, 40, 57, 130])
+def test_many_rows(form, dtype, dim):
+    """Whole tiles and ragged ends, with and without a mask; widths that are no whole pieces."""
+    new, lens, heads, kv_heads, d, room = FORMS[form]
+    d, g = dim or d, gen(50)
+    new, lens = [*new, max(new) - 13, 0], [*lens, 500, 10]
+    need = sum(-(-n // BLOCK) for n in lens)
+    cache = random_cache(g, need, kv_heads, d)
+    width = max(-(-n // BLOCK) for n in lens) + 4 * room
+    table, first = tables(g, lens, width, need), np.concatenate([[0], np.cumsum(new)])
+    q = normal(g, sum(new), heads * d).to(dtype).to(DEV)
+    for causal in (True, False):
+        out = chunk_call(cache, i32(table), i32(first), i32(lens), width * BLOCK, causal, q, heads, d ** -0.5)
+        check_chunk(out, *chunk_expected(cache, table, first, lens, width * BLOCK, causal, q, heads, d ** -0.5, dtype))
+
+
+@pytest.mark.parametrize("form", MANY)
+@pytest.mark.parametrize("dtype", TYPES)
+def test_many_rows_with_other_scales(form, dtype):
+    cache, table, first, lens, width, q, heads = a_call(form, 51)
+    q = q.to(dtype).to(DEV)
+    for scale in (-0.1, 0.0):
+        out = chunk_call(cache, i32(table), i32(first), i32(lens), width * BLOCK, True, q, heads, scale)
+        want, _ = chunk_expected(cache, table, first, lens, width * BLOCK, True, q, heads, scale, dtype)
+        _, tol = chunk_expected(cache, table, first, lens, width * BLOCK, True, q, heads, -scale, dtype)     # (depends on its magnitude)
+        check_chunk(out, want, tol + half_step(dtype, want))
+
+
+@pytest.mark.parametrize("form", MANY)
+@pytest.mark.parametrize("dtype", TYPES)
+def test_many_rows_keep_bad_queries_apart(form, dtype):
+    cache, table, first, lens, width, good, heads = a_call(form, 52)
+    T, d, good = len(good), cache.head_dim, good.to(dtype)
+    q = good.clone()
+    q[3, 5], q[25, d + d - 1], q[T - 1, 2 * d + 8], q[30, :d] = math.nan, math.inf, -math.inf, math.inf
+    args = cache, i32(table), i32(first), i32(lens), width * BLOCK, True
+    out, clean = (chunk_call(*args, x.to(DEV), heads, 0.1).view(T, heads, d) for x in (q, good))
+    bad = (~torch.isfinite(q)).view(T, heads, d).any(-1).to(DEV)
+    assert torch.isnan(out[bad]).all() and torch.equal(out[~bad], clean[~bad])
+
+
+@pytest.mark.parametrize("form", MANY)
+def test_many_rows_with_bad_lists_and_tables(form):
+    """Lists that descend or leave their range, lengths out of theirs, entries that are no block: nothing outside the rows is written."""
+    cache, table, _, lens, width, q, heads = a_call(form, 53)
+    T, B = len(q), len(lens)
+    table[:, 1::3], q = cache.blocks + 5, q.to(BF16).to(DEV)
+    store = torch.full((T + 20, q.shape[1]), 7.0, dtype=BF16, device=DEV)
+    for first in ([5, 2, T], [T, 0, T], [-9, T + 5, 3]):
+        for n in ([1 << 30, -5], [300, 900]):
+            chunk_call(cache, i32(table), i32(first[:B + 1]), i32(n[:B]), width * BLOCK, True, q, heads, 0.1, store[10:10 + T])
+            assert (store[:10] == 7.0).all() and (store[10 + T:] == 7.0).all() and not torch.isnan(store).any()
+
+
+@pytest.mark.parametrize("form", MANY)
+@pytest.mark.parametrize("dtype", TYPES)
+def test_many_rows_in_place_captured_and_beside_another_stream(form, dtype):
+    cache, table, first, lens, width, q, heads = a_call(form, 54)
+    g, q = gen(55), q.to(dtype).to(DEV)
+    args = cache, i32(table), i32(first), i32(lens), width * BLOCK, True, q, heads, 0.09
+    want = chunk_call(*args)
+    again = q.clone()
+    chunk_call(*args[:6], again, *args[7:], out=again)
+    assert torch.equal(again, want)
+    out = torch.zeros_like(q)
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.graph(graph):
+        chunk_call(*args, out=out)
+    for i in range(3):
+        q.copy_(normal(g, *q.shape).to(dtype))
+        out.zero_()
+        beside = torch.zeros_like(q)
+        want = chunk_call(*args)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            chunk_call(*args, out=beside)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.equal(beside, want), i
