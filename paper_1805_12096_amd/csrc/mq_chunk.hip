@@ -119,9 +119,9 @@ __device__ __forceinline__ unsigned seen_by(const ChunkParams& p, const Tile& t,
 // ---- equal shares ---------------------------------------------------------------------------------------------------------
 //
 // Lengths are known on the device only, so a first small launch sums up the blocks that each tile of rows sees.  The workgroups,
-// as many as run at once, share the blocks of all tiles and kv heads in one line equally: each has some tiles whole, and parts of
+// as many as have room at once, share the blocks of all tiles and kv heads in one line equally: each has some tiles whole, and parts of
 // the tiles at its two ends, which go to the workspace and are joined.  (Instead of runs of equal length, a workgroup each, as many
-// of every tile as the longest needs: 64 sequences of 512 .. 4096 tokens with 256 new ones, 526 us; equal shares 453.)
+// of every tile as the longest needs: four pieces of 300 .. 1100 tokens on 2000 .. 16000, 526 us when equal shares were new, at 453.)
 
 constexpr int kPlan = 1024;           // threads of the workgroup that plans
 
@@ -1087,13 +1087,14 @@ struct Form {
 // The form for many rows is for calls whose rows of a sequence and kv head, on average, fill its tiles (256 or 128 rows; past their rows it
 // works for nothing), and that are long enough for its plan, its longer start and its parts, some 30 us.  Few rows / many, us of a call
 // (rows, then rows x longest sequence x width of all heads in 10^9):
-// heads of 128, 32 over 8, 8 sequences on 4000: bfloat16 (tiles of 256) 160 (5.3) 73 / 77, 192 (6.3) 82 / 79, 256 (8.5) 96 / 85, 288 (9.6) 127 /
-//   135, 384 (13) 144 / 128; binary16 (128) 128 (4.2) 89 / 97, 192 (6.3) 115 / 130, 256 (8.5) 139 / 132; binary32 (128) 192 134 / 138, 256 164 / 145;
-//   16 over 16, 16 on 2000, binary16, 128 (8.9) 171 / 129, 192 (13) 246 / 230; 8 over 8, 64 on 1000, 96 (6.9) 179 / 126;
+// heads of 128, 32 over 8, 8 sequences on 4000: bfloat16 (tiles of 256) 160 (5.3) 73 / 77, 192 (6.4) 82 / 79, 256 (8.5) 96 / 85, 288 (9.6) 127 /
+//   135, 384 (13) 144 / 128; binary16 (128) 128 (4.2) 67 / 101, 192 (6.4) 108 / 133, 256 129 / 132, 384 182 / 169; binary32 (128) 192 121 / 139,
+//   256 149 / 145; 16 over 16, 16 on 2000, binary16, 128 (8.9) 154 / 128; 8 over 8, 64 on 1000, 96 (6.9) 180 / 128;
 // of 64, 16 over 4, 16 on 8000: bfloat16 (256) 256 (8.5) 101 / 103, 384 (13) 148 / 166, 512 (17) 189 / 169; binary32 (128) 256 142 / 132, 384
 //   209 / 185; 8 over 8, 64 on 1000: bfloat16 256 (11) 112 / 122, 384 (17) 171 / 230, binary32 256 151 / 156;
-// of 256, 8 over 4, 4 on 4000: bfloat16 (128) 512 (8.9) 119 / 148, 768 (14) 180 / 173, 1024 (19) 221 / 201; of 192, 16 over 4, 768 (9.9) 139 / 136.
-constexpr size_t kManyWork[] = {(size_t)3 << 32, (size_t)3 << 31, (size_t)5 << 31};       // heads up to 64, 128, 256
+// of 256, 8 over 4, 4 on 4000: bfloat16 (128) 256 (4.3) 77 / 79, 384 (6.6) 101 / 92, 1024 (19) 220 / 163; 8 over 8, 16 on 4000, 64 (8.5) 132 / 143,
+//   96 196 / 149; of 192, 16 over 4, 16 on 4000, 128 (6.3) 85 / 92, 192 (9.6) 141 / 133.
+constexpr size_t many_work(size_t d) { return d <= 64 ? (size_t)3 << 32 : (size_t)3 << 31; }
 constexpr bool many_rows(size_t rows, size_t tile, size_t d) { return rows * 8 >= round_up(rows, tile) * (d <= 64 ? 7 : 6); }
 // Blocks of the longest sequence up to which a workgroup takes all of a tile's: where equal shares would be one turn of the waves at
 // most (three blocks a workgroup), and else.  One workgroup / shares, us: bfloat16, 32 heads over 8 of 128, 4 new tokens, 1 sequence
@@ -1106,15 +1107,17 @@ Form form_of(int dtype, size_t B, size_t T, size_t max_len, int heads, int kv_he
   const bool wide = (dtype == MQ_BF16 && d <= 128) || (d <= 64 && dtype == MQ_F16);
   const size_t rows = T * per / B, tile = wide ? 256 : 128;
   // (binary32 queries of wide heads do not fit beside the sums)
-  f.many = rows > 0 && many_rows(rows, tile, d) && T * (size_t)heads * d >= kManyWork[d <= 64 ? 0 : d <= 128 ? 1 : 2] / max_len &&
-           !(dtype == MQ_F32 && d > 128);
+  f.many = rows > 0 && many_rows(rows, tile, d) && T * (size_t)heads * d >= many_work(d) / max_len && !(dtype == MQ_F32 && d > 128);
   f.shares = f.many || blocks > kLong;
   f.tile_rows = kRows;
   f.least = f.many ? 8 : 4;
-  f.groups = d <= 64 ? 768 : d <= 128 ? 512 : 256;
+  // as many as there is room for at once: LDS holds three, two (of bfloat16) or one; of the form for many rows one of eight waves, two
+  // of four, or one of wide heads.  (Twice as many, in two rounds, begin and join twice: 32 heads over 8 of 128, binary16, 4 new tokens of
+  // 32 sequences on 4000 109 us instead of 79, 32 of 8 90 instead of 65; 8 over 4 of 256, bfloat16, 800 of 4 on 4000 275 instead of 236.)
+  f.groups = d <= 64 ? 768 : d <= 128 && dtype == MQ_BF16 ? 512 : 256;
   if (f.many) {
     f.tile_rows = (unsigned)tile;
-    f.groups = wide ? 256 : 512;
+    f.groups = wide || d > 128 ? 256 : 512;
   }
   f.slots = T * per / f.tile_rows + B;
   if (blocks > kShort && f.slots <= kHere && f.slots * blocks * kv_heads <= (size_t)3 * f.groups) f.shares = true;
