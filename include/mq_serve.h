@@ -116,7 +116,7 @@ int mq_add_rms_norm_pack8(const void* x, size_t ldx, const void* r, size_t ldr, 
  *   mq_w4_pack: codes device uint8 [N x K] (the low four bits count), scales device float [N x groups], zeros device uint8
  *     [N x groups] or NULL (8 everywhere).
  *   mq_w4_prepare: codes and scales of a device float [N x K]: z = 8, s = max |w| of the group / 7 (rounded to what is held),
- *     c = 8 + clamp(rne(w / s), -8, 7).  NaNs become 0.
+ *     c = 8 + clamp(rne(w / s), -8, 7).  NaNs become 0; a group that holds an infinity comes out as NaN altogether.
  *   mq_w4_unpack: w device float [N x K] receives (c - z) s. */
 size_t mq_w4_bytes(size_t N, size_t K, int group);
 int mq_w4_pack(const uint8_t* codes, const float* scales, const uint8_t* zeros, size_t N, size_t K, int group, void* packed,

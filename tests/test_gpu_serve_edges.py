@@ -363,3 +363,18 @@ def test_many_rows_in_place_captured_and_beside_another_stream(form, dtype):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, want) and torch.equal(beside, want), i
+
+
+@pytest.mark.parametrize("group", [32, 128])
+def test_an_infinity_costs_its_group_and_nothing_else(group):
+    """A scale that holds an infinity is one: the group comes out as NaN, as the header says; other groups and rows are what they were."""
+    g, N, K = gen(60), 20, 300
+    w = normal(g, N, K)
+    bad = w.clone()
+    bad[3, group + 5], bad[17, 299] = math.inf, -math.inf
+    back = [torch.empty((N, K), device=DEV) for _ in range(2)]
+    for x, y in zip((w, bad), back):
+        mq.mq_w4_unpack(mq.w4_prepare(x.to(DEV), group), N, K, group, y)
+    lost = torch.zeros((N, K), dtype=torch.bool, device=DEV)
+    lost[3, group:2 * group], lost[17, 299 // group * group:] = True, True
+    assert torch.isnan(back[1][lost]).all() and torch.equal(back[1][~lost], back[0][~lost])
