@@ -308,7 +308,7 @@ __device__ __forceinline__ void each_part(const ChunkParams& p, const unsigned* 
 //
 // A workgroup has 32 rows; its waves take the blocks in turn, each through its own part of LDS with no barrier, and join there.
 // Bound by the bytes of the cache where sequences are long: 32 sequences of 4 new tokens, 32 heads over 8 of 128, 16000 tokens
-// held, 1.05 GB in 207 us, 5.1 TB/s (a copy, half of it writes, reaches 4.7); 1000 .. 9000 held, 243 MB in 72 us (3.4 TB/s), of
+// held, 1.05 GB in 211 us, 5.0 TB/s (a copy, half of it writes, reaches 4.7); 1000 .. 9000 held, 243 MB in 74 us (3.3 TB/s), of
 // which plan, start and join take 15.  Few tokens are bound by the way of one block, some 1.5 us: 64 sequences of up to 512 8.4 us.
 // Blocks come by the loads that go to LDS directly, 1 KB each in whole lines (a lane that loads its own row is an access of its own
 // to the nearest cache, 64 a load: 117 us), keys of the next block as soon as this one's are in registers, values likewise.
@@ -645,9 +645,10 @@ __global__ __launch_bounds__(kWaves * kWave, DC > 2 ? 1 : 2) void k_chunk_few(co
 // LDS for keys, since this block's and the next one's are read while those of the one after come, two for values.
 // The scale of a block's values goes into the exponent (for binary32, whose 24 bits the logarithm would cost some, into a product).
 // Bound by what a SIMD can issue: 32 heads of 128 over 8, four pieces of 300 .. 1100 tokens on 2000 .. 16000, bfloat16, 328 GFLOP
-// in 410 us (800 TFLOP/s of 1236 that a large library product reaches).  Of the 794 thousand clocks of a SIMD the matrix unit has
-// 338 and the vector unit 431, which hardly overlap: exponentials, conversions, masks and sums cost as much as the products.
-// One workgroup of eight waves shares each block where registers let two waves stay on a SIMD (with four of 64 rows each: 714 us).
+// in 535 us (613 TFLOP/s of 1236 that a large library product reaches; 492 GFLOP of products, since probabilities are two parts).  Of the
+// 1043 thousand clocks of a SIMD the matrix unit has 494 and the vector unit 597, which hardly overlap: exponentials, their parts,
+// conversions, masks and sums cost more than the products.  One workgroup of eight waves shares each block where registers let two waves
+// stay on a SIMD (four of 64 rows each, with probabilities of one part: 714 us, eight of 32 then 526).
 
 // Sums of matrix instructions times a factor, from accumulation registers and back.  (The compiler would otherwise take the
 // copies that the vector unit needs out of the branch, into every step.)

@@ -218,10 +218,10 @@ constexpr unsigned kFewWaves = 4;      // of a workgroup, at most
 
 // Few rows, of whole 16-byte pieces.  A workgroup has 16 rows of the parameter and 16 MT rows of x; its waves take the
 // fragments in turn, the next ones' loads ahead of this one's products, and join in LDS.  Bound by the start and the way to memory of
-// one round of workgroups more than by bytes: 11000 x 4096, groups of 64, 24 rows of 8 bits 25 MB in 11.6 us (2.2 TB/s).  A lane of an operand has a row of x of its
-// own; loaded like that, every lane would be an access to the nearest cache of its own (64 a load instead of 8 .. 16, which bound
-// this form).  So x comes in lines, and each wave turns its lines, as operand parts, in a part of LDS; of rows that are not there
-// nothing is turned.
+// one round of workgroups more than by bytes: 11000 x 4096, groups of 64, 24 rows of 8 bits 25 MB in 11.6 us (2.2 TB/s).  A lane of an
+// operand has a row of x of its own; loaded like that, every lane would be an access to the nearest cache of its own (64 a load
+// instead of 8 .. 16, which bound this form).  So x comes in lines, and each wave turns its lines, as operand parts, in a part of LDS;
+// of rows that are not there nothing is turned.
 // (Two workgroups to a compute unit: the compiler then keeps sums in vector registers, with no copies; 12.6 -> 11.8 us.)
 template <int XT, int GROUP, int MT>
 __global__ __launch_bounds__(kFewWaves * kWave, 2) void k_w4_few(const W4Params p) {
@@ -360,10 +360,11 @@ __global__ __launch_bounds__(kFewWaves * kWave, 2) void k_w4_few(const W4Params 
   }
 }
 
-// Many rows.  150 rows of binary32, 2048 x 8000, groups of 32: 31.5 us, of which x 4.5, the product 22 and the join 4.5; the product is
-// bound by vector instructions (codes, scales and zeros: 52 % of the clocks, matrix ones 30 %).  x comes as operand parts and sums of groups from a launch of its own (each is used by every row tile of the
-// parameter); a workgroup has 16 NT x 16 MT results and a run of fragments, its waves take the run's fragments in turn and join in
-// LDS, runs through the workspace.
+// Many rows.  150 rows of binary32, 2048 x 8000, groups of 32: 29 us, of which x 4.5, the product 20 and the join 4; the product is
+// bound by vector instructions (codes less zeros, scales: 57 % of the clocks, matrix ones 34 %).  x comes as operand parts, and (but for
+// binary32) sums of groups, from a launch of its own: each is used by every row tile of the parameter.  A workgroup has
+// 16 NT x 16 MT results and a run of fragments, its waves take the run's fragments in turn and join in LDS, runs through the
+// workspace.
 // (of several parts of x only half as many rows fit the registers beside those of the next step)
 constexpr int many_mt(int parts) { return parts == 1 ? 4 : 2; }
 constexpr int kManyNT = 4, kManyWaves = 4;
