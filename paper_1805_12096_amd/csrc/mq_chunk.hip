@@ -6,8 +6,8 @@
 // a, 32 query rows as operand b.  Lane l then has, for row l % 32, the scores of tokens 8 (r / 4) + 4 (l / 32) + r % 4 of 32, and
 // the cache keeps the values of a block in an order (kv_place) in which these lanes' probabilities are operand b of out^T = V^T p^T
 // as they are.  The cache's integers are bfloat16 values exactly (8 bits); queries enter as one, two or three bfloat16 parts,
-// probabilities as two or three.  Scales: a block's for the keys goes into the scores' factor, a block's for the values into the probabilities,
-// so sums stay in the accumulators from block to block.
+// probabilities as two or three.  Scales: a block's for the keys goes into the scores' factor, a block's for the values into the
+// probabilities, so sums stay in the accumulators from block to block.
 #include <type_traits>
 
 #include "mq_glue.h"
@@ -1089,10 +1089,11 @@ struct Form {
 // works for nothing), and that are long enough for its plan, its longer start and its parts, some 30 us.  Few rows / many, us of a call
 // (rows, then rows x longest sequence x width of all heads in 10^9):
 // heads of 128, 32 over 8, 8 sequences on 4000: bfloat16 (tiles of 256) 160 (5.3) 73 / 77, 192 (6.4) 82 / 79, 256 (8.5) 96 / 85, 288 (9.6) 127 /
-//   135, 384 (13) 144 / 128; binary16 (128) 128 (4.2) 67 / 101, 192 (6.4) 108 / 133, 256 129 / 132, 384 182 / 169; binary32 (128) 192 121 / 139,
-//   256 149 / 145; 16 over 16, 16 on 2000, binary16, 128 (8.9) 154 / 128; 8 over 8, 64 on 1000, 96 (6.9) 180 / 128;
-// of 64, 16 over 4, 16 on 8000: bfloat16 (256) 256 (8.5) 101 / 103, 384 (13) 148 / 166, 512 (17) 189 / 169; binary32 (128) 256 142 / 132, 384
-//   209 / 185; 8 over 8, 64 on 1000: bfloat16 256 (11) 112 / 122, 384 (17) 171 / 230, binary32 256 151 / 156;
+//   135, 384 (13) 144 / 128; binary16 (128) 128 (4.2) 66 / 78, 192 (6.4) 106 / 109, 256 127 / 109, 288 146 / 144; binary32 (128) 192 120 / 118,
+//   256 149 / 124; 16 over 16, 16 on 2000, binary16, 128 (8.9) 155 / 107, 160 (11) 187 / 192, 192 (14) 223 / 196; 8 over 8, 64 on 1000, 96 (6.9)
+//   180 / 128;
+// of 64, 16 over 4, 16 on 8000: bfloat16 (256) 256 (8.5) 101 / 103, 384 (13) 148 / 166, 512 (17) 189 / 169; binary32 (128) 256 128 / 131, 384
+//   204 / 185; 8 over 8, 64 on 1000: bfloat16 256 (11) 112 / 122, 384 (17) 171 / 230, binary32 256 149 / 156, 512 (25) 326 / 326;
 // of 256, 8 over 4, 4 on 4000: bfloat16 (128) 256 (4.3) 77 / 79, 384 (6.6) 101 / 92, 1024 (19) 220 / 163; 8 over 8, 16 on 4000, 64 (8.5) 132 / 143,
 //   96 196 / 149; of 192, 16 over 4, 16 on 4000, 128 (6.3) 85 / 92, 192 (9.6) 141 / 133.
 constexpr size_t many_work(size_t d) { return d <= 64 ? (size_t)3 << 32 : (size_t)3 << 31; }
@@ -1112,13 +1113,14 @@ Form form_of(int dtype, size_t B, size_t T, size_t max_len, int heads, int kv_he
   f.shares = f.many || blocks > kLong;
   f.tile_rows = kRows;
   f.least = f.many ? 8 : 4;
-  // as many as there is room for at once: LDS holds three, two (of bfloat16) or one; of the form for many rows one of eight waves, two
-  // of four, or one of wide heads.  (Twice as many, in two rounds, begin and join twice: 32 heads over 8 of 128, binary16, 4 new tokens of
-  // 32 sequences on 4000 109 us instead of 79, 32 of 8 90 instead of 65; 8 over 4 of 256, bfloat16, 800 of 4 on 4000 275 instead of 236.)
-  f.groups = d <= 64 ? 768 : d <= 128 && dtype == MQ_BF16 ? 512 : 256;
+  // as many as there is room for at once: registers and LDS hold three (binary32: two), two (of bfloat16) or one; of the form for many rows
+  // one of eight waves, and two of four waves (their registers) up to 64 columns only.  (More, in rounds, begin and join again: 32 heads over
+  // 8 of 128, binary16, 4 new tokens of 32 sequences on 4000 109 us instead of 79, 32 of 8 90 instead of 65, 256 of 8 364 instead of 336; 8
+  // over 4 of 256, bfloat16, 800 of 4 on 4000 275 instead of 236; 8 of 64, binary32, 1 of 64 on 2500 74 instead of 53.)
+  f.groups = d <= 64 ? (dtype == MQ_F32 ? 512 : 768) : d <= 128 && dtype == MQ_BF16 ? 512 : 256;
   if (f.many) {
     f.tile_rows = (unsigned)tile;
-    f.groups = wide || d > 128 ? 256 : 512;
+    f.groups = wide || d > 64 ? 256 : 512;
   }
   f.slots = T * per / f.tile_rows + B;
   if (blocks > kShort && f.slots <= kHere && f.slots * blocks * kv_heads <= (size_t)3 * f.groups) f.shares = true;
